@@ -289,6 +289,96 @@ gg_status gg_gct_step(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype g_dt
                       const gg_seg *w, const float *step, int32_t k, int32_t qmin, int32_t qmax,
                       double eta, double lambda, double eps, int64_t t, void *stream);
 
+/* ---- a training step around the pass: layer norm, gradient norm, AdamW --------------------------- */
+
+/* Layer norm over the rows of a row-major matrix (no counterpart in the paper: the layer whose outputs
+ * are the activations that gg_fused measures per token):
+ *     y = weight * (x - mean) * rstd + bias,   rstd = 1 / sqrt(mean of (x - mean)^2 + eps)
+ * with mean and rstd those of the row.  Element (r, c) of x lies at x[r * x_ld + c], that of y at
+ * y[r * y_ld + c]; sums are taken in 32 bits or more and y is rounded once.  y may be x (the same address
+ * and ld).  A row that holds an inf or a nan becomes nan; no other row does. */
+typedef struct {
+    const void *x;               /* device, `dtype`                                           */
+    int64_t     rows, cols, x_ld;/* ld >= cols, in elements                                   */
+    int32_t     dtype;           /* gg_dtype of x and y                                       */
+    const void *weight, *bias;   /* device [cols] of w_dtype; each may be NULL (1 and 0)      */
+    int32_t     w_dtype;
+    double      eps;             /* >= 0                                                      */
+    void       *y;               /* device, output                                            */
+    int64_t     y_ld;
+    float      *mean, *rstd;     /* device [rows], outputs for the gradient; each may be NULL */
+} gg_layer_norm_args;
+gg_status gg_layer_norm(gg_ctx *ctx, const gg_layer_norm_args *args, void *stream);
+
+/* Its gradient, for dy = dL/dy and the mean and rstd that gg_layer_norm wrote.  With d = weight * dy and
+ * xhat = (x - mean) * rstd:
+ *     dx      = rstd * (d - mean over the row of d - xhat * mean over the row of (d * xhat))
+ *     dweight = sum over the rows of dy * xhat,     dbias = sum over the rows of dy
+ * The sums over the rows are reduced in a fixed order (no atomics): the same call gives the same bits.  dx may be
+ * dy or x (the same address and ld).  The first call that needs more scratch for the sums than any before
+ * allocates it (blocking). */
+typedef struct {
+    const void  *dy, *x;         /* device, `dtype`                                           */
+    int64_t      rows, cols, dy_ld, x_ld;
+    int32_t      dtype;          /* gg_dtype of dy, x and dx                                  */
+    const float *mean, *rstd;    /* device [rows]                                             */
+    const void  *weight;         /* device [cols] of w_dtype or NULL (1)                      */
+    int32_t      w_dtype;
+    void        *dx;             /* device or NULL (not wanted)                               */
+    int64_t      dx_ld;
+    float       *dweight, *dbias;/* device [cols]; each may be NULL                           */
+    int32_t      accumulate;     /* 0: dweight, dbias = the sums; 1: += (dx is always written)*/
+} gg_layer_norm_grad_args;
+gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *args, void *stream);
+
+/* Global norm of a gradient that lies in many tensors, and the factor that clips it, both left on the
+ * device: norm = sqrt(sum over all segments of g^2), scale = min(1, max_norm / norm).  An inf or nan anywhere
+ * makes both nan.  gg_adamw_step takes `scale` as its grad_scale.
+ *   max_norm   > 0; INFINITY: scale is 1
+ *   norm       device double[1] (may be NULL)
+ *   scale      device float[1] (may be NULL) */
+gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dtype, double max_norm,
+                       double *norm, float *scale, void *stream);
+
+/* One AdamW step over a list of tensors, in place, one launch for up to 512 of them:
+ *     g <- grad_scale * g
+ *     m <- beta1 m + (1 - beta1) g
+ *     v <- beta2 v + (1 - beta2) g^2
+ *     w <- w (1 - lr * decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32 arithmetic whatever the types.  A grad_scale that is inf or nan (as gg_grad_norm writes it for a
+ * gradient that overflowed) makes the step a no-op: nothing is written.  Without it an inf or nan in g reaches its own
+ * element's w, m and v and no other.  Needs no plan: tables travel with the launch, so addresses may differ from step
+ * to step, and nothing is allocated.
+ * Types: w fp32 or bf16, g fp32 or bf16, m and v fp32 (state_bits 32) or 8 bits (state_bits 8).  bf16 weights are
+ * rounded stochastically: a step is mostly smaller than their spacing, and rounding to nearest would lose it.
+ * 8-bit states: m and sqrt(v) as e4m3 codes (1 byte an element), each block of GG_ADAMW_BLOCK elements of a tensor,
+ * counted from its start, with a scale of its own: the value is code * scale.  The scales of all tensors follow one
+ * another, ceil(len / GG_ADAMW_BLOCK) for each in the order of the list.  The step updates w from m and v before they
+ * are rounded; the codes are then rounded stochastically (sqrt(v) > 0 never to 0).  A block of which the largest
+ * magnitude is below 2^-110 is stored as zeros.  Zeroed codes and scales are the state before the first step.
+ * The noise of the rounding is Philox4x32-10 at counter (j, j div 2^32, t, segment index) and key `seed`, 128 bits for
+ * elements 8j .. 8j+7 of a segment: the same call gives the same bits. */
+#define GG_ADAMW_BLOCK 256
+typedef struct {
+    int32_t       n_seg;
+    const gg_seg *w;             /* host array [n_seg]: weights, w_dtype                      */
+    int32_t       w_dtype;
+    const gg_seg *g;             /* host array [n_seg]: gradients, g_dtype, same lengths      */
+    int32_t       g_dtype;
+    const gg_seg *w_copy;        /* host array [n_seg] or NULL: the new weights, rounded to nearest
+                                    in bf16 (what the next forward pass reads)                */
+    int32_t       state_bits;    /* 32 or 8                                                   */
+    const gg_seg *m, *v;         /* host arrays [n_seg]: fp32 moments, or codes of m and of sqrt(v) */
+    float        *m_scale, *v_scale;   /* device, state_bits 8 only: one per block            */
+    double        lr, beta1, beta2, eps;   /* lr, eps >= 0; 0 <= beta < 1                     */
+    double        weight_decay;  /* of every segment, if decay is NULL                        */
+    const float  *decay;         /* device [n_seg] or NULL: the decay of each segment         */
+    const float  *grad_scale;    /* device [1] or NULL: 1                                     */
+    int64_t       t;             /* the step, 1-based                                         */
+    uint64_t      seed;          /* of the rounding; bf16 weights and 8-bit states only       */
+} gg_adamw_args;
+gg_status gg_adamw_step(gg_ctx *ctx, const gg_adamw_args *args, void *stream);
+
 /* Optional device timing of the sweeps inside gg_fused (no counterpart in the paper: measurement
  * support).  While enabled, gg_fused records a CUDA event pair on the caller's stream around its
  * first sweep (moments, or the single combined sweep of GG_PARAMS_GIVEN) and around its second

@@ -22,6 +22,7 @@ FLAG_DEGENERATE, FLAG_BETA_CLAMPED_LO, FLAG_BETA_CLAMPED_HI, FLAG_NONFINITE, FLA
 FLAG_TIMEOUT = 32
 HOOK_RESIDENT_MODE, HOOK_EXTRA_ARRIVALS, HOOK_WAIT_CAP, HOOK_CLUSTER_MODE = 0, 1, 2, 3
 BETA_LO, BETA_HI = 0.05, 20.0
+ADAMW_BLOCK = 256          # elements that share one scale of an 8-bit AdamW state
 
 _SEG_DTYPE = np.dtype([("ptr", np.uint64), ("len", np.int64)])
 _P = ctypes.c_void_p
@@ -54,6 +55,35 @@ class ChannelArgs(ctypes.Structure):
         ("accumulate_grad", ctypes.c_int32), ("penalty", _P),
         ("step", ctypes.c_float), ("qmin", ctypes.c_int32), ("qmax", ctypes.c_int32),
         ("hist", _P), ("accumulate_hist", ctypes.c_int32), ("entropy_bits", _P), ("clamped_lo_hi", _P),
+    ]
+
+
+class LayerNormArgs(ctypes.Structure):
+    """Mirror of gg_layer_norm_args."""
+    _fields_ = [
+        ("x", _P), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("x_ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+        ("weight", _P), ("bias", _P), ("w_dtype", ctypes.c_int32), ("eps", ctypes.c_double),
+        ("y", _P), ("y_ld", ctypes.c_int64), ("mean", _P), ("rstd", _P),
+    ]
+
+
+class LayerNormGradArgs(ctypes.Structure):
+    """Mirror of gg_layer_norm_grad_args."""
+    _fields_ = [
+        ("dy", _P), ("x", _P), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("dy_ld", ctypes.c_int64),
+        ("x_ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("mean", _P), ("rstd", _P),
+        ("weight", _P), ("w_dtype", ctypes.c_int32), ("dx", _P), ("dx_ld", ctypes.c_int64),
+        ("dweight", _P), ("dbias", _P), ("accumulate", ctypes.c_int32),
+    ]
+
+
+class AdamwArgs(ctypes.Structure):
+    """Mirror of gg_adamw_args."""
+    _fields_ = [
+        ("n_seg", ctypes.c_int32), ("w", _P), ("w_dtype", ctypes.c_int32), ("g", _P), ("g_dtype", ctypes.c_int32),
+        ("w_copy", _P), ("state_bits", ctypes.c_int32), ("m", _P), ("v", _P), ("m_scale", _P), ("v_scale", _P),
+        ("lr", ctypes.c_double), ("beta1", ctypes.c_double), ("beta2", ctypes.c_double), ("eps", ctypes.c_double),
+        ("weight_decay", ctypes.c_double), ("decay", _P), ("grad_scale", _P), ("t", ctypes.c_int64), ("seed", ctypes.c_uint64),
     ]
 
 
@@ -114,6 +144,12 @@ def lib():
         L.gg_eg_rate_grad.argtypes = [_P, _P, i32, ctypes.c_int, _P, i32, d, i32, i32, _P, ctypes.c_int, ctypes.c_int, _P]
         L.gg_code_stats.argtypes = [_P, _P, i32, i32, i32, i32, _P, _P, _P, _P]
         L.gg_gct_step.argtypes = [_P, _P, i32, ctypes.c_int, _P, _P, _P, i32, i32, i32, d, d, d, i64, _P]
+        L.gg_layer_norm.argtypes = [_P, ctypes.POINTER(LayerNormArgs), _P]
+        L.gg_layer_norm_grad.argtypes = [_P, ctypes.POINTER(LayerNormGradArgs), _P]
+        L.gg_grad_norm.argtypes = [_P, _P, i32, ctypes.c_int, d, _P, _P, _P]
+        L.gg_adamw_step.argtypes = [_P, ctypes.POINTER(AdamwArgs), _P]
+        for name in ("gg_layer_norm", "gg_layer_norm_grad", "gg_grad_norm", "gg_adamw_step"):
+            getattr(L, name).restype = ctypes.c_int
         L.gg_compression_ratio.argtypes = [d, d]
         L.gg_compression_ratio.restype = d
         for name in ("gg_eg_rate", "gg_eg_rate_grad", "gg_code_stats", "gg_gct_step"):
@@ -241,6 +277,11 @@ def _as_segments(x):
 
 def _ptr(t):
     return None if t is None else t.data_ptr()
+
+
+def _ld(t):
+    """Row stride of a 2-D tensor, in elements."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
 def _stream_ptr(device):
@@ -592,6 +633,181 @@ class Context:
             raise TypeError("ghat and w are float32")
         self._check(lib().gg_gct_step(self._h, gs.ptr, len(gs), gs.code, hs.ptr, ws.ptr, _ptr(step), int(k), int(qmin),
                                       int(qmax), float(eta), float(lam), float(eps), int(t), _stream_ptr(self.device)))
+
+    # -------------------------------------------------------------- layer norm
+    def make_layer_norm(self, x, weight=None, bias=None, eps=1e-5, out=None, want_stats=True):
+        """Layer norm over the rows of the 2-D tensor x (rows may be strided: x.stride(1) == 1).
+
+        Allocates the outputs once (y unless `out` is given; it may be x) and returns a callable that enqueues the
+        pass and returns dict(y, mean, rstd); mean and rstd (float32 per row) are what the gradient needs."""
+        rows, cols = self._rows(x, "x")
+        y = self._new(x.shape, x.dtype) if out is None else out
+        self._rows(y, "out", x)
+        res = dict(y=y, mean=self._new(rows, torch.float32) if want_stats else None,
+                   rstd=self._new(rows, torch.float32) if want_stats else None)
+        a = LayerNormArgs()
+        a.x, a.rows, a.cols, a.x_ld, a.dtype = _ptr(x), rows, cols, _ld(x), _dtype_code(x.dtype)
+        a.weight, a.bias, a.w_dtype = self._affine(cols, weight, bias)
+        a.eps, a.y, a.y_ld, a.mean, a.rstd = float(eps), _ptr(y), _ld(y), _ptr(res["mean"]), _ptr(res["rstd"])
+        return self._callable("gg_layer_norm", a, res, [x, weight, bias, y])
+
+    def gg_layer_norm(self, x, weight=None, bias=None, **kw):
+        """One-shot form of make_layer_norm(...)()."""
+        return self.make_layer_norm(x, weight, bias, **kw)()
+
+    def make_layer_norm_grad(self, dy, x, mean, rstd, weight=None, dx=None, dweight=None, dbias=None, want_dx=True,
+                             want_dweight=None, accumulate=False):
+        """Gradient of layer norm for dy, the x of the forward pass and the mean and rstd that it returned.
+
+        Allocates dx (like x, unless given; it may be dy or x) and dweight, dbias (float32 [cols], unless given) once
+        and returns a callable that enqueues the pass and returns dict(dx, dweight, dbias).  want_dweight: None = if
+        there is a weight or a tensor for the sums; accumulate adds to dweight and dbias instead of overwriting."""
+        rows, cols = self._rows(x, "x")
+        self._rows(dy, "dy", x)
+        for name, t in (("mean", mean), ("rstd", rstd)):
+            self._vector(name, t, rows)
+        if dx is None and want_dx:
+            dx = self._new(x.shape, x.dtype)
+        if dx is not None:
+            self._rows(dx, "dx", x)
+        if want_dweight is None:
+            want_dweight = weight is not None
+        if accumulate and want_dweight and (dweight is None or dbias is None):
+            raise ValueError("accumulate adds to dweight and dbias: give both")
+        if want_dweight:
+            dweight = self._new(cols, torch.float32) if dweight is None else dweight
+            dbias = self._new(cols, torch.float32) if dbias is None else dbias
+        for name, t in (("dweight", dweight), ("dbias", dbias)):
+            if t is not None:
+                self._vector(name, t, cols)
+        a = LayerNormGradArgs()
+        a.dy, a.x, a.rows, a.cols, a.dy_ld, a.x_ld, a.dtype = _ptr(dy), _ptr(x), rows, cols, _ld(dy), _ld(x), _dtype_code(x.dtype)
+        a.mean, a.rstd = _ptr(mean), _ptr(rstd)
+        a.weight, _, a.w_dtype = self._affine(cols, weight, None)
+        a.dx, a.dx_ld = _ptr(dx), cols if dx is None else _ld(dx)
+        a.dweight, a.dbias, a.accumulate = _ptr(dweight), _ptr(dbias), int(bool(accumulate))
+        return self._callable("gg_layer_norm_grad", a, dict(dx=dx, dweight=dweight, dbias=dbias), [dy, x, mean, rstd, weight])
+
+    def gg_layer_norm_grad(self, dy, x, mean, rstd, weight=None, **kw):
+        """One-shot form of make_layer_norm_grad(...)()."""
+        return self.make_layer_norm_grad(dy, x, mean, rstd, weight, **kw)()
+
+    def _rows(self, t, name, like=None):
+        if t.dim() != 2 or (t.shape[1] > 1 and t.stride(1) != 1) or (t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name} must be 2-D with contiguous rows")
+        if t.device.type != "cuda":
+            raise ValueError(f"{name} must be a CUDA tensor")
+        if like is not None and (t.shape != like.shape or t.dtype != like.dtype):
+            raise ValueError(f"{name} must have the shape and dtype of x")
+        return t.shape
+
+    def _vector(self, name, t, n, dtype=torch.float32):
+        if t.device.type != "cuda" or t.dtype != dtype or t.numel() != n or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous CUDA tensor of {n} {dtype} values")
+
+    def _affine(self, cols, weight, bias):
+        given = [t for t in (weight, bias) if t is not None]
+        for t in given:
+            self._vector("weight and bias", t, cols, given[0].dtype)
+        return _ptr(weight), _ptr(bias), _dtype_code(given[0].dtype) if given else GG_F32
+
+    def _callable(self, entry, a, res, keep):
+        call, arg = getattr(lib(), entry), ctypes.byref(a)
+
+        def run():
+            self._check(call(self._h, arg, _stream_ptr(self.device)))
+            return res
+
+        run.outputs = res
+        run.args = a
+        run._keep = keep
+        return run
+
+    # ------------------------------------------------- gradient norm and AdamW
+    def gg_grad_norm(self, g, max_norm=float("inf"), out=None):
+        """dict(norm, scale), on the device: the norm of all segments together (float64) and min(1, max_norm / norm)
+        (float32), both nan if an entry is not finite."""
+        segs = _as_segments(g)
+        if out is None:
+            out = dict(norm=self._new(1, torch.float64), scale=self._new(1, torch.float32))
+        self._check(lib().gg_grad_norm(self._h, segs.ptr, len(segs), segs.code, float(max_norm), _ptr(out["norm"]),
+                                       _ptr(out["scale"]), _stream_ptr(self.device)))
+        return out
+
+    def adamw_state(self, w, bits=32):
+        """The state before the first step for the segments w: dict(m, v) of lists of tensors, with 8 bits also
+        scales = (m_scale, v_scale).  The keys are arguments of make_adamw_step."""
+        segs = _as_segments(w)
+        if bits not in (32, 8):
+            raise ValueError("states have 32 or 8 bits")
+        dtype = torch.float32 if bits == 32 else torch.float8_e4m3fn
+        lens = [int(n) for n in segs.lens]
+        out = {k: [torch.zeros(n, dtype=dtype, device=self.device) for n in lens] for k in ("m", "v")}
+        if bits == 8:
+            blocks = sum(-(-n // ADAMW_BLOCK) for n in lens)
+            out["scales"] = tuple(torch.zeros(blocks, dtype=torch.float32, device=self.device) for _ in range(2))
+        return out
+
+    def make_adamw_step(self, w, g, m, v, scales=None, w_copy=None, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
+                        max_norm=None, grad_scale=None, seed=0):
+        """Returns step(t, lr), which enqueues one AdamW step over all segments, in place.
+
+        w (float32 or bfloat16), g (float32 or bfloat16) and the states m, v (float32; float8_e4m3fn with `scales`)
+        are lists of tensors or Segments of the same lengths; w_copy: bfloat16 segments that get the new weights.
+        weight_decay: a number, or a float32 device tensor with one entry per segment.  max_norm clips the gradient
+        by its global norm first; grad_scale (float32 [1], on the device) scales it instead.  seed: of the rounding of
+        bfloat16 weights and 8-bit states.  step returns dict(norm, scale) (of the clipping, else empty)."""
+        ws, gs, ms, vs = (_as_segments(t) for t in (w, g, m, v))
+        cs = None if w_copy is None else _as_segments(w_copy)
+        states = (torch.float32,) if scales is None else (torch.float8_e4m3fn, torch.uint8)
+        if ms.dtype not in states or vs.dtype not in states:
+            raise TypeError("m and v are float32, or float8_e4m3fn with scales")
+        if cs is not None and cs.dtype != torch.bfloat16:
+            raise TypeError("w_copy is bfloat16")
+        if max_norm is not None and grad_scale is not None:
+            raise ValueError("max_norm or grad_scale, not both")
+        for name, t in (("g", gs), ("m", ms), ("v", vs), ("w_copy", cs)):
+            if t is not None and not np.array_equal(t.lens, ws.lens):
+                raise ValueError(f"{name} must have the lengths of w")
+        a = AdamwArgs()
+        a.n_seg, a.w, a.w_dtype, a.g, a.g_dtype = len(ws), ws.ptr, ws.code, gs.ptr, gs.code
+        a.w_copy = None if cs is None else cs.ptr
+        a.state_bits, a.m, a.v = 32 if scales is None else 8, ms.ptr, vs.ptr
+        if scales is not None:
+            blocks = int((-(-ws.lens // ADAMW_BLOCK)).sum())
+            for name, t in zip(("m_scale", "v_scale"), scales, strict=True):
+                self._vector(name, t, blocks)
+            a.m_scale, a.v_scale = _ptr(scales[0]), _ptr(scales[1])
+        a.beta1, a.beta2, a.eps, a.seed = float(beta1), float(beta2), float(eps), int(seed) & (2 ** 64 - 1)
+        if isinstance(weight_decay, torch.Tensor):
+            self._vector("weight_decay", weight_decay, len(ws))
+            a.decay = _ptr(weight_decay)
+        else:
+            a.weight_decay = float(weight_decay)
+        out = {}
+        if max_norm is not None:
+            out = dict(norm=self._new(1, torch.float64), scale=self._new(1, torch.float32))
+            grad_scale = out["scale"]
+        if grad_scale is not None:
+            self._vector("grad_scale", grad_scale, 1)
+            a.grad_scale = _ptr(grad_scale)
+        call, arg = lib().gg_adamw_step, ctypes.byref(a)
+
+        def step(t, lr):
+            if max_norm is not None:
+                self.gg_grad_norm(gs, max_norm, out)
+            a.t, a.lr = int(t), float(lr)
+            self._check(call(self._h, arg, _stream_ptr(self.device)))
+            return out
+
+        step.outputs = out
+        step.args = a
+        step._keep = [ws, gs, ms, vs, cs, scales, weight_decay, grad_scale]
+        return step
+
+    def gg_adamw_step(self, w, g, m, v, t, lr, **kw):
+        """One-shot form of make_adamw_step(...)(t, lr)."""
+        return self.make_adamw_step(w, g, m, v, **kw)(t, lr)
 
     # ------------------------------------------------------------------ timing
     def timing_enable(self, on=True):

@@ -14,6 +14,7 @@
 
 #include <nvtx3/nvToolsExt.h>
 
+#include "gg_adamw.cuh"
 #include "gg_internal.h"
 
 using namespace gg;
@@ -86,6 +87,8 @@ struct gg_ctx {
     uint32_t *small_counts = nullptr;   // scratch of the short-segment kernel: one slot of count cells per CTA
     void *chan_buf = nullptr;     // scratch of gg_fused_channels (partials per row block and column)
     int64_t chan_bytes = 0;
+    void *norm_part = nullptr;    // scratch of gg_layer_norm_grad (partial sums over the rows)
+    int64_t norm_part_bytes = 0;
     double *seed = nullptr;       // device table that seeds the moment-ratio inversion of the short-segment kernel
     int resident_grid[2][8];      // CTAs the one-launch pass may use, by gradient type and sweep flags (-1: not asked yet)
     bool can_cooperate = false, can_cluster = false;
@@ -614,6 +617,7 @@ gg_status gg_destroy(gg_ctx *ctx)
     if (ctx->seed) cudaFree(ctx->seed);
     if (ctx->small_counts) cudaFree(ctx->small_counts);
     if (ctx->chan_buf) cudaFree(ctx->chan_buf);
+    if (ctx->norm_part) cudaFree(ctx->norm_part);
     if (ctx->ent_part) cudaFree(ctx->ent_part);
     if (ctx->ent_done) cudaFree(ctx->ent_done);
     delete ctx;
@@ -1487,6 +1491,186 @@ gg_status gg_gct_step(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype g_dt
     mark_used(pg, static_cast<cudaStream_t>(stream));
     mark_used(pw, static_cast<cudaStream_t>(stream));
     return GG_OK;
+}
+
+}  // extern "C"
+
+// ---- layer norm, gradient norm, AdamW
+
+namespace {
+
+// A matrix of `dtype` elements: null, misaligned or with too short a stride?
+gg_status check_matrix(const void *p, int64_t rows, int64_t cols, int64_t ld, int dtype)
+{
+    if (ld < cols) return GG_ERR_INVALID_ARG;
+    if (rows > 0 && cols > 0 && p == nullptr) return GG_ERR_INVALID_ARG;
+    return reinterpret_cast<uintptr_t>(p) % esize(dtype) != 0 ? GG_ERR_ALIGNMENT : GG_OK;
+}
+
+gg_status check_f32(const float *p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0 ? GG_ERR_ALIGNMENT : GG_OK; }
+
+// The entries of `list` have the lengths of `w`, a pointer where there is something, and the alignment of their type.
+gg_status check_list(const gg_seg *w, const gg_seg *list, int32_t n_seg, size_t element)
+{
+    for (int32_t s = 0; s < n_seg; ++s) {
+        if (list[s].len != w[s].len || (list[s].len > 0 && list[s].ptr == nullptr)) return GG_ERR_INVALID_ARG;
+        if (reinterpret_cast<uintptr_t>(list[s].ptr) % element != 0) return GG_ERR_ALIGNMENT;
+    }
+    return GG_OK;
+}
+
+// Fills the table with the non-empty tensors from `s` on, and returns the first that did not fit.  `block` is the
+// scale of the first block of tensor s; on return that of the next tensor.
+template <int N>
+int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int32_t s, int64_t &block)
+{
+    tab.n = 0;
+    tab.tile0[0] = 0;
+    for (; s < a.n_seg; ++s) {
+        const int64_t len = a.w[s].len, blocks = (len + kBlock - 1) / kBlock;
+        if (len == 0) continue;
+        const int64_t tiles = (blocks + kTileBlocks - 1) / kTileBlocks;
+        if (tab.n == N || tab.tile0[tab.n] + tiles > 0x7FFFFFFFll) break;
+        const int i = tab.n++;
+        tab.w[i] = a.w[s].ptr; tab.g[i] = a.g[s].ptr; tab.m[i] = a.m[s].ptr; tab.v[i] = a.v[s].ptr;
+        tab.copy[i] = a.w_copy ? a.w_copy[s].ptr : nullptr;
+        tab.len[i] = len;
+        tab.block0[i] = (int32_t)block;
+        tab.id[i] = s;
+        tab.tile0[i + 1] = (int32_t)(tab.tile0[i] + tiles);
+        block += blocks;
+    }
+    return s;
+}
+
+template <int N>
+gg_status run_adamw(gg_ctx *ctx, const gg_adamw_args &a, const StepScalars &c, cudaStream_t cs)
+{
+    StepTable<N> tab;
+    int64_t block = 0;
+    for (int32_t s = 0; s < a.n_seg;) {
+        s = fill_table(tab, a, s, block);
+        if (tab.n == 0) break;
+        GG_CUDA(ctx, launch_adamw(tab, c, a.w_dtype, a.g_dtype, a.state_bits == 8, cs));
+        ctx->launches += 1;
+    }
+    return GG_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gg_status gg_layer_norm(gg_ctx *ctx, const gg_layer_norm_args *a, void *stream)
+{
+    if (!ctx || !a || a->rows < 0 || a->cols < 0 || !(a->eps >= 0.0)) return GG_ERR_INVALID_ARG;
+    if (!dtype_ok(a->dtype) || ((a->weight || a->bias) && !dtype_ok(a->w_dtype))) return GG_ERR_DTYPE;
+    gg_status st = check_matrix(a->x, a->rows, a->cols, a->x_ld, a->dtype);
+    if (st == GG_OK) st = check_matrix(a->y, a->rows, a->cols, a->y_ld, a->dtype);
+    if (st == GG_OK && (reinterpret_cast<uintptr_t>(a->weight) | reinterpret_cast<uintptr_t>(a->bias)) % esize(a->w_dtype) != 0)
+        st = GG_ERR_ALIGNMENT;
+    if (st == GG_OK) st = check_f32(a->mean);
+    if (st == GG_OK) st = check_f32(a->rstd);
+    if (st != GG_OK) return st;
+    if (a->rows == 0 || a->cols == 0) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    GG_CUDA(ctx, launch_layer_norm(*a, static_cast<cudaStream_t>(stream)));
+    ctx->launches += 1;
+    return GG_OK;
+}
+
+gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *a, void *stream)
+{
+    if (!ctx || !a || a->rows < 0 || a->cols < 0) return GG_ERR_INVALID_ARG;
+    if (!dtype_ok(a->dtype) || (a->weight && !dtype_ok(a->w_dtype))) return GG_ERR_DTYPE;
+    gg_status st = check_matrix(a->x, a->rows, a->cols, a->x_ld, a->dtype);
+    if (st == GG_OK) st = check_matrix(a->dy, a->rows, a->cols, a->dy_ld, a->dtype);
+    if (st == GG_OK && a->dx) st = check_matrix(a->dx, a->rows, a->cols, a->dx_ld, a->dtype);
+    if (st == GG_OK && a->rows > 0 && a->cols > 0 && (!a->mean || !a->rstd)) st = GG_ERR_INVALID_ARG;
+    if (st == GG_OK && a->weight && reinterpret_cast<uintptr_t>(a->weight) % esize(a->w_dtype) != 0) st = GG_ERR_ALIGNMENT;
+    for (const float *p : {a->mean, a->rstd, (const float *)a->dweight, (const float *)a->dbias})
+        if (st == GG_OK) st = check_f32(p);
+    if (st != GG_OK) return st;
+    if (a->cols == 0 || (!a->dx && !a->dweight && !a->dbias)) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    const int slices = layer_norm_grad_slices(a->rows, a->cols, ctx->sm_count);
+    if (a->dweight || a->dbias) {
+        st = grow(ctx, &ctx->norm_part, &ctx->norm_part_bytes, (int64_t)sizeof(float) * 2 * slices * a->cols);
+        if (st != GG_OK) return st;
+    }
+    int launches = 0;
+    GG_CUDA(ctx, launch_layer_norm_grad(*a, static_cast<float *>(ctx->norm_part), slices, &launches, static_cast<cudaStream_t>(stream)));
+    ctx->launches += launches;
+    return GG_OK;
+}
+
+gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dtype, double max_norm, double *norm, float *scale,
+                       void *stream)
+{
+    if (!ctx || !(max_norm > 0.0)) return GG_ERR_INVALID_ARG;
+    gg_status st = check_segs(g, n_seg, dtype);
+    if (st == GG_OK && reinterpret_cast<uintptr_t>(norm) % 8 != 0) st = GG_ERR_ALIGNMENT;
+    if (st == GG_OK) st = check_f32(scale);
+    if (st != GG_OK) return st;
+    if (!norm && !scale) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    // the squares are summed tile by tile by the moments sweep of the fit
+    Plan *p = nullptr;
+    if (n_seg > 0) {
+        st = get_plan(ctx, g, n_seg, dtype, nullptr, 0, nullptr, &p, stream);
+        if (st != GG_OK) return st;
+        StreamArgs sa{};
+        sa.map = p->map;
+        sa.part = p->part;
+        GG_CUDA(ctx, launch_sweep(ctx, kMoments, dtype, GG_F32, false, sa, cs));
+        ctx->launches += p->n_tiles > 0;
+    }
+    GG_CUDA(ctx, launch_grad_norm(p ? p->part.s2 : nullptr, p ? p->part.bad : nullptr, p ? p->n_tiles : 0, max_norm, norm, scale, cs));
+    ctx->launches += 1;
+    mark_used(p, cs);
+    return GG_OK;
+}
+
+gg_status gg_adamw_step(gg_ctx *ctx, const gg_adamw_args *a, void *stream)
+{
+    if (!ctx || !a || a->n_seg < 0 || (a->n_seg > 0 && (!a->w || !a->g || !a->m || !a->v))) return GG_ERR_INVALID_ARG;
+    if (a->state_bits != 32 && a->state_bits != 8) return GG_ERR_INVALID_ARG;
+    if (!(a->lr >= 0.0) || !isfinite(a->lr) || !(a->eps >= 0.0) || !isfinite(a->weight_decay) || a->t < 1) return GG_ERR_INVALID_ARG;
+    if (!(a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0)) return GG_ERR_INVALID_ARG;
+    if (!dtype_ok(a->w_dtype) || !dtype_ok(a->g_dtype)) return GG_ERR_DTYPE;
+    gg_status st = check_segs(a->w, a->n_seg, a->w_dtype);
+    const size_t state = a->state_bits == 8 ? 1 : 4;
+    if (st == GG_OK) st = check_list(a->w, a->g, a->n_seg, esize(a->g_dtype));
+    if (st == GG_OK) st = check_list(a->w, a->m, a->n_seg, state);
+    if (st == GG_OK) st = check_list(a->w, a->v, a->n_seg, state);
+    if (st == GG_OK && a->w_copy) st = check_list(a->w, a->w_copy, a->n_seg, 2);
+    for (const float *p : {a->decay, a->grad_scale, (const float *)a->m_scale, (const float *)a->v_scale})
+        if (st == GG_OK) st = check_f32(p);
+    if (st != GG_OK) return st;
+    int64_t blocks = 0, full = 0;
+    for (int32_t s = 0; s < a->n_seg; ++s) {
+        blocks += (a->w[s].len + kBlock - 1) / kBlock;
+        full += a->w[s].len > 0;
+    }
+    if (full == 0) return GG_OK;
+    if (blocks > 0x7FFFFFFFll) return GG_ERR_WORKSPACE;
+    if (a->state_bits == 8 && (!a->m_scale || !a->v_scale)) return GG_ERR_INVALID_ARG;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    StepScalars c{};
+    c.grad_scale = a->grad_scale; c.decay = a->decay; c.m_scale = a->m_scale; c.v_scale = a->v_scale;
+    c.b1 = (float)a->beta1; c.one_b1 = (float)(1.0 - a->beta1);
+    c.b2 = (float)a->beta2; c.one_b2 = (float)(1.0 - a->beta2);
+    c.lr = (float)a->lr; c.decay_all = (float)a->weight_decay; c.eps = (float)a->eps;
+    c.step = (float)(a->lr / (1.0 - pow(a->beta1, (double)a->t)));
+    c.root = (float)(1.0 / sqrt(1.0 - pow(a->beta2, (double)a->t)));
+    c.t = (uint32_t)a->t; c.seed_lo = (uint32_t)a->seed; c.seed_hi = (uint32_t)(a->seed >> 32);
+    cudaStream_t cs = static_cast<cudaStream_t>(stream);
+    return full <= kTableSmall ? run_adamw<kTableSmall>(ctx, *a, c, cs) : run_adamw<kTableLarge>(ctx, *a, c, cs);
 }
 
 }  // extern "C"

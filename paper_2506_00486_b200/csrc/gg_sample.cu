@@ -11,33 +11,13 @@
 #include <cuda_bf16.h>
 
 #include "gg_internal.h"
+#include "gg_philox.cuh"
 
 namespace gg {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr uint32_t kMaxAttempts = 64;
-
-struct Block4 { uint32_t w0, w1, w2, w3; };
-
-// Philox4x32 with 10 rounds (Salmon et al., SC'11).
-__device__ __forceinline__ Block4 philox4x32_10(uint32_t c0, uint32_t c1, uint32_t c2, uint32_t c3,
-                                                uint32_t k0, uint32_t k1)
-{
-    constexpr uint32_t M0 = 0xD2511F53u, M1 = 0xCD9E8D57u, W0 = 0x9E3779B9u, W1 = 0xBB67AE85u;
-#pragma unroll
-    for (int r = 0; r < 10; ++r) {
-        const uint32_t hi0 = __umulhi(M0, c0), lo0 = M0 * c0;
-        const uint32_t hi1 = __umulhi(M1, c2), lo1 = M1 * c2;
-        c0 = hi1 ^ c1 ^ k0;
-        c1 = lo1;
-        c2 = hi0 ^ c3 ^ k1;
-        c3 = lo0;
-        k0 += W0;
-        k1 += W1;
-    }
-    return Block4{c0, c1, c2, c3};
-}
 
 __device__ __forceinline__ double u01(uint32_t r) { return ((double)r + 0.5) * (1.0 / 4294967296.0); }
 
