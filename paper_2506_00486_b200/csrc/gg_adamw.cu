@@ -15,6 +15,8 @@
 // The random bits come from Philox4x32-10 at counter (j, j / 2^32, t, tensor) and key = seed; a block serves the
 // elements 8 j .. 8 j + 7 of a tensor with 16 bits u each: element e takes u[e] for m, u[e + 4] for r and u[e + 2]
 // for w (indices modulo 8), so that the three roundings of one element are independent.
+#include <cuda_fp16.h>
+
 #include "gg_adamw.cuh"
 #include "gg_device.cuh"
 #include "gg_element.cuh"
@@ -73,6 +75,17 @@ __device__ __forceinline__ float block_top(const float (&x)[kPerLane])
     return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, top));
 }
 
+// The scale of a block and what its values are multiplied by.
+struct BlockScale {
+    float scale, inv;
+    __device__ __forceinline__ explicit BlockScale(float top)
+    {
+        const bool fits = top > 0x1p-110f;
+        inv = fits ? __fdiv_rn(448.0f, top) : 0.0f;
+        scale = fits ? __fmul_rn(top, 1.0f / 448.0f) : 0.0f;
+    }
+};
+
 // x times `inv` (448 / top, or 0) as an e4m3 code.  Below 2^-6 the codes are spaced like the binade above it: adding
 // 2^-6 puts both cases on one grid of 2^20 units of the fp32 pattern.  A value that was inf or nan becomes nan.
 __device__ __forceinline__ uint8_t e4m3_stochastic(float x, float inv, uint32_t u, bool keep_above_zero)
@@ -95,84 +108,302 @@ __device__ __forceinline__ float e4m3_value(uint8_t code)
     return __uint_as_float(__float_as_uint(a) | s);
 }
 
-// One warp per block of kBlock elements, lane l at elements l, l + 32, ...: any alignment.
+// What a warp knows of the block of elements that it steps.
+template <typename TW, typename TG>
+struct BlockAt {
+    TW *w;
+    const TG *g;
+    void *m, *v;          // float or codes
+    uint16_t *copy;       // or null
+    float *m_scale, *v_scale;
+    uint64_t block;       // of the tensor
+    uint32_t id;
+    int n;                // elements, <= kBlock
+};
+
+template <typename TW, typename TG, bool kNarrow>
+constexpr bool kNoise = kNarrow || sizeof(TW) == 2;
+
+template <typename TW, typename TG>
+__device__ __forceinline__ Block4 block_noise(const BlockAt<TW, TG> &at, const StepScalars &c)
+{
+    const uint64_t j = at.block * 32u + (threadIdx.x & 31);
+    return philox4x32_10((uint32_t)j, (uint32_t)(j >> 32), c.t, at.id, c.seed_lo, c.seed_hi);
+}
+
+// Any alignment, any length, any values: lane l takes the elements l, l + 32, ...
+template <typename TW, typename TG, bool kNarrow>
+__device__ __noinline__ void step_block_any(const BlockAt<TW, TG> at, const StepScalars &c, float keep, float gscale, uint32_t *noise)
+{
+    const int lane = threadIdx.x & 31;
+    const uint16_t *u = reinterpret_cast<const uint16_t *>(noise);
+    if (kNoise<TW, TG, kNarrow>) {
+        const Block4 q = block_noise(at, c);
+        __syncwarp();
+        reinterpret_cast<uint4 *>(noise)[lane] = make_uint4(q.w0, q.w1, q.w2, q.w3);
+        __syncwarp();
+    }
+    uint8_t *m8 = static_cast<uint8_t *>(at.m), *v8 = static_cast<uint8_t *>(at.v);
+    float *m32 = static_cast<float *>(at.m), *v32 = static_cast<float *>(at.v);
+    const float m_scale = kNarrow ? *at.m_scale : 1.0f, v_scale = kNarrow ? *at.v_scale : 1.0f;
+    float mm[kPerLane], rr[kPerLane];
+#pragma unroll
+    for (int k = 0; k < kPerLane; ++k) {
+        const int e = 32 * k + lane;
+        mm[k] = rr[k] = 0.0f;
+        if (e >= at.n) continue;
+        float m, v;
+        if (kNarrow) {
+            m = __fmul_rn(e4m3_value(m8[e]), m_scale);
+            v = __fmul_rn(e4m3_value(v8[e]), v_scale);
+            v = __fmul_rn(v, v);
+        } else {
+            m = m32[e];
+            v = v32[e];
+        }
+        const Element x = adamw_element(c, keep, widen<TW>(at.w[e]), __fmul_rn(widen<TG>(at.g[e]), gscale), m, v);
+        if (sizeof(TW) == 2) reinterpret_cast<uint16_t *>(at.w)[e] = bf16_stochastic(x.w, u[(e & ~7) + ((e + 2) & 7)]);
+        else reinterpret_cast<float *>(at.w)[e] = x.w;
+        if (at.copy) at.copy[e] = narrow<uint16_t>(x.w);
+        if (kNarrow) {
+            mm[k] = x.m;
+            rr[k] = x.r;
+        } else {
+            m32[e] = x.m;
+            v32[e] = x.v;
+        }
+    }
+    if (kNarrow) {
+        const BlockScale ms(block_top(mm)), vs(block_top(rr));
+#pragma unroll
+        for (int k = 0; k < kPerLane; ++k) {
+            const int e = 32 * k + lane;
+            if (e >= at.n) continue;
+            m8[e] = e4m3_stochastic(mm[k], ms.inv, u[e], false);
+            v8[e] = e4m3_stochastic(rr[k], vs.inv, u[(e & ~7) + ((e + 4) & 7)], true);
+        }
+        if (lane == 0) {
+            *at.m_scale = ms.scale;
+            *at.v_scale = vs.scale;
+        }
+    }
+}
+
+// A whole block at vector boundaries: lane l takes the eight elements from 8 l on, in pairs.
+template <typename TW, typename TG, bool kNarrow>
+struct FastBlock;
+
+// States in fp32: bound by memory with room to spare, so the arithmetic is the plain one.
+template <typename TW, typename TG>
+struct FastBlock<TW, TG, false> {
+    Eight<TW> w;
+    Eight<TG> g;
+    Eight<float> m, v;
+    __device__ __forceinline__ void load(const BlockAt<TW, TG> &at)
+    {
+        const int e = 8 * (threadIdx.x & 31);
+        g.load(at.g + e);
+        w.load(at.w + e);
+        m.load(static_cast<const float *>(at.m) + e);
+        v.load(static_cast<const float *>(at.v) + e);
+    }
+    __device__ __forceinline__ void step(const BlockAt<TW, TG> &at, const StepScalars &c, float keep, float gscale, uint32_t *)
+    {
+        const int e = 8 * (threadIdx.x & 31);
+        f32x2 wn[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 wf = halves(w.get(i)), gf = halves(g.get(i)), mf = halves(m.get(i)), vf = halves(v.get(i));
+            const Element x = adamw_element(c, keep, wf.x, __fmul_rn(gf.x, gscale), mf.x, vf.x);
+            const Element y = adamw_element(c, keep, wf.y, __fmul_rn(gf.y, gscale), mf.y, vf.y);
+            wn[i] = pair(x.w, y.w);
+            m.v[i] = pair(x.m, y.m);
+            v.v[i] = pair(x.v, y.v);
+        }
+        Eight<float>::store(static_cast<float *>(at.m) + e, m.v);
+        Eight<float>::store(static_cast<float *>(at.v) + e, v.v);
+        if (sizeof(TW) == 2) {
+            const Block4 q = block_noise(at, c);
+            const uint32_t word[4] = {q.w1, q.w2, q.w3, q.w0};      // element e takes u[e + 2]
+            uint32_t out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 f = halves(wn[i]);
+                out[i] = (uint32_t)bf16_stochastic(f.x, word[i] & 0xFFFFu) | ((uint32_t)bf16_stochastic(f.y, word[i] >> 16) << 16);
+            }
+            Eight<uint16_t>::store_words(reinterpret_cast<uint16_t *>(at.w) + e, out[0], out[1], out[2], out[3]);
+        } else {
+            Eight<float>::store(reinterpret_cast<float *>(at.w) + e, wn);
+        }
+        if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
+    }
+};
+
+// The two e4m3 codes of a 16-bit half.
+__device__ __forceinline__ f32x2 e4m3_pair(uint32_t h)
+{
+    uint32_t d;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)h));
+    const __half2 t = *reinterpret_cast<const __half2 *>(&d);
+    const float2 f = __half22float2(t);
+    return pair(f.x, f.y);
+}
+
+// sqrt of finite values >= 0: an approximate reciprocal root and one Newton step, s + (v - s^2) / (2 sqrt(v)), which
+// leaves the rounding of the last sum (and, once in about a million, the neighbour of the nearest value).  Below
+// 2^-126 the result is only of the right size; the step divides by the root plus eps, so nothing there matters.
+__device__ __forceinline__ f32x2 sqrt2(f32x2 v)
+{
+    const float2 f = halves(v);
+    float a, b;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(f.x));
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(f.y));
+    const f32x2 y = pair(fminf(a, 0x1p63f), fminf(b, 0x1p63f));       // (infinite at 0)
+    const f32x2 s = mul2(v, y);
+    const float2 sf = halves(s);
+    const f32x2 e = fma2(pair(-sf.x, -sf.y), s, v);
+    return fma2(e, mul2(y, both(0.5f)), s);
+}
+
+// States in 8 bits move 10 to 14 bytes an element, in which time an SM can issue about 50 instructions for it: here the
+// arithmetic is what counts, and everything goes in pairs.  Codes: multiplied by 2^-120 the range of e4m3 becomes that
+// of the smallest fp32 numbers, subnormals on subnormals, and a code is bits 20 .. 26 of the fp32 pattern.  A block that
+// holds an inf or nan goes through step_block_any (nothing is stored before that is known).
+template <typename TW, typename TG>
+struct FastBlock<TW, TG, true> {
+    Eight<TW> w;
+    Eight<TG> g;
+    uint2 m, v;
+    float m_scale, v_scale;
+    __device__ __forceinline__ void load(const BlockAt<TW, TG> &at)
+    {
+        const int e = 8 * (threadIdx.x & 31);
+        g.load(at.g + e);
+        w.load(at.w + e);
+        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(m.x), "=r"(m.y) : "l"(static_cast<const uint8_t *>(at.m) + e));
+        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(static_cast<const uint8_t *>(at.v) + e));
+        m_scale = *at.m_scale;
+        v_scale = *at.v_scale;
+    }
+    // codes of the four values whose scaled patterns (plus noise) are t: seven bits each in order, and their signs
+    static __device__ __forceinline__ uint32_t pack(const uint32_t (&t)[4], bool with_sign)
+    {
+        const uint32_t lo = __byte_perm(t[0], t[1], 0x7632), hi = __byte_perm(t[2], t[3], 0x7632);
+        uint32_t c = __byte_perm(lo >> 4 & 0x007F007Fu, hi >> 4 & 0x007F007Fu, 0x6420);
+        c -= (c + 0x01010101u & 0x80808080u) >> 7;       // 127 is nan: the largest code is 126
+        if (with_sign) c |= __byte_perm(lo, hi, 0x7531) & 0x80808080u;
+        return c;
+    }
+    __device__ __forceinline__ void step(const BlockAt<TW, TG> &at, const StepScalars &c, float keep, float gscale, uint32_t *noise)
+    {
+        const int lane = threadIdx.x & 31, e = 8 * lane;
+        f32x2 wn[4], mn[4], rn[4];
+        f32x2 sum = 0;
+        uint32_t m_top = 0, r_top = 0;
+        const f32x2 b1 = both(c.b1), one_b1 = both(c.one_b1), b2 = both(c.b2), one_b2 = both(c.one_b2), gs = both(gscale);
+        const f32x2 ms = both(m_scale), vs = both(v_scale), root = both(c.root), eps = both(c.eps), step = both(-c.step), keep2 = both(keep);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t mw = i < 2 ? m.x : m.y, vw = i < 2 ? v.x : v.y;
+            const f32x2 gi = mul2(g.get(i), gs);
+            const f32x2 mo = mul2(e4m3_pair(i & 1 ? mw >> 16 : mw), ms), ro = mul2(e4m3_pair(i & 1 ? vw >> 16 : vw), vs);
+            mn[i] = add2(mul2(b1, mo), mul2(one_b1, gi));
+            rn[i] = sqrt2(add2(mul2(b2, mul2(ro, ro)), mul2(one_b2, mul2(gi, gi))));
+            const float2 d = halves(fma2(rn[i], root, eps));
+            wn[i] = fma2(step, mul2(mn[i], pair(rcp_approx(d.x), rcp_approx(d.y))), mul2(w.get(i), keep2));
+            sum = i == 0 ? wn[0] : add2(sum, wn[i]);
+            const float2 mf = halves(mn[i]), rf = halves(rn[i]);
+            m_top = max(m_top, max(__float_as_uint(mf.x) & 0x7FFFFFFFu, __float_as_uint(mf.y) & 0x7FFFFFFFu));
+            r_top = max(r_top, max(__float_as_uint(rf.x), __float_as_uint(rf.y)));       // (>= 0, or the positive nan of an operation)
+        }
+        const float2 sf = halves(sum);
+        if (!isfinite(sf.x + sf.y)) m_top = 0x7F800000u;
+        m_top = __reduce_max_sync(0xFFFFFFFFu, m_top);
+        r_top = __reduce_max_sync(0xFFFFFFFFu, r_top);
+        if (max(m_top, r_top) >= 0x7F800000u) {
+            step_block_any<TW, TG, true>(at, c, keep, gscale, noise);
+            return;
+        }
+        const BlockScale m_to(__uint_as_float(m_top)), v_to(__uint_as_float(r_top));
+        const Block4 q = block_noise(at, c);
+        const uint32_t word[4] = {q.w0, q.w1, q.w2, q.w3};
+        uint32_t u[8], mt[8], vt[8];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            u[2 * i] = word[i] << 4 & 0xFFFF0u | 8u;
+            u[2 * i + 1] = word[i] >> 12 & 0xFFFF0u | 8u;
+        }
+        const f32x2 m_inv = both(m_to.inv), v_inv = both(v_to.inv), down = both(0x1p-120f);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 zm = halves(mul2(mul2(mn[i], m_inv), down)), zr = halves(mul2(mul2(rn[i], v_inv), down)), rf = halves(rn[i]);
+            mt[2 * i] = __float_as_uint(zm.x) + u[2 * i];
+            mt[2 * i + 1] = __float_as_uint(zm.y) + u[2 * i + 1];
+            // (a root that is not 0 is above 2^-75, so its pattern is above that of code 1; a block below 2^-110 has none)
+            const uint32_t floor_x = v_to.inv > 0.0f ? 0x100000u : 0u;
+            vt[2 * i] = max(__float_as_uint(zr.x) + u[2 * i + 4 & 7], min(__float_as_uint(rf.x), floor_x));
+            vt[2 * i + 1] = max(__float_as_uint(zr.y) + u[2 * i + 5 & 7], min(__float_as_uint(rf.y), floor_x));
+        }
+        const uint32_t m0[4] = {mt[0], mt[1], mt[2], mt[3]}, m1[4] = {mt[4], mt[5], mt[6], mt[7]};
+        const uint32_t v0[4] = {vt[0], vt[1], vt[2], vt[3]}, v1[4] = {vt[4], vt[5], vt[6], vt[7]};
+        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.m) + e), "r"(pack(m0, true)), "r"(pack(m1, true)) : "memory");
+        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.v) + e), "r"(pack(v0, false)), "r"(pack(v1, false)) : "memory");
+        if (sizeof(TW) == 2) {
+            uint32_t out[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {       // element e takes u[e + 2]
+                const float2 f = halves(wn[i]);
+                const uint32_t n = word[i + 1 & 3];
+                out[i] = __byte_perm(__float_as_uint(f.x) + (n & 0xFFFFu), __float_as_uint(f.y) + (n >> 16), 0x7632);
+            }
+            Eight<uint16_t>::store_words(reinterpret_cast<uint16_t *>(at.w) + e, out[0], out[1], out[2], out[3]);
+        } else {
+            Eight<float>::store(reinterpret_cast<float *>(at.w) + e, wn);
+        }
+        if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
+        if (lane == 0) {
+            *at.m_scale = m_to.scale;
+            *at.v_scale = v_to.scale;
+        }
+    }
+};
+
+// A CTA per tile of kTileBlocks blocks, a warp per block, the loads of a warp's blocks ahead of all arithmetic.
 template <typename TW, typename TG, bool kNarrow, int N>
 __global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ StepTable<N> tab, const StepScalars c)
 {
     __shared__ uint32_t noise[kWarps][kBlock / 2];
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
-    if (!isfinite(gscale)) return;
+    constexpr int kMine = kTileBlocks / kWarps;
+    const int warp = threadIdx.x >> 5;
     const int s = find_entry(tab, (int32_t)blockIdx.x);
     const int64_t len = tab.len[s];
-    const float keep = 1.0f - c.lr * (c.decay ? __ldg(c.decay + tab.id[s]) : c.decay_all);
-    TW *w = static_cast<TW *>(tab.w[s]);
-    const TG *g = static_cast<const TG *>(tab.g[s]);
-    uint16_t *copy = static_cast<uint16_t *>(tab.copy[s]);
-    constexpr bool kNoise = kNarrow || sizeof(TW) == 2;
-    const uint16_t *u = reinterpret_cast<const uint16_t *>(noise[warp]);
-
-    for (int b = warp; b < kTileBlocks; b += kWarps) {
-        const int64_t block = (int64_t)(blockIdx.x - tab.tile0[s]) * kTileBlocks + b;      // of the tensor
-        const int64_t i0 = block * kBlock;
-        if (i0 >= len) break;
-        const int n = (int)min((int64_t)kBlock, len - i0);
-        if (kNoise) {
-            const uint64_t j = (uint64_t)block * 32u + lane;
-            const Block4 q = philox4x32_10((uint32_t)j, (uint32_t)(j >> 32), c.t, (uint32_t)tab.id[s], c.seed_lo, c.seed_hi);
-            __syncwarp();
-            reinterpret_cast<uint4 *>(noise[warp])[lane] = make_uint4(q.w0, q.w1, q.w2, q.w3);
-            __syncwarp();
-        }
-        float m_scale = 1.0f, v_scale = 1.0f;
-        if (kNarrow) {
-            m_scale = c.m_scale[tab.block0[s] + block];
-            v_scale = c.v_scale[tab.block0[s] + block];
-        }
-        float mm[kPerLane], rr[kPerLane];
+    const int32_t id = tab.id[s];
+    BlockAt<TW, TG> at[kMine];
+    FastBlock<TW, TG, kNarrow> data[kMine];
+    bool fast[kMine];
 #pragma unroll
-        for (int k = 0; k < kPerLane; ++k) {
-            const int e = 32 * k + lane;
-            mm[k] = rr[k] = 0.0f;
-            if (e >= n) continue;
-            const int64_t i = i0 + e;
-            float m, v;
-            if (kNarrow) {
-                m = __fmul_rn(e4m3_value(static_cast<const uint8_t *>(tab.m[s])[i]), m_scale);
-                v = __fmul_rn(e4m3_value(static_cast<const uint8_t *>(tab.v[s])[i]), v_scale);
-                v = __fmul_rn(v, v);
-            } else {
-                m = static_cast<const float *>(tab.m[s])[i];
-                v = static_cast<const float *>(tab.v[s])[i];
-            }
-            const Element x = adamw_element(c, keep, widen<TW>(w[i]), __fmul_rn(widen<TG>(g[i]), gscale), m, v);
-            if (sizeof(TW) == 2) reinterpret_cast<uint16_t *>(w)[i] = bf16_stochastic(x.w, u[(e & ~7) + ((e + 2) & 7)]);
-            else reinterpret_cast<float *>(w)[i] = x.w;
-            if (copy) copy[i] = narrow<uint16_t>(x.w);
-            if (kNarrow) {
-                mm[k] = x.m;
-                rr[k] = x.r;
-            } else {
-                static_cast<float *>(tab.m[s])[i] = x.m;
-                static_cast<float *>(tab.v[s])[i] = x.v;
-            }
-        }
-        if (kNarrow) {
-            const float m_top = block_top(mm), r_top = block_top(rr);
-            const bool m_fits = m_top > 0x1p-110f, r_fits = r_top > 0x1p-110f;
-            const float m_inv = m_fits ? __fdiv_rn(448.0f, m_top) : 0.0f, r_inv = r_fits ? __fdiv_rn(448.0f, r_top) : 0.0f;
+    for (int k = 0; k < kMine; ++k) {
+        at[k].block = (uint64_t)(blockIdx.x - tab.tile0[s]) * kTileBlocks + warp + k * kWarps;
+        at[k].id = (uint32_t)(id & ~kAligned);
+        const int64_t i = (int64_t)at[k].block * kBlock;
+        at[k].n = (int)min((int64_t)kBlock, len - i);
+        at[k].w = static_cast<TW *>(tab.w[s]) + i;
+        at[k].g = static_cast<const TG *>(tab.g[s]) + i;
+        at[k].m = static_cast<uint8_t *>(tab.m[s]) + i * (kNarrow ? 1 : 4);
+        at[k].v = static_cast<uint8_t *>(tab.v[s]) + i * (kNarrow ? 1 : 4);
+        at[k].copy = tab.copy[s] ? static_cast<uint16_t *>(tab.copy[s]) + i : nullptr;
+        at[k].m_scale = kNarrow ? c.m_scale + tab.block0[s] + at[k].block : nullptr;
+        at[k].v_scale = kNarrow ? c.v_scale + tab.block0[s] + at[k].block : nullptr;
+        fast[k] = id < 0 && at[k].n == kBlock;
+        if (fast[k]) data[k].load(at[k]);
+    }
+    const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
+    if (!isfinite(gscale)) return;
+    const float keep = 1.0f - c.lr * (c.decay ? __ldg(c.decay + (id & ~kAligned)) : c.decay_all);
 #pragma unroll
-            for (int k = 0; k < kPerLane; ++k) {
-                const int e = 32 * k + lane;
-                if (e >= n) continue;
-                static_cast<uint8_t *>(tab.m[s])[i0 + e] = e4m3_stochastic(mm[k], m_inv, u[e], false);
-                static_cast<uint8_t *>(tab.v[s])[i0 + e] = e4m3_stochastic(rr[k], r_inv, u[(e & ~7) + ((e + 4) & 7)], true);
-            }
-            if (lane == 0) {
-                c.m_scale[tab.block0[s] + block] = m_fits ? __fmul_rn(m_top, 1.0f / 448.0f) : 0.0f;
-                c.v_scale[tab.block0[s] + block] = r_fits ? __fmul_rn(r_top, 1.0f / 448.0f) : 0.0f;
-            }
-        }
+    for (int k = 0; k < kMine; ++k) {
+        if (fast[k]) data[k].step(at[k], c, keep, gscale, noise[warp]);
+        else if (at[k].n > 0) step_block_any<TW, TG, kNarrow>(at[k], c, keep, gscale, noise[warp]);
     }
 }
 

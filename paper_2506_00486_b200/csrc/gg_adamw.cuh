@@ -21,9 +21,10 @@ struct StepTable {
     int64_t len[N];
     int32_t tile0[N + 1];      // first tile of each tensor; [n]: the number of tiles
     int32_t block0[N];         // first scale of each tensor (8-bit states)
-    int32_t id[N];             // its place in the caller's list
+    int32_t id[N];             // its place in the caller's list; bit 31: every array starts where Eight wants it
     int32_t n;
 };
+constexpr int32_t kAligned = (int32_t)0x80000000;
 static_assert(sizeof(StepTable<512>) <= 32 * 1024 - 256, "the table and the scalars have to fit the kernel parameters");
 
 struct StepScalars {

@@ -1536,7 +1536,11 @@ int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int32_t s, int64_t
         tab.copy[i] = a.w_copy ? a.w_copy[s].ptr : nullptr;
         tab.len[i] = len;
         tab.block0[i] = (int32_t)block;
-        tab.id[i] = s;
+        const uintptr_t narrow = a.state_bits == 8 ? 8 : 32, w_at = a.w_dtype == GG_F32 ? 32 : 16, g_at = a.g_dtype == GG_F32 ? 32 : 16;
+        const bool aligned = reinterpret_cast<uintptr_t>(tab.w[i]) % w_at == 0 && reinterpret_cast<uintptr_t>(tab.g[i]) % g_at == 0 &&
+                             (reinterpret_cast<uintptr_t>(tab.m[i]) | reinterpret_cast<uintptr_t>(tab.v[i])) % narrow == 0 &&
+                             reinterpret_cast<uintptr_t>(tab.copy[i]) % 16 == 0;
+        tab.id[i] = aligned ? s | kAligned : s;
         tab.tile0[i + 1] = (int32_t)(tab.tile0[i] + tiles);
         block += blocks;
     }
