@@ -26,8 +26,7 @@
 namespace gg {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
+constexpr int kThreads = kStepWarps * 32;
 constexpr int kPerLane = kBlock / 32;
 
 // The entry of the table that owns tile t.
@@ -53,6 +52,21 @@ __device__ __forceinline__ Element adamw_element(const StepScalars &c, float kee
     e.v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.one_b2, __fmul_rn(g, g)));
     e.r = __fsqrt_rn(e.v);
     e.w = __fmul_rn(w, keep) - c.step * (e.m / (e.r * c.root + c.eps));
+    return e;
+}
+
+// The same with the cheaper root and reciprocal of the 8-bit path, bit for bit what FastBlock does with pairs.
+__device__ __forceinline__ Element adamw_element_narrow(const StepScalars &c, float keep, float w, float g, float m, float v)
+{
+    Element e;
+    e.m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.one_b1, g));
+    e.v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.one_b2, __fmul_rn(g, g)));
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(e.v));
+    y = fminf(y, 0x1p63f);
+    const float r = __fmul_rn(e.v, y);
+    e.r = e.v < INFINITY ? __fmaf_rn(r, __fmaf_rn(__fmul_rn(y, -0.5f), r, 0.5f), r) : e.v;
+    e.w = __fmaf_rn(-c.step, __fmul_rn(e.m, rcp_approx(__fmaf_rn(e.r, c.root, c.eps))), __fmul_rn(w, keep));
     return e;
 }
 
@@ -108,7 +122,7 @@ __device__ __forceinline__ float e4m3_value(uint8_t code)
     return __uint_as_float(__float_as_uint(a) | s);
 }
 
-// What a warp knows of the block of elements that it steps.
+// A block of a tensor that a warp steps.
 template <typename TW, typename TG>
 struct BlockAt {
     TW *w;
@@ -119,6 +133,22 @@ struct BlockAt {
     uint64_t block;       // of the tensor
     uint32_t id;
     int n;                // elements, <= kBlock
+
+    template <bool kNarrow>
+    __device__ __forceinline__ void next(int64_t len)
+    {
+        w += kBlock;
+        g += kBlock;
+        m = static_cast<char *>(m) + kBlock * (kNarrow ? 1 : 4);
+        v = static_cast<char *>(v) + kBlock * (kNarrow ? 1 : 4);
+        if (copy) copy += kBlock;
+        if (kNarrow) {
+            ++m_scale;
+            ++v_scale;
+        }
+        ++block;
+        n = (int)min((int64_t)kBlock, len - (int64_t)block * kBlock);
+    }
 };
 
 template <typename TW, typename TG, bool kNarrow>
@@ -128,7 +158,7 @@ template <typename TW, typename TG>
 __device__ __forceinline__ Block4 block_noise(const BlockAt<TW, TG> &at, const StepScalars &c)
 {
     const uint64_t j = at.block * 32u + (threadIdx.x & 31);
-    return philox4x32_10((uint32_t)j, (uint32_t)(j >> 32), c.t, at.id, c.seed_lo, c.seed_hi);
+    return philox4x32_10((uint32_t)j, (uint32_t)(j >> 32), c.t, at.id, c.key);
 }
 
 // Any alignment, any length, any values: lane l takes the elements l, l + 32, ...
@@ -161,7 +191,8 @@ __device__ __noinline__ void step_block_any(const BlockAt<TW, TG> at, const Step
             m = m32[e];
             v = v32[e];
         }
-        const Element x = adamw_element(c, keep, widen<TW>(at.w[e]), __fmul_rn(widen<TG>(at.g[e]), gscale), m, v);
+        const float wf = widen<TW>(at.w[e]), gf = __fmul_rn(widen<TG>(at.g[e]), gscale);
+        const Element x = kNarrow ? adamw_element_narrow(c, keep, wf, gf, m, v) : adamw_element(c, keep, wf, gf, m, v);
         if (sizeof(TW) == 2) reinterpret_cast<uint16_t *>(at.w)[e] = bf16_stochastic(x.w, u[(e & ~7) + ((e + 2) & 7)]);
         else reinterpret_cast<float *>(at.w)[e] = x.w;
         if (at.copy) at.copy[e] = narrow<uint16_t>(x.w);
@@ -189,7 +220,7 @@ __device__ __noinline__ void step_block_any(const BlockAt<TW, TG> at, const Step
     }
 }
 
-// A whole block at vector boundaries: lane l takes the eight elements from 8 l on, in pairs.
+// A block at vector boundaries with a multiple of eight elements: lane l takes the eight from 8 l on, in pairs.
 template <typename TW, typename TG, bool kNarrow>
 struct FastBlock;
 
@@ -202,6 +233,7 @@ struct FastBlock<TW, TG, false> {
     __device__ __forceinline__ void load(const BlockAt<TW, TG> &at)
     {
         const int e = 8 * (threadIdx.x & 31);
+        if (e >= at.n) return;
         g.load(at.g + e);
         w.load(at.w + e);
         m.load(static_cast<const float *>(at.m) + e);
@@ -210,6 +242,7 @@ struct FastBlock<TW, TG, false> {
     __device__ __forceinline__ void step(const BlockAt<TW, TG> &at, const StepScalars &c, float keep, float gscale, uint32_t *)
     {
         const int e = 8 * (threadIdx.x & 31);
+        if (e >= at.n) return;
         f32x2 wn[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -249,8 +282,8 @@ __device__ __forceinline__ f32x2 e4m3_pair(uint32_t h)
     return pair(f.x, f.y);
 }
 
-// sqrt of finite values >= 0: an approximate reciprocal root and one Newton step, s + (v - s^2) / (2 sqrt(v)), which
-// leaves the rounding of the last sum (and, once in about a million, the neighbour of the nearest value).  Below
+// sqrt of finite values >= 0 by one Newton step on an approximate reciprocal root y: g = v y, g + g (1/2 - g y / 2).
+// That leaves the rounding of the last sum (and, once in about a million, the neighbour of the nearest value).  Below
 // 2^-126 the result is only of the right size; the step divides by the root plus eps, so nothing there matters.
 __device__ __forceinline__ f32x2 sqrt2(f32x2 v)
 {
@@ -259,16 +292,16 @@ __device__ __forceinline__ f32x2 sqrt2(f32x2 v)
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(f.x));
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(f.y));
     const f32x2 y = pair(fminf(a, 0x1p63f), fminf(b, 0x1p63f));       // (infinite at 0)
-    const f32x2 s = mul2(v, y);
-    const float2 sf = halves(s);
-    const f32x2 e = fma2(pair(-sf.x, -sf.y), s, v);
-    return fma2(e, mul2(y, both(0.5f)), s);
+    const f32x2 g = mul2(v, y);
+    return fma2(g, fma2(mul2(y, both(-0.5f)), g, both(0.5f)), g);
 }
 
 // States in 8 bits move 10 to 14 bytes an element, in which time an SM can issue about 50 instructions for it: here the
 // arithmetic is what counts, and everything goes in pairs.  Codes: multiplied by 2^-120 the range of e4m3 becomes that
-// of the smallest fp32 numbers, subnormals on subnormals, and a code is bits 20 .. 26 of the fp32 pattern.  A block that
-// holds an inf or nan goes through step_block_any (nothing is stored before that is known).
+// of the smallest fp32 numbers, subnormals on subnormals, and a code is bits 20 .. 26 of the fp32 pattern; shifted by
+// four it is the top byte.  The largest code cannot round up past 126: x (448 / top) exceeds 448 by at most two units
+// of its pattern, and the noise stays eight short of a whole code.  A block that holds an inf or nan goes through
+// step_block_any; nothing is stored before that is known.
 template <typename TW, typename TG>
 struct FastBlock<TW, TG, true> {
     Eight<TW> w;
@@ -278,28 +311,28 @@ struct FastBlock<TW, TG, true> {
     __device__ __forceinline__ void load(const BlockAt<TW, TG> &at)
     {
         const int e = 8 * (threadIdx.x & 31);
+        m_scale = *at.m_scale;
+        v_scale = *at.v_scale;
+        m = v = make_uint2(0u, 0u);
+        g.zero();
+        w.zero();
+        if (e >= at.n) return;
         g.load(at.g + e);
         w.load(at.w + e);
         asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(m.x), "=r"(m.y) : "l"(static_cast<const uint8_t *>(at.m) + e));
         asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(static_cast<const uint8_t *>(at.v) + e));
-        m_scale = *at.m_scale;
-        v_scale = *at.v_scale;
     }
-    // codes of the four values whose scaled patterns (plus noise) are t: seven bits each in order, and their signs
-    static __device__ __forceinline__ uint32_t pack(const uint32_t (&t)[4], bool with_sign)
+    // the top bytes of four words, in order
+    static __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
     {
-        const uint32_t lo = __byte_perm(t[0], t[1], 0x7632), hi = __byte_perm(t[2], t[3], 0x7632);
-        uint32_t c = __byte_perm(lo >> 4 & 0x007F007Fu, hi >> 4 & 0x007F007Fu, 0x6420);
-        c -= (c + 0x01010101u & 0x80808080u) >> 7;       // 127 is nan: the largest code is 126
-        if (with_sign) c |= __byte_perm(lo, hi, 0x7531) & 0x80808080u;
-        return c;
+        return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
     }
     __device__ __forceinline__ void step(const BlockAt<TW, TG> &at, const StepScalars &c, float keep, float gscale, uint32_t *noise)
     {
         const int lane = threadIdx.x & 31, e = 8 * lane;
         f32x2 wn[4], mn[4], rn[4];
         f32x2 sum = 0;
-        uint32_t m_top = 0, r_top = 0;
+        float m_top = 0.0f, r_top = 0.0f;
         const f32x2 b1 = both(c.b1), one_b1 = both(c.one_b1), b2 = both(c.b2), one_b2 = both(c.one_b2), gs = both(gscale);
         const f32x2 ms = both(m_scale), vs = both(v_scale), root = both(c.root), eps = both(c.eps), step = both(-c.step), keep2 = both(keep);
 #pragma unroll
@@ -313,41 +346,58 @@ struct FastBlock<TW, TG, true> {
             wn[i] = fma2(step, mul2(mn[i], pair(rcp_approx(d.x), rcp_approx(d.y))), mul2(w.get(i), keep2));
             sum = i == 0 ? wn[0] : add2(sum, wn[i]);
             const float2 mf = halves(mn[i]), rf = halves(rn[i]);
-            m_top = max(m_top, max(__float_as_uint(mf.x) & 0x7FFFFFFFu, __float_as_uint(mf.y) & 0x7FFFFFFFu));
-            r_top = max(r_top, max(__float_as_uint(rf.x), __float_as_uint(rf.y)));       // (>= 0, or the positive nan of an operation)
+            m_top = fmaxf(m_top, fmaxf(fabsf(mf.x), fabsf(mf.y)));
+            r_top = fmaxf(r_top, fmaxf(rf.x, rf.y));
         }
+        // (a maximum passes over a nan, but a nan in m or r is one in w too, and so in the sum)
         const float2 sf = halves(sum);
-        if (!isfinite(sf.x + sf.y)) m_top = 0x7F800000u;
-        m_top = __reduce_max_sync(0xFFFFFFFFu, m_top);
-        r_top = __reduce_max_sync(0xFFFFFFFFu, r_top);
-        if (max(m_top, r_top) >= 0x7F800000u) {
+        if (!isfinite(sf.x + sf.y)) m_top = INFINITY;
+        m_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m_top)));
+        r_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(r_top)));
+        if (fmaxf(m_top, r_top) == INFINITY) {
             step_block_any<TW, TG, true>(at, c, keep, gscale, noise);
             return;
         }
-        const BlockScale m_to(__uint_as_float(m_top)), v_to(__uint_as_float(r_top));
+        const BlockScale m_to(m_top), v_to(r_top);
+        if (lane == 0) {
+            *at.m_scale = m_to.scale;
+            *at.v_scale = v_to.scale;
+        }
+        if (e >= at.n) return;
         const Block4 q = block_noise(at, c);
         const uint32_t word[4] = {q.w0, q.w1, q.w2, q.w3};
         uint32_t u[8], mt[8], vt[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            u[2 * i] = word[i] << 4 & 0xFFFF0u | 8u;
-            u[2 * i + 1] = word[i] >> 12 & 0xFFFF0u | 8u;
+        for (int i = 0; i < 4; ++i) {       // (u[e] * 16 + 8) * 16
+            u[2 * i] = __byte_perm(word[i], 0x80u, 0x5104);
+            u[2 * i + 1] = __byte_perm(word[i], 0x80u, 0x5324);
         }
         const f32x2 m_inv = both(m_to.inv), v_inv = both(v_to.inv), down = both(0x1p-120f);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 zm = halves(mul2(mul2(mn[i], m_inv), down)), zr = halves(mul2(mul2(rn[i], v_inv), down)), rf = halves(rn[i]);
-            mt[2 * i] = __float_as_uint(zm.x) + u[2 * i];
-            mt[2 * i + 1] = __float_as_uint(zm.y) + u[2 * i + 1];
-            // (a root that is not 0 is above 2^-75, so its pattern is above that of code 1; a block below 2^-110 has none)
-            const uint32_t floor_x = v_to.inv > 0.0f ? 0x100000u : 0u;
-            vt[2 * i] = max(__float_as_uint(zr.x) + u[2 * i + 4 & 7], min(__float_as_uint(rf.x), floor_x));
-            vt[2 * i + 1] = max(__float_as_uint(zr.y) + u[2 * i + 5 & 7], min(__float_as_uint(rf.y), floor_x));
+            const float2 zm = halves(mul2(mul2(mn[i], m_inv), down)), zr = halves(mul2(mul2(rn[i], v_inv), down));
+            mt[2 * i] = (__float_as_uint(zm.x) << 4) + u[2 * i];
+            mt[2 * i + 1] = (__float_as_uint(zm.y) << 4) + u[2 * i + 1];
+            vt[2 * i] = (__float_as_uint(zr.x) << 4) + u[2 * i + 4 & 7];
+            vt[2 * i + 1] = (__float_as_uint(zr.y) << 4) + u[2 * i + 5 & 7];
         }
-        const uint32_t m0[4] = {mt[0], mt[1], mt[2], mt[3]}, m1[4] = {mt[4], mt[5], mt[6], mt[7]};
-        const uint32_t v0[4] = {vt[0], vt[1], vt[2], vt[3]}, v1[4] = {vt[4], vt[5], vt[6], vt[7]};
-        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.m) + e), "r"(pack(m0, true)), "r"(pack(m1, true)) : "memory");
-        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.v) + e), "r"(pack(v0, false)), "r"(pack(v1, false)) : "memory");
+        uint32_t mc[2], vc[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const float2 s0 = halves(mn[2 * h]), s1 = halves(mn[2 * h + 1]);
+            const uint32_t sign = top_bytes(__float_as_uint(s0.x), __float_as_uint(s0.y), __float_as_uint(s1.x), __float_as_uint(s1.y));
+            mc[h] = top_bytes(mt[4 * h], mt[4 * h + 1], mt[4 * h + 2], mt[4 * h + 3]) | sign & 0x80808080u;
+            vc[h] = top_bytes(vt[4 * h], vt[4 * h + 1], vt[4 * h + 2], vt[4 * h + 3]);
+            if ((vc[h] - 0x01010101u & ~vc[h] & 0x80808080u) != 0u && v_to.inv > 0.0f) {       // a code of 0: 1 unless the root is 0
+                const float2 r0 = halves(rn[2 * h]), r1 = halves(rn[2 * h + 1]);
+                const float r[4] = {r0.x, r0.y, r1.x, r1.y};
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if ((vc[h] >> 8 * i & 0xFFu) == 0u && r[i] > 0.0f) vc[h] |= 1u << 8 * i;
+            }
+        }
+        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.m) + e), "r"(mc[0]), "r"(mc[1]) : "memory");
+        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.v) + e), "r"(vc[0]), "r"(vc[1]) : "memory");
         if (sizeof(TW) == 2) {
             uint32_t out[4];
 #pragma unroll
@@ -361,49 +411,45 @@ struct FastBlock<TW, TG, true> {
             Eight<float>::store(reinterpret_cast<float *>(at.w) + e, wn);
         }
         if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
-        if (lane == 0) {
-            *at.m_scale = m_to.scale;
-            *at.v_scale = v_to.scale;
-        }
     }
 };
 
-// A CTA per tile of kTileBlocks blocks, a warp per block, the loads of a warp's blocks ahead of all arithmetic.
+// A CTA per tile.  A warp steps consecutive blocks and loads each one while it computes the one before.
 template <typename TW, typename TG, bool kNarrow, int N>
-__global__ void __launch_bounds__(kThreads) adamw_kernel(const __grid_constant__ StepTable<N> tab, const StepScalars c)
+__global__ void __launch_bounds__(kThreads, kNarrow ? 3 : 2) adamw_kernel(const __grid_constant__ StepTable<N> tab, const __grid_constant__ StepScalars c)
 {
-    __shared__ uint32_t noise[kWarps][kBlock / 2];
-    constexpr int kMine = kTileBlocks / kWarps;
+    __shared__ uint32_t noise[kStepWarps][kBlock / 2];
     const int warp = threadIdx.x >> 5;
     const int s = find_entry(tab, (int32_t)blockIdx.x);
     const int64_t len = tab.len[s];
     const int32_t id = tab.id[s];
-    BlockAt<TW, TG> at[kMine];
-    FastBlock<TW, TG, kNarrow> data[kMine];
-    bool fast[kMine];
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-        at[k].block = (uint64_t)(blockIdx.x - tab.tile0[s]) * kTileBlocks + warp + k * kWarps;
-        at[k].id = (uint32_t)(id & ~kAligned);
-        const int64_t i = (int64_t)at[k].block * kBlock;
-        at[k].n = (int)min((int64_t)kBlock, len - i);
-        at[k].w = static_cast<TW *>(tab.w[s]) + i;
-        at[k].g = static_cast<const TG *>(tab.g[s]) + i;
-        at[k].m = static_cast<uint8_t *>(tab.m[s]) + i * (kNarrow ? 1 : 4);
-        at[k].v = static_cast<uint8_t *>(tab.v[s]) + i * (kNarrow ? 1 : 4);
-        at[k].copy = tab.copy[s] ? static_cast<uint16_t *>(tab.copy[s]) + i : nullptr;
-        at[k].m_scale = kNarrow ? c.m_scale + tab.block0[s] + at[k].block : nullptr;
-        at[k].v_scale = kNarrow ? c.v_scale + tab.block0[s] + at[k].block : nullptr;
-        fast[k] = id < 0 && at[k].n == kBlock;
-        if (fast[k]) data[k].load(at[k]);
-    }
+    BlockAt<TW, TG> at;
+    at.block = ((uint64_t)(blockIdx.x - tab.tile0[s]) * kStepWarps + warp) * tab.per_warp;
+    at.id = (uint32_t)(id & ~kAligned);
+    const int64_t i = (int64_t)at.block * kBlock;
+    at.n = (int)min((int64_t)kBlock, len - i);
+    at.w = static_cast<TW *>(tab.w[s]) + i;
+    at.g = static_cast<const TG *>(tab.g[s]) + i;
+    at.m = static_cast<char *>(tab.m[s]) + i * (kNarrow ? 1 : 4);
+    at.v = static_cast<char *>(tab.v[s]) + i * (kNarrow ? 1 : 4);
+    at.copy = tab.copy[s] ? static_cast<uint16_t *>(tab.copy[s]) + i : nullptr;
+    at.m_scale = kNarrow ? c.m_scale + tab.block0[s] + at.block : nullptr;
+    at.v_scale = kNarrow ? c.v_scale + tab.block0[s] + at.block : nullptr;
+    FastBlock<TW, TG, kNarrow> data;
+    auto fast = [&](const BlockAt<TW, TG> &b) { return id < 0 && b.n > 0 && b.n % 8 == 0; };
+    if (fast(at)) data.load(at);
     const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
     if (!isfinite(gscale)) return;
     const float keep = 1.0f - c.lr * (c.decay ? __ldg(c.decay + (id & ~kAligned)) : c.decay_all);
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-        if (fast[k]) data[k].step(at[k], c, keep, gscale, noise[warp]);
-        else if (at[k].n > 0) step_block_any<TW, TG, kNarrow>(at[k], c, keep, gscale, noise[warp]);
+    for (int k = tab.per_warp; k > 0 && at.n > 0; --k) {
+        BlockAt<TW, TG> after = at;
+        after.template next<kNarrow>(len);
+        FastBlock<TW, TG, kNarrow> ahead;
+        if (k > 1 && fast(after)) ahead.load(after);
+        if (fast(at)) data.step(at, c, keep, gscale, noise[warp]);
+        else step_block_any<TW, TG, kNarrow>(at, c, keep, gscale, noise[warp]);
+        at = after;
+        data = ahead;
     }
 }
 

@@ -8,11 +8,13 @@
 namespace gg {
 
 constexpr int kBlock = GG_ADAMW_BLOCK;      // elements that share one scale of an 8-bit state
-constexpr int kTileBlocks = 16;             // blocks of a CTA: 4096 elements
-constexpr int kTableSmall = 16, kTableLarge = 512;
+constexpr int kStepWarps = 8;               // warps of a CTA
+constexpr int kTableSmall = 64, kTableLarge = 512;
 
 // The tensors of one launch, passed by value: kernel parameters may take 32,764 bytes, which holds 512 tensors.  A
 // step so needs no device memory of its own, no upload and no cache, whatever addresses the tensors have this time.
+// Two sizes: a launch with up to 4 KB of parameters costs the host 2.7 us, one with 30 KB 5.5 us (and 4 us more until
+// the kernel has ended), so up to 64 tensors take the small table.
 template <int N>
 struct StepTable {
     void *w[N];
@@ -23,6 +25,7 @@ struct StepTable {
     int32_t block0[N];         // first scale of each tensor (8-bit states)
     int32_t id[N];             // its place in the caller's list; bit 31: every array starts where Eight wants it
     int32_t n;
+    int32_t per_warp;          // blocks of a tensor that one warp steps, one after the other; a tile is kStepWarps times that
 };
 constexpr int32_t kAligned = (int32_t)0x80000000;
 static_assert(sizeof(StepTable<512>) <= 32 * 1024 - 256, "the table and the scalars have to fit the kernel parameters");
@@ -35,7 +38,8 @@ struct StepScalars {
     float step;                    // lr / (1 - b1^t)
     float root;                    // 1 / sqrt(1 - b2^t)
     float eps;
-    uint32_t t, seed_lo, seed_hi;
+    uint32_t t;
+    uint32_t key[20];              // the key of each round of Philox: seed mod 2^32 + r * W0, seed div 2^32 + r * W1
 };
 
 cudaError_t launch_adamw(const StepTable<kTableSmall> &tab, const StepScalars &c, int w_dtype, int g_dtype, bool narrow_states, cudaStream_t st);

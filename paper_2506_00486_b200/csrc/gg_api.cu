@@ -16,6 +16,7 @@
 
 #include "gg_adamw.cuh"
 #include "gg_internal.h"
+#include "gg_philox.cuh"
 
 using namespace gg;
 
@@ -1522,14 +1523,16 @@ gg_status check_list(const gg_seg *w, const gg_seg *list, int32_t n_seg, size_t 
 // Fills the table with the non-empty tensors from `s` on, and returns the first that did not fit.  `block` is the
 // scale of the first block of tensor s; on return that of the next tensor.
 template <int N>
-int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int32_t s, int64_t &block)
+int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int per_warp, int32_t s, int64_t &block)
 {
+    const int tile_blocks = per_warp * kStepWarps;
+    tab.per_warp = per_warp;
     tab.n = 0;
     tab.tile0[0] = 0;
     for (; s < a.n_seg; ++s) {
         const int64_t len = a.w[s].len, blocks = (len + kBlock - 1) / kBlock;
         if (len == 0) continue;
-        const int64_t tiles = (blocks + kTileBlocks - 1) / kTileBlocks;
+        const int64_t tiles = (blocks + tile_blocks - 1) / tile_blocks;
         if (tab.n == N || tab.tile0[tab.n] + tiles > 0x7FFFFFFFll) break;
         const int i = tab.n++;
         tab.w[i] = a.w[s].ptr; tab.g[i] = a.g[s].ptr; tab.m[i] = a.m[s].ptr; tab.v[i] = a.v[s].ptr;
@@ -1548,12 +1551,12 @@ int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int32_t s, int64_t
 }
 
 template <int N>
-gg_status run_adamw(gg_ctx *ctx, const gg_adamw_args &a, const StepScalars &c, cudaStream_t cs)
+gg_status run_adamw(gg_ctx *ctx, const gg_adamw_args &a, int per_warp, const StepScalars &c, cudaStream_t cs)
 {
     StepTable<N> tab;
     int64_t block = 0;
     for (int32_t s = 0; s < a.n_seg;) {
-        s = fill_table(tab, a, s, block);
+        s = fill_table(tab, a, per_warp, s, block);
         if (tab.n == 0) break;
         GG_CUDA(ctx, launch_adamw(tab, c, a.w_dtype, a.g_dtype, a.state_bits == 8, cs));
         ctx->launches += 1;
@@ -1672,9 +1675,17 @@ gg_status gg_adamw_step(gg_ctx *ctx, const gg_adamw_args *a, void *stream)
     c.lr = (float)a->lr; c.decay_all = (float)a->weight_decay; c.eps = (float)a->eps;
     c.step = (float)(a->lr / (1.0 - pow(a->beta1, (double)a->t)));
     c.root = (float)(1.0 / sqrt(1.0 - pow(a->beta2, (double)a->t)));
-    c.t = (uint32_t)a->t; c.seed_lo = (uint32_t)a->seed; c.seed_hi = (uint32_t)(a->seed >> 32);
+    c.t = (uint32_t)a->t;
+    for (uint32_t r = 0; r < 10; ++r) {
+        c.key[2 * r] = (uint32_t)a->seed + r * kPhiloxW0;
+        c.key[2 * r + 1] = (uint32_t)(a->seed >> 32) + r * kPhiloxW1;
+    }
+    // a warp steps up to 8 blocks, the more the better as each prefetches the next; but only as many as leave the
+    // SMs about four tiles for each CTA that they hold at once
+    const int64_t share = blocks / ((int64_t)ctx->sm_count * 2 * kStepWarps * 4);
+    const int per_warp = (int)(share < 1 ? 1 : share > 8 ? 8 : share);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
-    return full <= kTableSmall ? run_adamw<kTableSmall>(ctx, *a, c, cs) : run_adamw<kTableLarge>(ctx, *a, c, cs);
+    return full <= kTableSmall ? run_adamw<kTableSmall>(ctx, *a, per_warp, c, cs) : run_adamw<kTableLarge>(ctx, *a, per_warp, c, cs);
 }
 
 }  // extern "C"

@@ -61,6 +61,7 @@ __device__ __forceinline__ uint32_t narrow2(f32x2 v)
 template <typename T> struct Eight;
 template <> struct Eight<float> {
     f32x2 v[4];
+    __device__ __forceinline__ void zero() { v[0] = v[1] = v[2] = v[3] = 0; }
     __device__ __forceinline__ void load(const float *p)
     {
         asm volatile("ld.global.L1::no_allocate.v4.b64 {%0, %1, %2, %3}, [%4];" : "=l"(v[0]), "=l"(v[1]), "=l"(v[2]), "=l"(v[3]) : "l"(p));
@@ -73,6 +74,7 @@ template <> struct Eight<float> {
 };
 template <> struct Eight<uint16_t> {
     uint4 v;
+    __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
     __device__ __forceinline__ void load(const uint16_t *p)
     {
         asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
