@@ -28,6 +28,7 @@ namespace {
 
 constexpr int kThreads = kStepWarps * 32;
 constexpr int kPerLane = kBlock / 32;
+constexpr int kDepth = 3;                  // blocks of a warp in flight or at work
 
 // The entry of the table that owns tile t.
 template <int N>
@@ -89,14 +90,19 @@ __device__ __forceinline__ float block_top(const float (&x)[kPerLane])
     return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, top));
 }
 
-// The scale of a block and what its values are multiplied by.
+// The scale of a block and what its values are multiplied by, 448 / top: a quotient from the approximate reciprocal with
+// one Newton step on its remainder, which rounds to nearest (but for about one in a million).
+constexpr float kLargeTop = 16384.0f;
+template <bool kAny>
 struct BlockScale {
     float scale, inv;
     __device__ __forceinline__ explicit BlockScale(float top)
     {
         const bool fits = top > 0x1p-110f;
-        inv = fits ? __fdiv_rn(448.0f, top) : 0.0f;
+        const float y = rcp_approx(top), q = __fmul_rn(448.0f, y);
+        inv = fits ? __fmaf_rn(__fmaf_rn(-top, q, 448.0f), y, q) : 0.0f;
         scale = fits ? __fmul_rn(top, 1.0f / 448.0f) : 0.0f;
+        if (kAny && top > kLargeTop) inv = __fdiv_rn(448.0f, top);       // (the reciprocal of the largest numbers is subnormal)
     }
 };
 
@@ -122,155 +128,151 @@ __device__ __forceinline__ float e4m3_value(uint8_t code)
     return __uint_as_float(__float_as_uint(a) | s);
 }
 
-// A block of a tensor that a warp steps.
-template <typename TW, typename TG>
-struct BlockAt {
+template <bool kNarrow> struct State { using type = float; };
+template <> struct State<true> { using type = uint8_t; };
+
+// Where a warp is in its tensor.
+template <typename TW, typename TG, bool kNarrow>
+struct Place {
+    using TS = typename State<kNarrow>::type;
     TW *w;
     const TG *g;
-    void *m, *v;          // float or codes
-    uint16_t *copy;       // or null
-    float *m_scale, *v_scale;
-    uint64_t block;       // of the tensor
+    TS *m, *v;
+    uint16_t *copy;            // or null
+    uint64_t block;            // of the tensor
     uint32_t id;
-    int n;                // elements, <= kBlock
 
-    template <bool kNarrow>
-    __device__ __forceinline__ void next(int64_t len)
+    __device__ __forceinline__ void advance(int blocks)
     {
-        w += kBlock;
-        g += kBlock;
-        m = static_cast<char *>(m) + kBlock * (kNarrow ? 1 : 4);
-        v = static_cast<char *>(v) + kBlock * (kNarrow ? 1 : 4);
-        if (copy) copy += kBlock;
-        if (kNarrow) {
-            ++m_scale;
-            ++v_scale;
-        }
-        ++block;
-        n = (int)min((int64_t)kBlock, len - (int64_t)block * kBlock);
+        w += blocks * kBlock;
+        g += blocks * kBlock;
+        m += blocks * kBlock;
+        v += blocks * kBlock;
+        if (copy) copy += blocks * kBlock;
+        block += (uint64_t)blocks;
+    }
+    // The noise of the eight elements from 8 * lane on.
+    __device__ __forceinline__ Block4 noise(const StepScalars &c, int lane) const
+    {
+        const uint64_t j = block * 32u + (uint32_t)lane;
+        return philox4x32_10((uint32_t)j, (uint32_t)(j >> 32), c.t, id, c.key);
     }
 };
 
+// One block of n elements at any alignment, with any values: lane l takes the elements l, l + 32, ...  Takes and returns the
+// scales of the block's states in m and in sqrt(v).
 template <typename TW, typename TG, bool kNarrow>
-constexpr bool kNoise = kNarrow || sizeof(TW) == 2;
-
-template <typename TW, typename TG>
-__device__ __forceinline__ Block4 block_noise(const BlockAt<TW, TG> &at, const StepScalars &c)
-{
-    const uint64_t j = at.block * 32u + (threadIdx.x & 31);
-    return philox4x32_10((uint32_t)j, (uint32_t)(j >> 32), c.t, at.id, c.key);
-}
-
-// Any alignment, any length, any values: lane l takes the elements l, l + 32, ...
-template <typename TW, typename TG, bool kNarrow>
-__device__ __noinline__ void step_block_any(const BlockAt<TW, TG> at, const StepScalars &c, float keep, float gscale, uint32_t *noise)
+__device__ __noinline__ float2 step_block_any(const Place<TW, TG, kNarrow> at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
 {
     const int lane = threadIdx.x & 31;
     const uint16_t *u = reinterpret_cast<const uint16_t *>(noise);
-    if (kNoise<TW, TG, kNarrow>) {
-        const Block4 q = block_noise(at, c);
+    if (kNarrow || sizeof(TW) == 2) {
+        const Block4 q = at.noise(c, lane);
         __syncwarp();
         reinterpret_cast<uint4 *>(noise)[lane] = make_uint4(q.w0, q.w1, q.w2, q.w3);
         __syncwarp();
     }
-    uint8_t *m8 = static_cast<uint8_t *>(at.m), *v8 = static_cast<uint8_t *>(at.v);
-    float *m32 = static_cast<float *>(at.m), *v32 = static_cast<float *>(at.v);
-    const float m_scale = kNarrow ? *at.m_scale : 1.0f, v_scale = kNarrow ? *at.v_scale : 1.0f;
     float mm[kPerLane], rr[kPerLane];
 #pragma unroll
     for (int k = 0; k < kPerLane; ++k) {
         const int e = 32 * k + lane;
         mm[k] = rr[k] = 0.0f;
-        if (e >= at.n) continue;
-        float m, v;
-        if (kNarrow) {
-            m = __fmul_rn(e4m3_value(m8[e]), m_scale);
-            v = __fmul_rn(e4m3_value(v8[e]), v_scale);
-            v = __fmul_rn(v, v);
-        } else {
-            m = m32[e];
-            v = v32[e];
-        }
+        if (e >= n) continue;
         const float wf = widen<TW>(at.w[e]), gf = __fmul_rn(widen<TG>(at.g[e]), gscale);
-        const Element x = kNarrow ? adamw_element_narrow(c, keep, wf, gf, m, v) : adamw_element(c, keep, wf, gf, m, v);
-        if (sizeof(TW) == 2) reinterpret_cast<uint16_t *>(at.w)[e] = bf16_stochastic(x.w, u[(e & ~7) + ((e + 2) & 7)]);
-        else reinterpret_cast<float *>(at.w)[e] = x.w;
-        if (at.copy) at.copy[e] = narrow<uint16_t>(x.w);
-        if (kNarrow) {
+        Element x;
+        if constexpr (kNarrow) {
+            const float r = __fmul_rn(e4m3_value(at.v[e]), scale.y);
+            x = adamw_element_narrow(c, keep, wf, gf, __fmul_rn(e4m3_value(at.m[e]), scale.x), __fmul_rn(r, r));
             mm[k] = x.m;
             rr[k] = x.r;
         } else {
-            m32[e] = x.m;
-            v32[e] = x.v;
+            x = adamw_element(c, keep, wf, gf, at.m[e], at.v[e]);
+            at.m[e] = x.m;
+            at.v[e] = x.v;
         }
+        if constexpr (sizeof(TW) == 2) at.w[e] = bf16_stochastic(x.w, u[(e & ~7) + ((e + 2) & 7)]);
+        else at.w[e] = x.w;
+        if (at.copy) at.copy[e] = narrow<uint16_t>(x.w);
     }
-    if (kNarrow) {
-        const BlockScale ms(block_top(mm)), vs(block_top(rr));
+    if constexpr (kNarrow) {
+        const BlockScale<true> ms(block_top(mm)), vs(block_top(rr));
 #pragma unroll
         for (int k = 0; k < kPerLane; ++k) {
             const int e = 32 * k + lane;
-            if (e >= at.n) continue;
-            m8[e] = e4m3_stochastic(mm[k], ms.inv, u[e], false);
-            v8[e] = e4m3_stochastic(rr[k], vs.inv, u[(e & ~7) + ((e + 4) & 7)], true);
+            if (e >= n) continue;
+            at.m[e] = e4m3_stochastic(mm[k], ms.inv, u[e], false);
+            at.v[e] = e4m3_stochastic(rr[k], vs.inv, u[(e & ~7) + ((e + 4) & 7)], true);
         }
-        if (lane == 0) {
-            *at.m_scale = ms.scale;
-            *at.v_scale = vs.scale;
-        }
+        scale = make_float2(ms.scale, vs.scale);
     }
+    return scale;
 }
 
-// A block at vector boundaries with a multiple of eight elements: lane l takes the eight from 8 l on, in pairs.
+// Blocks at vector boundaries with a multiple of eight elements: lane l takes the eight from 8 l on, in pairs.
 template <typename TW, typename TG, bool kNarrow>
-struct FastBlock;
+struct Operands {
+    using TS = typename State<kNarrow>::type;
+    static constexpr int kSlot = 32 * (Eight<TW>::kSlot + Eight<TG>::kSlot + 2 * Eight<TS>::kSlot);
+    Eight<TW> w;
+    Eight<TG> g;
+    Eight<TS> m, v;
+    // the block `ahead` elements on, n elements of it (a whole block, or a multiple of 8)
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const Place<TW, TG, kNarrow> &at, int ahead, int n)
+    {
+        Eight<TG>::fetch(slot, lane, at.g + ahead, n);
+        slot += 32 * Eight<TG>::kSlot;
+        Eight<TW>::fetch(slot, lane, at.w + ahead, n);
+        slot += 32 * Eight<TW>::kSlot;
+        Eight<TS>::fetch(slot, lane, at.m + ahead, n);
+        slot += 32 * Eight<TS>::kSlot;
+        Eight<TS>::fetch(slot, lane, at.v + ahead, n);
+    }
+    __device__ __forceinline__ void read(uint32_t slot, int lane)
+    {
+        g.read(slot, lane);
+        slot += 32 * Eight<TG>::kSlot;
+        w.read(slot, lane);
+        slot += 32 * Eight<TW>::kSlot;
+        m.read(slot, lane);
+        slot += 32 * Eight<TS>::kSlot;
+        v.read(slot, lane);
+    }
+};
 
 // States in fp32: bound by memory with room to spare, so the arithmetic is the plain one.
 template <typename TW, typename TG>
-struct FastBlock<TW, TG, false> {
-    Eight<TW> w;
-    Eight<TG> g;
-    Eight<float> m, v;
-    __device__ __forceinline__ void load(const BlockAt<TW, TG> &at)
-    {
-        const int e = 8 * (threadIdx.x & 31);
-        if (e >= at.n) return;
-        g.load(at.g + e);
-        w.load(at.w + e);
-        m.load(static_cast<const float *>(at.m) + e);
-        v.load(static_cast<const float *>(at.v) + e);
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const Place<TW, TG, false> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *)
+{
+    const int lane = threadIdx.x & 31, e = 8 * lane;
+    if (e >= n) return scale;
+    f32x2 wn[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 wf = halves(x.w.get(i)), gf = halves(x.g.get(i)), mf = halves(x.m.get(i)), vf = halves(x.v.get(i));
+        const Element a = adamw_element(c, keep, wf.x, __fmul_rn(gf.x, gscale), mf.x, vf.x);
+        const Element b = adamw_element(c, keep, wf.y, __fmul_rn(gf.y, gscale), mf.y, vf.y);
+        wn[i] = pair(a.w, b.w);
+        x.m.v[i] = pair(a.m, b.m);
+        x.v.v[i] = pair(a.v, b.v);
     }
-    __device__ __forceinline__ void step(const BlockAt<TW, TG> &at, const StepScalars &c, float keep, float gscale, uint32_t *)
-    {
-        const int e = 8 * (threadIdx.x & 31);
-        if (e >= at.n) return;
-        f32x2 wn[4];
+    Eight<float>::store(at.m + e, x.m.v);
+    Eight<float>::store(at.v + e, x.v.v);
+    if constexpr (sizeof(TW) == 2) {
+        const Block4 q = at.noise(c, lane);
+        const uint32_t word[4] = {q.w1, q.w2, q.w3, q.w0};      // element e takes u[e + 2]
+        uint32_t out[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const float2 wf = halves(w.get(i)), gf = halves(g.get(i)), mf = halves(m.get(i)), vf = halves(v.get(i));
-            const Element x = adamw_element(c, keep, wf.x, __fmul_rn(gf.x, gscale), mf.x, vf.x);
-            const Element y = adamw_element(c, keep, wf.y, __fmul_rn(gf.y, gscale), mf.y, vf.y);
-            wn[i] = pair(x.w, y.w);
-            m.v[i] = pair(x.m, y.m);
-            v.v[i] = pair(x.v, y.v);
+            const float2 f = halves(wn[i]);
+            out[i] = (uint32_t)bf16_stochastic(f.x, word[i] & 0xFFFFu) | ((uint32_t)bf16_stochastic(f.y, word[i] >> 16) << 16);
         }
-        Eight<float>::store(static_cast<float *>(at.m) + e, m.v);
-        Eight<float>::store(static_cast<float *>(at.v) + e, v.v);
-        if (sizeof(TW) == 2) {
-            const Block4 q = block_noise(at, c);
-            const uint32_t word[4] = {q.w1, q.w2, q.w3, q.w0};      // element e takes u[e + 2]
-            uint32_t out[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 f = halves(wn[i]);
-                out[i] = (uint32_t)bf16_stochastic(f.x, word[i] & 0xFFFFu) | ((uint32_t)bf16_stochastic(f.y, word[i] >> 16) << 16);
-            }
-            Eight<uint16_t>::store_words(reinterpret_cast<uint16_t *>(at.w) + e, out[0], out[1], out[2], out[3]);
-        } else {
-            Eight<float>::store(reinterpret_cast<float *>(at.w) + e, wn);
-        }
-        if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
+        Eight<uint16_t>::store_words(at.w + e, out[0], out[1], out[2], out[3]);
+    } else {
+        Eight<float>::store(at.w + e, wn);
     }
-};
+    if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
+    return scale;
+}
 
 // The two e4m3 codes of a 16-bit half.
 __device__ __forceinline__ f32x2 e4m3_pair(uint32_t h)
@@ -296,54 +298,37 @@ __device__ __forceinline__ f32x2 sqrt2(f32x2 v)
     return fma2(g, fma2(mul2(y, both(-0.5f)), g, both(0.5f)), g);
 }
 
+// The top bytes of four words, in order.
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
+{
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+
 // States in 8 bits move 10 to 14 bytes an element, in which time an SM can issue about 50 instructions for it: here the
 // arithmetic is what counts, and everything goes in pairs.  Codes: multiplied by 2^-120 the range of e4m3 becomes that
 // of the smallest fp32 numbers, subnormals on subnormals, and a code is bits 20 .. 26 of the fp32 pattern; shifted by
 // four it is the top byte.  The largest code cannot round up past 126: x (448 / top) exceeds 448 by at most two units
-// of its pattern, and the noise stays eight short of a whole code.  A block that holds an inf or nan goes through
-// step_block_any; nothing is stored before that is known.
+// of its pattern, and the noise stays eight short of a whole code.  A block that holds an inf or nan, or values so
+// large that 2^-120 448 / top is not a normal number, goes through step_block_any; nothing is stored before that is known.
 template <typename TW, typename TG>
-struct FastBlock<TW, TG, true> {
-    Eight<TW> w;
-    Eight<TG> g;
-    uint2 m, v;
-    float m_scale, v_scale;
-    __device__ __forceinline__ void load(const BlockAt<TW, TG> &at)
-    {
-        const int e = 8 * (threadIdx.x & 31);
-        m_scale = *at.m_scale;
-        v_scale = *at.v_scale;
-        m = v = make_uint2(0u, 0u);
-        g.zero();
-        w.zero();
-        if (e >= at.n) return;
-        g.load(at.g + e);
-        w.load(at.w + e);
-        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(m.x), "=r"(m.y) : "l"(static_cast<const uint8_t *>(at.m) + e));
-        asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(static_cast<const uint8_t *>(at.v) + e));
-    }
-    // the top bytes of four words, in order
-    static __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d)
-    {
-        return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
-    }
-    __device__ __forceinline__ void step(const BlockAt<TW, TG> &at, const StepScalars &c, float keep, float gscale, uint32_t *noise)
-    {
-        const int lane = threadIdx.x & 31, e = 8 * lane;
-        f32x2 wn[4], mn[4], rn[4];
-        f32x2 sum = 0;
-        float m_top = 0.0f, r_top = 0.0f;
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Place<TW, TG, true> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
+{
+    const int lane = threadIdx.x & 31, e = 8 * lane;
+    f32x2 wn[4], mn[4], rn[4];
+    f32x2 sum = 0;
+    float m_top = 0.0f, r_top = 0.0f;
+    if (e < n) {
         const f32x2 b1 = both(c.b1), one_b1 = both(c.one_b1), b2 = both(c.b2), one_b2 = both(c.one_b2), gs = both(gscale);
-        const f32x2 ms = both(m_scale), vs = both(v_scale), root = both(c.root), eps = both(c.eps), step = both(-c.step), keep2 = both(keep);
+        const f32x2 ms = both(scale.x), vs = both(scale.y), root = both(c.root), eps = both(c.eps), step = both(-c.step), keep2 = both(keep);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t mw = i < 2 ? m.x : m.y, vw = i < 2 ? v.x : v.y;
-            const f32x2 gi = mul2(g.get(i), gs);
+            const uint32_t mw = i < 2 ? x.m.v.x : x.m.v.y, vw = i < 2 ? x.v.v.x : x.v.v.y;
+            const f32x2 gi = mul2(x.g.get(i), gs);
             const f32x2 mo = mul2(e4m3_pair(i & 1 ? mw >> 16 : mw), ms), ro = mul2(e4m3_pair(i & 1 ? vw >> 16 : vw), vs);
             mn[i] = add2(mul2(b1, mo), mul2(one_b1, gi));
             rn[i] = sqrt2(add2(mul2(b2, mul2(ro, ro)), mul2(one_b2, mul2(gi, gi))));
             const float2 d = halves(fma2(rn[i], root, eps));
-            wn[i] = fma2(step, mul2(mn[i], pair(rcp_approx(d.x), rcp_approx(d.y))), mul2(w.get(i), keep2));
+            wn[i] = fma2(step, mul2(mn[i], pair(rcp_approx(d.x), rcp_approx(d.y))), mul2(x.w.get(i), keep2));
             sum = i == 0 ? wn[0] : add2(sum, wn[i]);
             const float2 mf = halves(mn[i]), rf = halves(rn[i]);
             m_top = fmaxf(m_top, fmaxf(fabsf(mf.x), fabsf(mf.y)));
@@ -352,123 +337,157 @@ struct FastBlock<TW, TG, true> {
         // (a maximum passes over a nan, but a nan in m or r is one in w too, and so in the sum)
         const float2 sf = halves(sum);
         if (!isfinite(sf.x + sf.y)) m_top = INFINITY;
-        m_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m_top)));
-        r_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(r_top)));
-        if (fmaxf(m_top, r_top) == INFINITY) {
-            step_block_any<TW, TG, true>(at, c, keep, gscale, noise);
-            return;
-        }
-        const BlockScale m_to(m_top), v_to(r_top);
-        if (lane == 0) {
-            *at.m_scale = m_to.scale;
-            *at.v_scale = v_to.scale;
-        }
-        if (e >= at.n) return;
-        const Block4 q = block_noise(at, c);
-        const uint32_t word[4] = {q.w0, q.w1, q.w2, q.w3};
-        uint32_t u[8], mt[8], vt[8];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {       // (u[e] * 16 + 8) * 16
-            u[2 * i] = __byte_perm(word[i], 0x80u, 0x5104);
-            u[2 * i + 1] = __byte_perm(word[i], 0x80u, 0x5324);
-        }
-        const f32x2 m_inv = both(m_to.inv), v_inv = both(v_to.inv), down = both(0x1p-120f);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 zm = halves(mul2(mul2(mn[i], m_inv), down)), zr = halves(mul2(mul2(rn[i], v_inv), down));
-            mt[2 * i] = (__float_as_uint(zm.x) << 4) + u[2 * i];
-            mt[2 * i + 1] = (__float_as_uint(zm.y) << 4) + u[2 * i + 1];
-            vt[2 * i] = (__float_as_uint(zr.x) << 4) + u[2 * i + 4 & 7];
-            vt[2 * i + 1] = (__float_as_uint(zr.y) << 4) + u[2 * i + 5 & 7];
-        }
-        uint32_t mc[2], vc[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float2 s0 = halves(mn[2 * h]), s1 = halves(mn[2 * h + 1]);
-            const uint32_t sign = top_bytes(__float_as_uint(s0.x), __float_as_uint(s0.y), __float_as_uint(s1.x), __float_as_uint(s1.y));
-            mc[h] = top_bytes(mt[4 * h], mt[4 * h + 1], mt[4 * h + 2], mt[4 * h + 3]) | sign & 0x80808080u;
-            vc[h] = top_bytes(vt[4 * h], vt[4 * h + 1], vt[4 * h + 2], vt[4 * h + 3]);
-            if ((vc[h] - 0x01010101u & ~vc[h] & 0x80808080u) != 0u && v_to.inv > 0.0f) {       // a code of 0: 1 unless the root is 0
-                const float2 r0 = halves(rn[2 * h]), r1 = halves(rn[2 * h + 1]);
-                const float r[4] = {r0.x, r0.y, r1.x, r1.y};
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if ((vc[h] >> 8 * i & 0xFFu) == 0u && r[i] > 0.0f) vc[h] |= 1u << 8 * i;
-            }
-        }
-        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.m) + e), "r"(mc[0]), "r"(mc[1]) : "memory");
-        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(static_cast<uint8_t *>(at.v) + e), "r"(vc[0]), "r"(vc[1]) : "memory");
-        if (sizeof(TW) == 2) {
-            uint32_t out[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {       // element e takes u[e + 2]
-                const float2 f = halves(wn[i]);
-                const uint32_t n = word[i + 1 & 3];
-                out[i] = __byte_perm(__float_as_uint(f.x) + (n & 0xFFFFu), __float_as_uint(f.y) + (n >> 16), 0x7632);
-            }
-            Eight<uint16_t>::store_words(reinterpret_cast<uint16_t *>(at.w) + e, out[0], out[1], out[2], out[3]);
-        } else {
-            Eight<float>::store(reinterpret_cast<float *>(at.w) + e, wn);
-        }
-        if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
     }
-};
+    m_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m_top)));
+    r_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(r_top)));
+    if (fmaxf(m_top, r_top) > kLargeTop) {
+        return step_block_any<TW, TG, true>(at, n, c, keep, gscale, scale, noise);
+    }
+    const BlockScale<false> m_to(m_top), v_to(r_top);
+    scale = make_float2(m_to.scale, v_to.scale);
+    if (e >= n) return scale;
+    const Block4 q = at.noise(c, lane);
+    const uint32_t word[4] = {q.w0, q.w1, q.w2, q.w3};
+    uint32_t u[8], mt[8], vt[8];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {       // (u[e] * 16 + 8) * 16
+        u[2 * i] = __byte_perm(word[i], 0x80u, 0x5104);
+        u[2 * i + 1] = __byte_perm(word[i], 0x80u, 0x5324);
+    }
+    const f32x2 m_inv = both(m_to.inv * 0x1p-120f), v_inv = both(v_to.inv * 0x1p-120f);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 zm = halves(mul2(mn[i], m_inv)), zr = halves(mul2(rn[i], v_inv));
+        mt[2 * i] = (__float_as_uint(zm.x) << 4) + u[2 * i];
+        mt[2 * i + 1] = (__float_as_uint(zm.y) << 4) + u[2 * i + 1];
+        vt[2 * i] = (__float_as_uint(zr.x) << 4) + u[2 * i + 4 & 7];
+        vt[2 * i + 1] = (__float_as_uint(zr.y) << 4) + u[2 * i + 5 & 7];
+    }
+    uint32_t mc[2], vc[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const float2 s0 = halves(mn[2 * h]), s1 = halves(mn[2 * h + 1]);
+        const uint32_t sign = top_bytes(__float_as_uint(s0.x), __float_as_uint(s0.y), __float_as_uint(s1.x), __float_as_uint(s1.y));
+        mc[h] = top_bytes(mt[4 * h], mt[4 * h + 1], mt[4 * h + 2], mt[4 * h + 3]) | sign & 0x80808080u;
+        vc[h] = top_bytes(vt[4 * h], vt[4 * h + 1], vt[4 * h + 2], vt[4 * h + 3]);
+        if ((vc[h] - 0x01010101u & ~vc[h] & 0x80808080u) != 0u && v_to.inv > 0.0f) {       // a code of 0: 1 unless the root is 0
+            const float2 r0 = halves(rn[2 * h]), r1 = halves(rn[2 * h + 1]);
+            const float r[4] = {r0.x, r0.y, r1.x, r1.y};
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if ((vc[h] >> 8 * i & 0xFFu) == 0u && r[i] > 0.0f) vc[h] |= 1u << 8 * i;
+        }
+    }
+    Eight<uint8_t>::store(at.m + e, mc[0], mc[1]);
+    Eight<uint8_t>::store(at.v + e, vc[0], vc[1]);
+    if constexpr (sizeof(TW) == 2) {
+        uint32_t out[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {       // element e takes u[e + 2]
+            const float2 f = halves(wn[i]);
+            const uint32_t k = word[i + 1 & 3];
+            out[i] = __byte_perm(__float_as_uint(f.x) + (k & 0xFFFFu), __float_as_uint(f.y) + (k >> 16), 0x7632);
+        }
+        Eight<uint16_t>::store_words(at.w + e, out[0], out[1], out[2], out[3]);
+    } else {
+        Eight<float>::store(at.w + e, wn);
+    }
+    if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
+    return scale;
+}
 
-// A CTA per tile.  A warp steps consecutive blocks and loads each one while it computes the one before.
+// A CTA per tile, a warp per run of blocks.  A warp fetches its operands kDepth - 1 blocks ahead into places of shared
+// memory that are its own (no barrier of the CTA), so that neither registers nor occupancy limit what is in flight.
 template <typename TW, typename TG, bool kNarrow, int N>
 __global__ void __launch_bounds__(kThreads, kNarrow ? 3 : 2) adamw_kernel(const __grid_constant__ StepTable<N> tab, const __grid_constant__ StepScalars c)
 {
-    __shared__ uint32_t noise[kStepWarps][kBlock / 2];
-    const int warp = threadIdx.x >> 5;
+    using Data = Operands<TW, TG, kNarrow>;
+    extern __shared__ __align__(16) unsigned char ring[];
+    __shared__ __align__(16) uint32_t noise[kStepWarps][kBlock / 2];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int s = find_entry(tab, (int32_t)blockIdx.x);
-    const int64_t len = tab.len[s];
     const int32_t id = tab.id[s];
-    BlockAt<TW, TG> at;
-    at.block = ((uint64_t)(blockIdx.x - tab.tile0[s]) * kStepWarps + warp) * tab.per_warp;
+    Place<TW, TG, kNarrow> at;
+    at.block = ((uint64_t)(blockIdx.x - tab.tile0[s]) * kStepWarps + warp) * (uint32_t)tab.per_warp;
     at.id = (uint32_t)(id & ~kAligned);
-    const int64_t i = (int64_t)at.block * kBlock;
-    at.n = (int)min((int64_t)kBlock, len - i);
-    at.w = static_cast<TW *>(tab.w[s]) + i;
-    at.g = static_cast<const TG *>(tab.g[s]) + i;
-    at.m = static_cast<char *>(tab.m[s]) + i * (kNarrow ? 1 : 4);
-    at.v = static_cast<char *>(tab.v[s]) + i * (kNarrow ? 1 : 4);
-    at.copy = tab.copy[s] ? static_cast<uint16_t *>(tab.copy[s]) + i : nullptr;
-    at.m_scale = kNarrow ? c.m_scale + tab.block0[s] + at.block : nullptr;
-    at.v_scale = kNarrow ? c.v_scale + tab.block0[s] + at.block : nullptr;
-    FastBlock<TW, TG, kNarrow> data;
-    auto fast = [&](const BlockAt<TW, TG> &b) { return id < 0 && b.n > 0 && b.n % 8 == 0; };
-    if (fast(at)) data.load(at);
-    const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
-    if (!isfinite(gscale)) return;
-    const float keep = 1.0f - c.lr * (c.decay ? __ldg(c.decay + (id & ~kAligned)) : c.decay_all);
-    for (int k = tab.per_warp; k > 0 && at.n > 0; --k) {
-        BlockAt<TW, TG> after = at;
-        after.template next<kNarrow>(len);
-        FastBlock<TW, TG, kNarrow> ahead;
-        if (k > 1 && fast(after)) ahead.load(after);
-        if (fast(at)) data.step(at, c, keep, gscale, noise[warp]);
-        else step_block_any<TW, TG, kNarrow>(at, c, keep, gscale, noise[warp]);
-        at = after;
-        data = ahead;
+    const int64_t first = (int64_t)at.block * kBlock;
+    int left = (int)min((int64_t)tab.per_warp * kBlock, tab.len[s] - first);      // elements of this warp
+    if (left <= 0) return;
+    at.w = static_cast<TW *>(tab.w[s]) + first;
+    at.g = static_cast<const TG *>(tab.g[s]) + first;
+    at.m = static_cast<typename State<kNarrow>::type *>(tab.m[s]) + first;
+    at.v = static_cast<typename State<kNarrow>::type *>(tab.v[s]) + first;
+    at.copy = tab.copy[s] ? static_cast<uint16_t *>(tab.copy[s]) + first : nullptr;
+    // lane l holds the scales of block l of the run
+    const int64_t my_scale = (int64_t)tab.block0[s] + (int64_t)at.block + lane;
+    const bool has_scale = kNarrow && lane * kBlock < left;
+    float2 scales = has_scale ? make_float2(c.m_scale[my_scale], c.v_scale[my_scale]) : make_float2(0.0f, 0.0f);
+
+    int fast = id < 0 ? (left % 8 == 0 ? left : left & ~(kBlock - 1)) : 0;        // of these, through the ring
+    left -= fast;
+    const uint32_t slots = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kDepth * Data::kSlot);
+#pragma unroll
+    for (int d = 0; d < kDepth - 1; ++d) {
+        Data::fetch(slots + d * Data::kSlot, lane, at, d * kBlock, fast - d * kBlock);
+        copies_commit();
     }
+    const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
+    const float keep = 1.0f - c.lr * (c.decay ? __ldg(c.decay + (id & ~kAligned)) : c.decay_all);
+    if (!isfinite(gscale)) {
+        copies_wait<0>();
+        return;
+    }
+    int k = 0;
+    auto scale_of = [&]() { return kNarrow ? make_float2(__shfl_sync(0xFFFFFFFFu, scales.x, k), __shfl_sync(0xFFFFFFFFu, scales.y, k)) : scales; };
+    for (uint32_t d = 0; fast > 0; d = d == kDepth - 1 ? 0 : d + 1) {
+        __syncwarp();      // every lane has read the place of the block before this one: the block after the next ones goes there
+        Data::fetch(slots + (d == 0 ? kDepth - 1 : d - 1) * Data::kSlot, lane, at, (kDepth - 1) * kBlock, fast - (kDepth - 1) * kBlock);
+        copies_commit();
+        copies_wait<kDepth - 1>();
+        __syncwarp();      // every lane's copies of this block have arrived
+        Data x;
+        x.read(slots + d * Data::kSlot, lane);
+        const float2 now = step_eight(x, at, min(fast, kBlock), c, keep, gscale, scale_of(), noise[warp]);
+        if (lane == k) scales = now;
+        at.advance(1);
+        fast -= kBlock;
+        ++k;
+    }
+    for (; left > 0; left -= kBlock) {
+        const float2 now = step_block_any<TW, TG, kNarrow>(at, min(left, kBlock), c, keep, gscale, scale_of(), noise[warp]);
+        if (lane == k) scales = now;
+        at.advance(1);
+        ++k;
+    }
+    if (has_scale) {
+        c.m_scale[my_scale] = scales.x;
+        c.v_scale[my_scale] = scales.y;
+    }
+}
+
+template <typename TW, typename TG, bool kNarrow, int N>
+cudaError_t launch_one(const StepTable<N> &tab, const StepScalars &c, cudaStream_t st)
+{
+    constexpr int kBytes = kStepWarps * kDepth * Operands<TW, TG, kNarrow>::kSlot;
+    const cudaError_t e = cudaFuncSetAttribute(adamw_kernel<TW, TG, kNarrow, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
+    if (e != cudaSuccess) return e;
+    adamw_kernel<TW, TG, kNarrow, N><<<(unsigned)tab.tile0[tab.n], kThreads, kBytes, st>>>(tab, c);
+    return cudaGetLastError();
 }
 
 template <int N>
 cudaError_t launch_table(const StepTable<N> &tab, const StepScalars &c, int w_dtype, int g_dtype, bool narrow_states, cudaStream_t st)
 {
-    const dim3 grid((unsigned)tab.tile0[tab.n]), block(kThreads);
-    const int which = (w_dtype == GG_BF16 ? 4 : 0) | (g_dtype == GG_BF16 ? 2 : 0) | (narrow_states ? 1 : 0);
-    switch (which) {
-    case 0: adamw_kernel<float, float, false, N><<<grid, block, 0, st>>>(tab, c); break;
-    case 1: adamw_kernel<float, float, true, N><<<grid, block, 0, st>>>(tab, c); break;
-    case 2: adamw_kernel<float, uint16_t, false, N><<<grid, block, 0, st>>>(tab, c); break;
-    case 3: adamw_kernel<float, uint16_t, true, N><<<grid, block, 0, st>>>(tab, c); break;
-    case 4: adamw_kernel<uint16_t, float, false, N><<<grid, block, 0, st>>>(tab, c); break;
-    case 5: adamw_kernel<uint16_t, float, true, N><<<grid, block, 0, st>>>(tab, c); break;
-    case 6: adamw_kernel<uint16_t, uint16_t, false, N><<<grid, block, 0, st>>>(tab, c); break;
-    default: adamw_kernel<uint16_t, uint16_t, true, N><<<grid, block, 0, st>>>(tab, c); break;
+    switch ((w_dtype == GG_BF16 ? 4 : 0) | (g_dtype == GG_BF16 ? 2 : 0) | (narrow_states ? 1 : 0)) {
+    case 0: return launch_one<float, float, false>(tab, c, st);
+    case 1: return launch_one<float, float, true>(tab, c, st);
+    case 2: return launch_one<float, uint16_t, false>(tab, c, st);
+    case 3: return launch_one<float, uint16_t, true>(tab, c, st);
+    case 4: return launch_one<uint16_t, float, false>(tab, c, st);
+    case 5: return launch_one<uint16_t, float, true>(tab, c, st);
+    case 6: return launch_one<uint16_t, uint16_t, false>(tab, c, st);
+    default: return launch_one<uint16_t, uint16_t, true>(tab, c, st);
     }
-    return cudaGetLastError();
 }
 
 // sqrt(sum of squares) over the tile sums of a moments sweep, and the factor that brings it down to max_norm.

@@ -25,7 +25,7 @@ struct StepTable {
     int32_t block0[N];         // first scale of each tensor (8-bit states)
     int32_t id[N];             // its place in the caller's list; bit 31: every array starts where Eight wants it
     int32_t n;
-    int32_t per_warp;          // blocks of a tensor that one warp steps, one after the other; a tile is kStepWarps times that
+    int32_t per_warp;          // (at most 32) blocks of a tensor that one warp steps, one after the other; a tile is kStepWarps times that
 };
 constexpr int32_t kAligned = (int32_t)0x80000000;
 static_assert(sizeof(StepTable<512>) <= 32 * 1024 - 256, "the table and the scalars have to fit the kernel parameters");

@@ -1582,7 +1582,7 @@ gg_status gg_layer_norm(gg_ctx *ctx, const gg_layer_norm_args *a, void *stream)
     if (a->rows == 0 || a->cols == 0) return GG_OK;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return GG_ERR_CUDA;
-    GG_CUDA(ctx, launch_layer_norm(*a, static_cast<cudaStream_t>(stream)));
+    GG_CUDA(ctx, launch_layer_norm(*a, ctx->sm_count, static_cast<cudaStream_t>(stream)));
     ctx->launches += 1;
     return GG_OK;
 }
@@ -1602,13 +1602,13 @@ gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *a, void
     if (a->cols == 0 || (!a->dx && !a->dweight && !a->dbias)) return GG_OK;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return GG_ERR_CUDA;
-    const int slices = layer_norm_grad_slices(a->rows, a->cols, ctx->sm_count);
+    const int slices = layer_norm_grad_slices(*a, ctx->sm_count);
     if (a->dweight || a->dbias) {
         st = grow(ctx, &ctx->norm_part, &ctx->norm_part_bytes, (int64_t)sizeof(float) * 2 * slices * a->cols);
         if (st != GG_OK) return st;
     }
     int launches = 0;
-    GG_CUDA(ctx, launch_layer_norm_grad(*a, static_cast<float *>(ctx->norm_part), slices, &launches, static_cast<cudaStream_t>(stream)));
+    GG_CUDA(ctx, launch_layer_norm_grad(*a, static_cast<float *>(ctx->norm_part), slices, ctx->sm_count, &launches, static_cast<cudaStream_t>(stream)));
     ctx->launches += launches;
     return GG_OK;
 }

@@ -57,14 +57,109 @@ __device__ __forceinline__ uint32_t narrow2(f32x2 v)
     return d;
 }
 
-// Eight consecutive elements as four pairs; fp32 at a 32-byte boundary, bf16 at 16.  Streamed past L1.
-template <typename T> struct Eight;
-template <> struct Eight<float> {
-    f32x2 v[4];
-    __device__ __forceinline__ void zero() { v[0] = v[1] = v[2] = v[3] = 0; }
+// Eight consecutive elements as four pairs; fp32 at a 32-byte boundary, bf16 at 16, codes of one byte at 8.  They come in
+// by asynchronous copies through a warp's place in shared memory (kSlot bytes a lane), and go out past L1.  A copy
+// instruction of the warp reads consecutive bytes: with two 16-byte pieces 32 bytes apart per lane, as an fp32 vector of
+// eight has them, L2 would see every sector twice (2.89 against 2.25 ms for the step of a decoder with fp32 states).  So piece c
+// of the 64 comes in by lane c modulo 32, and lies at c ^ (c / 8 & 1), where the reads of a quarter warp hit all banks.
+__device__ __forceinline__ void copy16(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t to, const void *from)
+{
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
+
+// kVec consecutive elements at p: 16 bytes of them at a 16-byte boundary, or one.  Streamed past L1, which keeps what is
+// read again.
+template <typename T, int kVec> struct Few;
+template <> struct Few<float, 1> {
+    float v;
+    __device__ __forceinline__ void load(const float *p) { asm volatile("ld.global.L1::no_allocate.f32 %0, [%1];" : "=f"(v) : "l"(p)); }
+    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = v; }
+    static __device__ __forceinline__ void store(float *p, const float (&x)[1]) { *p = x[0]; }
+};
+template <> struct Few<uint16_t, 1> {
+    uint16_t v;
+    __device__ __forceinline__ void load(const uint16_t *p) { asm volatile("ld.global.L1::no_allocate.u16 %0, [%1];" : "=h"(v) : "l"(p)); }
+    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = widen<uint16_t>(v); }
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&x)[1]) { *p = narrow<uint16_t>(x[0]); }
+};
+template <> struct Few<float, 4> {
+    float4 v;
     __device__ __forceinline__ void load(const float *p)
     {
-        asm volatile("ld.global.L1::no_allocate.v4.b64 {%0, %1, %2, %3}, [%4];" : "=l"(v[0]), "=l"(v[1]), "=l"(v[2]), "=l"(v[3]) : "l"(p));
+        asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+    }
+    __device__ __forceinline__ void get(float (&x)[4]) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
+    static __device__ __forceinline__ void store(float *p, const float (&x)[4])
+    {
+        asm volatile("st.global.L1::no_allocate.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]) : "memory");
+    }
+};
+template <> struct Few<uint16_t, 8> {
+    uint4 v;
+    __device__ __forceinline__ void load(const uint16_t *p)
+    {
+        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+    }
+    __device__ __forceinline__ void get(float (&x)[8]) const
+    {
+        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            x[2 * i] = __uint_as_float(w[i] << 16);
+            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        }
+    }
+    static __device__ __forceinline__ void store(uint16_t *p, const float (&x)[8])
+    {
+        asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(narrow2(pair(x[0], x[1]))), "r"(narrow2(pair(x[2], x[3]))),
+                     "r"(narrow2(pair(x[4], x[5]))), "r"(narrow2(pair(x[6], x[7]))) : "memory");
+    }
+};
+// The same elements of a vector that every row reads, kept in L1.
+template <int kVec> __device__ __forceinline__ void read_shared_vector(const float *p, float (&x)[kVec])
+{
+    if constexpr (kVec == 1) x[0] = __ldg(p);
+    else
+#pragma unroll
+        for (int i = 0; i < kVec; i += 4) {
+            const float4 t = __ldg(reinterpret_cast<const float4 *>(p + i));
+            x[i] = t.x; x[i + 1] = t.y; x[i + 2] = t.z; x[i + 3] = t.w;
+        }
+}
+template <int kVec> __device__ __forceinline__ void read_shared_vector(const uint16_t *p, float (&x)[kVec])
+{
+    if constexpr (kVec == 1) x[0] = widen<uint16_t>(__ldg(p));
+    else
+#pragma unroll
+        for (int i = 0; i < kVec; i += 4) {
+            const uint2 t = __ldg(reinterpret_cast<const uint2 *>(p + i));
+            x[i] = __uint_as_float(t.x << 16); x[i + 1] = __uint_as_float(t.x & 0xFFFF0000u);
+            x[i + 2] = __uint_as_float(t.y << 16); x[i + 3] = __uint_as_float(t.y & 0xFFFF0000u);
+        }
+}
+
+template <typename T> struct Eight;
+template <> struct Eight<float> {
+    static constexpr int kSlot = 32;
+    f32x2 v[4];
+    // p: the block's first element; n: its elements
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const float *p, int n)
+    {
+        const uint32_t to = slot + (uint32_t)(lane ^ (lane >> 3 & 1)) * 16u;
+        if (4 * lane < n) copy16(to, p + 4 * lane);
+        if (4 * lane + 128 < n) copy16(to + 512u, p + 4 * lane + 128);
+    }
+    __device__ __forceinline__ void read(uint32_t slot, int lane)
+    {
+        const uint32_t from = slot + (uint32_t)lane * 32u, odd = (uint32_t)(lane >> 2 & 1) * 16u;
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(from + odd) : "memory");
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[2]), "=l"(v[3]) : "r"(from + 16u - odd) : "memory");
     }
     __device__ __forceinline__ f32x2 get(int i) const { return v[i]; }
     static __device__ __forceinline__ void store(float *p, const f32x2 (&x)[4])
@@ -73,11 +168,15 @@ template <> struct Eight<float> {
     }
 };
 template <> struct Eight<uint16_t> {
+    static constexpr int kSlot = 16;
     uint4 v;
-    __device__ __forceinline__ void zero() { v = make_uint4(0u, 0u, 0u, 0u); }
-    __device__ __forceinline__ void load(const uint16_t *p)
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint16_t *p, int n)
     {
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+        if (8 * lane < n) copy16(slot + lane * 16, p + 8 * lane);
+    }
+    __device__ __forceinline__ void read(uint32_t slot, int lane)
+    {
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slot + lane * 16) : "memory");
     }
     __device__ __forceinline__ f32x2 get(int i) const { return widen2(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
     static __device__ __forceinline__ void store_words(uint16_t *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d)
@@ -87,6 +186,22 @@ template <> struct Eight<uint16_t> {
     static __device__ __forceinline__ void store(uint16_t *p, const f32x2 (&x)[4])
     {
         store_words(p, narrow2(x[0]), narrow2(x[1]), narrow2(x[2]), narrow2(x[3]));
+    }
+};
+template <> struct Eight<uint8_t> {
+    static constexpr int kSlot = 8;
+    uint2 v;
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint8_t *p, int n)
+    {
+        if (8 * lane < n) copy8(slot + lane * 8, p + 8 * lane);
+    }
+    __device__ __forceinline__ void read(uint32_t slot, int lane)
+    {
+        asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(slot + lane * 8) : "memory");
+    }
+    static __device__ __forceinline__ void store(uint8_t *p, uint32_t a, uint32_t b)
+    {
+        asm volatile("st.global.L1::no_allocate.v2.u32 [%0], {%1, %2};" ::"l"(p), "r"(a), "r"(b) : "memory");
     }
 };
 

@@ -244,9 +244,9 @@ cudaError_t launch_sample(const TileMap &map, gg_dtype dtype, const double *beta
 // Layer norm and its gradient (gg_layer_norm.cu): the arguments of the interface, checked.
 using LayerNormArgs = gg_layer_norm_args;
 using LayerNormGradArgs = gg_layer_norm_grad_args;
-cudaError_t launch_layer_norm(const LayerNormArgs &a, cudaStream_t st);
+cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t st);
 // part: 2 * slices * cols floats of scratch (layer_norm_grad_slices); launches: kernels launched
-int layer_norm_grad_slices(int64_t rows, int64_t cols, int sm_count);
-cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int slices, int *launches, cudaStream_t st);
+int layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count);
+cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int slices, int sm_count, int *launches, cudaStream_t st);
 
 }  // namespace gg
