@@ -57,11 +57,7 @@ __device__ __forceinline__ uint32_t narrow2(f32x2 v)
     return d;
 }
 
-// Eight consecutive elements as four pairs; fp32 at a 32-byte boundary, bf16 at 16, codes of one byte at 8.  They come in
-// by asynchronous copies through a warp's place in shared memory (kSlot bytes a lane), and go out past L1.  A copy
-// instruction of the warp reads consecutive bytes: with two 16-byte pieces 32 bytes apart per lane, as an fp32 vector of
-// eight has them, L2 would see every sector twice (2.89 against 2.25 ms for the step of a decoder with fp32 states).  So piece c
-// of the 64 comes in by lane c modulo 32, and lies at c ^ (c / 8 & 1), where the reads of a quarter warp hit all banks.
+// Asynchronous copies into shared memory (its 32-bit address).
 __device__ __forceinline__ void copy16(uint32_t to, const void *from)
 {
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory");
@@ -73,77 +69,72 @@ __device__ __forceinline__ void copy8(uint32_t to, const void *from)
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
-// kVec consecutive elements at p: 16 bytes of them at a 16-byte boundary, or one.  Streamed past L1, which keeps what is
-// read again.
-template <typename T, int kVec> struct Few;
-template <> struct Few<float, 1> {
-    float v;
-    __device__ __forceinline__ void load(const float *p) { asm volatile("ld.global.L1::no_allocate.f32 %0, [%1];" : "=f"(v) : "l"(p)); }
-    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = v; }
-    static __device__ __forceinline__ void store(float *p, const float (&x)[1]) { *p = x[0]; }
-};
-template <> struct Few<uint16_t, 1> {
-    uint16_t v;
-    __device__ __forceinline__ void load(const uint16_t *p) { asm volatile("ld.global.L1::no_allocate.u16 %0, [%1];" : "=h"(v) : "l"(p)); }
-    __device__ __forceinline__ void get(float (&x)[1]) const { x[0] = widen<uint16_t>(v); }
-    static __device__ __forceinline__ void store(uint16_t *p, const float (&x)[1]) { *p = narrow<uint16_t>(x[0]); }
-};
-template <> struct Few<float, 4> {
-    float4 v;
-    __device__ __forceinline__ void load(const float *p)
+// 16 bytes of consecutive elements as pairs: read from shared memory, or through L1 (what every row reads), and streamed
+// out past L1.
+template <typename T> struct Few;
+template <> struct Few<float> {
+    static constexpr int kPairs = 2;
+    f32x2 v[2];
+    __device__ __forceinline__ void read(uint32_t at)
     {
-        asm volatile("ld.global.L1::no_allocate.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "l"(p));
+        asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(v[0]), "=l"(v[1]) : "r"(at) : "memory");
     }
-    __device__ __forceinline__ void get(float (&x)[4]) const { x[0] = v.x; x[1] = v.y; x[2] = v.z; x[3] = v.w; }
-    static __device__ __forceinline__ void store(float *p, const float (&x)[4])
+    __device__ __forceinline__ void read(const float *p)
     {
-        asm volatile("st.global.L1::no_allocate.v4.f32 [%0], {%1, %2, %3, %4};" ::"l"(p), "f"(x[0]), "f"(x[1]), "f"(x[2]), "f"(x[3]) : "memory");
+        const float4 t = __ldg(reinterpret_cast<const float4 *>(p));
+        v[0] = pair(t.x, t.y);
+        v[1] = pair(t.z, t.w);
+    }
+    __device__ __forceinline__ f32x2 get(int i) const { return v[i]; }
+    static __device__ __forceinline__ void store(float *p, const f32x2 (&x)[2])
+    {
+        asm volatile("st.global.L1::no_allocate.v2.b64 [%0], {%1, %2};" ::"l"(p), "l"(x[0]), "l"(x[1]) : "memory");
     }
 };
-template <> struct Few<uint16_t, 8> {
-    uint4 v;
-    __device__ __forceinline__ void load(const uint16_t *p)
+template <> struct Few<uint16_t> {
+    static constexpr int kPairs = 4;
+    uint32_t v[4];
+    __device__ __forceinline__ void read(uint32_t at)
     {
-        asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+        asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]) : "r"(at) : "memory");
     }
-    __device__ __forceinline__ void get(float (&x)[8]) const
+    __device__ __forceinline__ void read(const uint16_t *p)
     {
-        const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            x[2 * i] = __uint_as_float(w[i] << 16);
-            x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-        }
+        const uint4 t = __ldg(reinterpret_cast<const uint4 *>(p));
+        v[0] = t.x; v[1] = t.y; v[2] = t.z; v[3] = t.w;
     }
-    static __device__ __forceinline__ void store(uint16_t *p, const float (&x)[8])
+    __device__ __forceinline__ f32x2 get(int i) const { return widen2(v[i]); }
+    static __device__ __forceinline__ void store(uint16_t *p, const f32x2 (&x)[4])
     {
-        asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(narrow2(pair(x[0], x[1]))), "r"(narrow2(pair(x[2], x[3]))),
-                     "r"(narrow2(pair(x[4], x[5]))), "r"(narrow2(pair(x[6], x[7]))) : "memory");
+        asm volatile("st.global.L1::no_allocate.v4.u32 [%0], {%1, %2, %3, %4};" ::"l"(p), "r"(narrow2(x[0])), "r"(narrow2(x[1])), "r"(narrow2(x[2])),
+                     "r"(narrow2(x[3])) : "memory");
     }
 };
-// The same elements of a vector that every row reads, kept in L1.
-template <int kVec> __device__ __forceinline__ void read_shared_vector(const float *p, float (&x)[kVec])
+// kPairs pairs of a vector that every row reads, from element p on (a 16-byte boundary).
+template <typename TW, int kPairs>
+__device__ __forceinline__ void read_vector(const TW *p, f32x2 (&x)[kPairs])
 {
-    if constexpr (kVec == 1) x[0] = __ldg(p);
-    else
+    constexpr int kEach = Few<TW>::kPairs;
+    if constexpr (kEach > kPairs) {      // fp32 rows, bf16 vector: 8 bytes of it
+        const uint2 t = __ldg(reinterpret_cast<const uint2 *>(p));
+        x[0] = widen2(t.x);
+        x[1] = widen2(t.y);
+    } else {
 #pragma unroll
-        for (int i = 0; i < kVec; i += 4) {
-            const float4 t = __ldg(reinterpret_cast<const float4 *>(p + i));
-            x[i] = t.x; x[i + 1] = t.y; x[i + 2] = t.z; x[i + 3] = t.w;
-        }
-}
-template <int kVec> __device__ __forceinline__ void read_shared_vector(const uint16_t *p, float (&x)[kVec])
-{
-    if constexpr (kVec == 1) x[0] = widen<uint16_t>(__ldg(p));
-    else
+        for (int i = 0; i < kPairs; i += kEach) {
+            Few<TW> t;
+            t.read(p + 2 * i);
 #pragma unroll
-        for (int i = 0; i < kVec; i += 4) {
-            const uint2 t = __ldg(reinterpret_cast<const uint2 *>(p + i));
-            x[i] = __uint_as_float(t.x << 16); x[i + 1] = __uint_as_float(t.x & 0xFFFF0000u);
-            x[i + 2] = __uint_as_float(t.y << 16); x[i + 3] = __uint_as_float(t.y & 0xFFFF0000u);
+            for (int j = 0; j < kEach; ++j) x[i + j] = t.get(j);
         }
+    }
 }
 
+// Eight consecutive elements as four pairs; fp32 at a 32-byte boundary, bf16 at 16, codes of one byte at 8.  They come in
+// by asynchronous copies through a warp's place in shared memory (kSlot bytes a lane), and go out past L1.  A copy
+// instruction of the warp reads consecutive bytes: with two 16-byte pieces 32 bytes apart per lane, as an fp32 vector of
+// eight has them, L2 would see every sector twice (2.89 against 2.25 ms for the step of a decoder with fp32 states).  So piece c
+// of the 64 comes in by lane c modulo 32, and lies at c ^ (c / 8 & 1), where the reads of a quarter warp hit all banks.
 template <typename T> struct Eight;
 template <> struct Eight<float> {
     static constexpr int kSlot = 32;

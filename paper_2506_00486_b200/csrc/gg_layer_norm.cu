@@ -34,195 +34,368 @@ __device__ __forceinline__ void block_sum(double (&v)[N], double (*sh)[kWarps])
     }
 }
 
-// ---- rows that fit the registers of their threads
-
-// A row belongs to `warps` warps: to one warp of four in a CTA, which then need no barrier, or to all warps of its CTA.
-// Thread i of a row holds the vectors i, i + T, i + 2 T, ... (T threads a row, kNum vectors each).
-constexpr int kSoloWarps = 4;
-template <int kNum> constexpr int kMostThreads = kNum == 1 ? 1024 : 512;        // 64 or 128 registers a thread
-
-// Sums over the threads of a row, the same bits in every one.  `sh` alternates between two halves, so that one barrier a
-// sum is enough: a thread writes a half again only after a barrier that follows every read of it.
-template <int N>
-__device__ __forceinline__ void row_sum(float (&v)[N], float (*sh)[N][32], int warps, int &half)
+// 1 / sqrt(v): the approximate reciprocal root with one Newton step (v is a normal number wherever the result matters: an
+// fp32 variance that is not zero, plus eps; zero gives infinity).
+__device__ __forceinline__ float rsqrt_of(float v)
 {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
-    if (warps == 1) return;
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    if (lane == 0)
-#pragma unroll
-        for (int i = 0; i < N; ++i) sh[half][i][warp] = v[i];
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        v[i] = lane < warps ? sh[half][i][lane] : 0.0f;
-#pragma unroll
-        for (int o = 16; o > 0; o >>= 1) v[i] += __shfl_xor_sync(0xFFFFFFFFu, v[i], o);
-    }
-    half ^= 1;
+    const float y = rsqrtf(v), h = 0.5f * v * y;
+    return v > 0.0f && v < INFINITY ? fmaf(y, fmaf(-h, y, 0.5f), y) : y;
 }
 
-template <typename T, typename TW, int kVec, int kNum>
-__global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(const LayerNormArgs a, int warps)
+// ---- rows of 16-byte vectors that fit the registers of their threads
+
+// A row belongs to T threads: to 2^k lanes of a warp (short rows: a CTA of four warps then holds several, and needs no
+// barrier), or to all of its CTA.  Thread i of a row holds the vectors i, i + T, i + 2 T, ..., kNum of them at most.  The
+// rows come in by asynchronous copies, kDepth - 1 ahead of the one at work, each thread's vectors into places of shared
+// memory that are its own: what is in flight then depends neither on registers nor on how long a row's sums take.
+// (Loads into registers, one row at a time, measured 60 against 47 us forward and 133 against 77 us backward on bf16 [16384, 4096].)
+constexpr int kSoloWarps = 4;
+constexpr int kDepth = 3;
+template <int kNum> constexpr int kMostThreads = kNum == 1 ? 1024 : 512;        // 64 or 128 registers a thread
+
+// Sums over the threads of a row, the same bits in every one.  kSolo: `threads` lanes of a warp.  Else all of the CTA, over
+// `sh`, which alternates between two halves, so that one barrier a sum is enough: a thread writes a half again only after a
+// barrier that follows every read of it.
+template <bool kSolo>
+__device__ __forceinline__ float row_sum(float v, float (*sh)[32], int threads, int &half)
 {
-    __shared__ float sh[2][1][32];
-    const int threads = warps * 32, tid = warps == 1 ? threadIdx.x & 31 : threadIdx.x;
-    const int64_t row0 = warps == 1 ? (int64_t)blockIdx.x * kSoloWarps + (threadIdx.x >> 5) : blockIdx.x;
-    const int64_t stride = warps == 1 ? (int64_t)gridDim.x * kSoloWarps : gridDim.x;
-    const int cols = (int)a.cols;
-    const float n_inv = 1.0f / (float)cols;
-    const TW *weight = static_cast<const TW *>(a.weight), *bias = static_cast<const TW *>(a.bias);
-    int half = 0;
-    for (int64_t r = row0; r < a.rows; r += stride) {
-        const T *xr = static_cast<const T *>(a.x) + r * a.x_ld;
-        T *yr = static_cast<T *>(a.y) + r * a.y_ld;
-        Few<T, kVec> raw[kNum];
-#pragma unroll
-        for (int k = 0; k < kNum; ++k) {
-            const int c = (k * threads + tid) * kVec;
-            if (c < cols) raw[k].load(xr + c);
-        }
-        float s[1] = {0.0f};
-#pragma unroll
-        for (int k = 0; k < kNum; ++k)
-            if ((k * threads + tid) * kVec < cols) {
-                float x[kVec], t = 0.0f;
-                raw[k].get(x);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) t += x[i];
-                s[0] += t;
-            }
-        row_sum(s, sh, warps, half);
-        const float mean = s[0] * n_inv;
-        s[0] = 0.0f;
-#pragma unroll
-        for (int k = 0; k < kNum; ++k)
-            if ((k * threads + tid) * kVec < cols) {
-                float x[kVec], t = 0.0f;
-                raw[k].get(x);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) t = fmaf(x[i] - mean, x[i] - mean, t);
-                s[0] += t;
-            }
-        row_sum(s, sh, warps, half);
-        const float rstd = 1.0f / sqrtf(s[0] * n_inv + (float)a.eps);
-#pragma unroll
-        for (int k = 0; k < kNum; ++k) {
-            const int c = (k * threads + tid) * kVec;
-            if (c < cols) {
-                float x[kVec], w[kVec], b[kVec];
-                raw[k].get(x);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    w[i] = 1.0f;
-                    b[i] = 0.0f;
-                }
-                if (weight) read_shared_vector<kVec>(weight + c, w);
-                if (bias) read_shared_vector<kVec>(bias + c, b);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) x[i] = fmaf((x[i] - mean) * rstd, w[i], b[i]);
-                Few<T, kVec>::store(yr + c, x);
-            }
-        }
-        if (tid == 0) {
-            if (a.mean) a.mean[r] = mean;
-            if (a.rstd) a.rstd[r] = rstd;
-        }
+    if (kSolo) {
+        for (int o = threads >> 1; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+        return v;
     }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if ((threadIdx.x & 31) == 0) sh[half][threadIdx.x >> 5] = v;
+    __syncthreads();
+    // (the places beyond the last warp are zero)
+    const int quads = (threads + 127) >> 7;
+    v = 0.0f;
+    for (int q = 0; q < quads; ++q) {
+        const float4 t = reinterpret_cast<const float4 *>(sh[half])[q];
+        v += (t.x + t.y) + (t.z + t.w);
+    }
+    half ^= 1;
+    return v;
+}
+
+// Two sums at once.
+template <bool kSolo>
+__device__ __forceinline__ float2 row_sum2(float v0, float v1, float2 (*sh)[32], int threads, int &half)
+{
+    if (kSolo) {
+        for (int o = threads >> 1; o > 0; o >>= 1) {
+            v0 += __shfl_xor_sync(0xFFFFFFFFu, v0, o);
+            v1 += __shfl_xor_sync(0xFFFFFFFFu, v1, o);
+        }
+        return make_float2(v0, v1);
+    }
+    // the lower half warp goes on with the first, the upper with the second
+    const int lane = threadIdx.x & 31;
+    const bool upper = lane & 16;
+    float v = (upper ? v1 : v0) + __shfl_xor_sync(0xFFFFFFFFu, upper ? v0 : v1, 16);
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
+    if ((lane & 15) == 0) reinterpret_cast<float *>(&sh[half][threadIdx.x >> 5])[lane >> 4] = v;
+    __syncthreads();
+    const int twos = (threads + 63) >> 6;
+    f32x2 t = 0;
+    for (int q = 0; q < twos; ++q) {
+        const ulonglong2 p = reinterpret_cast<const ulonglong2 *>(sh[half])[q];
+        t = add2(t, add2(p.x, p.y));
+    }
+    half ^= 1;
+    return halves(t);
+}
+
+// What is known of a launch.  kRagged: nothing.  kFull: every thread has all of its vectors (the widths of models mostly do),
+// and nothing is asked.  kKept: besides, weight and bias are there, in the type of x, and a thread keeps its columns of them
+// in registers (read from L1 for each row they cost 51 against 47 us on bf16 [16384, 4096]).
+enum Known { kRagged, kFull, kKept };
+
+// The rows of a thread and its vectors of them: kOperands rows for each of kDepth stages of the ring.
+template <typename T, int kNum, int kOperands, bool kWhole, bool kSolo>
+struct Rows {
+    static constexpr int kVec = 16 / sizeof(T);
+    int threads, tid, cols;
+    int64_t first, stride;             // rows of this thread
+    uint32_t base, step, stage_bytes;  // in shared memory: this thread's first place, from one vector to the next, a stage
+    __device__ __forceinline__ Rows(int t, int c, unsigned char *shared) : threads(t), cols(c)
+    {
+        if (kSolo) {
+            const int each = 32 / t;                                           // rows of a warp
+            tid = threadIdx.x & (t - 1);
+            first = ((int64_t)blockIdx.x * kSoloWarps + (threadIdx.x >> 5)) * each + (threadIdx.x & 31) / t;
+            stride = (int64_t)gridDim.x * kSoloWarps * each;
+        } else {
+            tid = threadIdx.x;
+            first = blockIdx.x;
+            stride = gridDim.x;
+        }
+        step = blockDim.x * 16u;
+        stage_bytes = kOperands * kNum * step;
+        base = (uint32_t)__cvta_generic_to_shared(shared) + threadIdx.x * 16u;
+    }
+    __device__ __forceinline__ bool has(int k) const { return kWhole || (k * threads + tid) * kVec < cols; }
+    __device__ __forceinline__ int column(int k) const { return (k * threads + tid) * kVec; }
+    // row: where this thread's first vector of it is
+    __device__ __forceinline__ void fetch(uint32_t slot, int operand, const T *row) const
+    {
+#pragma unroll
+        for (int k = 0; k < kNum; ++k)
+            if (has(k)) copy16(slot + (operand * kNum + k) * step, row + k * threads * kVec);
+    }
+    __device__ __forceinline__ void read(uint32_t slot, int operand, Few<T> (&v)[kNum]) const
+    {
+#pragma unroll
+        for (int k = 0; k < kNum; ++k)
+            if (has(k)) v[k].read(slot + (operand * kNum + k) * step);
+    }
+    __device__ __forceinline__ uint32_t after(uint32_t slot) const { return slot == base + (kDepth - 1) * stage_bytes ? base : slot + stage_bytes; }
+    __device__ __forceinline__ uint32_t before(uint32_t slot) const { return slot == base ? base + (kDepth - 1) * stage_bytes : slot - stage_bytes; }
+    // whether there is another round of rows: the lanes of a warp stay together, since they form their sums together
+    __device__ __forceinline__ bool more(int64_t r, int64_t rows) const { return kSolo ? __any_sync(0xFFFFFFFFu, r < rows) : r < rows; }
+};
+
+template <typename T, typename TW, int kNum, Known kKnown, bool kSolo>
+__global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(const __grid_constant__ LayerNormArgs a, int threads)
+{
+    constexpr int kPairs = Few<T>::kPairs;
+    __shared__ __align__(16) float sh[2][32];
+    extern __shared__ __align__(16) unsigned char shared[];
+    const Rows<T, kNum, 1, kKnown != kRagged, kSolo> rows(threads, (int)a.cols, shared);
+    const float n_inv = 1.0f / (float)rows.cols, eps = (float)a.eps;
+    const TW *weight = static_cast<const TW *>(a.weight), *bias = static_cast<const TW *>(a.bias);
+    const T *x_ahead = static_cast<const T *>(a.x) + rows.first * a.x_ld + rows.column(0);
+    T *y = static_cast<T *>(a.y) + rows.first * a.y_ld + rows.column(0);
+    const int64_t x_step = rows.stride * a.x_ld, y_step = rows.stride * a.y_ld;
+    Few<TW> kept_w[kNum], kept_b[kNum];
+    if constexpr (kKnown == kKept)
+#pragma unroll
+        for (int k = 0; k < kNum; ++k) {
+            kept_w[k].read(weight + rows.column(k));
+            kept_b[k].read(bias + rows.column(k));
+        }
+    int half = 0;
+    uint32_t slot = rows.base;
+    if (!kSolo) {
+        if (threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
+        __syncthreads();
+    }
+    int64_t r_ahead = rows.first;
+    for (int d = 0; d < kDepth - 1; ++d) {
+        if (r_ahead < a.rows) rows.fetch(rows.base + d * rows.stage_bytes, 0, x_ahead);
+        copies_commit();
+        x_ahead += x_step;
+        r_ahead += rows.stride;
+    }
+    for (int64_t r = rows.first; rows.more(r, a.rows); r += rows.stride) {
+        if (r_ahead < a.rows) rows.fetch(rows.before(slot), 0, x_ahead);
+        copies_commit();
+        x_ahead += x_step;
+        r_ahead += rows.stride;
+        copies_wait<kDepth - 1>();
+        const bool live = !kSolo || r < a.rows;
+        f32x2 x[kNum][kPairs], t = 0;
+        if (live) {
+            Few<T> raw[kNum];
+            rows.read(slot, 0, raw);
+#pragma unroll
+            for (int k = 0; k < kNum; ++k)
+                if (rows.has(k))
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        x[k][i] = raw[k].get(i);
+                        t = add2(t, x[k][i]);
+                    }
+        }
+        slot = rows.after(slot);
+        float2 f = halves(t);
+        const float mean = row_sum<kSolo>(f.x + f.y, sh, threads, half) * n_inv;
+        t = 0;
+        if (live) {
+            const f32x2 minus = both(-mean);
+#pragma unroll
+            for (int k = 0; k < kNum; ++k)
+                if (rows.has(k))
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        x[k][i] = add2(x[k][i], minus);
+                        t = fma2(x[k][i], x[k][i], t);
+                    }
+        }
+        f = halves(t);
+        const float rstd = rsqrt_of(fmaf(row_sum<kSolo>(f.x + f.y, sh, threads, half), n_inv, eps));
+        if (live) {
+            const f32x2 by = both(rstd);
+#pragma unroll
+            for (int k = 0; k < kNum; ++k)
+                if (rows.has(k)) {
+                    const int c = rows.column(k);
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) x[k][i] = mul2(x[k][i], by);
+                    if constexpr (kKnown == kKept) {
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) x[k][i] = fma2(x[k][i], kept_w[k].get(i), kept_b[k].get(i));
+                    } else if (weight && bias) {
+                        f32x2 w[kPairs], b[kPairs];
+                        read_vector(weight + c, w);
+                        read_vector(bias + c, b);
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) x[k][i] = fma2(x[k][i], w[i], b[i]);
+                    } else if (weight || bias) {
+                        f32x2 o[kPairs];
+                        read_vector((weight ? weight : bias) + c, o);
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) x[k][i] = weight ? mul2(x[k][i], o[i]) : add2(x[k][i], o[i]);
+                    }
+                    Few<T>::store(y + k * threads * rows.kVec, x[k]);
+                }
+            if (rows.tid == 0) {
+                if (a.mean) a.mean[r] = mean;
+                if (a.rstd) a.rstd[r] = rstd;
+            }
+        }
+        y += y_step;
+    }
+    copies_wait<0>();
 }
 
 // The gradient: each thread keeps the sums of its columns over the rows of its CTA and leaves them as slice blockIdx.x of
 // `part` ([2][gridDim.x][cols]); layer_norm_dw_finish_kernel adds the slices.
-template <typename T, typename TW, int kVec, int kNum>
-__global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kernel(const LayerNormGradArgs a, float *part, int warps)
+template <typename T, typename TW, int kNum, Known kKnown, bool kSolo>
+__global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *part, int threads)
 {
-    __shared__ float sh[2][2][32];
-    extern __shared__ float columns[];      // rows of single warps: [2][cols], where the CTA's four warps meet
-    const int threads = warps * 32, tid = warps == 1 ? threadIdx.x & 31 : threadIdx.x;
-    const int64_t row0 = warps == 1 ? (int64_t)blockIdx.x * kSoloWarps + (threadIdx.x >> 5) : blockIdx.x;
-    const int64_t stride = warps == 1 ? (int64_t)gridDim.x * kSoloWarps : gridDim.x;
-    const int cols = (int)a.cols;
-    const float n_inv = 1.0f / (float)cols;
+    constexpr int kPairs = Few<T>::kPairs;
+    __shared__ __align__(16) float2 sh[2][32];
+    extern __shared__ __align__(16) unsigned char shared[];
+    const Rows<T, kNum, 2, kKnown != kRagged, kSolo> rows(threads, (int)a.cols, shared);
+    cudaTriggerProgrammaticLaunchCompletion();       // (the kernel that adds the slices may take its places as these CTAs leave them)
+    const float n_inv = 1.0f / (float)rows.cols;
     const TW *weight = static_cast<const TW *>(a.weight);
-    float dw[kNum][kVec], db[kNum][kVec];
+    const T *x_ahead = static_cast<const T *>(a.x) + rows.first * a.x_ld + rows.column(0);
+    const T *dy_ahead = static_cast<const T *>(a.dy) + rows.first * a.dy_ld + rows.column(0);
+    T *dx = static_cast<T *>(a.dx) + rows.first * a.dx_ld + rows.column(0);
+    const int64_t x_step = rows.stride * a.x_ld, dy_step = rows.stride * a.dy_ld, dx_step = rows.stride * a.dx_ld;
+    f32x2 dw[kNum][kPairs], db[kNum][kPairs];
 #pragma unroll
     for (int k = 0; k < kNum; ++k)
 #pragma unroll
-        for (int i = 0; i < kVec; ++i) dw[k][i] = db[k][i] = 0.0f;
+        for (int i = 0; i < kPairs; ++i) dw[k][i] = db[k][i] = 0;
     int half = 0;
-    for (int64_t r = row0; r < a.rows; r += stride) {
-        const T *xr = static_cast<const T *>(a.x) + r * a.x_ld, *dyr = static_cast<const T *>(a.dy) + r * a.dy_ld;
-        Few<T, kVec> raw_x[kNum], raw_dy[kNum];
-#pragma unroll
-        for (int k = 0; k < kNum; ++k) {
-            const int c = (k * threads + tid) * kVec;
-            if (c < cols) {
-                raw_dy[k].load(dyr + c);
-                raw_x[k].load(xr + c);
-            }
-        }
-        const float mean = __ldg(a.mean + r), rstd = __ldg(a.rstd + r);
-        float s[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int k = 0; k < kNum; ++k) {
-            const int c = (k * threads + tid) * kVec;
-            if (c < cols) {
-                float x[kVec], dy[kVec], w[kVec], t0 = 0.0f, t1 = 0.0f;
-                raw_x[k].get(x);
-                raw_dy[k].get(dy);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) w[i] = 1.0f;
-                if (weight) read_shared_vector<kVec>(weight + c, w);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) {
-                    const float xhat = (x[i] - mean) * rstd, d = dy[i] * w[i];
-                    t0 += d;
-                    t1 = fmaf(d, xhat, t1);
-                    dw[k][i] = fmaf(dy[i], xhat, dw[k][i]);
-                    db[k][i] += dy[i];
-                }
-                s[0] += t0;
-                s[1] += t1;
-            }
-        }
-        if (a.dx == nullptr) continue;
-        row_sum(s, sh, warps, half);
-        const float c1 = s[0] * n_inv, c2 = s[1] * n_inv;
-        T *dxr = static_cast<T *>(a.dx) + r * a.dx_ld;
-#pragma unroll
-        for (int k = 0; k < kNum; ++k) {
-            const int c = (k * threads + tid) * kVec;
-            if (c < cols) {
-                float x[kVec], dy[kVec], w[kVec];
-                raw_x[k].get(x);
-                raw_dy[k].get(dy);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) w[i] = 1.0f;
-                if (weight) read_shared_vector<kVec>(weight + c, w);
-#pragma unroll
-                for (int i = 0; i < kVec; ++i) x[i] = rstd * (fmaf(dy[i], w[i], -c1) - (x[i] - mean) * rstd * c2);
-                Few<T, kVec>::store(dxr + c, x);
-            }
-        }
+    uint32_t slot = rows.base;
+    if (!kSolo) {
+        if (threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = make_float2(0.0f, 0.0f);
+        __syncthreads();
     }
-    if (part == nullptr) return;
-    float *out_w = part + (int64_t)blockIdx.x * cols, *out_b = out_w + (int64_t)gridDim.x * cols;
-    if (warps == 1) {
-        for (int turn = 0; turn < kSoloWarps; ++turn) {
-            if ((int)(threadIdx.x >> 5) == turn)
+    int64_t r_ahead = rows.first;
+    for (int d = 0; d < kDepth - 1; ++d) {
+        if (r_ahead < a.rows) {
+            rows.fetch(rows.base + d * rows.stage_bytes, 0, dy_ahead);
+            rows.fetch(rows.base + d * rows.stage_bytes, 1, x_ahead);
+        }
+        copies_commit();
+        x_ahead += x_step;
+        dy_ahead += dy_step;
+        r_ahead += rows.stride;
+    }
+    const float *mean_at = a.mean + rows.first, *rstd_at = a.rstd + rows.first;
+    float mean = 0.0f, rstd = 0.0f;
+    if (rows.first < a.rows) {
+        mean = __ldg(mean_at);
+        rstd = __ldg(rstd_at);
+    }
+    for (int64_t r = rows.first; rows.more(r, a.rows); r += rows.stride) {
+        if (r_ahead < a.rows) {
+            const uint32_t to = rows.before(slot);
+            rows.fetch(to, 0, dy_ahead);
+            rows.fetch(to, 1, x_ahead);
+        }
+        copies_commit();
+        x_ahead += x_step;
+        dy_ahead += dy_step;
+        r_ahead += rows.stride;
+        const f32x2 minus = both(-mean), by = both(rstd);
+        const float scale = -rstd * n_inv;
+        mean_at += rows.stride;
+        rstd_at += rows.stride;
+        if (r + rows.stride < a.rows) {
+            mean = __ldg(mean_at);
+            rstd = __ldg(rstd_at);
+        }
+        copies_wait<kDepth - 1>();
+        const bool live = !kSolo || r < a.rows;
+        f32x2 xhat[kNum][kPairs], d[kNum][kPairs], t0 = 0, t1 = 0;
+        if (live) {
+            Few<T> raw_x[kNum], raw_dy[kNum];
+            rows.read(slot, 0, raw_dy);
+            rows.read(slot, 1, raw_x);
 #pragma unroll
-                for (int k = 0; k < kNum; ++k) {
-                    const int c = (k * threads + tid) * kVec;
-                    if (c < cols)
+            for (int k = 0; k < kNum; ++k)
+                if (rows.has(k)) {
 #pragma unroll
-                        for (int i = 0; i < kVec; ++i) {
-                            columns[c + i] = turn ? columns[c + i] + dw[k][i] : dw[k][i];
-                            columns[cols + c + i] = turn ? columns[cols + c + i] + db[k][i] : db[k][i];
-                        }
+                    for (int i = 0; i < kPairs; ++i) {
+                        xhat[k][i] = mul2(add2(raw_x[k].get(i), minus), by);
+                        d[k][i] = raw_dy[k].get(i);
+                        dw[k][i] = fma2(d[k][i], xhat[k][i], dw[k][i]);
+                        db[k][i] = add2(db[k][i], d[k][i]);
+                    }
+                    if (weight) {
+                        f32x2 w[kPairs];
+                        read_vector(weight + rows.column(k), w);
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) d[k][i] = mul2(d[k][i], w[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) {
+                        t0 = add2(t0, d[k][i]);
+                        t1 = fma2(d[k][i], xhat[k][i], t1);
+                    }
                 }
+        }
+        slot = rows.after(slot);
+        if (a.dx == nullptr) continue;
+        const float2 f0 = halves(t0), f1 = halves(t1);
+        const float2 c = row_sum2<kSolo>(f0.x + f0.y, f1.x + f1.y, sh, threads, half);
+        if (live) {
+            // rstd (d - c1 - xhat c2)
+            const f32x2 c1 = both(c.x * scale), c2 = both(c.y * scale);
+#pragma unroll
+            for (int k = 0; k < kNum; ++k)
+                if (rows.has(k)) {
+#pragma unroll
+                    for (int i = 0; i < kPairs; ++i) d[k][i] = fma2(xhat[k][i], c2, fma2(d[k][i], by, c1));
+                    Few<T>::store(dx + k * threads * rows.kVec, d[k]);
+                }
+        }
+        dx += dx_step;
+    }
+    copies_wait<0>();
+    if (part == nullptr) return;
+    const int cols = rows.cols;
+    float *out_w = part + (int64_t)blockIdx.x * cols, *out_b = out_w + (int64_t)gridDim.x * cols;
+    if (kSolo) {
+        // the rows of a warp, then the warps of the CTA in order, in shared memory (whose rows are done with): [2][cols]
+        float *columns = reinterpret_cast<float *>(shared);
+#pragma unroll
+        for (int k = 0; k < kNum; ++k)
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i)
+                for (int o = threads; o < 32; o <<= 1) {
+                    dw[k][i] = add2(dw[k][i], __shfl_xor_sync(0xFFFFFFFFu, dw[k][i], o));
+                    db[k][i] = add2(db[k][i], __shfl_xor_sync(0xFFFFFFFFu, db[k][i], o));
+                }
+        __syncthreads();
+        for (int turn = 0; turn < kSoloWarps; ++turn) {
+            if ((int)(threadIdx.x >> 5) == turn && (threadIdx.x & 31) < threads)
+#pragma unroll
+                for (int k = 0; k < kNum; ++k)
+                    if (rows.has(k))
+#pragma unroll
+                        for (int i = 0; i < kPairs; ++i) {
+                            f32x2 *w = reinterpret_cast<f32x2 *>(columns + rows.column(k)) + i, *b = reinterpret_cast<f32x2 *>(columns + cols + rows.column(k)) + i;
+                            *w = turn ? add2(*w, dw[k][i]) : dw[k][i];
+                            *b = turn ? add2(*b, db[k][i]) : db[k][i];
+                        }
             __syncthreads();
         }
         for (int c = threadIdx.x; c < cols; c += kSoloWarps * 32) {
@@ -232,15 +405,264 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
         return;
     }
 #pragma unroll
-    for (int k = 0; k < kNum; ++k) {
-        const int c = (k * threads + tid) * kVec;
-        if (c < cols)
+    for (int k = 0; k < kNum; ++k)
+        if (rows.has(k))
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                out_w[c + i] = dw[k][i];
-                out_b[c + i] = db[k][i];
+            for (int i = 0; i < kPairs; i += 2) {
+                const f32x2 w[2] = {dw[k][i], dw[k][i + 1]}, b[2] = {db[k][i], db[k][i + 1]};
+                Few<float>::store(out_w + rows.column(k) + 2 * i, w);
+                Few<float>::store(out_b + rows.column(k) + 2 * i, b);
             }
+}
+
+// ---- rows that are not made of 16-byte vectors, or do not start on their boundaries
+
+// Room for the pieces of a row of n elements, wherever it starts.
+template <typename T>
+__host__ __device__ constexpr uint32_t piece_bytes(int n) { return ((uint32_t)n * (uint32_t)sizeof(T) + 15u + 15u) / 16u * 16u; }
+
+template <int N>
+struct Index {
+    static constexpr int value = N;
+    __device__ __forceinline__ constexpr operator int() const { return N; }
+};
+
+// The same plan with single elements.  Each warp computes 32 kNum consecutive elements, lane l those at l, l + 32, ...: all
+// offsets within a row are then constants (with a stride of the row's threads they were most of 82 instructions an element,
+// 260 against 103 us on bf16 [16384, 4095]).  The rows come in as the aligned 16-byte pieces that cover them.  A piece may
+// hold elements of the rows beside, or of what lies between two rows; one that reaches out of the matrix at its very start
+// or end is loaded element by element.  A row is fetched while the one before it is at work.
+template <typename T, int kNum, int kOperands, bool kSolo>
+struct Pieces {
+    int threads, tid, cols;
+    int column, left, whole;           // this thread's first element, how many the row has from there on, how many every lane has
+    int64_t first, stride;
+    uint32_t base, row_bytes, stage_bytes;
+    __device__ __forceinline__ Pieces(int t, int c, unsigned char *shared) : threads(t), cols(c)
+    {
+        row_bytes = piece_bytes<T>(c);
+        stage_bytes = kOperands * row_bytes;
+        base = (uint32_t)__cvta_generic_to_shared(shared);
+        if (kSolo) {
+            tid = threadIdx.x & 31;
+            first = (int64_t)blockIdx.x * kSoloWarps + (threadIdx.x >> 5);
+            stride = (int64_t)gridDim.x * kSoloWarps;
+            base += (threadIdx.x >> 5) * 2 * stage_bytes;
+        } else {
+            tid = threadIdx.x;
+            first = blockIdx.x;
+            stride = gridDim.x;
+        }
+        column = (kSolo ? 0 : (int)(threadIdx.x >> 5) * 32 * kNum) + (int)(threadIdx.x & 31);
+        left = c - column;
+        whole = (c - column + (int)(threadIdx.x & 31)) / 32;
     }
+    __device__ __forceinline__ void sync() const
+    {
+        if (kSolo) __syncwarp();
+        else __syncthreads();
+    }
+    // [from, to): the matrix
+    __device__ __forceinline__ void fetch(uint32_t slot, const T *row, uintptr_t from, uintptr_t to) const
+    {
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = reinterpret_cast<uintptr_t>(row + cols), origin = begin & ~(uintptr_t)15;
+        for (uintptr_t p = origin + 16u * tid; p < end; p += 16u * threads) {
+            const uint32_t at = slot + (uint32_t)(p - origin);
+            if (p >= from && p + 16 <= to) {
+                copy16(at, reinterpret_cast<const void *>(p));
+            } else {
+                for (uintptr_t q = p > begin ? p : begin; q < p + 16 && q < end; q += sizeof(T))
+                    put(at + (uint32_t)(q - p), *reinterpret_cast<const T *>(q));
+            }
+        }
+    }
+    static __device__ __forceinline__ void put(uint32_t at, float v) { asm volatile("st.shared.f32 [%0], %1;" ::"r"(at), "f"(v) : "memory"); }
+    static __device__ __forceinline__ void put(uint32_t at, uint16_t v) { asm volatile("st.shared.u16 [%0], %1;" ::"r"(at), "h"(v) : "memory"); }
+    // where this thread's first element is, for a row at this address
+    __device__ __forceinline__ uint32_t place(uint32_t slot, const T *row) const
+    {
+        return slot + (uint32_t)(reinterpret_cast<uintptr_t>(row) & 15u) + (uint32_t)column * (uint32_t)sizeof(T);
+    }
+    template <int k>
+    static __device__ __forceinline__ float get(uint32_t at)
+    {
+        if constexpr (sizeof(T) == 4) {
+            float v;
+            asm volatile("ld.shared.f32 %0, [%1 + %2];" : "=f"(v) : "r"(at), "n"(k * 32 * 4) : "memory");
+            return v;
+        } else {
+            uint16_t h;
+            asm volatile("ld.shared.u16 %0, [%1 + %2];" : "=h"(h) : "r"(at), "n"(k * 32 * 2) : "memory");
+            return widen<uint16_t>(h);
+        }
+    }
+    // f(k) for every element 32 k of this thread that the row has (the number as a type, so that it can be an offset): four
+    // at a time without a question, as long as all lanes have them, and the last four one by one.
+    template <int k = 0, typename F>
+    __device__ __forceinline__ void each(F f) const
+    {
+        if constexpr (k < kNum) {
+            if (k + 4 <= whole) {
+                f(Index<k>());
+                f(Index<k + 1>());
+                f(Index<k + 2>());
+                f(Index<k + 3>());
+            } else {
+                if (32 * k < left) f(Index<k>());
+                if (32 * (k + 1) < left) f(Index<k + 1>());
+                if (32 * (k + 2) < left) f(Index<k + 2>());
+                if (32 * (k + 3) < left) f(Index<k + 3>());
+                if (whole < k) return;
+            }
+            each<k + 4>(f);
+        }
+    }
+};
+
+template <typename T, typename TW, int kNum, bool kSolo>
+__global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 6 : 1) layer_norm_pieces_kernel(const __grid_constant__ LayerNormArgs a, int threads)
+{
+    __shared__ __align__(16) float sh[2][32];
+    extern __shared__ __align__(16) unsigned char shared[];
+    const Pieces<T, kNum, 1, kSolo> rows(threads, (int)a.cols, shared);
+    const float n_inv = 1.0f / (float)rows.cols, eps = (float)a.eps;
+    const TW *weight = a.weight ? static_cast<const TW *>(a.weight) + rows.column : nullptr;
+    const TW *bias = a.bias ? static_cast<const TW *>(a.bias) + rows.column : nullptr;
+    const T *x = static_cast<const T *>(a.x) + rows.first * a.x_ld;
+    T *y = static_cast<T *>(a.y) + rows.first * a.y_ld + rows.column;
+    const uintptr_t from = reinterpret_cast<uintptr_t>(a.x), to = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.x) + (a.rows - 1) * a.x_ld + a.cols);
+    const int64_t x_step = rows.stride * a.x_ld, y_step = rows.stride * a.y_ld;
+    if (!kSolo && threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
+    int half = 0;
+    uint32_t slot = rows.base, other = rows.base + rows.stage_bytes;
+    if (rows.first < a.rows) rows.fetch(slot, x, from, to);
+    copies_commit();
+    for (int64_t r = rows.first; r < a.rows; r += rows.stride) {
+        copies_wait<0>();
+        rows.sync();       // everyone's pieces of this row are here, and everyone is done with the row before
+        if (r + rows.stride < a.rows) rows.fetch(other, x + x_step, from, to);
+        copies_commit();
+        const uint32_t at = rows.place(slot, x);
+        float v[kNum], t = 0.0f;
+        rows.each([&](auto k) {
+            v[k] = rows.template get<decltype(k)::value>(at);
+            t += v[k];
+        });
+        const float mean = row_sum<kSolo>(t, sh, threads, half) * n_inv;
+        t = 0.0f;
+        rows.each([&](auto k) {
+            v[k] -= mean;
+            t = fmaf(v[k], v[k], t);
+        });
+        const float rstd = rsqrt_of(fmaf(row_sum<kSolo>(t, sh, threads, half), n_inv, eps));
+        if (weight && bias)
+            rows.each([&](auto k) { y[32 * k] = narrow<T>(fmaf(v[k] * rstd, widen<TW>(__ldg(weight + 32 * k)), widen<TW>(__ldg(bias + 32 * k)))); });
+        else
+            rows.each([&](auto k) {
+                y[32 * k] = narrow<T>(fmaf(v[k] * rstd, weight ? widen<TW>(__ldg(weight + 32 * k)) : 1.0f, bias ? widen<TW>(__ldg(bias + 32 * k)) : 0.0f));
+            });
+        if (rows.tid == 0) {
+            if (a.mean) a.mean[r] = mean;
+            if (a.rstd) a.rstd[r] = rstd;
+        }
+        x += x_step;
+        y += y_step;
+        const uint32_t swap = slot;
+        slot = other;
+        other = swap;
+    }
+}
+
+template <typename T, typename TW, int kNum, bool kSolo>
+__global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) layer_norm_pieces_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *part, int threads)
+{
+    __shared__ __align__(16) float2 sh[2][32];
+    extern __shared__ __align__(16) unsigned char shared[];
+    const Pieces<T, kNum, 2, kSolo> rows(threads, (int)a.cols, shared);
+    cudaTriggerProgrammaticLaunchCompletion();
+    const float n_inv = 1.0f / (float)rows.cols;
+    const TW *weight = a.weight ? static_cast<const TW *>(a.weight) + rows.column : nullptr;
+    const T *x = static_cast<const T *>(a.x) + rows.first * a.x_ld, *dy = static_cast<const T *>(a.dy) + rows.first * a.dy_ld;
+    T *dx = static_cast<T *>(a.dx) + rows.first * a.dx_ld + rows.column;
+    const uintptr_t x_from = reinterpret_cast<uintptr_t>(a.x), x_to = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.x) + (a.rows - 1) * a.x_ld + a.cols);
+    const uintptr_t dy_from = reinterpret_cast<uintptr_t>(a.dy), dy_to = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.dy) + (a.rows - 1) * a.dy_ld + a.cols);
+    const int64_t x_step = rows.stride * a.x_ld, dy_step = rows.stride * a.dy_ld, dx_step = rows.stride * a.dx_ld;
+    float dw[kNum], db[kNum];
+#pragma unroll
+    for (int k = 0; k < kNum; ++k) dw[k] = db[k] = 0.0f;
+    if (!kSolo && threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = make_float2(0.0f, 0.0f);
+    int half = 0;
+    uint32_t slot = rows.base, other = rows.base + rows.stage_bytes;
+    float next_mean = 0.0f, next_rstd = 0.0f;
+    if (rows.first < a.rows) {
+        rows.fetch(slot, dy, dy_from, dy_to);
+        rows.fetch(slot + rows.row_bytes, x, x_from, x_to);
+        next_mean = __ldg(a.mean + rows.first);
+        next_rstd = __ldg(a.rstd + rows.first);
+    }
+    copies_commit();
+    for (int64_t r = rows.first; r < a.rows; r += rows.stride) {
+        copies_wait<0>();
+        rows.sync();       // everyone's pieces of this row are here, and everyone is done with the row before
+        const float mean = next_mean, rstd = next_rstd;
+        if (r + rows.stride < a.rows) {
+            rows.fetch(other, dy + dy_step, dy_from, dy_to);
+            rows.fetch(other + rows.row_bytes, x + x_step, x_from, x_to);
+            next_mean = __ldg(a.mean + r + rows.stride);
+            next_rstd = __ldg(a.rstd + r + rows.stride);
+        }
+        copies_commit();
+        const uint32_t dy_at = rows.place(slot, dy), x_at = rows.place(slot + rows.row_bytes, x);
+        float t0 = 0.0f, t1 = 0.0f;
+        rows.each([&](auto k) {
+            const float g = rows.template get<decltype(k)::value>(dy_at), xhat = (rows.template get<decltype(k)::value>(x_at) - mean) * rstd;
+            const float d = weight ? g * widen<TW>(__ldg(weight + 32 * k)) : g;
+            dw[k] = fmaf(g, xhat, dw[k]);
+            db[k] += g;
+            t0 += d;
+            t1 = fmaf(d, xhat, t1);
+        });
+        if (a.dx != nullptr) {
+            const float2 s = row_sum2<kSolo>(t0, t1, sh, threads, half);
+            const float c1 = -rstd * (s.x * n_inv), c2 = -rstd * (s.y * n_inv);
+            rows.each([&](auto k) {       // rstd (d - c1 - xhat c2)
+                const float g = rows.template get<decltype(k)::value>(dy_at), xhat = (rows.template get<decltype(k)::value>(x_at) - mean) * rstd;
+                const float d = weight ? g * widen<TW>(__ldg(weight + 32 * k)) : g;
+                dx[32 * k] = narrow<T>(fmaf(xhat, c2, fmaf(d, rstd, c1)));
+            });
+        }
+        x += x_step;
+        dy += dy_step;
+        dx += dx_step;
+        const uint32_t swap = slot;
+        slot = other;
+        other = swap;
+    }
+    if (part == nullptr) return;
+    const int cols = rows.cols;
+    float *out_w = part + (int64_t)blockIdx.x * cols, *out_b = out_w + (int64_t)gridDim.x * cols;
+    if (kSolo) {       // the warps of the CTA in order, where their rows were
+        float *columns = reinterpret_cast<float *>(shared);
+        __syncthreads();
+        for (int turn = 0; turn < kSoloWarps; ++turn) {
+            if ((int)(threadIdx.x >> 5) == turn)
+                rows.each([&](auto k) {
+                    float *w = columns + 32 * k + rows.column, *b = w + cols;
+                    *w = turn ? *w + dw[k] : dw[k];
+                    *b = turn ? *b + db[k] : db[k];
+                });
+            __syncthreads();
+        }
+        for (int c = threadIdx.x; c < cols; c += kSoloWarps * 32) {
+            out_w[c] = columns[c];
+            out_b[c] = columns[cols + c];
+        }
+        return;
+    }
+    rows.each([&](auto k) {
+        out_w[32 * k + rows.column] = dw[k];
+        out_b[32 * k + rows.column] = db[k];
+    });
 }
 
 // ---- any row length
@@ -333,8 +755,8 @@ __global__ void __launch_bounds__(kThreads) layer_norm_dw_kernel(const LayerNorm
     }
 }
 
-// Adds the slices of a column: 32 columns a CTA, a warp for every sixteenth slice, the warps in order.
-constexpr int kFinishWarps = 16;
+// Adds the slices of a column: 32 columns a CTA, a warp for every 32nd slice, the warps in order.
+constexpr int kFinishWarps = 32;
 __global__ void __launch_bounds__(kFinishWarps * 32) layer_norm_dw_finish_kernel(const float *part, int slices, int64_t cols, float *dweight,
                                                                                 float *dbias, int accumulate)
 {
@@ -347,7 +769,7 @@ __global__ void __launch_bounds__(kFinishWarps * 32) layer_norm_dw_finish_kernel
     const float *p = part + (int64_t)blockIdx.y * slices * cols + c;
     float s = 0.0f;
     if (c < cols)
-#pragma unroll 8
+#pragma unroll 16
         for (int i = warp; i < slices; i += kFinishWarps) s += p[(int64_t)i * cols];
     sh[warp][lane] = s;
     __syncthreads();
@@ -359,33 +781,58 @@ __global__ void __launch_bounds__(kFinishWarps * 32) layer_norm_dw_finish_kernel
 
 inline unsigned row_grid(int64_t rows) { return (unsigned)(rows < (1 << 20) ? rows : (1 << 20)); }
 
-// How the rows of a matrix are laid over threads: elements a vector, vectors a thread, warps a row; num == 0: not at all.
+// How the rows of a matrix are laid over threads: vectors a thread, threads a row; num == 0: not at all.
 struct RowShape {
-    int vec = 1, num = 0, warps = 0;
-    unsigned threads() const { return (unsigned)(warps == 1 ? kSoloWarps : warps) * 32; }
+    int num = 0, threads = 0;
+    bool pieces = false;
+    unsigned block() const { return (unsigned)(threads <= 32 ? kSoloWarps * 32 : threads); }
+    int64_t rows_a_cta() const { return threads <= 32 ? kSoloWarps * (32 / threads) : 1; }
 };
 
-RowShape row_shape(int64_t rows, int64_t cols, int vec, int most, int sm_count)
+// Few rows are spread over as many threads as they can use (one vector each); many over as few as give a thread `wanted`
+// vectors, or more where a CTA of 512 would not hold them otherwise.
+constexpr int kMostNum = 4;
+constexpr int kMostShared = kDepth * 2 * kMostNum * 512 * 16;      // of any launch (the same for all: a kernel has one such limit)
+RowShape row_shape(int64_t rows, int64_t cols, int vec, int wanted, int sm_count)
 {
     RowShape s;
-    s.vec = vec;
     const int64_t vecs = cols / vec;
-    // few rows: spread each over as many warps as it can use; many: over as few as hold it
-    const bool few = rows < 4 * (int64_t)sm_count;
-    for (int num = few ? 1 : most; num <= most && num >= 1; num = few ? num * 2 : num / 2) {
-        const int64_t warps = (vecs + 32 * num - 1) / (32 * num);
-        if (warps * 32 > (num == 1 ? 1024 : 512)) {
-            if (few) continue;
-            break;
+    if (rows < 4 * (int64_t)sm_count) wanted = 1;
+    while (wanted > 1 && vecs <= 8 * wanted) wanted /= 2;      // (short rows: not fewer than 16 lanes for one)
+    for (int num = wanted; num <= kMostNum && s.num == 0; num *= 2) {
+        int64_t threads = (vecs + num - 1) / num;
+        if (threads <= 32) {
+            int p = 1;
+            while (p < threads) p *= 2;
+            threads = p;
+        } else {
+            threads = (threads + 31) / 32 * 32;
         }
+        if (threads > (num == 1 ? 1024 : 512)) continue;
         s.num = num;
-        s.warps = (int)warps;
-        if (few || vecs > 16 * num) break;      // (many rows: fewer vectors a thread, where a warp would be half empty)
+        s.threads = (int)threads;
     }
     return s;
 }
 
-// CTAs of a launch: one wave, or less if there are fewer rows.
+// Single elements: `wanted` a thread for many rows, eight for few.  (Forward 32: the fewer threads, the less the sums of a row
+// cost.  Backward 16, and eight below eight million elements, where a wave of wide threads has only a row or two for each:
+// fp32 [4099, 1023] takes 35, 25 and 23 us with 32, 16 and 8, bf16 [16384, 1023] 56, 54 and 56.)  Wider rows, or rows of
+// which two stages do not fit shared memory, have no shape.
+RowShape piece_shape(int64_t rows, int64_t cols, int64_t bytes_a_row, int wanted, int sm_count)
+{
+    RowShape s;
+    s.pieces = true;
+    int num = rows < 4 * (int64_t)sm_count || cols <= 256 ? 8 : cols <= 512 ? 16 : wanted;
+    if (cols > 512 * num) num = 32;
+    const int64_t threads = (cols + 32 * num - 1) / (32 * num) * 32;
+    if (threads > 512 || (threads > 32 && 2 * bytes_a_row > kMostShared)) return s;
+    s.num = num;
+    s.threads = (int)threads;
+    return s;
+}
+
+// A launch of a kernel over rows: one wave of CTAs, or less if there are fewer rows.
 struct RowLaunch {
     const void *kernel = nullptr;
     RowShape shape;
@@ -393,22 +840,23 @@ struct RowLaunch {
     int64_t grid(int64_t rows, int sm_count) const
     {
         // (asking takes microseconds: the answers are kept)
-        struct Known { const void *kernel; unsigned threads; size_t shared; int ctas; };
+        struct Known { const void *kernel; unsigned block; size_t shared; int ctas; };
         static thread_local Known known[32];
         static thread_local int n_known = 0, next = 0;
         int ctas = 0;
         for (int i = 0; i < n_known && ctas == 0; ++i)
-            if (known[i].kernel == kernel && known[i].threads == shape.threads() && known[i].shared == shared) ctas = known[i].ctas;
+            if (known[i].kernel == kernel && known[i].block == shape.block() && known[i].shared == shared) ctas = known[i].ctas;
         if (ctas == 0) {
-            if (cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, (int)shape.threads(), shared) != cudaSuccess || ctas < 1) {
+            if ((shared > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) != cudaSuccess) ||
+                cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, (int)shape.block(), shared) != cudaSuccess || ctas < 1) {
                 cudaGetLastError();
                 ctas = 1;
             }
-            known[next] = Known{kernel, shape.threads(), shared, ctas};
+            known[next] = Known{kernel, shape.block(), shared, ctas};
             next = (next + 1) % 32;
             if (n_known < 32) ++n_known;
         }
-        const int64_t each = shape.warps == 1 ? kSoloWarps : 1, want = (rows + each - 1) / each, wave = (int64_t)sm_count * ctas;
+        const int64_t each = shape.rows_a_cta(), want = (rows + each - 1) / each, wave = (int64_t)sm_count * ctas;
         return want < wave ? want : wave;
     }
 };
@@ -421,65 +869,100 @@ bool rows_on_16_bytes(const void *p, int64_t rows, int64_t ld, int dtype)
     return on_16_bytes(p) && (rows <= 1 || ld * (dtype == GG_F32 ? 4 : 2) % 16 == 0);
 }
 
-int forward_vec(const LayerNormArgs &a)
+template <typename T, typename TW, int kNum>
+const void *forward_kernel(const RowShape &s, int64_t cols, bool affine)
 {
-    const int vec = a.dtype == GG_F32 ? 4 : 8;
-    const bool ok = a.cols % vec == 0 && rows_on_16_bytes(a.x, a.rows, a.x_ld, a.dtype) && rows_on_16_bytes(a.y, a.rows, a.y_ld, a.dtype) &&
-                    on_16_bytes(a.weight) && on_16_bytes(a.bias);
-    return ok ? vec : 1;
-}
-
-int backward_vec(const LayerNormGradArgs &a)
-{
-    const int vec = a.dtype == GG_F32 ? 4 : 8;
-    const bool ok = a.cols % vec == 0 && rows_on_16_bytes(a.x, a.rows, a.x_ld, a.dtype) && rows_on_16_bytes(a.dy, a.rows, a.dy_ld, a.dtype) &&
-                    rows_on_16_bytes(a.dx, a.rows, a.dx_ld, a.dtype) && on_16_bytes(a.weight);
-    return ok ? vec : 1;
-}
-
-constexpr int kMostVec = 4, kMostOne = 16;      // vectors, single elements that a thread may hold of a row
-
-template <typename T, typename TW, int kVec, int kNum>
-const void *forward_kernel(int num)
-{
-    if (num == kNum) return reinterpret_cast<const void *>(layer_norm_rows_kernel<T, TW, kVec, kNum>);
-    if constexpr (kNum > 1) return forward_kernel<T, TW, kVec, kNum / 2>(num);
+    if (s.num == kNum) {
+        const bool full = cols * (int64_t)sizeof(T) == (int64_t)s.num * s.threads * 16;
+        if (s.threads <= 32)
+            return full ? reinterpret_cast<const void *>(layer_norm_rows_kernel<T, TW, kNum, kFull, true>)
+                        : reinterpret_cast<const void *>(layer_norm_rows_kernel<T, TW, kNum, kRagged, true>);
+        if constexpr (sizeof(T) == sizeof(TW))
+            if (full && affine) return reinterpret_cast<const void *>(layer_norm_rows_kernel<T, TW, kNum, kKept, false>);
+        return full ? reinterpret_cast<const void *>(layer_norm_rows_kernel<T, TW, kNum, kFull, false>)
+                    : reinterpret_cast<const void *>(layer_norm_rows_kernel<T, TW, kNum, kRagged, false>);
+    }
+    if constexpr (kNum > 1) return forward_kernel<T, TW, kNum / 2>(s, cols, affine);
     return nullptr;
 }
 
-template <typename T, typename TW, int kVec, int kNum>
-const void *backward_kernel(int num)
+template <typename T, typename TW, int kNum>
+const void *backward_kernel(const RowShape &s, int64_t cols)
 {
-    if (num == kNum) return reinterpret_cast<const void *>(layer_norm_rows_grad_kernel<T, TW, kVec, kNum>);
-    if constexpr (kNum > 1) return backward_kernel<T, TW, kVec, kNum / 2>(num);
+    if (s.num == kNum) {
+        const bool full = cols * (int64_t)sizeof(T) == (int64_t)s.num * s.threads * 16;
+        if (s.threads <= 32)
+            return full ? reinterpret_cast<const void *>(layer_norm_rows_grad_kernel<T, TW, kNum, kFull, true>)
+                        : reinterpret_cast<const void *>(layer_norm_rows_grad_kernel<T, TW, kNum, kRagged, true>);
+        return full ? reinterpret_cast<const void *>(layer_norm_rows_grad_kernel<T, TW, kNum, kFull, false>)
+                    : reinterpret_cast<const void *>(layer_norm_rows_grad_kernel<T, TW, kNum, kRagged, false>);
+    }
+    if constexpr (kNum > 1) return backward_kernel<T, TW, kNum / 2>(s, cols);
+    return nullptr;
+}
+
+template <typename T, typename TW, int kNum>
+const void *forward_pieces(const RowShape &s)
+{
+    if (s.num == kNum)
+        return s.threads <= 32 ? reinterpret_cast<const void *>(layer_norm_pieces_kernel<T, TW, kNum, true>)
+                               : reinterpret_cast<const void *>(layer_norm_pieces_kernel<T, TW, kNum, false>);
+    if constexpr (kNum > 8) return forward_pieces<T, TW, kNum / 2>(s);
+    return nullptr;
+}
+
+template <typename T, typename TW, int kNum>
+const void *backward_pieces(const RowShape &s)
+{
+    if (s.num == kNum)
+        return s.threads <= 32 ? reinterpret_cast<const void *>(layer_norm_pieces_grad_kernel<T, TW, kNum, true>)
+                               : reinterpret_cast<const void *>(layer_norm_pieces_grad_kernel<T, TW, kNum, false>);
+    if constexpr (kNum > 8) return backward_pieces<T, TW, kNum / 2>(s);
     return nullptr;
 }
 
 template <typename T, typename TW>
 cudaError_t forward(const LayerNormArgs &a, int sm_count, cudaStream_t st)
 {
+    constexpr int kVec = 16 / sizeof(T);
+    const bool vectors = a.cols % kVec == 0 && rows_on_16_bytes(a.x, a.rows, a.x_ld, a.dtype) && rows_on_16_bytes(a.y, a.rows, a.y_ld, a.dtype) &&
+                         on_16_bytes(a.weight) && on_16_bytes(a.bias);
     RowLaunch l;
-    const int vec = forward_vec(a);
-    l.shape = row_shape(a.rows, a.cols, vec, vec == 1 ? kMostOne : kMostVec, sm_count);
+    if (vectors) l.shape = row_shape(a.rows, a.cols, kVec, 4, sm_count);
+    if (l.shape.num == 0 && a.cols <= 1 << 16) l.shape = piece_shape(a.rows, a.cols, piece_bytes<T>((int)a.cols), 32, sm_count);
     if (l.shape.num == 0) {
         layer_norm_kernel<T, TW><<<row_grid(a.rows), kThreads, 0, st>>>(a);
         return cudaGetLastError();
     }
-    l.kernel = vec == 1 ? forward_kernel<T, TW, 1, kMostOne>(l.shape.num) : forward_kernel<T, TW, 16 / sizeof(T), kMostVec>(l.shape.num);
-    void *args[] = {const_cast<LayerNormArgs *>(&a), &l.shape.warps};
-    return cudaLaunchKernel(l.kernel, dim3((unsigned)l.grid(a.rows, sm_count)), dim3(l.shape.threads()), args, 0, st);
+    if (l.shape.pieces) {
+        l.kernel = forward_pieces<T, TW, 32>(l.shape);
+        l.shared = (size_t)2 * piece_bytes<T>((int)a.cols) * (l.shape.threads <= 32 ? kSoloWarps : 1);
+    } else {
+        l.kernel = forward_kernel<T, TW, kMostNum>(l.shape, a.cols, a.weight && a.bias);
+        l.shared = (size_t)kDepth * l.shape.num * l.shape.block() * 16;
+    }
+    void *args[] = {const_cast<LayerNormArgs *>(&a), &l.shape.threads};
+    return cudaLaunchKernel(l.kernel, dim3((unsigned)l.grid(a.rows, sm_count)), dim3(l.shape.block()), args, l.shared, st);
 }
 
 template <typename T, typename TW>
 RowLaunch backward_launch(const LayerNormGradArgs &a, int sm_count)
 {
+    constexpr int kVec = 16 / sizeof(T);
+    const bool vectors = a.cols % kVec == 0 && rows_on_16_bytes(a.x, a.rows, a.x_ld, a.dtype) && rows_on_16_bytes(a.dy, a.rows, a.dy_ld, a.dtype) &&
+                         rows_on_16_bytes(a.dx, a.rows, a.dx_ld, a.dtype) && on_16_bytes(a.weight);
     RowLaunch l;
-    const int vec = backward_vec(a);
-    l.shape = row_shape(a.rows, a.cols, vec, vec == 1 ? kMostOne : kMostVec, sm_count);
-    if (a.rows == 0) l.shape.num = 0;
+    if (vectors && a.rows > 0) l.shape = row_shape(a.rows, a.cols, kVec, 2, sm_count);
+    if (l.shape.num == 0 && a.rows > 0 && a.cols <= 1 << 16) l.shape = piece_shape(a.rows, a.cols, 2 * (int64_t)piece_bytes<T>((int)a.cols),
+                                                                                       a.rows * a.cols < (8 << 20) ? 8 : 16, sm_count);
     if (l.shape.num == 0) return l;
-    l.kernel = vec == 1 ? backward_kernel<T, TW, 1, kMostOne>(l.shape.num) : backward_kernel<T, TW, 16 / sizeof(T), kMostVec>(l.shape.num);
-    if (l.shape.warps == 1 && (a.dweight || a.dbias)) l.shared = sizeof(float) * 2 * (size_t)a.cols;
+    if (l.shape.pieces) {      // (also room for the sums of the columns, 8 bytes each)
+        l.kernel = backward_pieces<T, TW, 32>(l.shape);
+        l.shared = (size_t)4 * piece_bytes<T>((int)a.cols) * (l.shape.threads <= 32 ? kSoloWarps : 1);
+    } else {                   // (the same: 32 lanes' columns)
+        l.kernel = backward_kernel<T, TW, kMostNum>(l.shape, a.cols);
+        l.shared = (size_t)kDepth * 2 * l.shape.num * l.shape.block() * 16;
+    }
     return l;
 }
 
@@ -537,9 +1020,9 @@ cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int 
     const RowLaunch l = backward_launch(a, sm_count);
     cudaError_t e;
     if (l.kernel != nullptr) {
-        int warps = l.shape.warps;
-        void *args[] = {const_cast<LayerNormGradArgs *>(&a), &part, &warps};
-        e = cudaLaunchKernel(l.kernel, dim3((unsigned)slices), dim3(l.shape.threads()), args, l.shared, st);
+        int threads = l.shape.threads;
+        void *args[] = {const_cast<LayerNormGradArgs *>(&a), &part, &threads};
+        e = cudaLaunchKernel(l.kernel, dim3((unsigned)slices), dim3(l.shape.block()), args, l.shared, st);
         *launches += 1;
     } else if (a.dtype == GG_F32 && a.w_dtype == GG_F32) {
         e = backward_any<float, float>(a, slices, part, launches, st);
