@@ -324,34 +324,46 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
         }
         copies_wait<kDepth - 1>();
         const bool live = !kSolo || r < a.rows;
+        // kAgain: 32 elements of a thread in fp32 twice, beside the sums of their columns, do not fit the registers: the second
+        // pass reads and computes them again
+        constexpr bool kAgain = kNum * kPairs > 8;
         f32x2 xhat[kNum][kPairs], d[kNum][kPairs], t0 = 0, t1 = 0;
-        if (live) {
-            Few<T> raw_x[kNum], raw_dy[kNum];
-            rows.read(slot, 0, raw_dy);
-            rows.read(slot, 1, raw_x);
+        const uint32_t now = slot;
+        auto load = [&](int k, f32x2 (&xh)[kPairs], f32x2 (&g)[kPairs]) {
+            Few<T> raw_dy, raw_x;
+            raw_dy.read(now + k * rows.step);
+            raw_x.read(now + (kNum + k) * rows.step);
+#pragma unroll
+            for (int i = 0; i < kPairs; ++i) {
+                xh[i] = mul2(add2(raw_x.get(i), minus), by);
+                g[i] = raw_dy.get(i);
+            }
+        };
+        auto weigh = [&](int k, f32x2 (&g)[kPairs]) {
+            if (weight) {
+                f32x2 w[kPairs];
+                read_vector(weight + rows.column(k), w);
+#pragma unroll
+                for (int i = 0; i < kPairs; ++i) g[i] = mul2(g[i], w[i]);
+            }
+        };
+        if (live)
 #pragma unroll
             for (int k = 0; k < kNum; ++k)
                 if (rows.has(k)) {
+                    load(k, xhat[k], d[k]);
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) {
-                        xhat[k][i] = mul2(add2(raw_x[k].get(i), minus), by);
-                        d[k][i] = raw_dy[k].get(i);
                         dw[k][i] = fma2(d[k][i], xhat[k][i], dw[k][i]);
                         db[k][i] = add2(db[k][i], d[k][i]);
                     }
-                    if (weight) {
-                        f32x2 w[kPairs];
-                        read_vector(weight + rows.column(k), w);
-#pragma unroll
-                        for (int i = 0; i < kPairs; ++i) d[k][i] = mul2(d[k][i], w[i]);
-                    }
+                    weigh(k, d[k]);
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) {
                         t0 = add2(t0, d[k][i]);
                         t1 = fma2(d[k][i], xhat[k][i], t1);
                     }
                 }
-        }
         slot = rows.after(slot);
         if (a.dx == nullptr) continue;
         const float2 f0 = halves(t0), f1 = halves(t1);
@@ -362,6 +374,10 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
 #pragma unroll
             for (int k = 0; k < kNum; ++k)
                 if (rows.has(k)) {
+                    if (kAgain) {
+                        load(k, xhat[k], d[k]);
+                        weigh(k, d[k]);
+                    }
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) d[k][i] = fma2(xhat[k][i], c2, fma2(d[k][i], by, c1));
                     Few<T>::store(dx + k * threads * rows.kVec, d[k]);
