@@ -354,8 +354,9 @@ gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dty
  * 8-bit states: m and sqrt(v) as e4m3 codes (1 byte an element), each block of GG_ADAMW_BLOCK elements of a tensor,
  * counted from its start, with a scale of its own: the value is code * scale.  The scales of all tensors follow one
  * another, ceil(len / GG_ADAMW_BLOCK) for each in the order of the list.  The step updates w from m and v before they
- * are rounded; the codes are then rounded stochastically (sqrt(v) > 0 never to 0).  A block of which the largest
- * magnitude is below 2^-110 is stored as zeros.  Zeroed codes and scales are the state before the first step.
+ * are rounded; the codes are then rounded stochastically (sqrt(v) above 2^-62 never to 0).  A block of which the
+ * largest |m| is below 2^-110, or the largest sqrt(v) below 2^-62, is stored as zeros.  Zeroed codes and scales are
+ * the state before the first step.
  * The noise of the rounding is Philox4x32-10 at counter (j, j div 2^32, t, segment index) and key `seed`, 128 bits for
  * elements 8j .. 8j+7 of a segment: the same call gives the same bits. */
 #define GG_ADAMW_BLOCK 256

@@ -28,6 +28,7 @@ namespace {
 
 constexpr int kThreads = kStepWarps * 32;
 constexpr int kPerLane = kBlock / 32;
+constexpr float kZeroRoot = 0x1p-62f;      // roots of v up to this count as 0 (see sqrt2)
 constexpr int kDepth = 3;                  // blocks of a warp in flight or at work
 
 // The entry of the table that owns tile t.
@@ -49,10 +50,10 @@ struct Element { float w, m, v, r; };
 __device__ __forceinline__ Element adamw_element(const StepScalars &c, float keep, float w, float g, float m, float v)
 {
     Element e;
-    e.m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.one_b1, g));
-    e.v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.one_b2, __fmul_rn(g, g)));
+    e.m = __fadd_rn(__fmul_rn(c.b1.x, m), __fmul_rn(c.one_b1.x, g));
+    e.v = __fadd_rn(__fmul_rn(c.b2.x, v), __fmul_rn(c.one_b2.x, __fmul_rn(g, g)));
     e.r = __fsqrt_rn(e.v);
-    e.w = __fmul_rn(w, keep) - c.step * (e.m / (e.r * c.root + c.eps));
+    e.w = __fmul_rn(w, keep) + c.step.x * (e.m / (e.r * c.root.x + c.eps.x));
     return e;
 }
 
@@ -60,14 +61,14 @@ __device__ __forceinline__ Element adamw_element(const StepScalars &c, float kee
 __device__ __forceinline__ Element adamw_element_narrow(const StepScalars &c, float keep, float w, float g, float m, float v)
 {
     Element e;
-    e.m = __fadd_rn(__fmul_rn(c.b1, m), __fmul_rn(c.one_b1, g));
-    e.v = __fadd_rn(__fmul_rn(c.b2, v), __fmul_rn(c.one_b2, __fmul_rn(g, g)));
+    e.m = __fadd_rn(__fmul_rn(c.b1.x, m), __fmul_rn(c.one_b1.x, g));
+    e.v = __fadd_rn(__fmul_rn(c.b2.x, v), __fmul_rn(c.one_b2.x, __fmul_rn(g, g)));
+    const float v1 = __fadd_rn(e.v, 0x1p-126f);
     float y;
-    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(e.v));
-    y = fminf(y, 0x1p63f);
-    const float r = __fmul_rn(e.v, y);
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v1));
+    const float r = __fmul_rn(v1, y);
     e.r = e.v < INFINITY ? __fmaf_rn(r, __fmaf_rn(__fmul_rn(y, -0.5f), r, 0.5f), r) : e.v;
-    e.w = __fmaf_rn(-c.step, __fmul_rn(e.m, rcp_approx(__fmaf_rn(e.r, c.root, c.eps))), __fmul_rn(w, keep));
+    e.w = __fmaf_rn(c.step.x, __fmul_rn(e.m, rcp_approx(__fmaf_rn(e.r, c.root.x, c.eps.x))), __fmul_rn(w, keep));
     return e;
 }
 
@@ -90,21 +91,18 @@ __device__ __forceinline__ float block_top(const float (&x)[kPerLane])
     return __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, top));
 }
 
-// The scale of a block and what its values are multiplied by, 448 / top: a quotient from the approximate reciprocal with
+// The scales of a block's states and what their values are multiplied by, 448 / top: a quotient from the approximate reciprocal with
 // one Newton step on its remainder, which rounds to nearest (but for about one in a million).
 constexpr float kLargeTop = 16384.0f;
-template <bool kAny>
-struct BlockScale {
-    float scale, inv;
-    __device__ __forceinline__ explicit BlockScale(float top)
-    {
-        const bool fits = top > 0x1p-110f;
-        const float y = rcp_approx(top), q = __fmul_rn(448.0f, y);
-        inv = fits ? __fmaf_rn(__fmaf_rn(-top, q, 448.0f), y, q) : 0.0f;
-        scale = fits ? __fmul_rn(top, 1.0f / 448.0f) : 0.0f;
-        if (kAny && top > kLargeTop) inv = __fdiv_rn(448.0f, top);       // (the reciprocal of the largest numbers is subnormal)
-    }
-};
+__device__ __forceinline__ float2 block_scales(float m_top, float r_top, float2 &scale)
+{
+    const f32x2 top = pair(m_top, r_top), y = pair(rcp_approx(m_top), rcp_approx(r_top)), q = mul2(y, both(448.0f));
+    const f32x2 rest = fma2(pair(-m_top, -r_top), q, both(448.0f));
+    const float2 inv = halves(fma2(rest, y, q)), s = halves(mul2(top, both(1.0f / 448.0f)));
+    const bool m_fits = m_top > 0x1p-110f, r_fits = r_top > kZeroRoot;
+    scale = make_float2(m_fits ? s.x : 0.0f, r_fits ? s.y : 0.0f);
+    return make_float2(m_fits ? inv.x : 0.0f, r_fits ? inv.y : 0.0f);
+}
 
 // x times `inv` (448 / top, or 0) as an e4m3 code.  Below 2^-6 the codes are spaced like the binade above it: adding
 // 2^-6 puts both cases on one grid of 2^20 units of the fp32 pattern.  A value that was inf or nan becomes nan.
@@ -115,7 +113,7 @@ __device__ __forceinline__ uint8_t e4m3_stochastic(float x, float inv, uint32_t 
     const float t = small ? __fadd_rn(a, 0.015625f) : a;
     uint32_t code = ((__float_as_uint(t) + (u * 16u + 8u)) >> 20) - (small ? 968u : 960u);
     code = min(code, 126u);
-    if (keep_above_zero && code == 0u && a > 0.0f) code = 1u;
+    if (keep_above_zero && code == 0u && a > 0.0f && x > kZeroRoot) code = 1u;
     if ((__float_as_uint(x) & 0x7F800000u) == 0x7F800000u) code = 127u;
     return (uint8_t)(code | (__float_as_uint(x) >> 31 << 7));
 }
@@ -131,7 +129,7 @@ __device__ __forceinline__ float e4m3_value(uint8_t code)
 template <bool kNarrow> struct State { using type = float; };
 template <> struct State<true> { using type = uint8_t; };
 
-// Where a warp is in its tensor.
+// Where a warp is in its tensor: each lane points at its eight elements of the block.
 template <typename TW, typename TG, bool kNarrow>
 struct Place {
     using TS = typename State<kNarrow>::type;
@@ -142,14 +140,19 @@ struct Place {
     uint64_t block;            // of the tensor
     uint32_t id;
 
-    __device__ __forceinline__ void advance(int blocks)
+    __device__ __forceinline__ void shift(int elements)
     {
-        w += blocks * kBlock;
-        g += blocks * kBlock;
-        m += blocks * kBlock;
-        v += blocks * kBlock;
-        if (copy) copy += blocks * kBlock;
-        block += (uint64_t)blocks;
+        w += elements;
+        g += elements;
+        m += elements;
+        v += elements;
+        if (copy) copy += elements;
+    }
+
+    __device__ __forceinline__ void advance()
+    {
+        shift(kBlock);
+        ++block;
     }
     // The noise of the eight elements from 8 * lane on.
     __device__ __forceinline__ Block4 noise(const StepScalars &c, int lane) const
@@ -162,9 +165,10 @@ struct Place {
 // One block of n elements at any alignment, with any values: lane l takes the elements l, l + 32, ...  Takes and returns the
 // scales of the block's states in m and in sqrt(v).
 template <typename TW, typename TG, bool kNarrow>
-__device__ __noinline__ float2 step_block_any(const Place<TW, TG, kNarrow> at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
+__device__ __noinline__ float2 step_block_any(Place<TW, TG, kNarrow> at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
 {
     const int lane = threadIdx.x & 31;
+    at.shift(-8 * lane);       // all lanes at the block's start
     const uint16_t *u = reinterpret_cast<const uint16_t *>(noise);
     if (kNarrow || sizeof(TW) == 2) {
         const Block4 q = at.noise(c, lane);
@@ -195,20 +199,22 @@ __device__ __noinline__ float2 step_block_any(const Place<TW, TG, kNarrow> at, i
         if (at.copy) at.copy[e] = narrow<uint16_t>(x.w);
     }
     if constexpr (kNarrow) {
-        const BlockScale<true> ms(block_top(mm)), vs(block_top(rr));
+        const float m_top = block_top(mm), r_top = block_top(rr);
+        float2 inv = block_scales(m_top, r_top, scale);
+        if (m_top > kLargeTop) inv.x = __fdiv_rn(448.0f, m_top);       // (the reciprocal of the largest numbers is subnormal)
+        if (r_top > kLargeTop) inv.y = __fdiv_rn(448.0f, r_top);
 #pragma unroll
         for (int k = 0; k < kPerLane; ++k) {
             const int e = 32 * k + lane;
             if (e >= n) continue;
-            at.m[e] = e4m3_stochastic(mm[k], ms.inv, u[e], false);
-            at.v[e] = e4m3_stochastic(rr[k], vs.inv, u[(e & ~7) + ((e + 4) & 7)], true);
+            at.m[e] = e4m3_stochastic(mm[k], inv.x, u[e], false);
+            at.v[e] = e4m3_stochastic(rr[k], inv.y, u[(e & ~7) + ((e + 4) & 7)], true);
         }
-        scale = make_float2(ms.scale, vs.scale);
     }
     return scale;
 }
 
-// Blocks at vector boundaries with a multiple of eight elements: lane l takes the eight from 8 l on, in pairs.
+// Whole blocks at vector boundaries: lane l takes the eight elements from 8 l on, in pairs.
 template <typename TW, typename TG, bool kNarrow>
 struct Operands {
     using TS = typename State<kNarrow>::type;
@@ -216,16 +222,16 @@ struct Operands {
     Eight<TW> w;
     Eight<TG> g;
     Eight<TS> m, v;
-    // the block `ahead` elements on, n elements of it (a whole block, or a multiple of 8)
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const Place<TW, TG, kNarrow> &at, int ahead, int n)
+    // the block `ahead` elements on
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const Place<TW, TG, kNarrow> &at, int ahead)
     {
-        Eight<TG>::fetch(slot, lane, at.g + ahead, n);
+        Eight<TG>::fetch(slot, lane, at.g + ahead);
         slot += 32 * Eight<TG>::kSlot;
-        Eight<TW>::fetch(slot, lane, at.w + ahead, n);
+        Eight<TW>::fetch(slot, lane, at.w + ahead);
         slot += 32 * Eight<TW>::kSlot;
-        Eight<TS>::fetch(slot, lane, at.m + ahead, n);
+        Eight<TS>::fetch(slot, lane, at.m + ahead);
         slot += 32 * Eight<TS>::kSlot;
-        Eight<TS>::fetch(slot, lane, at.v + ahead, n);
+        Eight<TS>::fetch(slot, lane, at.v + ahead);
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
@@ -241,10 +247,8 @@ struct Operands {
 
 // States in fp32: bound by memory with room to spare, so the arithmetic is the plain one.
 template <typename TW, typename TG>
-__device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const Place<TW, TG, false> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *)
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const Place<TW, TG, false> &at, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *)
 {
-    const int lane = threadIdx.x & 31, e = 8 * lane;
-    if (e >= n) return scale;
     f32x2 wn[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -255,10 +259,10 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const P
         x.m.v[i] = pair(a.m, b.m);
         x.v.v[i] = pair(a.v, b.v);
     }
-    Eight<float>::store(at.m + e, x.m.v);
-    Eight<float>::store(at.v + e, x.v.v);
+    Eight<float>::store(at.m, x.m.v);
+    Eight<float>::store(at.v, x.v.v);
     if constexpr (sizeof(TW) == 2) {
-        const Block4 q = at.noise(c, lane);
+        const Block4 q = at.noise(c, threadIdx.x & 31);
         const uint32_t word[4] = {q.w1, q.w2, q.w3, q.w0};      // element e takes u[e + 2]
         uint32_t out[4];
 #pragma unroll
@@ -266,35 +270,44 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const P
             const float2 f = halves(wn[i]);
             out[i] = (uint32_t)bf16_stochastic(f.x, word[i] & 0xFFFFu) | ((uint32_t)bf16_stochastic(f.y, word[i] >> 16) << 16);
         }
-        Eight<uint16_t>::store_words(at.w + e, out[0], out[1], out[2], out[3]);
+        Eight<uint16_t>::store_words(at.w, out[0], out[1], out[2], out[3]);
     } else {
-        Eight<float>::store(at.w + e, wn);
+        Eight<float>::store(at.w, wn);
     }
-    if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
+    if (at.copy) Eight<uint16_t>::store(at.copy, wn);
     return scale;
 }
 
-// The two e4m3 codes of a 16-bit half.
-__device__ __forceinline__ f32x2 e4m3_pair(uint32_t h)
+// The four e4m3 codes of a word, as two pairs.
+__device__ __forceinline__ void e4m3_pairs(uint32_t w, f32x2 &lo, f32x2 &hi)
 {
-    uint32_t d;
-    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(d) : "h"((uint16_t)h));
-    const __half2 t = *reinterpret_cast<const __half2 *>(&d);
-    const float2 f = __half22float2(t);
-    return pair(f.x, f.y);
+    uint32_t a, b;
+    asm("{\n\t.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.rn.f16x2.e4m3x2 %0, l;\n\tcvt.rn.f16x2.e4m3x2 %1, h;\n\t}" : "=r"(a), "=r"(b) : "r"(w));
+    const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&a)), g = __half22float2(*reinterpret_cast<const __half2 *>(&b));
+    lo = pair(f.x, f.y);
+    hi = pair(g.x, g.y);
+}
+
+// The largest of three; a nan is passed over.
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float d;
+    asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
 }
 
 // sqrt of finite values >= 0 by one Newton step on an approximate reciprocal root y: g = v y, g + g (1/2 - g y / 2).
-// That leaves the rounding of the last sum (and, once in about a million, the neighbour of the nearest value).  Below
-// 2^-126 the result is only of the right size; the step divides by the root plus eps, so nothing there matters.
+// That leaves the rounding of the last sum (and, once in about a million, the neighbour of the nearest value).  2^-126 is
+// added to v, so that y is finite: it changes no v above 2^-102, and the step divides by the root plus eps, so nothing
+// below that matters.  The root of 0 comes out as 2^-63, and roots up to kZeroRoot count as 0.
 __device__ __forceinline__ f32x2 sqrt2(f32x2 v)
 {
+    v = add2(v, both(0x1p-126f));
     const float2 f = halves(v);
     float a, b;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(f.x));
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(f.y));
-    const f32x2 y = pair(fminf(a, 0x1p63f), fminf(b, 0x1p63f));       // (infinite at 0)
-    const f32x2 g = mul2(v, y);
+    const f32x2 y = pair(a, b), g = mul2(v, y);
     return fma2(g, fma2(mul2(y, both(-0.5f)), g, both(0.5f)), g);
 }
 
@@ -311,28 +324,30 @@ __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c
 // of its pattern, and the noise stays eight short of a whole code.  A block that holds an inf or nan, or values so
 // large that 2^-120 448 / top is not a normal number, goes through step_block_any; nothing is stored before that is known.
 template <typename TW, typename TG>
-__device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Place<TW, TG, true> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Place<TW, TG, true> &at, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
 {
-    const int lane = threadIdx.x & 31, e = 8 * lane;
     f32x2 wn[4], mn[4], rn[4];
     f32x2 sum = 0;
     float m_top = 0.0f, r_top = 0.0f;
-    if (e < n) {
-        const f32x2 b1 = both(c.b1), one_b1 = both(c.one_b1), b2 = both(c.b2), one_b2 = both(c.one_b2), gs = both(gscale);
-        const f32x2 ms = both(scale.x), vs = both(scale.y), root = both(c.root), eps = both(c.eps), step = both(-c.step), keep2 = both(keep);
+    {
+        const f32x2 b1 = pair(c.b1), one_b1 = pair(c.one_b1), b2 = pair(c.b2), one_b2 = pair(c.one_b2), gs = both(gscale);
+        const f32x2 ms = both(scale.x), vs = both(scale.y), root = pair(c.root), eps = pair(c.eps), step = pair(c.step), keep2 = both(keep);
+        f32x2 m_old[4], r_old[4];
+        e4m3_pairs(x.m.v.x, m_old[0], m_old[1]);
+        e4m3_pairs(x.m.v.y, m_old[2], m_old[3]);
+        e4m3_pairs(x.v.v.x, r_old[0], r_old[1]);
+        e4m3_pairs(x.v.v.y, r_old[2], r_old[3]);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint32_t mw = i < 2 ? x.m.v.x : x.m.v.y, vw = i < 2 ? x.v.v.x : x.v.v.y;
-            const f32x2 gi = mul2(x.g.get(i), gs);
-            const f32x2 mo = mul2(e4m3_pair(i & 1 ? mw >> 16 : mw), ms), ro = mul2(e4m3_pair(i & 1 ? vw >> 16 : vw), vs);
+            const f32x2 gi = mul2(x.g.get(i), gs), mo = mul2(m_old[i], ms), ro = mul2(r_old[i], vs);
             mn[i] = add2(mul2(b1, mo), mul2(one_b1, gi));
             rn[i] = sqrt2(add2(mul2(b2, mul2(ro, ro)), mul2(one_b2, mul2(gi, gi))));
             const float2 d = halves(fma2(rn[i], root, eps));
             wn[i] = fma2(step, mul2(mn[i], pair(rcp_approx(d.x), rcp_approx(d.y))), mul2(x.w.get(i), keep2));
             sum = i == 0 ? wn[0] : add2(sum, wn[i]);
             const float2 mf = halves(mn[i]), rf = halves(rn[i]);
-            m_top = fmaxf(m_top, fmaxf(fabsf(mf.x), fabsf(mf.y)));
-            r_top = fmaxf(r_top, fmaxf(rf.x, rf.y));
+            m_top = max3(m_top, fabsf(mf.x), fabsf(mf.y));
+            r_top = max3(r_top, rf.x, rf.y);
         }
         // (a maximum passes over a nan, but a nan in m or r is one in w too, and so in the sum)
         const float2 sf = halves(sum);
@@ -341,12 +356,10 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
     m_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m_top)));
     r_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(r_top)));
     if (fmaxf(m_top, r_top) > kLargeTop) {
-        return step_block_any<TW, TG, true>(at, n, c, keep, gscale, scale, noise);
+        return step_block_any<TW, TG, true>(at, kBlock, c, keep, gscale, scale, noise);
     }
-    const BlockScale<false> m_to(m_top), v_to(r_top);
-    scale = make_float2(m_to.scale, v_to.scale);
-    if (e >= n) return scale;
-    const Block4 q = at.noise(c, lane);
+    const float2 inv = block_scales(m_top, r_top, scale);
+    const Block4 q = at.noise(c, threadIdx.x & 31);
     const uint32_t word[4] = {q.w0, q.w1, q.w2, q.w3};
     uint32_t u[8], mt[8], vt[8];
 #pragma unroll
@@ -354,7 +367,7 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
         u[2 * i] = __byte_perm(word[i], 0x80u, 0x5104);
         u[2 * i + 1] = __byte_perm(word[i], 0x80u, 0x5324);
     }
-    const f32x2 m_inv = both(m_to.inv * 0x1p-120f), v_inv = both(v_to.inv * 0x1p-120f);
+    const f32x2 m_inv = both(inv.x * 0x1p-120f), v_inv = both(inv.y * 0x1p-120f);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 zm = halves(mul2(mn[i], m_inv)), zr = halves(mul2(rn[i], v_inv));
@@ -370,16 +383,16 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
         const uint32_t sign = top_bytes(__float_as_uint(s0.x), __float_as_uint(s0.y), __float_as_uint(s1.x), __float_as_uint(s1.y));
         mc[h] = top_bytes(mt[4 * h], mt[4 * h + 1], mt[4 * h + 2], mt[4 * h + 3]) | sign & 0x80808080u;
         vc[h] = top_bytes(vt[4 * h], vt[4 * h + 1], vt[4 * h + 2], vt[4 * h + 3]);
-        if ((vc[h] - 0x01010101u & ~vc[h] & 0x80808080u) != 0u && v_to.inv > 0.0f) {       // a code of 0: 1 unless the root is 0
+        if ((vc[h] - 0x01010101u & ~vc[h] & 0x80808080u) != 0u && inv.y > 0.0f) {       // a code of 0: 1 unless the root is 0
             const float2 r0 = halves(rn[2 * h]), r1 = halves(rn[2 * h + 1]);
             const float r[4] = {r0.x, r0.y, r1.x, r1.y};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if ((vc[h] >> 8 * i & 0xFFu) == 0u && r[i] > 0.0f) vc[h] |= 1u << 8 * i;
+                if ((vc[h] >> 8 * i & 0xFFu) == 0u && r[i] > kZeroRoot) vc[h] |= 1u << 8 * i;
         }
     }
-    Eight<uint8_t>::store(at.m + e, mc[0], mc[1]);
-    Eight<uint8_t>::store(at.v + e, vc[0], vc[1]);
+    Eight<uint8_t>::store(at.m, mc[0], mc[1]);
+    Eight<uint8_t>::store(at.v, vc[0], vc[1]);
     if constexpr (sizeof(TW) == 2) {
         uint32_t out[4];
 #pragma unroll
@@ -388,18 +401,18 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
             const uint32_t k = word[i + 1 & 3];
             out[i] = __byte_perm(__float_as_uint(f.x) + (k & 0xFFFFu), __float_as_uint(f.y) + (k >> 16), 0x7632);
         }
-        Eight<uint16_t>::store_words(at.w + e, out[0], out[1], out[2], out[3]);
+        Eight<uint16_t>::store_words(at.w, out[0], out[1], out[2], out[3]);
     } else {
-        Eight<float>::store(at.w + e, wn);
+        Eight<float>::store(at.w, wn);
     }
-    if (at.copy) Eight<uint16_t>::store(at.copy + e, wn);
+    if (at.copy) Eight<uint16_t>::store(at.copy, wn);
     return scale;
 }
 
 // A CTA per tile, a warp per run of blocks.  A warp fetches its operands kDepth - 1 blocks ahead into places of shared
 // memory that are its own (no barrier of the CTA), so that neither registers nor occupancy limit what is in flight.
 template <typename TW, typename TG, bool kNarrow, int N>
-__global__ void __launch_bounds__(kThreads, kNarrow ? 3 : 2) adamw_kernel(const __grid_constant__ StepTable<N> tab, const __grid_constant__ StepScalars c)
+__global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constant__ StepTable<N> tab, const __grid_constant__ StepScalars c)
 {
     using Data = Operands<TW, TG, kNarrow>;
     extern __shared__ __align__(16) unsigned char ring[];
@@ -413,22 +426,27 @@ __global__ void __launch_bounds__(kThreads, kNarrow ? 3 : 2) adamw_kernel(const 
     const int64_t first = (int64_t)at.block * kBlock;
     int left = (int)min((int64_t)tab.per_warp * kBlock, tab.len[s] - first);      // elements of this warp
     if (left <= 0) return;
-    at.w = static_cast<TW *>(tab.w[s]) + first;
-    at.g = static_cast<const TG *>(tab.g[s]) + first;
-    at.m = static_cast<typename State<kNarrow>::type *>(tab.m[s]) + first;
-    at.v = static_cast<typename State<kNarrow>::type *>(tab.v[s]) + first;
-    at.copy = tab.copy[s] ? static_cast<uint16_t *>(tab.copy[s]) + first : nullptr;
+    at.w = static_cast<TW *>(tab.w[s]);
+    at.g = static_cast<const TG *>(tab.g[s]);
+    at.m = static_cast<typename State<kNarrow>::type *>(tab.m[s]);
+    at.v = static_cast<typename State<kNarrow>::type *>(tab.v[s]);
+    at.copy = static_cast<uint16_t *>(tab.copy[s]);
+    at.w += first + 8 * lane;
+    at.g += first + 8 * lane;
+    at.m += first + 8 * lane;
+    at.v += first + 8 * lane;
+    if (at.copy) at.copy += first + 8 * lane;
     // lane l holds the scales of block l of the run
     const int64_t my_scale = (int64_t)tab.block0[s] + (int64_t)at.block + lane;
     const bool has_scale = kNarrow && lane * kBlock < left;
     float2 scales = has_scale ? make_float2(c.m_scale[my_scale], c.v_scale[my_scale]) : make_float2(0.0f, 0.0f);
 
-    int fast = id < 0 ? (left % 8 == 0 ? left : left & ~(kBlock - 1)) : 0;        // of these, through the ring
+    int fast = id < 0 ? left & ~(kBlock - 1) : 0;        // of these, through the ring
     left -= fast;
     const uint32_t slots = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kDepth * Data::kSlot);
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) {
-        Data::fetch(slots + d * Data::kSlot, lane, at, d * kBlock, fast - d * kBlock);
+        if (d * kBlock < fast) Data::fetch(slots + d * Data::kSlot, lane, at, d * kBlock);
         copies_commit();
     }
     const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
@@ -441,22 +459,22 @@ __global__ void __launch_bounds__(kThreads, kNarrow ? 3 : 2) adamw_kernel(const 
     auto scale_of = [&]() { return kNarrow ? make_float2(__shfl_sync(0xFFFFFFFFu, scales.x, k), __shfl_sync(0xFFFFFFFFu, scales.y, k)) : scales; };
     for (uint32_t d = 0; fast > 0; d = d == kDepth - 1 ? 0 : d + 1) {
         __syncwarp();      // every lane has read the place of the block before this one: the block after the next ones goes there
-        Data::fetch(slots + (d == 0 ? kDepth - 1 : d - 1) * Data::kSlot, lane, at, (kDepth - 1) * kBlock, fast - (kDepth - 1) * kBlock);
+        if (fast > (kDepth - 1) * kBlock) Data::fetch(slots + (d == 0 ? kDepth - 1 : d - 1) * Data::kSlot, lane, at, (kDepth - 1) * kBlock);
         copies_commit();
         copies_wait<kDepth - 1>();
         __syncwarp();      // every lane's copies of this block have arrived
         Data x;
         x.read(slots + d * Data::kSlot, lane);
-        const float2 now = step_eight(x, at, min(fast, kBlock), c, keep, gscale, scale_of(), noise[warp]);
+        const float2 now = step_eight(x, at, c, keep, gscale, scale_of(), noise[warp]);
         if (lane == k) scales = now;
-        at.advance(1);
+        at.advance();
         fast -= kBlock;
         ++k;
     }
     for (; left > 0; left -= kBlock) {
         const float2 now = step_block_any<TW, TG, kNarrow>(at, min(left, kBlock), c, keep, gscale, scale_of(), noise[warp]);
         if (lane == k) scales = now;
-        at.advance(1);
+        at.advance();
         ++k;
     }
     if (has_scale) {
@@ -469,8 +487,8 @@ template <typename TW, typename TG, bool kNarrow, int N>
 cudaError_t launch_one(const StepTable<N> &tab, const StepScalars &c, cudaStream_t st)
 {
     constexpr int kBytes = kStepWarps * kDepth * Operands<TW, TG, kNarrow>::kSlot;
-    const cudaError_t e = cudaFuncSetAttribute(adamw_kernel<TW, TG, kNarrow, N>, cudaFuncAttributeMaxDynamicSharedMemorySize, kBytes);
-    if (e != cudaSuccess) return e;
+    constexpr int kNoise = kNarrow || sizeof(TW) == 2 ? kStepWarps * kBlock * 2 : 0;
+    static_assert(kBytes + kNoise <= 48 * 1024, "more would have to be asked for");
     adamw_kernel<TW, TG, kNarrow, N><<<(unsigned)tab.tile0[tab.n], kThreads, kBytes, st>>>(tab, c);
     return cudaGetLastError();
 }

@@ -8,7 +8,7 @@
 namespace gg {
 
 constexpr int kBlock = GG_ADAMW_BLOCK;      // elements that share one scale of an 8-bit state
-constexpr int kStepWarps = 8;               // warps of a CTA
+constexpr int kStepWarps = 4;               // warps of a CTA
 constexpr int kTableSmall = 64, kTableLarge = 512;
 
 // The tensors of one launch, passed by value: kernel parameters may take 32,764 bytes, which holds 512 tensors.  A
@@ -34,10 +34,12 @@ struct StepScalars {
     const float *grad_scale;       // device, or null
     const float *decay;            // device [n_seg], or null: decay_all
     float *m_scale, *v_scale;      // device, 8-bit states
-    float b1, one_b1, b2, one_b2, lr, decay_all;
-    float step;                    // lr / (1 - b1^t)
-    float root;                    // 1 / sqrt(1 - b2^t)
-    float eps;
+    // each twice, as the two halves of a pair
+    float2 b1, one_b1, b2, one_b2;
+    float2 step;                   // -lr / (1 - b1^t)
+    float2 root;                   // 1 / sqrt(1 - b2^t)
+    float2 eps;
+    float lr, decay_all;
     uint32_t t;
     uint32_t key[20];              // the key of each round of Philox: seed mod 2^32 + r * W0, seed div 2^32 + r * W1
 };

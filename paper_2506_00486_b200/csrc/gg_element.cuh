@@ -23,6 +23,7 @@ __device__ __forceinline__ f32x2 pair(float lo, float hi)
     return d;
 }
 __device__ __forceinline__ f32x2 both(float v) { return pair(v, v); }
+__device__ __forceinline__ f32x2 pair(const float2 &v) { return pair(v.x, v.y); }
 __device__ __forceinline__ float2 halves(f32x2 v)
 {
     float2 d;
@@ -139,12 +140,13 @@ template <typename T> struct Eight;
 template <> struct Eight<float> {
     static constexpr int kSlot = 32;
     f32x2 v[4];
-    // p: the block's first element; n: its elements
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const float *p, int n)
+    // p: the lane's eight elements of the warp's 256
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const float *p)
     {
+        p -= 4 * lane;
         const uint32_t to = slot + (uint32_t)(lane ^ (lane >> 3 & 1)) * 16u;
-        if (4 * lane < n) copy16(to, p + 4 * lane);
-        if (4 * lane + 128 < n) copy16(to + 512u, p + 4 * lane + 128);
+        copy16(to, p);
+        copy16(to + 512u, p + 128);
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
@@ -161,10 +163,7 @@ template <> struct Eight<float> {
 template <> struct Eight<uint16_t> {
     static constexpr int kSlot = 16;
     uint4 v;
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint16_t *p, int n)
-    {
-        if (8 * lane < n) copy16(slot + lane * 16, p + 8 * lane);
-    }
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint16_t *p) { copy16(slot + lane * 16, p); }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slot + lane * 16) : "memory");
@@ -182,10 +181,7 @@ template <> struct Eight<uint16_t> {
 template <> struct Eight<uint8_t> {
     static constexpr int kSlot = 8;
     uint2 v;
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint8_t *p, int n)
-    {
-        if (8 * lane < n) copy8(slot + lane * 8, p + 8 * lane);
-    }
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint8_t *p) { copy8(slot + lane * 8, p); }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
         asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(slot + lane * 8) : "memory");
