@@ -31,17 +31,16 @@ constexpr int kPerLane = kBlock / 32;
 constexpr float kZeroRoot = 0x1p-62f;      // roots of v up to this count as 0 (see sqrt2)
 constexpr int kDepth = 3;                  // blocks of a warp in flight or at work
 
-// The entry of the table that owns tile t.
+// The entry of the table that owns tile t: the lanes look at N / 32 evenly spaced entries each.  (All lanes of a warp at
+// once: a search by halves would wait for the parameters six to nine times over, about 2 us of a small step's 6.)
 template <int N>
 __device__ __forceinline__ int find_entry(const StepTable<N> &tab, int32_t t)
 {
-    int lo = 0, hi = tab.n;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) >> 1;
-        if (tab.tile0[mid] <= t) lo = mid;
-        else hi = mid;
-    }
-    return lo;
+    constexpr int kStride = N / 32;
+    const int lane = threadIdx.x & 31;
+    const int coarse = 31 - __clz(__ballot_sync(0xFFFFFFFFu, tab.tile0[lane * kStride] <= t));      // (entry 0 starts at tile 0)
+    const int fine = __ballot_sync(0xFFFFFFFFu, lane < kStride && tab.tile0[coarse * kStride + (lane & (kStride - 1))] <= t);
+    return coarse * kStride + 31 - __clz(fine);
 }
 
 struct Element { float w, m, v, r; };
@@ -419,25 +418,26 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constan
     __shared__ __align__(16) uint32_t noise[kStepWarps][kBlock / 2];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int s = find_entry(tab, (int32_t)blockIdx.x);
-    const int32_t id = tab.id[s];
+    const StepEntry &entry = tab.entry[s];
+    const int32_t id = entry.id;
     Place<TW, TG, kNarrow> at;
     at.block = ((uint64_t)(blockIdx.x - tab.tile0[s]) * kStepWarps + warp) * (uint32_t)tab.per_warp;
     at.id = (uint32_t)(id & ~kAligned);
     const int64_t first = (int64_t)at.block * kBlock;
-    int left = (int)min((int64_t)tab.per_warp * kBlock, tab.len[s] - first);      // elements of this warp
+    int left = (int)min((int64_t)tab.per_warp * kBlock, entry.len - first);      // elements of this warp
     if (left <= 0) return;
-    at.w = static_cast<TW *>(tab.w[s]);
-    at.g = static_cast<const TG *>(tab.g[s]);
-    at.m = static_cast<typename State<kNarrow>::type *>(tab.m[s]);
-    at.v = static_cast<typename State<kNarrow>::type *>(tab.v[s]);
-    at.copy = static_cast<uint16_t *>(tab.copy[s]);
+    at.w = static_cast<TW *>(entry.w);
+    at.g = static_cast<const TG *>(entry.g);
+    at.m = static_cast<typename State<kNarrow>::type *>(entry.m);
+    at.v = static_cast<typename State<kNarrow>::type *>(entry.v);
+    at.copy = static_cast<uint16_t *>(entry.copy);
     at.w += first + 8 * lane;
     at.g += first + 8 * lane;
     at.m += first + 8 * lane;
     at.v += first + 8 * lane;
     if (at.copy) at.copy += first + 8 * lane;
     // lane l holds the scales of block l of the run
-    const int64_t my_scale = (int64_t)tab.block0[s] + (int64_t)at.block + lane;
+    const int64_t my_scale = (int64_t)entry.block0 + (int64_t)at.block + lane;
     const bool has_scale = kNarrow && lane * kBlock < left;
     float2 scales = has_scale ? make_float2(c.m_scale[my_scale], c.v_scale[my_scale]) : make_float2(0.0f, 0.0f);
 
@@ -489,7 +489,7 @@ cudaError_t launch_one(const StepTable<N> &tab, const StepScalars &c, cudaStream
     constexpr int kBytes = kStepWarps * kDepth * Operands<TW, TG, kNarrow>::kSlot;
     constexpr int kNoise = kNarrow || sizeof(TW) == 2 ? kStepWarps * kBlock * 2 : 0;
     static_assert(kBytes + kNoise <= 48 * 1024, "more would have to be asked for");
-    adamw_kernel<TW, TG, kNarrow, N><<<(unsigned)tab.tile0[tab.n], kThreads, kBytes, st>>>(tab, c);
+    adamw_kernel<TW, TG, kNarrow, N><<<(unsigned)tab.tiles, kThreads, kBytes, st>>>(tab, c);
     return cudaGetLastError();
 }
 

@@ -9,26 +9,29 @@ namespace gg {
 
 constexpr int kBlock = GG_ADAMW_BLOCK;      // elements that share one scale of an 8-bit state
 constexpr int kStepWarps = 4;               // warps of a CTA
-constexpr int kTableSmall = 64, kTableLarge = 512;
+constexpr int kTableSmall = 64, kTableLarge = 512;      // (multiples of 64)
 
 // The tensors of one launch, passed by value: kernel parameters may take 32,764 bytes, which holds 512 tensors.  A
 // step so needs no device memory of its own, no upload and no cache, whatever addresses the tensors have this time.
 // Two sizes: a launch with up to 4 KB of parameters costs the host 2.7 us, one with 30 KB 5.5 us (and 4 us more until
 // the kernel has ended), so up to 64 tensors take the small table.
+struct StepEntry {
+    void *w;
+    const void *g;
+    void *m, *v, *copy;
+    int64_t len;
+    int32_t block0;            // first scale of the tensor (8-bit states)
+    int32_t id;                // its place in the caller's list; bit 31: every array starts where Eight wants it
+};
 template <int N>
 struct StepTable {
-    void *w[N];
-    const void *g[N];
-    void *m[N], *v[N], *copy[N];
-    int64_t len[N];
-    int32_t tile0[N + 1];      // first tile of each tensor; [n]: the number of tiles
-    int32_t block0[N];         // first scale of each tensor (8-bit states)
-    int32_t id[N];             // its place in the caller's list; bit 31: every array starts where Eight wants it
-    int32_t n;
+    int32_t tile0[N];          // first tile of each tensor; beyond the last, INT32_MAX
+    StepEntry entry[N];
+    int32_t n, tiles;
     int32_t per_warp;          // (at most 32) blocks of a tensor that one warp steps, one after the other; a tile is kStepWarps times that
 };
 constexpr int32_t kAligned = (int32_t)0x80000000;
-static_assert(sizeof(StepTable<512>) <= 32 * 1024 - 256, "the table and the scalars have to fit the kernel parameters");
+static_assert(sizeof(StepTable<512>) <= 32 * 1024 - 512 && sizeof(StepTable<64>) <= 4096 - 224, "the table and the scalars have to fit the kernel parameters");
 
 struct StepScalars {
     const float *grad_scale;       // device, or null

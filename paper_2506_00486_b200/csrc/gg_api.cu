@@ -1526,27 +1526,28 @@ template <int N>
 int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int per_warp, int32_t s, int64_t &block)
 {
     const int tile_blocks = per_warp * kStepWarps;
+    const uintptr_t state_at = a.state_bits == 8 ? 8 : 32, w_at = a.w_dtype == GG_F32 ? 32 : 16, g_at = a.g_dtype == GG_F32 ? 32 : 16;
+    auto on = [](const void *p, uintptr_t boundary) { return reinterpret_cast<uintptr_t>(p) % boundary == 0; };
     tab.per_warp = per_warp;
     tab.n = 0;
-    tab.tile0[0] = 0;
+    int64_t tiles = 0;
     for (; s < a.n_seg; ++s) {
         const int64_t len = a.w[s].len, blocks = (len + kBlock - 1) / kBlock;
         if (len == 0) continue;
-        const int64_t tiles = (blocks + tile_blocks - 1) / tile_blocks;
-        if (tab.n == N || tab.tile0[tab.n] + tiles > 0x7FFFFFFFll) break;
-        const int i = tab.n++;
-        tab.w[i] = a.w[s].ptr; tab.g[i] = a.g[s].ptr; tab.m[i] = a.m[s].ptr; tab.v[i] = a.v[s].ptr;
-        tab.copy[i] = a.w_copy ? a.w_copy[s].ptr : nullptr;
-        tab.len[i] = len;
-        tab.block0[i] = (int32_t)block;
-        const uintptr_t narrow = a.state_bits == 8 ? 8 : 32, w_at = a.w_dtype == GG_F32 ? 32 : 16, g_at = a.g_dtype == GG_F32 ? 32 : 16;
-        const bool aligned = reinterpret_cast<uintptr_t>(tab.w[i]) % w_at == 0 && reinterpret_cast<uintptr_t>(tab.g[i]) % g_at == 0 &&
-                             (reinterpret_cast<uintptr_t>(tab.m[i]) | reinterpret_cast<uintptr_t>(tab.v[i])) % narrow == 0 &&
-                             reinterpret_cast<uintptr_t>(tab.copy[i]) % 16 == 0;
-        tab.id[i] = aligned ? s | kAligned : s;
-        tab.tile0[i + 1] = (int32_t)(tab.tile0[i] + tiles);
+        const int64_t more = (blocks + tile_blocks - 1) / tile_blocks;
+        if (tab.n == N || tiles + more > 0x7FFFFFFEll) break;
+        StepEntry &e = tab.entry[tab.n];
+        e.w = a.w[s].ptr; e.g = a.g[s].ptr; e.m = a.m[s].ptr; e.v = a.v[s].ptr;
+        e.copy = a.w_copy ? a.w_copy[s].ptr : nullptr;
+        e.len = len;
+        e.block0 = (int32_t)block;
+        e.id = on(e.w, w_at) && on(e.g, g_at) && on(e.m, state_at) && on(e.v, state_at) && on(e.copy, 16) ? s | kAligned : s;
+        tab.tile0[tab.n++] = (int32_t)tiles;
+        tiles += more;
         block += blocks;
     }
+    tab.tiles = (int32_t)tiles;
+    for (int i = tab.n; i < N; ++i) tab.tile0[i] = 0x7FFFFFFF;
     return s;
 }
 
