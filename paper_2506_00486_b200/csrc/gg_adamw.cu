@@ -213,7 +213,8 @@ __device__ __noinline__ float2 step_block_any(Place<TW, TG, kNarrow> at, int n, 
     return scale;
 }
 
-// Whole blocks at vector boundaries: lane l takes the eight elements from 8 l on, in pairs.
+// Blocks at vector boundaries with a multiple of eight elements: lane l takes the eight from 8 l on, in pairs.  Lanes beyond the
+// block's end (`live` is false) compute on zeros and store nothing.
 template <typename TW, typename TG, bool kNarrow>
 struct Operands {
     using TS = typename State<kNarrow>::type;
@@ -221,16 +222,16 @@ struct Operands {
     Eight<TW> w;
     Eight<TG> g;
     Eight<TS> m, v;
-    // the block `ahead` elements on
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const Place<TW, TG, kNarrow> &at, int ahead)
+    // the block `ahead` elements on, n elements of it
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const Place<TW, TG, kNarrow> &at, int ahead, int n)
     {
-        Eight<TG>::fetch(slot, lane, at.g + ahead);
+        Eight<TG>::fetch(slot, lane, at.g + ahead, n);
         slot += 32 * Eight<TG>::kSlot;
-        Eight<TW>::fetch(slot, lane, at.w + ahead);
+        Eight<TW>::fetch(slot, lane, at.w + ahead, n);
         slot += 32 * Eight<TW>::kSlot;
-        Eight<TS>::fetch(slot, lane, at.m + ahead);
+        Eight<TS>::fetch(slot, lane, at.m + ahead, n);
         slot += 32 * Eight<TS>::kSlot;
-        Eight<TS>::fetch(slot, lane, at.v + ahead);
+        Eight<TS>::fetch(slot, lane, at.v + ahead, n);
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
@@ -246,8 +247,9 @@ struct Operands {
 
 // States in fp32: bound by memory with room to spare, so the arithmetic is the plain one.
 template <typename TW, typename TG>
-__device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const Place<TW, TG, false> &at, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *)
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const Place<TW, TG, false> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *)
 {
+    const bool live = 8 * (int)(threadIdx.x & 31) < n;
     f32x2 wn[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -258,6 +260,7 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const P
         x.m.v[i] = pair(a.m, b.m);
         x.v.v[i] = pair(a.v, b.v);
     }
+    if (!live) return scale;
     Eight<float>::store(at.m, x.m.v);
     Eight<float>::store(at.v, x.v.v);
     if constexpr (sizeof(TW) == 2) {
@@ -323,7 +326,7 @@ __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c
 // of its pattern, and the noise stays eight short of a whole code.  A block that holds an inf or nan, or values so
 // large that 2^-120 448 / top is not a normal number, goes through step_block_any; nothing is stored before that is known.
 template <typename TW, typename TG>
-__device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Place<TW, TG, true> &at, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Place<TW, TG, true> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
 {
     f32x2 wn[4], mn[4], rn[4];
     f32x2 sum = 0;
@@ -355,7 +358,7 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
     m_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(m_top)));
     r_top = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(r_top)));
     if (fmaxf(m_top, r_top) > kLargeTop) {
-        return step_block_any<TW, TG, true>(at, kBlock, c, keep, gscale, scale, noise);
+        return step_block_any<TW, TG, true>(at, n, c, keep, gscale, scale, noise);
     }
     const float2 inv = block_scales(m_top, r_top, scale);
     const Block4 q = at.noise(c, threadIdx.x & 31);
@@ -390,6 +393,7 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
                 if ((vc[h] >> 8 * i & 0xFFu) == 0u && r[i] > kZeroRoot) vc[h] |= 1u << 8 * i;
         }
     }
+    if (8 * (int)(threadIdx.x & 31) >= n) return scale;
     Eight<uint8_t>::store(at.m, mc[0], mc[1]);
     Eight<uint8_t>::store(at.v, vc[0], vc[1]);
     if constexpr (sizeof(TW) == 2) {
@@ -441,12 +445,12 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constan
     const bool has_scale = kNarrow && lane * kBlock < left;
     float2 scales = has_scale ? make_float2(c.m_scale[my_scale], c.v_scale[my_scale]) : make_float2(0.0f, 0.0f);
 
-    int fast = id < 0 ? left & ~(kBlock - 1) : 0;        // of these, through the ring
+    int fast = id < 0 ? (left % 8 == 0 ? left : left & ~(kBlock - 1)) : 0;        // of these, through the ring
     left -= fast;
     const uint32_t slots = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kDepth * Data::kSlot);
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) {
-        if (d * kBlock < fast) Data::fetch(slots + d * Data::kSlot, lane, at, d * kBlock);
+        if (d * kBlock < fast) Data::fetch(slots + d * Data::kSlot, lane, at, d * kBlock, fast - d * kBlock);
         copies_commit();
     }
     const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
@@ -459,13 +463,15 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constan
     auto scale_of = [&]() { return kNarrow ? make_float2(__shfl_sync(0xFFFFFFFFu, scales.x, k), __shfl_sync(0xFFFFFFFFu, scales.y, k)) : scales; };
     for (uint32_t d = 0; fast > 0; d = d == kDepth - 1 ? 0 : d + 1) {
         __syncwarp();      // every lane has read the place of the block before this one: the block after the next ones goes there
-        if (fast > (kDepth - 1) * kBlock) Data::fetch(slots + (d == 0 ? kDepth - 1 : d - 1) * Data::kSlot, lane, at, (kDepth - 1) * kBlock);
+        const uint32_t to = slots + (d == 0 ? kDepth - 1 : d - 1) * Data::kSlot;
+        if (fast >= kDepth * kBlock) Data::fetch(to, lane, at, (kDepth - 1) * kBlock, kBlock);
+        else if (fast > (kDepth - 1) * kBlock) Data::fetch(to, lane, at, (kDepth - 1) * kBlock, fast - (kDepth - 1) * kBlock);
         copies_commit();
         copies_wait<kDepth - 1>();
         __syncwarp();      // every lane's copies of this block have arrived
         Data x;
         x.read(slots + d * Data::kSlot, lane);
-        const float2 now = step_eight(x, at, c, keep, gscale, scale_of(), noise[warp]);
+        const float2 now = step_eight(x, at, min(fast, kBlock), c, keep, gscale, scale_of(), noise[warp]);
         if (lane == k) scales = now;
         at.advance();
         fast -= kBlock;

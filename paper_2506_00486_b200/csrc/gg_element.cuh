@@ -67,6 +67,7 @@ __device__ __forceinline__ void copy8(uint32_t to, const void *from)
 {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(to), "l"(from) : "memory");
 }
+__device__ __forceinline__ void zero16(uint32_t to) { asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(to), "r"(0u) : "memory"); }
 __device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int kLeft> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(kLeft) : "memory"); }
 
@@ -140,13 +141,15 @@ template <typename T> struct Eight;
 template <> struct Eight<float> {
     static constexpr int kSlot = 32;
     f32x2 v[4];
-    // p: the lane's eight elements of the warp's 256
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const float *p)
+    // p: the lane's eight elements of the warp's 256, of which the first n are there (a multiple of 8; the rest reads as 0)
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const float *p, int n)
     {
         p -= 4 * lane;
         const uint32_t to = slot + (uint32_t)(lane ^ (lane >> 3 & 1)) * 16u;
-        copy16(to, p);
-        copy16(to + 512u, p + 128);
+        if (4 * lane < n) copy16(to, p);
+        else zero16(to);
+        if (4 * lane + 128 < n) copy16(to + 512u, p + 128);
+        else zero16(to + 512u);
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
@@ -163,7 +166,11 @@ template <> struct Eight<float> {
 template <> struct Eight<uint16_t> {
     static constexpr int kSlot = 16;
     uint4 v;
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint16_t *p) { copy16(slot + lane * 16, p); }
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint16_t *p, int n)
+    {
+        if (8 * lane < n) copy16(slot + lane * 16, p);
+        else zero16(slot + lane * 16);
+    }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
         asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(slot + lane * 16) : "memory");
@@ -181,7 +188,11 @@ template <> struct Eight<uint16_t> {
 template <> struct Eight<uint8_t> {
     static constexpr int kSlot = 8;
     uint2 v;
-    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint8_t *p) { copy8(slot + lane * 8, p); }
+    static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint8_t *p, int n)
+    {
+        if (8 * lane < n) copy8(slot + lane * 8, p);
+        else asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(slot + lane * 8), "r"(0u) : "memory");
+    }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
         asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(slot + lane * 8) : "memory");
