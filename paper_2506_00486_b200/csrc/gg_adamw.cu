@@ -45,18 +45,24 @@ __device__ __forceinline__ int find_entry(const StepTable<N> &tab, int32_t t)
 
 struct Element { float w, m, v, r; };
 
-// One element: gradient g and states (m, v) in, new weight (before its rounding), states and root out.
+// One element with fp32 states: gradient g and states (m, v) in, new weight (before its rounding), states and root out.
+// The root and the quotient come from the approximate reciprocal root and reciprocal, the root with one Newton step (see
+// sqrt2): the weight is within a few units of the step's rounding, and no branch keeps eight elements from overlapping
+// (the correctly rounded root and division take 4.3 against 2.4 us for 49 vectors of 896).  A v below 2^-126 counts as 0.
 __device__ __forceinline__ Element adamw_element(const StepScalars &c, float keep, float w, float g, float m, float v)
 {
     Element e;
     e.m = __fadd_rn(__fmul_rn(c.b1.x, m), __fmul_rn(c.one_b1.x, g));
     e.v = __fadd_rn(__fmul_rn(c.b2.x, v), __fmul_rn(c.one_b2.x, __fmul_rn(g, g)));
-    e.r = __fsqrt_rn(e.v);
-    e.w = __fmul_rn(w, keep) + c.step.x * (e.m / (e.r * c.root.x + c.eps.x));
+    float y;
+    asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(e.v));
+    const float s = __fmul_rn(e.v, y), r = __fmaf_rn(s, __fmaf_rn(__fmul_rn(y, -0.5f), s, 0.5f), s);
+    e.r = e.v >= 0x1p-126f ? (e.v < INFINITY ? r : e.v) : (e.v >= 0.0f ? 0.0f : e.v);       // (nan stays nan)
+    e.w = __fmaf_rn(c.step.x, __fmul_rn(e.m, rcp_approx(__fmaf_rn(e.r, c.root.x, c.eps.x))), __fmul_rn(w, keep));
     return e;
 }
 
-// The same with the cheaper root and reciprocal of the 8-bit path, bit for bit what FastBlock does with pairs.
+// The same for 8-bit states, bit for bit what step_eight does with pairs.
 __device__ __forceinline__ Element adamw_element_narrow(const StepScalars &c, float keep, float w, float g, float m, float v)
 {
     Element e;

@@ -1510,14 +1510,31 @@ gg_status check_matrix(const void *p, int64_t rows, int64_t cols, int64_t ld, in
 
 gg_status check_f32(const float *p) { return reinterpret_cast<uintptr_t>(p) % 4 != 0 ? GG_ERR_ALIGNMENT : GG_OK; }
 
-// The entries of `list` have the lengths of `w`, a pointer where there is something, and the alignment of their type.
-gg_status check_list(const gg_seg *w, const gg_seg *list, int32_t n_seg, size_t element)
+// Is p on a boundary of so many bytes (a power of two)?
+inline bool on_boundary(const void *p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+
+// The tensors of an AdamW step: lengths, pointers where there is something, the alignment of each type.  Counts the
+// tensors that are not empty and their blocks.
+gg_status check_tensors(const gg_adamw_args &a, int64_t *full, int64_t *blocks)
 {
-    for (int32_t s = 0; s < n_seg; ++s) {
-        if (list[s].len != w[s].len || (list[s].len > 0 && list[s].ptr == nullptr)) return GG_ERR_INVALID_ARG;
-        if (reinterpret_cast<uintptr_t>(list[s].ptr) % element != 0) return GG_ERR_ALIGNMENT;
+    const gg_seg *lists[5] = {a.w, a.g, a.m, a.v, a.w_copy};
+    const uintptr_t state = a.state_bits == 8 ? 1 : 4, bytes[5] = {esize(a.w_dtype), esize(a.g_dtype), state, state, 2};
+    bool lengths = true, aligned = true;
+    int64_t n = 0, b = 0;
+    for (int32_t s = 0; s < a.n_seg; ++s) {
+        const int64_t len = a.w[s].len;
+        for (int i = 0; i < (a.w_copy ? 5 : 4); ++i) {
+            const gg_seg &t = lists[i][s];
+            lengths = lengths && len >= 0 && t.len == len && (len == 0 || t.ptr != nullptr);
+            aligned = aligned && on_boundary(t.ptr, bytes[i]);
+        }
+        n += len > 0;
+        if (len > 0) b += len / kBlock + (len % kBlock != 0);
+        if (b > 0x7FFFFFFFll) return lengths ? GG_ERR_WORKSPACE : GG_ERR_INVALID_ARG;
     }
-    return GG_OK;
+    *full = n;
+    *blocks = b;
+    return !lengths ? GG_ERR_INVALID_ARG : aligned ? GG_OK : GG_ERR_ALIGNMENT;
 }
 
 // Fills the table with the non-empty tensors from `s` on, and returns the first that did not fit.  `block` is the
@@ -1527,7 +1544,6 @@ int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int per_warp, int3
 {
     const int tile_blocks = per_warp * kStepWarps;
     const uintptr_t state_at = a.state_bits == 8 ? 8 : 32, w_at = a.w_dtype == GG_F32 ? 32 : 16, g_at = a.g_dtype == GG_F32 ? 32 : 16;
-    auto on = [](const void *p, uintptr_t boundary) { return reinterpret_cast<uintptr_t>(p) % boundary == 0; };
     tab.per_warp = per_warp;
     tab.n = 0;
     int64_t tiles = 0;
@@ -1541,7 +1557,10 @@ int32_t fill_table(StepTable<N> &tab, const gg_adamw_args &a, int per_warp, int3
         e.copy = a.w_copy ? a.w_copy[s].ptr : nullptr;
         e.len = len;
         e.block0 = (int32_t)block;
-        e.id = on(e.w, w_at) && on(e.g, g_at) && on(e.m, state_at) && on(e.v, state_at) && on(e.copy, 16) ? s | kAligned : s;
+        e.id = on_boundary(e.w, w_at) && on_boundary(e.g, g_at) && on_boundary(e.m, state_at) && on_boundary(e.v, state_at) &&
+                       on_boundary(e.copy, 16)
+                   ? s | kAligned
+                   : s;
         tab.tile0[tab.n++] = (int32_t)tiles;
         tiles += more;
         block += blocks;
@@ -1650,22 +1669,12 @@ gg_status gg_adamw_step(gg_ctx *ctx, const gg_adamw_args *a, void *stream)
     if (!(a->lr >= 0.0) || !isfinite(a->lr) || !(a->eps >= 0.0) || !isfinite(a->weight_decay) || a->t < 1) return GG_ERR_INVALID_ARG;
     if (!(a->beta1 >= 0.0 && a->beta1 < 1.0 && a->beta2 >= 0.0 && a->beta2 < 1.0)) return GG_ERR_INVALID_ARG;
     if (!dtype_ok(a->w_dtype) || !dtype_ok(a->g_dtype)) return GG_ERR_DTYPE;
-    gg_status st = check_segs(a->w, a->n_seg, a->w_dtype);
-    const size_t state = a->state_bits == 8 ? 1 : 4;
-    if (st == GG_OK) st = check_list(a->w, a->g, a->n_seg, esize(a->g_dtype));
-    if (st == GG_OK) st = check_list(a->w, a->m, a->n_seg, state);
-    if (st == GG_OK) st = check_list(a->w, a->v, a->n_seg, state);
-    if (st == GG_OK && a->w_copy) st = check_list(a->w, a->w_copy, a->n_seg, 2);
+    int64_t full = 0, blocks = 0;
+    gg_status st = check_tensors(*a, &full, &blocks);
     for (const float *p : {a->decay, a->grad_scale, (const float *)a->m_scale, (const float *)a->v_scale})
         if (st == GG_OK) st = check_f32(p);
     if (st != GG_OK) return st;
-    int64_t blocks = 0, full = 0;
-    for (int32_t s = 0; s < a->n_seg; ++s) {
-        blocks += (a->w[s].len + kBlock - 1) / kBlock;
-        full += a->w[s].len > 0;
-    }
     if (full == 0) return GG_OK;
-    if (blocks > 0x7FFFFFFFll) return GG_ERR_WORKSPACE;
     if (a->state_bits == 8 && (!a->m_scale || !a->v_scale)) return GG_ERR_INVALID_ARG;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return GG_ERR_CUDA;
