@@ -3,7 +3,8 @@
 //     m <- b1 m + (1 - b1) g        v <- b2 v + (1 - b2) g^2
 //     w <- w (1 - lr decay) - lr / (1 - b1^t) * m / (sqrt(v) / sqrt(1 - b2^t) + eps)
 //
-// Every product and sum is one fp32 rounding, none contracted: the 8-bit codes then depend on the definition alone.
+// Every product and sum of m and v is one fp32 rounding, none contracted: the 8-bit codes then depend on the definition
+// alone.
 //
 // 8-bit states: m and r = sqrt(v) are held as e4m3 codes with one fp32 scale for each kBlock elements of a tensor
 // (from its start), the largest magnitude of the block at 448.  e4m3 spans 2^18 from that down, so r spans 2^36 of
@@ -56,7 +57,7 @@ __device__ __forceinline__ Element adamw_element(const StepScalars &c, float kee
     e.v = __fadd_rn(__fmul_rn(c.b2.x, v), __fmul_rn(c.one_b2.x, __fmul_rn(g, g)));
     float y;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(e.v));
-    const float s = __fmul_rn(e.v, y), r = __fmaf_rn(s, __fmaf_rn(__fmul_rn(y, -0.5f), s, 0.5f), s);
+    const float s = __fmul_rn(e.v, y), r = __fmaf_rn(__fmaf_rn(-s, s, e.v), 0.5f * y, s);
     e.r = e.v >= 0x1p-126f ? (e.v < INFINITY ? r : e.v) : (e.v >= 0.0f ? 0.0f : e.v);       // (nan stays nan)
     e.w = __fmaf_rn(c.step.x, __fmul_rn(e.m, rcp_approx(__fmaf_rn(e.r, c.root.x, c.eps.x))), __fmul_rn(w, keep));
     return e;
@@ -72,7 +73,7 @@ __device__ __forceinline__ Element adamw_element_narrow(const StepScalars &c, fl
     float y;
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(v1));
     const float r = __fmul_rn(v1, y);
-    e.r = e.v < INFINITY ? __fmaf_rn(r, __fmaf_rn(__fmul_rn(y, -0.5f), r, 0.5f), r) : e.v;
+    e.r = e.v < INFINITY ? __fmaf_rn(__fmaf_rn(-r, r, v1), 0.5f * y, r) : e.v;
     e.w = __fmaf_rn(c.step.x, __fmul_rn(e.m, rcp_approx(__fmaf_rn(e.r, c.root.x, c.eps.x))), __fmul_rn(w, keep));
     return e;
 }
@@ -304,8 +305,9 @@ __device__ __forceinline__ float max3(float a, float b, float c)
     return d;
 }
 
-// sqrt of finite values >= 0 by one Newton step on an approximate reciprocal root y: g = v y, g + g (1/2 - g y / 2).
-// That leaves the rounding of the last sum (and, once in about a million, the neighbour of the nearest value).  2^-126 is
+// sqrt of finite values >= 0 by one Newton step from an approximate reciprocal root y: g = v y, g + (v - g^2) y / 2, the
+// remainder v - g^2 exact.  That leaves the rounding of the last sum (and, once in about a million, the neighbour of the
+// nearest value; with g (1/2 - g y / 2) for the step, half of the rounding of g stays, one value in ten).  2^-126 is
 // added to v, so that y is finite: it changes no v above 2^-102, and the step divides by the root plus eps, so nothing
 // below that matters.  The root of 0 comes out as 2^-63, and roots up to kZeroRoot count as 0.
 __device__ __forceinline__ f32x2 sqrt2(f32x2 v)
@@ -316,7 +318,7 @@ __device__ __forceinline__ f32x2 sqrt2(f32x2 v)
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(f.x));
     asm("rsqrt.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(f.y));
     const f32x2 y = pair(a, b), g = mul2(v, y);
-    return fma2(g, fma2(mul2(y, both(-0.5f)), g, both(0.5f)), g);
+    return fma2(fma2(mul2(g, both(-1.0f)), g, v), mul2(y, both(0.5f)), g);
 }
 
 // The top bytes of four words, in order.
@@ -348,8 +350,8 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const f32x2 gi = mul2(x.g.get(i), gs), mo = mul2(m_old[i], ms), ro = mul2(r_old[i], vs);
-            mn[i] = add2(mul2(b1, mo), mul2(one_b1, gi));
-            rn[i] = sqrt2(add2(mul2(b2, mul2(ro, ro)), mul2(one_b2, mul2(gi, gi))));
+            mn[i] = add2_apart(mul2(b1, mo), mul2(one_b1, gi));
+            rn[i] = sqrt2(add2_apart(mul2(b2, mul2(ro, ro)), mul2(one_b2, mul2(gi, gi))));
             const float2 d = halves(fma2(rn[i], root, eps));
             wn[i] = fma2(step, mul2(mn[i], pair(rcp_approx(d.x), rcp_approx(d.y))), mul2(x.w.get(i), keep2));
             sum = i == 0 ? wn[0] : add2(sum, wn[i]);

@@ -13,8 +13,9 @@ template <typename T> __device__ __forceinline__ T narrow(float v);
 template <> __device__ __forceinline__ float narrow<float>(float v) { return v; }
 template <> __device__ __forceinline__ uint16_t narrow<uint16_t>(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 
-// Two fp32 values in one register pair: one instruction does both (mul, add and fma of sm_100).  None of these is
-// contracted with another by the compiler.
+// Two fp32 values in one register pair: one instruction does both (mul, add and fma of sm_100).  The assembler may fuse a
+// mul2 and an add2 into a multiply-add, in spite of their .rn (nvcc 12.9, -fmad=false or not): add2_apart is the sum that
+// is never fused.
 using f32x2 = unsigned long long;
 __device__ __forceinline__ f32x2 pair(float lo, float hi)
 {
@@ -41,6 +42,11 @@ __device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b)
     f32x2 d;
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
     return d;
+}
+__device__ __forceinline__ f32x2 add2_apart(f32x2 a, f32x2 b)
+{
+    const float2 x = halves(a), y = halves(b);
+    return pair(__fadd_rn(x.x, y.x), __fadd_rn(x.y, y.y));
 }
 __device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c)
 {

@@ -42,6 +42,31 @@ __device__ __forceinline__ float rsqrt_of(float v)
     return v > 0.0f && v < INFINITY ? fmaf(y, fmaf(-h, y, 0.5f), y) : y;
 }
 
+// Few rows: the sums over the rows need no slices.  The launch of the kernel over rows gets one more CTA for each 32 columns
+// (of `strips` in all), which reads these columns of all rows again, from cache: one launch instead of two.
+template <typename T>
+__device__ __forceinline__ void sum_strip(const LayerNormGradArgs &a, int strip, float *shared)
+{
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, warps = blockDim.x >> 5;
+    const int64_t c = (int64_t)strip * 32 + lane;
+    float dw = 0.0f, db = 0.0f;
+    if (c < a.cols)
+#pragma unroll 4
+        for (int r = warp; r < (int)a.rows; r += warps) {
+            const float dy = widen<T>(static_cast<const T *>(a.dy)[r * a.dy_ld + c]), x = widen<T>(static_cast<const T *>(a.x)[r * a.x_ld + c]);
+            dw = fmaf(dy, (x - __ldg(a.mean + r)) * __ldg(a.rstd + r), dw);
+            db += dy;
+        }
+    shared[warp * 32 + lane] = dw;
+    shared[1024 + warp * 32 + lane] = db;
+    __syncthreads();
+    float *out = warp == 0 ? a.dweight : a.dbias;
+    if (warp >= 2 || out == nullptr || c >= a.cols) return;
+    double t = a.accumulate ? (double)out[c] : 0.0;
+    for (int w = 0; w < warps; ++w) t += (double)shared[warp * 1024 + w * 32 + lane];
+    out[c] = (float)t;
+}
+
 // ---- rows of 16-byte vectors that fit the registers of their threads
 
 // A row belongs to T threads: to 2^k lanes of a warp (short rows: a CTA of four warps then holds several, and needs no
@@ -119,17 +144,17 @@ struct Rows {
     int threads, tid, cols;
     int64_t first, stride;             // rows of this thread
     uint32_t base, step, stage_bytes;  // in shared memory: this thread's first place, from one vector to the next, a stage
-    __device__ __forceinline__ Rows(int t, int c, unsigned char *shared) : threads(t), cols(c)
+    __device__ __forceinline__ Rows(int t, int c, unsigned ctas, unsigned char *shared) : threads(t), cols(c)
     {
         if (kSolo) {
             const int each = 32 / t;                                           // rows of a warp
             tid = threadIdx.x & (t - 1);
             first = ((int64_t)blockIdx.x * kSoloWarps + (threadIdx.x >> 5)) * each + (threadIdx.x & 31) / t;
-            stride = (int64_t)gridDim.x * kSoloWarps * each;
+            stride = (int64_t)ctas * kSoloWarps * each;
         } else {
             tid = threadIdx.x;
             first = blockIdx.x;
-            stride = gridDim.x;
+            stride = ctas;
         }
         step = blockDim.x * 16u;
         stage_bytes = kOperands * kNum * step;
@@ -162,7 +187,7 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(con
     constexpr int kPairs = Few<T>::kPairs;
     __shared__ __align__(16) float sh[2][32];
     extern __shared__ __align__(16) unsigned char shared[];
-    const Rows<T, kNum, 1, kKnown != kRagged, kSolo> rows(threads, (int)a.cols, shared);
+    const Rows<T, kNum, 1, kKnown != kRagged, kSolo> rows(threads, (int)a.cols, gridDim.x, shared);
     const float n_inv = 1.0f / (float)rows.cols, eps = (float)a.eps;
     const TW *weight = static_cast<const TW *>(a.weight), *bias = static_cast<const TW *>(a.bias);
     const T *x_ahead = static_cast<const T *>(a.x) + rows.first * a.x_ld + rows.column(0);
@@ -263,12 +288,17 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(con
 // The gradient: each thread keeps the sums of its columns over the rows of its CTA and leaves them as slice blockIdx.x of
 // `part` ([2][gridDim.x][cols]); layer_norm_dw_finish_kernel adds the slices.
 template <typename T, typename TW, int kNum, Known kKnown, bool kSolo>
-__global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *part, int threads)
+__global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *part, int strips, int threads)
 {
     constexpr int kPairs = Few<T>::kPairs;
     __shared__ __align__(16) float2 sh[2][32];
     extern __shared__ __align__(16) unsigned char shared[];
-    const Rows<T, kNum, 2, kKnown != kRagged, kSolo> rows(threads, (int)a.cols, shared);
+    const unsigned row_ctas = gridDim.x - (unsigned)strips;
+    if (blockIdx.x >= row_ctas) {
+        sum_strip<T>(a, (int)(blockIdx.x - row_ctas), reinterpret_cast<float *>(shared));
+        return;
+    }
+    const Rows<T, kNum, 2, kKnown != kRagged, kSolo> rows(threads, (int)a.cols, row_ctas, shared);
     cudaTriggerProgrammaticLaunchCompletion();       // (the kernel that adds the slices may take its places as these CTAs leave them)
     const float n_inv = 1.0f / (float)rows.cols;
     const TW *weight = static_cast<const TW *>(a.weight);
@@ -454,7 +484,7 @@ struct Pieces {
     int column, left, whole;           // this thread's first element, how many the row has from there on, how many every lane has
     int64_t first, stride;
     uint32_t base, row_bytes, stage_bytes;
-    __device__ __forceinline__ Pieces(int t, int c, unsigned char *shared) : threads(t), cols(c)
+    __device__ __forceinline__ Pieces(int t, int c, unsigned ctas, unsigned char *shared) : threads(t), cols(c)
     {
         row_bytes = piece_bytes<T>(c);
         stage_bytes = kOperands * row_bytes;
@@ -462,12 +492,12 @@ struct Pieces {
         if (kSolo) {
             tid = threadIdx.x & 31;
             first = (int64_t)blockIdx.x * kSoloWarps + (threadIdx.x >> 5);
-            stride = (int64_t)gridDim.x * kSoloWarps;
+            stride = (int64_t)ctas * kSoloWarps;
             base += (threadIdx.x >> 5) * 2 * stage_bytes;
         } else {
             tid = threadIdx.x;
             first = blockIdx.x;
-            stride = gridDim.x;
+            stride = ctas;
         }
         column = (kSolo ? 0 : (int)(threadIdx.x >> 5) * 32 * kNum) + (int)(threadIdx.x & 31);
         left = c - column;
@@ -540,7 +570,7 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 6 : 1) 
 {
     __shared__ __align__(16) float sh[2][32];
     extern __shared__ __align__(16) unsigned char shared[];
-    const Pieces<T, kNum, 1, kSolo> rows(threads, (int)a.cols, shared);
+    const Pieces<T, kNum, 1, kSolo> rows(threads, (int)a.cols, gridDim.x, shared);
     const float n_inv = 1.0f / (float)rows.cols, eps = (float)a.eps;
     const TW *weight = a.weight ? static_cast<const TW *>(a.weight) + rows.column : nullptr;
     const TW *bias = a.bias ? static_cast<const TW *>(a.bias) + rows.column : nullptr;
@@ -590,11 +620,16 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 6 : 1) 
 }
 
 template <typename T, typename TW, int kNum, bool kSolo>
-__global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) layer_norm_pieces_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *part, int threads)
+__global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) layer_norm_pieces_grad_kernel(const __grid_constant__ LayerNormGradArgs a, float *part, int strips, int threads)
 {
     __shared__ __align__(16) float2 sh[2][32];
     extern __shared__ __align__(16) unsigned char shared[];
-    const Pieces<T, kNum, 2, kSolo> rows(threads, (int)a.cols, shared);
+    const unsigned row_ctas = gridDim.x - (unsigned)strips;
+    if (blockIdx.x >= row_ctas) {
+        sum_strip<T>(a, (int)(blockIdx.x - row_ctas), reinterpret_cast<float *>(shared));
+        return;
+    }
+    const Pieces<T, kNum, 2, kSolo> rows(threads, (int)a.cols, row_ctas, shared);
     cudaTriggerProgrammaticLaunchCompletion();
     const float n_inv = 1.0f / (float)rows.cols;
     const TW *weight = a.weight ? static_cast<const TW *>(a.weight) + rows.column : nullptr;
@@ -1027,6 +1062,10 @@ int layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count)
     return (int)(n < 1 ? 1 : n);
 }
 
+// So few rows for each warp of a CTA are summed by strips (33 rows of 896, four warps: 3.1 us on the GPU and 4.3 a call, against
+// 4.0 and 6.1 with slices; 64 rows 4.3, but 128 rows 7.1 against 5.4.  128 rows of 4096, sixteen warps: 3.8 against 6.8).
+constexpr int64_t kFewRows = 16;
+
 cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int slices, int sm_count, int *launches, cudaStream_t st)
 {
     *launches = 0;
@@ -1036,10 +1075,20 @@ cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int 
     const RowLaunch l = backward_launch(a, sm_count);
     cudaError_t e;
     if (l.kernel != nullptr) {
-        int threads = l.shape.threads;
-        void *args[] = {const_cast<LayerNormGradArgs *>(&a), &part, &threads};
-        e = cudaLaunchKernel(l.kernel, dim3((unsigned)slices), dim3(l.shape.block()), args, l.shared, st);
-        *launches += 1;
+        auto launch = [&](unsigned ctas, float *slices_of, int strips) {
+            int threads = l.shape.threads;
+            void *args[] = {const_cast<LayerNormGradArgs *>(&a), &slices_of, &strips, &threads};
+            *launches += 1;
+            const size_t shared = strips > 0 && l.shared < 8192 ? 8192 : l.shared;
+            return cudaLaunchKernel(l.kernel, dim3(ctas + (unsigned)strips), dim3(l.shape.block()), args, shared, st);
+        };
+        if (sums && a.rows <= kFewRows * (int64_t)(l.shape.block() / 32)) {
+            const int strips = (int)((a.cols + 31) / 32);
+            const bool over = a.dx == a.x || a.dx == a.dy;       // (then the strips have to be done before dx is written)
+            e = launch(a.dx && !over ? (unsigned)slices : 0u, nullptr, strips);
+            return e == cudaSuccess && a.dx && over ? launch((unsigned)slices, nullptr, 0) : e;
+        }
+        e = launch((unsigned)slices, part, 0);
     } else if (a.dtype == GG_F32 && a.w_dtype == GG_F32) {
         e = backward_any<float, float>(a, slices, part, launches, st);
     } else if (a.dtype == GG_F32) {
