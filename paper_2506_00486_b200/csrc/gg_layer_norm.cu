@@ -467,6 +467,9 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
 template <typename T>
 __host__ __device__ constexpr uint32_t piece_bytes(int n) { return ((uint32_t)n * (uint32_t)sizeof(T) + 15u + 15u) / 16u * 16u; }
 
+// Room for `each` fp32 values a column.
+__host__ __device__ constexpr uint32_t affine_bytes(int n, int each) { return ((uint32_t)n * (uint32_t)each * 4u + 15u) / 16u * 16u; }
+
 template <int N>
 struct Index {
     static constexpr int value = N;
@@ -484,11 +487,12 @@ struct Pieces {
     int column, left, whole;           // this thread's first element, how many the row has from there on, how many every lane has
     int64_t first, stride;
     uint32_t base, row_bytes, stage_bytes;
-    __device__ __forceinline__ Pieces(int t, int c, unsigned ctas, unsigned char *shared) : threads(t), cols(c)
+    // shared: the rows, behind `ahead` bytes of something else
+    __device__ __forceinline__ Pieces(int t, int c, unsigned ctas, unsigned char *shared, uint32_t ahead) : threads(t), cols(c)
     {
         row_bytes = piece_bytes<T>(c);
         stage_bytes = kOperands * row_bytes;
-        base = (uint32_t)__cvta_generic_to_shared(shared);
+        base = (uint32_t)__cvta_generic_to_shared(shared) + ahead;
         if (kSolo) {
             tid = threadIdx.x & 31;
             first = (int64_t)blockIdx.x * kSoloWarps + (threadIdx.x >> 5);
@@ -511,14 +515,21 @@ struct Pieces {
     // [from, to): the matrix
     __device__ __forceinline__ void fetch(uint32_t slot, const T *row, uintptr_t from, uintptr_t to) const
     {
-        const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = reinterpret_cast<uintptr_t>(row + cols), origin = begin & ~(uintptr_t)15;
-        for (uintptr_t p = origin + 16u * tid; p < end; p += 16u * threads) {
-            const uint32_t at = slot + (uint32_t)(p - origin);
-            if (p >= from && p + 16 <= to) {
-                copy16(at, reinterpret_cast<const void *>(p));
+        const uintptr_t begin = reinterpret_cast<uintptr_t>(row), end = begin + (uint32_t)cols * (uint32_t)sizeof(T), origin = begin & ~(uintptr_t)15;
+        const char *p = reinterpret_cast<const char *>(origin) + 16 * tid;
+        const int pieces = (int)((uint32_t)(end - origin + 15u) / 16u);
+        slot += 16u * tid;
+        if (origin >= from && origin + 16u * (uint32_t)pieces <= to) {
+            for (int i = tid; i < pieces; i += threads, p += 16 * threads, slot += 16u * threads) copy16(slot, p);
+            return;
+        }
+        for (int i = tid; i < pieces; i += threads, p += 16 * threads, slot += 16u * threads) {
+            const uintptr_t at = reinterpret_cast<uintptr_t>(p);
+            if (at >= from && at + 16 <= to) {
+                copy16(slot, p);
             } else {
-                for (uintptr_t q = p > begin ? p : begin; q < p + 16 && q < end; q += sizeof(T))
-                    put(at + (uint32_t)(q - p), *reinterpret_cast<const T *>(q));
+                for (uintptr_t q = at > begin ? at : begin; q < at + 16 && q < end; q += sizeof(T))
+                    put(slot + (uint32_t)(q - at), *reinterpret_cast<const T *>(q));
             }
         }
     }
@@ -534,79 +545,111 @@ struct Pieces {
     {
         if constexpr (sizeof(T) == 4) {
             float v;
-            asm volatile("ld.shared.f32 %0, [%1 + %2];" : "=f"(v) : "r"(at), "n"(k * 32 * 4) : "memory");
+            asm volatile("ld.shared.f32 %0, [%1 + %2];" : "=f"(v) : "r"(at), "n"(k * 32 * 4));
             return v;
         } else {
             uint16_t h;
-            asm volatile("ld.shared.u16 %0, [%1 + %2];" : "=h"(h) : "r"(at), "n"(k * 32 * 2) : "memory");
+            asm volatile("ld.shared.u16 %0, [%1 + %2];" : "=h"(h) : "r"(at), "n"(k * 32 * 2));
             return widen<uint16_t>(h);
         }
     }
-    // f(k) for every element 32 k of this thread that the row has (the number as a type, so that it can be an offset): four
-    // at a time without a question, as long as all lanes have them, and the last four one by one.
-    template <int k = 0, typename F>
+    // The elements 2 j and 2 j + 1 of this thread, as many of them as the row has (all: two).
+    template <int j>
+    static __device__ __forceinline__ f32x2 get2(uint32_t at, int n)
+    {
+        const float lo = n > 0 ? get<2 * j>(at) : 0.0f, hi = n > 1 ? get<2 * j + 1>(at) : 0.0f;
+        return pair(lo, hi);
+    }
+    // f(j, n) for the pairs of elements 32 (2 j), 32 (2 j + 1) of this thread (the number as a type, so that it can be an
+    // offset), n of which the row has: two pairs at a time without a question, as long as all lanes have them.
+    template <int j = 0, typename F>
     __device__ __forceinline__ void each(F f) const
     {
-        if constexpr (k < kNum) {
-            if (k + 4 <= whole) {
-                f(Index<k>());
-                f(Index<k + 1>());
-                f(Index<k + 2>());
-                f(Index<k + 3>());
+        if constexpr (2 * j < kNum) {
+            if (2 * j + 4 <= whole) {
+                f(Index<j>(), Index<2>());
+                f(Index<j + 1>(), Index<2>());
             } else {
-                if (32 * k < left) f(Index<k>());
-                if (32 * (k + 1) < left) f(Index<k + 1>());
-                if (32 * (k + 2) < left) f(Index<k + 2>());
-                if (32 * (k + 3) < left) f(Index<k + 3>());
-                if (whole < k) return;
+                f(Index<j>(), count(2 * j));
+                f(Index<j + 1>(), count(2 * j + 2));
+                if (whole < 2 * j) return;
             }
-            each<k + 4>(f);
+            each<j + 2>(f);
         }
     }
+    __device__ __forceinline__ int count(int k) const { return 32 * k >= left ? 0 : 32 * (k + 1) >= left ? 1 : 2; }
 };
 
-template <typename T, typename TW, int kNum, bool kSolo>
+// v where there is an element, else 0
+__device__ __forceinline__ f32x2 only(f32x2 v, int n)
+{
+    const float2 f = halves(v);
+    return pair(n > 0 ? f.x : 0.0f, n > 1 ? f.y : 0.0f);
+}
+
+// kStaged: weight and bias (1 and 0 where there is none) wait in shared memory as fp32, which saves the loads from L1 and their
+// conversions (bf16 [16384, 4095]: 89 against 103 us), but takes a while to fill and room from other CTAs (fp32 [3000, 5001]:
+// 45 against 37 us; bf16 [1000, 2001]: 12.4 against 8.4).
+template <typename T, typename TW, int kNum, bool kSolo, bool kStaged>
 __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 6 : 1) layer_norm_pieces_kernel(const __grid_constant__ LayerNormArgs a, int threads)
 {
     __shared__ __align__(16) float sh[2][32];
     extern __shared__ __align__(16) unsigned char shared[];
-    const Pieces<T, kNum, 1, kSolo> rows(threads, (int)a.cols, gridDim.x, shared);
+    const Pieces<T, kNum, 1, kSolo> rows(threads, (int)a.cols, gridDim.x, shared, kStaged ? affine_bytes((int)a.cols, 2) : 0u);
     const float n_inv = 1.0f / (float)rows.cols, eps = (float)a.eps;
-    const TW *weight = a.weight ? static_cast<const TW *>(a.weight) + rows.column : nullptr;
-    const TW *bias = a.bias ? static_cast<const TW *>(a.bias) + rows.column : nullptr;
     const T *x = static_cast<const T *>(a.x) + rows.first * a.x_ld;
     T *y = static_cast<T *>(a.y) + rows.first * a.y_ld + rows.column;
     const uintptr_t from = reinterpret_cast<uintptr_t>(a.x), to = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.x) + (a.rows - 1) * a.x_ld + a.cols);
     const int64_t x_step = rows.stride * a.x_ld, y_step = rows.stride * a.y_ld;
-    if (!kSolo && threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
     int half = 0;
     uint32_t slot = rows.base, other = rows.base + rows.stage_bytes;
     if (rows.first < a.rows) rows.fetch(slot, x, from, to);
     copies_commit();
+    const TW *weight = static_cast<const TW *>(a.weight), *bias = static_cast<const TW *>(a.bias);
+    auto from_l1 = [&](int c) { return make_float2(weight ? widen<TW>(__ldg(weight + c)) : 1.0f, bias ? widen<TW>(__ldg(bias + c)) : 0.0f); };
+    float2 *affine = reinterpret_cast<float2 *>(shared);
+    if (kStaged) {
+        for (int c = threadIdx.x; c < rows.cols; c += blockDim.x) affine[c] = from_l1(c);
+        affine += rows.column;
+    } else {
+        if (weight) weight += rows.column;
+        if (bias) bias += rows.column;
+    }
+    if (!kSolo && threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = 0.0f;
+    __syncthreads();
     for (int64_t r = rows.first; r < a.rows; r += rows.stride) {
         copies_wait<0>();
         rows.sync();       // everyone's pieces of this row are here, and everyone is done with the row before
         if (r + rows.stride < a.rows) rows.fetch(other, x + x_step, from, to);
         copies_commit();
         const uint32_t at = rows.place(slot, x);
-        float v[kNum], t = 0.0f;
-        rows.each([&](auto k) {
-            v[k] = rows.template get<decltype(k)::value>(at);
-            t += v[k];
+        f32x2 v[kNum / 2], t = 0;
+        rows.each([&](auto j, auto n) {
+            v[j] = rows.template get2<decltype(j)::value>(at, n);
+            t = add2(t, v[j]);
         });
-        const float mean = row_sum<kSolo>(t, sh, threads, half) * n_inv;
-        t = 0.0f;
-        rows.each([&](auto k) {
-            v[k] -= mean;
-            t = fmaf(v[k], v[k], t);
+        float2 f = halves(t);
+        const float mean = row_sum<kSolo>(f.x + f.y, sh, threads, half) * n_inv;
+        const f32x2 minus = both(-mean);
+        t = 0;
+        rows.each([&](auto j, auto n) {
+            v[j] = only(add2(v[j], minus), n);
+            t = fma2(v[j], v[j], t);
         });
-        const float rstd = rsqrt_of(fmaf(row_sum<kSolo>(t, sh, threads, half), n_inv, eps));
-        if (weight && bias)
-            rows.each([&](auto k) { y[32 * k] = narrow<T>(fmaf(v[k] * rstd, widen<TW>(__ldg(weight + 32 * k)), widen<TW>(__ldg(bias + 32 * k)))); });
-        else
-            rows.each([&](auto k) {
-                y[32 * k] = narrow<T>(fmaf(v[k] * rstd, weight ? widen<TW>(__ldg(weight + 32 * k)) : 1.0f, bias ? widen<TW>(__ldg(bias + 32 * k)) : 0.0f));
-            });
+        f = halves(t);
+        const float rstd = rsqrt_of(fmaf(row_sum<kSolo>(f.x + f.y, sh, threads, half), n_inv, eps));
+        const f32x2 by = both(rstd);
+        rows.each([&](auto j, auto n) {
+            const float2 o = halves(mul2(v[j], by));
+            if (n > 0) {
+                const float2 w = kStaged ? affine[64 * j] : from_l1(64 * j);
+                y[64 * j] = narrow<T>(fmaf(o.x, w.x, w.y));
+            }
+            if (n > 1) {
+                const float2 w = kStaged ? affine[64 * j + 32] : from_l1(64 * j + 32);
+                y[64 * j + 32] = narrow<T>(fmaf(o.y, w.x, w.y));
+            }
+        });
         if (rows.tid == 0) {
             if (a.mean) a.mean[r] = mean;
             if (a.rstd) a.rstd[r] = rstd;
@@ -629,19 +672,17 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) 
         sum_strip<T>(a, (int)(blockIdx.x - row_ctas), reinterpret_cast<float *>(shared));
         return;
     }
-    const Pieces<T, kNum, 2, kSolo> rows(threads, (int)a.cols, row_ctas, shared);
+    const Pieces<T, kNum, 2, kSolo> rows(threads, (int)a.cols, row_ctas, shared, affine_bytes((int)a.cols, 1));
     cudaTriggerProgrammaticLaunchCompletion();
     const float n_inv = 1.0f / (float)rows.cols;
-    const TW *weight = a.weight ? static_cast<const TW *>(a.weight) + rows.column : nullptr;
     const T *x = static_cast<const T *>(a.x) + rows.first * a.x_ld, *dy = static_cast<const T *>(a.dy) + rows.first * a.dy_ld;
     T *dx = static_cast<T *>(a.dx) + rows.first * a.dx_ld + rows.column;
     const uintptr_t x_from = reinterpret_cast<uintptr_t>(a.x), x_to = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.x) + (a.rows - 1) * a.x_ld + a.cols);
     const uintptr_t dy_from = reinterpret_cast<uintptr_t>(a.dy), dy_to = reinterpret_cast<uintptr_t>(static_cast<const T *>(a.dy) + (a.rows - 1) * a.dy_ld + a.cols);
     const int64_t x_step = rows.stride * a.x_ld, dy_step = rows.stride * a.dy_ld, dx_step = rows.stride * a.dx_ld;
-    float dw[kNum], db[kNum];
+    f32x2 dw[kNum / 2], db[kNum / 2];
 #pragma unroll
-    for (int k = 0; k < kNum; ++k) dw[k] = db[k] = 0.0f;
-    if (!kSolo && threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = make_float2(0.0f, 0.0f);
+    for (int j = 0; j < kNum / 2; ++j) dw[j] = db[j] = 0;
     int half = 0;
     uint32_t slot = rows.base, other = rows.base + rows.stage_bytes;
     float next_mean = 0.0f, next_rstd = 0.0f;
@@ -652,10 +693,16 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) 
         next_rstd = __ldg(a.rstd + rows.first);
     }
     copies_commit();
+    float *weight = reinterpret_cast<float *>(shared);
+    for (int c = threadIdx.x; c < rows.cols; c += blockDim.x) weight[c] = a.weight ? widen<TW>(__ldg(static_cast<const TW *>(a.weight) + c)) : 1.0f;
+    weight += rows.column;
+    if (!kSolo && threadIdx.x < 64) sh[threadIdx.x >> 5][threadIdx.x & 31] = make_float2(0.0f, 0.0f);
+    __syncthreads();
     for (int64_t r = rows.first; r < a.rows; r += rows.stride) {
         copies_wait<0>();
         rows.sync();       // everyone's pieces of this row are here, and everyone is done with the row before
-        const float mean = next_mean, rstd = next_rstd;
+        const f32x2 minus = both(-next_mean), by = both(next_rstd);
+        const float scale = -next_rstd * n_inv;
         if (r + rows.stride < a.rows) {
             rows.fetch(other, dy + dy_step, dy_from, dy_to);
             rows.fetch(other + rows.row_bytes, x + x_step, x_from, x_to);
@@ -664,22 +711,31 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) 
         }
         copies_commit();
         const uint32_t dy_at = rows.place(slot, dy), x_at = rows.place(slot + rows.row_bytes, x);
-        float t0 = 0.0f, t1 = 0.0f;
-        rows.each([&](auto k) {
-            const float g = rows.template get<decltype(k)::value>(dy_at), xhat = (rows.template get<decltype(k)::value>(x_at) - mean) * rstd;
-            const float d = weight ? g * widen<TW>(__ldg(weight + 32 * k)) : g;
-            dw[k] = fmaf(g, xhat, dw[k]);
-            db[k] += g;
-            t0 += d;
-            t1 = fmaf(d, xhat, t1);
+        auto load = [&](auto j, auto n, f32x2 &g, f32x2 &xhat) {       // (an element that is not there counts nothing: its dy is 0)
+            g = rows.template get2<decltype(j)::value>(dy_at, n);
+            xhat = mul2(add2(rows.template get2<decltype(j)::value>(x_at, n), minus), by);
+        };
+        auto weigh = [&](auto j, auto n, f32x2 g) { return mul2(g, pair(n > 0 ? weight[64 * j] : 0.0f, n > 1 ? weight[64 * j + 32] : 0.0f)); };
+        f32x2 t0 = 0, t1 = 0;
+        rows.each([&](auto j, auto n) {
+            f32x2 g, xhat;
+            load(j, n, g, xhat);
+            dw[j] = fma2(g, xhat, dw[j]);
+            db[j] = add2(db[j], g);
+            const f32x2 d = weigh(j, n, g);
+            t0 = add2(t0, d);
+            t1 = fma2(d, xhat, t1);
         });
         if (a.dx != nullptr) {
-            const float2 s = row_sum2<kSolo>(t0, t1, sh, threads, half);
-            const float c1 = -rstd * (s.x * n_inv), c2 = -rstd * (s.y * n_inv);
-            rows.each([&](auto k) {       // rstd (d - c1 - xhat c2)
-                const float g = rows.template get<decltype(k)::value>(dy_at), xhat = (rows.template get<decltype(k)::value>(x_at) - mean) * rstd;
-                const float d = weight ? g * widen<TW>(__ldg(weight + 32 * k)) : g;
-                dx[32 * k] = narrow<T>(fmaf(xhat, c2, fmaf(d, rstd, c1)));
+            const float2 f0 = halves(t0), f1 = halves(t1);
+            const float2 s = row_sum2<kSolo>(f0.x + f0.y, f1.x + f1.y, sh, threads, half);
+            const f32x2 c1 = both(s.x * scale), c2 = both(s.y * scale);
+            rows.each([&](auto j, auto n) {       // rstd (d - c1 - xhat c2)
+                f32x2 g, xhat;
+                load(j, n, g, xhat);
+                const float2 o = halves(fma2(xhat, c2, fma2(weigh(j, n, g), by, c1)));
+                if (n > 0) dx[64 * j] = narrow<T>(o.x);
+                if (n > 1) dx[64 * j + 32] = narrow<T>(o.y);
             });
         }
         x += x_step;
@@ -692,15 +748,19 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) 
     if (part == nullptr) return;
     const int cols = rows.cols;
     float *out_w = part + (int64_t)blockIdx.x * cols, *out_b = out_w + (int64_t)gridDim.x * cols;
+    auto add = [&](float *at, f32x2 v, auto n, bool onto) {
+        const float2 f = halves(v);
+        if (n > 0) at[0] = onto ? at[0] + f.x : f.x;
+        if (n > 1) at[32] = onto ? at[32] + f.y : f.y;
+    };
     if (kSolo) {       // the warps of the CTA in order, where their rows were
         float *columns = reinterpret_cast<float *>(shared);
         __syncthreads();
         for (int turn = 0; turn < kSoloWarps; ++turn) {
             if ((int)(threadIdx.x >> 5) == turn)
-                rows.each([&](auto k) {
-                    float *w = columns + 32 * k + rows.column, *b = w + cols;
-                    *w = turn ? *w + dw[k] : dw[k];
-                    *b = turn ? *b + db[k] : db[k];
+                rows.each([&](auto j, auto n) {
+                    add(columns + rows.column + 64 * j, dw[j], n, turn > 0);
+                    add(columns + cols + rows.column + 64 * j, db[j], n, turn > 0);
                 });
             __syncthreads();
         }
@@ -710,9 +770,9 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) 
         }
         return;
     }
-    rows.each([&](auto k) {
-        out_w[32 * k + rows.column] = dw[k];
-        out_b[32 * k + rows.column] = db[k];
+    rows.each([&](auto j, auto n) {
+        add(out_w + rows.column + 64 * j, dw[j], n, false);
+        add(out_b + rows.column + 64 * j, db[j], n, false);
     });
 }
 
@@ -869,15 +929,15 @@ RowShape row_shape(int64_t rows, int64_t cols, int vec, int wanted, int sm_count
 // Single elements: `wanted` a thread for many rows, eight for few.  (Forward 32: the fewer threads, the less the sums of a row
 // cost.  Backward 16, and eight below eight million elements, where a wave of wide threads has only a row or two for each:
 // fp32 [4099, 1023] takes 35, 25 and 23 us with 32, 16 and 8, bf16 [16384, 1023] 56, 54 and 56.)  Wider rows, or rows of
-// which two stages do not fit shared memory, have no shape.
-RowShape piece_shape(int64_t rows, int64_t cols, int64_t bytes_a_row, int wanted, int sm_count)
+// which two stages (`bytes`, with the affine part) do not fit shared memory, have no shape.
+RowShape piece_shape(int64_t rows, int64_t cols, int64_t bytes, int wanted, int sm_count)
 {
     RowShape s;
     s.pieces = true;
     int num = rows < 4 * (int64_t)sm_count || cols <= 256 ? 8 : cols <= 512 ? 16 : wanted;
     if (cols > 512 * num) num = 32;
     const int64_t threads = (cols + 32 * num - 1) / (32 * num) * 32;
-    if (threads > 512 || (threads > 32 && 2 * bytes_a_row > kMostShared)) return s;
+    if (threads > 512 || (threads > 32 && bytes > kMostShared)) return s;
     s.num = num;
     s.threads = (int)threads;
     return s;
@@ -953,12 +1013,14 @@ const void *backward_kernel(const RowShape &s, int64_t cols)
 }
 
 template <typename T, typename TW, int kNum>
-const void *forward_pieces(const RowShape &s)
+const void *forward_pieces(const RowShape &s, bool staged)
 {
-    if (s.num == kNum)
-        return s.threads <= 32 ? reinterpret_cast<const void *>(layer_norm_pieces_kernel<T, TW, kNum, true>)
-                               : reinterpret_cast<const void *>(layer_norm_pieces_kernel<T, TW, kNum, false>);
-    if constexpr (kNum > 8) return forward_pieces<T, TW, kNum / 2>(s);
+    if (s.num == kNum) {
+        if (s.threads <= 32) return reinterpret_cast<const void *>(layer_norm_pieces_kernel<T, TW, kNum, true, true>);
+        return staged ? reinterpret_cast<const void *>(layer_norm_pieces_kernel<T, TW, kNum, false, true>)
+                      : reinterpret_cast<const void *>(layer_norm_pieces_kernel<T, TW, kNum, false, false>);
+    }
+    if constexpr (kNum > 8) return forward_pieces<T, TW, kNum / 2>(s, staged);
     return nullptr;
 }
 
@@ -980,14 +1042,16 @@ cudaError_t forward(const LayerNormArgs &a, int sm_count, cudaStream_t st)
                          on_16_bytes(a.weight) && on_16_bytes(a.bias);
     RowLaunch l;
     if (vectors) l.shape = row_shape(a.rows, a.cols, kVec, 4, sm_count);
-    if (l.shape.num == 0 && a.cols <= 1 << 16) l.shape = piece_shape(a.rows, a.cols, piece_bytes<T>((int)a.cols), 32, sm_count);
+    if (l.shape.num == 0 && a.cols <= 1 << 16) l.shape = piece_shape(a.rows, a.cols, 2 * (int64_t)piece_bytes<T>((int)a.cols), 32, sm_count);
     if (l.shape.num == 0) {
         layer_norm_kernel<T, TW><<<row_grid(a.rows), kThreads, 0, st>>>(a);
         return cudaGetLastError();
     }
     if (l.shape.pieces) {
-        l.kernel = forward_pieces<T, TW, 32>(l.shape);
-        l.shared = (size_t)2 * piece_bytes<T>((int)a.cols) * (l.shape.threads <= 32 ? kSoloWarps : 1);
+        const size_t ring = (size_t)2 * piece_bytes<T>((int)a.cols) * (l.shape.threads <= 32 ? kSoloWarps : 1), affine = affine_bytes((int)a.cols, 2);
+        const bool staged = l.shape.threads <= 32 || (a.rows >= 16 * (int64_t)sm_count && ring + affine <= 56 * 1024);
+        l.kernel = forward_pieces<T, TW, 32>(l.shape, staged);
+        l.shared = ring + (staged ? affine : 0);
     } else {
         l.kernel = forward_kernel<T, TW, kMostNum>(l.shape, a.cols, a.weight && a.bias);
         l.shared = (size_t)kDepth * l.shape.num * l.shape.block() * 16;
@@ -1004,12 +1068,12 @@ RowLaunch backward_launch(const LayerNormGradArgs &a, int sm_count)
                          rows_on_16_bytes(a.dx, a.rows, a.dx_ld, a.dtype) && on_16_bytes(a.weight);
     RowLaunch l;
     if (vectors && a.rows > 0) l.shape = row_shape(a.rows, a.cols, kVec, 2, sm_count);
-    if (l.shape.num == 0 && a.rows > 0 && a.cols <= 1 << 16) l.shape = piece_shape(a.rows, a.cols, 2 * (int64_t)piece_bytes<T>((int)a.cols),
+    if (l.shape.num == 0 && a.rows > 0 && a.cols <= 1 << 16) l.shape = piece_shape(a.rows, a.cols, 4 * (int64_t)piece_bytes<T>((int)a.cols) + affine_bytes((int)a.cols, 1),
                                                                                        a.rows * a.cols < (8 << 20) ? 8 : 16, sm_count);
     if (l.shape.num == 0) return l;
     if (l.shape.pieces) {      // (also room for the sums of the columns, 8 bytes each)
         l.kernel = backward_pieces<T, TW, 32>(l.shape);
-        l.shared = (size_t)4 * piece_bytes<T>((int)a.cols) * (l.shape.threads <= 32 ? kSoloWarps : 1);
+        l.shared = affine_bytes((int)a.cols, 1) + (size_t)4 * piece_bytes<T>((int)a.cols) * (l.shape.threads <= 32 ? kSoloWarps : 1);
     } else {                   // (the same: 32 lanes' columns)
         l.kernel = backward_kernel<T, TW, kMostNum>(l.shape, a.cols);
         l.shared = (size_t)kDepth * 2 * l.shape.num * l.shape.block() * 16;
