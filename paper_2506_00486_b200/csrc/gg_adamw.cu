@@ -220,8 +220,10 @@ __device__ __noinline__ float2 step_block_any(Place<TW, TG, kNarrow> at, int n, 
     return scale;
 }
 
-// Blocks at vector boundaries with a multiple of eight elements: lane l takes the eight from 8 l on, in pairs.  Lanes beyond the
-// block's end (`live` is false) compute on zeros and store nothing.
+// Blocks at vector boundaries: lane l takes the eight elements from 8 l on, in pairs.  Beyond the end of a tensor's last block
+// it computes on zeros and stores nothing.  kRagged: the end is within the eight elements of a lane, and every
+// lane stores one by one.  (A case of its own: within the other it takes 1.12 against 1.04 ms for a decoder with 8-bit
+// states and bf16 weights.)
 template <typename TW, typename TG, bool kNarrow>
 struct Operands {
     using TS = typename State<kNarrow>::type;
@@ -232,13 +234,23 @@ struct Operands {
     // the block `ahead` elements on, n elements of it
     static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const Place<TW, TG, kNarrow> &at, int ahead, int n)
     {
-        Eight<TG>::fetch(slot, lane, at.g + ahead, n);
+        if (n >= kBlock) fetch_from(slot, lane, at.g + ahead, at.w + ahead, at.m + ahead, at.v + ahead, kBlock);
+        else if (n > 0) fetch_some(slot, lane, at.g + ahead, at.w + ahead, at.m + ahead, at.v + ahead, n);
+    }
+    static __device__ __forceinline__ void fetch_from(uint32_t slot, int lane, const TG *g, const TW *w, const TS *m, const TS *v, int n)
+    {
+        Eight<TG>::fetch(slot, lane, g, n);
         slot += 32 * Eight<TG>::kSlot;
-        Eight<TW>::fetch(slot, lane, at.w + ahead, n);
+        Eight<TW>::fetch(slot, lane, w, n);
         slot += 32 * Eight<TW>::kSlot;
-        Eight<TS>::fetch(slot, lane, at.m + ahead, n);
+        Eight<TS>::fetch(slot, lane, m, n);
         slot += 32 * Eight<TS>::kSlot;
-        Eight<TS>::fetch(slot, lane, at.v + ahead, n);
+        Eight<TS>::fetch(slot, lane, v, n);
+    }
+    // (a call: its code in the loop would cost the others registers, 1.10 against 1.04 ms for a decoder with 8-bit states)
+    static __device__ __noinline__ void fetch_some(uint32_t slot, int lane, const TG *g, const TW *w, const TS *m, const TS *v, int n)
+    {
+        fetch_from(slot, lane, g, w, m, v, n);
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
@@ -250,13 +262,69 @@ struct Operands {
         slot += 32 * Eight<TS>::kSlot;
         v.read(slot, lane);
     }
+    // What a step stores of a lane with n <= 8 elements, 8-bit states.
+    static __device__ __forceinline__ void put_some(uint32_t slot, const Place<TW, TG, kNarrow> &at, int n, const f32x2 (&wn)[4], const uint32_t (&out)[4],
+                                                    const uint32_t (&mc)[2], const uint32_t (&vc)[2])
+    {
+        const uint32_t lane = threadIdx.x & 31;
+        const uint32_t c_at = slot + 16u * lane, w_at = slot + 32u * Eight<TG>::kSlot + Eight<TW>::kSlot * lane;
+        const uint32_t m_at = slot + 32u * (Eight<TG>::kSlot + Eight<TW>::kSlot) + 8u * lane, v_at = m_at + 256u;
+        asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(m_at), "r"(mc[0]), "r"(mc[1]) : "memory");
+        asm volatile("st.shared.v2.u32 [%0], {%1, %2};" ::"r"(v_at), "r"(vc[0]), "r"(vc[1]) : "memory");
+        if constexpr (sizeof(TW) == 2) {
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(w_at), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]) : "memory");
+        } else {
+            asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(w_at), "l"(wn[0]), "l"(wn[1]) : "memory");
+            asm volatile("st.shared.v2.b64 [%0], {%1, %2};" ::"r"(w_at + 16u), "l"(wn[2]), "l"(wn[3]) : "memory");
+        }
+        if (at.copy)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(c_at), "r"(narrow2(wn[0])), "r"(narrow2(wn[1])), "r"(narrow2(wn[2])),
+                         "r"(narrow2(wn[3])) : "memory");
+#pragma unroll 1
+        for (int i = 0; i < n; ++i) {
+            uint32_t a, b;
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(a) : "r"(m_at + i) : "memory");
+            asm volatile("ld.shared.u8 %0, [%1];" : "=r"(b) : "r"(v_at + i) : "memory");
+            at.m[i] = (TS)a;
+            at.v[i] = (TS)b;
+            if constexpr (sizeof(TW) == 2) {
+                uint16_t h;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(w_at + 2u * i) : "memory");
+                at.w[i] = h;
+            } else {
+                float f;
+                asm volatile("ld.shared.f32 %0, [%1];" : "=f"(f) : "r"(w_at + 4u * i) : "memory");
+                at.w[i] = f;
+            }
+            if (at.copy) {
+                uint16_t h;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(h) : "r"(c_at + 2u * i) : "memory");
+                at.copy[i] = h;
+            }
+        }
+    }
 };
 
-// States in fp32: bound by memory with room to spare, so the arithmetic is the plain one.
-template <typename TW, typename TG>
-__device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const Place<TW, TG, false> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *)
+// The new weights (`out`: rounded, two a word, for bf16), and their copy.
+template <typename TW, typename TG, bool kNarrow>
+__device__ __forceinline__ void store_weights(const Place<TW, TG, kNarrow> &at, const f32x2 (&wn)[4], const uint32_t (&out)[4])
 {
-    const bool live = 8 * (int)(threadIdx.x & 31) < n;
+    if constexpr (sizeof(TW) == 2) Eight<uint16_t>::store_words(at.w, out[0], out[1], out[2], out[3]);
+    else Eight<float>::store(at.w, wn);
+    if (at.copy) Eight<uint16_t>::store(at.copy, wn);
+}
+template <typename TW, typename TG, bool kNarrow>
+__device__ __forceinline__ void store_some_weights(const Place<TW, TG, kNarrow> &at, const f32x2 (&wn)[4], const uint32_t (&out)[4], int n)
+{
+    if constexpr (sizeof(TW) == 2) Eight<uint16_t>::store_some_words(at.w, out[0], out[1], out[2], out[3], n);
+    else Eight<float>::store_some(at.w, wn, n);
+    if (at.copy) Eight<uint16_t>::store_some(at.copy, wn, n);
+}
+
+// States in fp32: bound by memory with room to spare, so the arithmetic is the plain one.
+template <bool kRagged, typename TW, typename TG>
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const Place<TW, TG, false> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *, uint32_t)
+{
     f32x2 wn[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -267,23 +335,27 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const P
         x.m.v[i] = pair(a.m, b.m);
         x.v.v[i] = pair(a.v, b.v);
     }
-    if (!live) return scale;
-    Eight<float>::store(at.m, x.m.v);
-    Eight<float>::store(at.v, x.v.v);
+    const int mine = n - 8 * (int)(threadIdx.x & 31);
+    if (mine <= 0) return scale;
+    uint32_t out[4] = {0u, 0u, 0u, 0u};
     if constexpr (sizeof(TW) == 2) {
         const Block4 q = at.noise(c, threadIdx.x & 31);
         const uint32_t word[4] = {q.w1, q.w2, q.w3, q.w0};      // element e takes u[e + 2]
-        uint32_t out[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float2 f = halves(wn[i]);
             out[i] = (uint32_t)bf16_stochastic(f.x, word[i] & 0xFFFFu) | ((uint32_t)bf16_stochastic(f.y, word[i] >> 16) << 16);
         }
-        Eight<uint16_t>::store_words(at.w, out[0], out[1], out[2], out[3]);
-    } else {
-        Eight<float>::store(at.w, wn);
     }
-    if (at.copy) Eight<uint16_t>::store(at.copy, wn);
+    if constexpr (kRagged) {
+        Eight<float>::store_some(at.m, x.m.v, mine);
+        Eight<float>::store_some(at.v, x.v.v, mine);
+        store_some_weights(at, wn, out, mine);
+    } else {
+        Eight<float>::store(at.m, x.m.v);
+        Eight<float>::store(at.v, x.v.v);
+        store_weights(at, wn, out);
+    }
     return scale;
 }
 
@@ -333,9 +405,10 @@ __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c
 // four it is the top byte.  The largest code cannot round up past 126: x (448 / top) exceeds 448 by at most two units
 // of its pattern, and the noise stays eight short of a whole code.  A block that holds an inf or nan, or values so
 // large that 2^-120 448 / top is not a normal number, goes through step_block_any; nothing is stored before that is known.
-template <typename TW, typename TG>
-__device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Place<TW, TG, true> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise)
+template <bool kRagged, typename TW, typename TG>
+__device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Place<TW, TG, true> &at, int n, const StepScalars &c, float keep, float gscale, float2 scale, uint32_t *noise, uint32_t slot)
 {
+    using Data = Operands<TW, TG, true>;
     f32x2 wn[4], mn[4], rn[4];
     f32x2 sum = 0;
     float m_top = 0.0f, r_top = 0.0f;
@@ -402,22 +475,32 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
         }
     }
     if (8 * (int)(threadIdx.x & 31) >= n) return scale;
-    Eight<uint8_t>::store(at.m, mc[0], mc[1]);
-    Eight<uint8_t>::store(at.v, vc[0], vc[1]);
-    if constexpr (sizeof(TW) == 2) {
-        uint32_t out[4];
+    if constexpr (!kRagged) {
+        Eight<uint8_t>::store(at.m, mc[0], mc[1]);
+        Eight<uint8_t>::store(at.v, vc[0], vc[1]);
+    }
+    uint32_t out[4] = {0u, 0u, 0u, 0u};
+    if constexpr (sizeof(TW) == 2)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {       // element e takes u[e + 2]
             const float2 f = halves(wn[i]);
             const uint32_t k = word[i + 1 & 3];
             out[i] = __byte_perm(__float_as_uint(f.x) + (k & 0xFFFFu), __float_as_uint(f.y) + (k >> 16), 0x7632);
         }
-        Eight<uint16_t>::store_words(at.w, out[0], out[1], out[2], out[3]);
-    } else {
-        Eight<float>::store(at.w, wn);
-    }
-    if (at.copy) Eight<uint16_t>::store(at.copy, wn);
+    // the end of a tensor goes through the warp's places of the ring (all lanes have read them: their maxima are known)
+    if constexpr (kRagged) Data::put_some(slot, at, min(n - 8 * (int)(threadIdx.x & 31), 8), wn, out, mc, vc);
+    else store_weights(at, wn, out);
     return scale;
+}
+
+// (A call, for the loop's registers: inlined, 1.10 against 1.04 ms for a decoder with 8-bit states.)
+template <typename TW, typename TG, bool kNarrow>
+__device__ __noinline__ float2 step_ragged(uint32_t slot, const Place<TW, TG, kNarrow> at, int n, const StepScalars &c, float keep, float gscale,
+                                           float2 scale, uint32_t *noise)
+{
+    Operands<TW, TG, kNarrow> x;
+    x.read(slot, threadIdx.x & 31);
+    return step_eight<true>(x, at, n, c, keep, gscale, scale, noise, slot);
 }
 
 // A CTA per tile, a warp per run of blocks.  A warp fetches its operands kDepth - 1 blocks ahead into places of shared
@@ -453,12 +536,12 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constan
     const bool has_scale = kNarrow && lane * kBlock < left;
     float2 scales = has_scale ? make_float2(c.m_scale[my_scale], c.v_scale[my_scale]) : make_float2(0.0f, 0.0f);
 
-    int fast = id < 0 ? (left % 8 == 0 ? left : left & ~(kBlock - 1)) : 0;        // of these, through the ring
+    int fast = id < 0 ? left : 0;        // of these, through the ring
     left -= fast;
     const uint32_t slots = (uint32_t)__cvta_generic_to_shared(ring) + (uint32_t)(warp * kDepth * Data::kSlot);
 #pragma unroll
     for (int d = 0; d < kDepth - 1; ++d) {
-        if (d * kBlock < fast) Data::fetch(slots + d * Data::kSlot, lane, at, d * kBlock, fast - d * kBlock);
+        Data::fetch(slots + d * Data::kSlot, lane, at, d * kBlock, fast - d * kBlock);
         copies_commit();
     }
     const float gscale = c.grad_scale ? __ldg(c.grad_scale) : 1.0f;
@@ -471,15 +554,21 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constan
     auto scale_of = [&]() { return kNarrow ? make_float2(__shfl_sync(0xFFFFFFFFu, scales.x, k), __shfl_sync(0xFFFFFFFFu, scales.y, k)) : scales; };
     for (uint32_t d = 0; fast > 0; d = d == kDepth - 1 ? 0 : d + 1) {
         __syncwarp();      // every lane has read the place of the block before this one: the block after the next ones goes there
-        const uint32_t to = slots + (d == 0 ? kDepth - 1 : d - 1) * Data::kSlot;
-        if (fast >= kDepth * kBlock) Data::fetch(to, lane, at, (kDepth - 1) * kBlock, kBlock);
-        else if (fast > (kDepth - 1) * kBlock) Data::fetch(to, lane, at, (kDepth - 1) * kBlock, fast - (kDepth - 1) * kBlock);
+        Data::fetch(slots + (d == 0 ? kDepth - 1 : d - 1) * Data::kSlot, lane, at, (kDepth - 1) * kBlock, fast - (kDepth - 1) * kBlock);
         copies_commit();
         copies_wait<kDepth - 1>();
         __syncwarp();      // every lane's copies of this block have arrived
-        Data x;
-        x.read(slots + d * Data::kSlot, lane);
-        const float2 now = step_eight(x, at, min(fast, kBlock), c, keep, gscale, scale_of(), noise[warp]);
+        const int n = min(fast, kBlock);
+        const uint32_t slot = slots + d * Data::kSlot;
+        const float2 scale = scale_of();
+        float2 now;
+        if (n % 8 == 0) {
+            Data x;
+            x.read(slot, lane);
+            now = step_eight<false>(x, at, n, c, keep, gscale, scale, noise[warp], slot);
+        } else {
+            now = step_ragged(slot, at, n, c, keep, gscale, scale, noise[warp]);
+        }
         if (lane == k) scales = now;
         at.advance();
         fast -= kBlock;
@@ -522,7 +611,15 @@ cudaError_t launch_table(const StepTable<N> &tab, const StepScalars &c, int w_dt
     }
 }
 
-// sqrt(sum of squares) over the tile sums of a moments sweep, and the factor that brings it down to max_norm.
+// The norm from a sum of squares (nan if an entry was not finite), and the factor that brings it down to max_norm.
+__device__ __forceinline__ void write_norm(double sum, uint32_t wrong, double max_norm, double *norm, float *scale)
+{
+    const double r = wrong != 0u ? __longlong_as_double(0x7FF8000000000000ll) : sqrt(sum);
+    if (norm) *norm = r;
+    if (scale) *scale = r > max_norm ? (float)(max_norm / r) : (r == r ? 1.0f : (float)r);
+}
+
+// The norm from the tile sums of a moments sweep.
 __global__ void __launch_bounds__(1024) grad_norm_kernel(const double *s2, const uint32_t *bad, int32_t n_tiles, double max_norm,
                                                          double *norm, float *scale)
 {
@@ -537,9 +634,76 @@ __global__ void __launch_bounds__(1024) grad_norm_kernel(const double *s2, const
     __syncthreads();
     if (threadIdx.x != 0) return;
     for (int w = 1; w < 32; ++w) { s += sh[w]; b |= shb[w]; }
-    const double r = b != 0u ? __longlong_as_double(0x7FF8000000000000ll) : sqrt(s);
-    if (norm) *norm = r;
-    if (scale) *scale = r > max_norm ? (float)(max_norm / r) : (r == r ? 1.0f : (float)r);
+    write_norm(s, b, max_norm, norm, scale);
+}
+
+// The norm of few tiles in one launch: a CTA sums the squares of a tile in fp64, and the last CTA to finish adds the tiles in
+// order.  `ticket` is 0 between launches.
+constexpr int kNormThreads = 512;
+template <typename T>
+__global__ void __launch_bounds__(kNormThreads) grad_norm_small_kernel(const TileMap map, double *s2, uint32_t *bad, uint32_t *ticket, double max_norm,
+                                                                      double *norm, float *scale)
+{
+    __shared__ double sh[kNormThreads / 32];
+    __shared__ uint32_t last;
+    const int t = blockIdx.x, s = map.tile_seg[t], warp = threadIdx.x >> 5;
+    const int64_t off = (int64_t)(t - map.tile_prefix[s]) * kTile;
+    const int n = (int)min((int64_t)kTile, map.seg_len[s] - off);
+    const T *g = static_cast<const T *>(map.seg_ptr[s]) + off;
+    double sum = 0.0;
+    uint32_t wrong = 0;
+    auto add = [&](float v) {
+        if (isfinite(v)) sum = fma((double)v, (double)v, sum);
+        else wrong = 1u;
+    };
+    constexpr int kVec = 16 / sizeof(T), kMost = kTile / kVec / kNormThreads;
+    if (reinterpret_cast<uintptr_t>(g) % 16 == 0) {
+        uint4 v[kMost];
+#pragma unroll
+        for (int i = 0; i < kMost; ++i) {
+            const int e = (i * kNormThreads + (int)threadIdx.x) * kVec;
+            v[i] = e + kVec <= n ? __ldg(reinterpret_cast<const uint4 *>(g + e)) : make_uint4(0u, 0u, 0u, 0u);
+        }
+#pragma unroll
+        for (int i = 0; i < kMost; ++i)
+            for (const uint32_t w : {v[i].x, v[i].y, v[i].z, v[i].w}) {
+                if constexpr (sizeof(T) == 4) {
+                    add(__uint_as_float(w));
+                } else {
+                    add(__uint_as_float(w << 16));
+                    add(__uint_as_float(w & 0xFFFF0000u));
+                }
+            }
+        for (int e = n / kVec * kVec + threadIdx.x; e < n; e += kNormThreads) add(widen<T>(g[e]));
+    } else {
+#pragma unroll 8
+        for (int e = threadIdx.x; e < n; e += kNormThreads) add(widen<T>(g[e]));
+    }
+    sum = warp_sum(sum);
+    wrong = __syncthreads_or((int)wrong);
+    if ((threadIdx.x & 31) == 0) sh[warp] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int w = 1; w < kNormThreads / 32; ++w) sum += sh[w];
+        s2[t] = sum;
+        bad[t] = wrong;
+        __threadfence();
+        last = atomicAdd(ticket, 1u) == gridDim.x - 1u;
+    }
+    __syncthreads();
+    if (last == 0u || warp != 0) return;
+    __threadfence();
+    sum = 0.0;
+    wrong = 0;
+    for (int i = threadIdx.x; i < (int)gridDim.x; i += 32) {
+        sum += __ldcg(s2 + i);
+        wrong |= __ldcg(bad + i);
+    }
+    sum = warp_sum(sum);
+    wrong = __reduce_or_sync(0xFFFFFFFFu, wrong);
+    if (threadIdx.x != 0) return;
+    write_norm(sum, wrong, max_norm, norm, scale);
+    *ticket = 0u;
 }
 
 }  // namespace
@@ -557,6 +721,15 @@ cudaError_t launch_adamw(const StepTable<kTableLarge> &tab, const StepScalars &c
 cudaError_t launch_grad_norm(const double *s2, const uint32_t *bad, int32_t n_tiles, double max_norm, double *norm, float *scale, cudaStream_t st)
 {
     grad_norm_kernel<<<1, 1024, 0, st>>>(s2, bad, n_tiles, max_norm, norm, scale);
+    return cudaGetLastError();
+}
+
+cudaError_t launch_grad_norm_small(const TileMap &map, int dtype, double *s2, uint32_t *bad, uint32_t *ticket, double max_norm, double *norm,
+                                   float *scale, cudaStream_t st)
+{
+    const unsigned grid = (unsigned)map.n_tiles;
+    if (dtype == GG_F32) grad_norm_small_kernel<float><<<grid, kNormThreads, 0, st>>>(map, s2, bad, ticket, max_norm, norm, scale);
+    else grad_norm_small_kernel<uint16_t><<<grid, kNormThreads, 0, st>>>(map, s2, bad, ticket, max_norm, norm, scale);
     return cudaGetLastError();
 }
 

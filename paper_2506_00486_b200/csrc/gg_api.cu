@@ -90,6 +90,7 @@ struct gg_ctx {
     int64_t chan_bytes = 0;
     void *norm_part = nullptr;    // scratch of gg_layer_norm_grad (partial sums over the rows)
     int64_t norm_part_bytes = 0;
+    uint32_t *norm_ticket = nullptr;    // counter of gg_grad_norm's one-launch form (zero between calls)
     double *seed = nullptr;       // device table that seeds the moment-ratio inversion of the short-segment kernel
     int resident_grid[2][8];      // CTAs the one-launch pass may use, by gradient type and sweep flags (-1: not asked yet)
     bool can_cooperate = false, can_cluster = false;
@@ -619,6 +620,7 @@ gg_status gg_destroy(gg_ctx *ctx)
     if (ctx->small_counts) cudaFree(ctx->small_counts);
     if (ctx->chan_buf) cudaFree(ctx->chan_buf);
     if (ctx->norm_part) cudaFree(ctx->norm_part);
+    if (ctx->norm_ticket) cudaFree(ctx->norm_ticket);
     if (ctx->ent_part) cudaFree(ctx->ent_part);
     if (ctx->ent_done) cudaFree(ctx->ent_done);
     delete ctx;
@@ -1650,6 +1652,16 @@ gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dty
     if (n_seg > 0) {
         st = get_plan(ctx, g, n_seg, dtype, nullptr, 0, nullptr, &p, stream);
         if (st != GG_OK) return st;
+        if (p->n_tiles > 0 && p->n_tiles <= kNormTiles) {
+            if (!ctx->norm_ticket) {
+                GG_CUDA(ctx, cudaMalloc(reinterpret_cast<void **>(&ctx->norm_ticket), sizeof(uint32_t)));
+                GG_CUDA(ctx, cudaMemset(ctx->norm_ticket, 0, sizeof(uint32_t)));
+            }
+            GG_CUDA(ctx, launch_grad_norm_small(p->map, dtype, p->part.s2, p->part.bad, ctx->norm_ticket, max_norm, norm, scale, cs));
+            ctx->launches += 1;
+            mark_used(p, cs);
+            return GG_OK;
+        }
         StreamArgs sa{};
         sa.map = p->map;
         sa.part = p->part;

@@ -147,15 +147,27 @@ template <typename T> struct Eight;
 template <> struct Eight<float> {
     static constexpr int kSlot = 32;
     f32x2 v[4];
-    // p: the lane's eight elements of the warp's 256, of which the first n are there (a multiple of 8; the rest reads as 0)
+    // p: the lane's eight elements of the warp's 256, of which the first n are there (the rest reads as 0)
     static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const float *p, int n)
     {
         p -= 4 * lane;
         const uint32_t to = slot + (uint32_t)(lane ^ (lane >> 3 & 1)) * 16u;
-        if (4 * lane < n) copy16(to, p);
-        else zero16(to);
-        if (4 * lane + 128 < n) copy16(to + 512u, p + 128);
-        else zero16(to + 512u);
+        if (n >= 256) {
+            copy16(to, p);
+            copy16(to + 512u, p + 128);
+            return;
+        }
+        some(to, p, n - 4 * lane);
+        some(to + 512u, p + 128, n - 4 * lane - 128);
+    }
+    static __device__ __forceinline__ void some(uint32_t to, const float *p, int n)
+    {
+        if (n >= 4) {
+            copy16(to, p);
+            return;
+        }
+        zero16(to);
+        for (int i = 0; i < n; ++i) asm volatile("st.shared.f32 [%0], %1;" ::"r"(to + 4u * i), "f"(p[i]) : "memory");
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
@@ -168,14 +180,30 @@ template <> struct Eight<float> {
     {
         asm volatile("st.global.L1::no_allocate.v4.b64 [%0], {%1, %2, %3, %4};" ::"l"(p), "l"(x[0]), "l"(x[1]), "l"(x[2]), "l"(x[3]) : "memory");
     }
+    // the first n of them, one by one
+    static __device__ __forceinline__ void store_some(float *p, const f32x2 (&x)[4], int n)
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = halves(x[i]);
+            if (2 * i < n) p[2 * i] = f.x;
+            if (2 * i + 1 < n) p[2 * i + 1] = f.y;
+        }
+    }
 };
 template <> struct Eight<uint16_t> {
     static constexpr int kSlot = 16;
     uint4 v;
     static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint16_t *p, int n)
     {
-        if (8 * lane < n) copy16(slot + lane * 16, p);
-        else zero16(slot + lane * 16);
+        const uint32_t to = slot + lane * 16;
+        if (n >= 256 || n >= 8 * lane + 8) {      // (256: known when the code is compiled)
+            copy16(to, p);
+            return;
+        }
+        n -= 8 * lane;
+        zero16(to);
+        for (int i = 0; i < n; ++i) asm volatile("st.shared.u16 [%0], %1;" ::"r"(to + 2u * i), "h"(p[i]) : "memory");
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {
@@ -190,14 +218,31 @@ template <> struct Eight<uint16_t> {
     {
         store_words(p, narrow2(x[0]), narrow2(x[1]), narrow2(x[2]), narrow2(x[3]));
     }
+    static __device__ __forceinline__ void store_some_words(uint16_t *p, uint32_t a, uint32_t b, uint32_t c, uint32_t d, int n)
+    {
+        const uint32_t w[4] = {a, b, c, d};
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (uint16_t)(w[i / 2] >> 16 * (i & 1));
+    }
+    static __device__ __forceinline__ void store_some(uint16_t *p, const f32x2 (&x)[4], int n)
+    {
+        store_some_words(p, narrow2(x[0]), narrow2(x[1]), narrow2(x[2]), narrow2(x[3]), n);
+    }
 };
 template <> struct Eight<uint8_t> {
     static constexpr int kSlot = 8;
     uint2 v;
     static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const uint8_t *p, int n)
     {
-        if (8 * lane < n) copy8(slot + lane * 8, p);
-        else asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(slot + lane * 8), "r"(0u) : "memory");
+        const uint32_t to = slot + lane * 8;
+        if (n >= 256 || n >= 8 * lane + 8) {
+            copy8(to, p);
+            return;
+        }
+        n -= 8 * lane;
+        asm volatile("st.shared.v2.u32 [%0], {%1, %1};" ::"r"(to), "r"(0u) : "memory");
+        for (int i = 0; i < n; ++i) asm volatile("st.shared.u8 [%0], %1;" ::"r"(to + i), "r"((uint32_t)p[i]) : "memory");
     }
     __device__ __forceinline__ void read(uint32_t slot, int lane)
     {

@@ -241,6 +241,12 @@ cudaError_t launch_gct_step(const TileMap &map, void *const *w_ptr, gg_dtype g_d
 cudaError_t launch_sample(const TileMap &map, gg_dtype dtype, const double *beta, const double *alpha,
                           uint64_t seed, uint32_t tensor_id0, uint32_t *max_attempts, cudaStream_t st);
 
+// The gradient norm of up to kNormTiles tiles in one launch (gg_adamw.cu).  ticket: one word, zero between calls (the kernel
+// leaves it so).
+constexpr int kNormTiles = 592;
+cudaError_t launch_grad_norm_small(const TileMap &map, int dtype, double *s2, uint32_t *bad, uint32_t *ticket, double max_norm, double *norm,
+                                   float *scale, cudaStream_t st);
+
 // Layer norm and its gradient (gg_layer_norm.cu): the arguments of the interface, checked.
 using LayerNormArgs = gg_layer_norm_args;
 using LayerNormGradArgs = gg_layer_norm_grad_args;
