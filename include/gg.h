@@ -345,7 +345,7 @@ gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dty
  *     m <- beta1 m + (1 - beta1) g
  *     v <- beta2 v + (1 - beta2) g^2
  *     w <- w (1 - lr * decay) - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
- * in fp32 arithmetic whatever the types.  A grad_scale that is inf or nan (as gg_grad_norm writes it for a
+ * in fp32 arithmetic whatever the types (a v below 2^-126 counts as 0).  A grad_scale that is inf or nan (as gg_grad_norm writes it for a
  * gradient that overflowed) makes the step a no-op: nothing is written.  Without it an inf or nan in g reaches its own
  * element's w, m and v and no other.  Needs no plan: tables travel with the launch, so addresses may differ from step
  * to step, and nothing is allocated.

@@ -950,20 +950,21 @@ struct RowLaunch {
     size_t shared = 0;
     int64_t grid(int64_t rows, int sm_count) const
     {
-        // (asking takes microseconds: the answers are kept)
-        struct Known { const void *kernel; unsigned block; size_t shared; int ctas; };
+        // (asking takes microseconds: the answers are kept, for each device, whose kernels have limits of their own)
+        struct Known { const void *kernel; unsigned block; size_t shared; int device, ctas; };
         static thread_local Known known[32];
         static thread_local int n_known = 0, next = 0;
-        int ctas = 0;
+        int ctas = 0, device = -1;
+        if (cudaGetDevice(&device) != cudaSuccess) cudaGetLastError();
         for (int i = 0; i < n_known && ctas == 0; ++i)
-            if (known[i].kernel == kernel && known[i].block == shape.block() && known[i].shared == shared) ctas = known[i].ctas;
+            if (known[i].device == device && known[i].kernel == kernel && known[i].block == shape.block() && known[i].shared == shared) ctas = known[i].ctas;
         if (ctas == 0) {
             if ((shared > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) != cudaSuccess) ||
                 cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, (int)shape.block(), shared) != cudaSuccess || ctas < 1) {
                 cudaGetLastError();
                 ctas = 1;
             }
-            known[next] = Known{kernel, shape.block(), shared, ctas};
+            known[next] = Known{kernel, shape.block(), shared, device, ctas};
             next = (next + 1) % 32;
             if (n_known < 32) ++n_known;
         }
