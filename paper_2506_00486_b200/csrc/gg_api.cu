@@ -1624,7 +1624,8 @@ gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *a, void
     if (a->cols == 0 || (!a->dx && !a->dweight && !a->dbias)) return GG_OK;
     DeviceGuard guard(ctx->device);
     if (!guard.ok) return GG_ERR_CUDA;
-    const int slices = layer_norm_grad_slices(*a, ctx->sm_count);
+    int slices = 0;
+    GG_CUDA(ctx, layer_norm_grad_slices(*a, ctx->sm_count, &slices));
     if (a->dweight || a->dbias) {
         st = grow(ctx, &ctx->norm_part, &ctx->norm_part_bytes, (int64_t)sizeof(float) * 2 * slices * a->cols);
         if (st != GG_OK) return st;

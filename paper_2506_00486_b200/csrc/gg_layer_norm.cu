@@ -903,7 +903,11 @@ struct RowShape {
 // Few rows are spread over as many threads as they can use (one vector each); many over as few as give a thread `wanted`
 // vectors, or more where a CTA of 512 would not hold them otherwise.
 constexpr int kMostNum = 4;
-constexpr int kMostShared = kDepth * 2 * kMostNum * 512 * 16;      // of any launch (the same for all: a kernel has one such limit)
+// Dynamic shared memory of any launch: every size is tested against it, and every kernel that wants more than 40 KB is allowed it.
+// (An SM has 227 KB for a CTA, of which these kernels' own variables take up to 512 bytes.  With 192 KB fp32 [4096, 12288] forward, then
+// not staged, takes 118 against 91 us; the gradient of fp32 [4096, 11000], then by the kernels for any row length, 295 against 125.)
+constexpr int64_t kMostShared = 224 * 1024;
+static_assert(kDepth * 2 * kMostNum * 512 * 16 <= kMostShared, "the vector form has no test of its own");
 RowShape row_shape(int64_t rows, int64_t cols, int vec, int wanted, int sm_count)
 {
     RowShape s;
@@ -948,28 +952,30 @@ struct RowLaunch {
     const void *kernel = nullptr;
     RowShape shape;
     size_t shared = 0;
-    int64_t grid(int64_t rows, int sm_count) const
+    // The CTAs of a launch over so many rows.
+    cudaError_t grid(int64_t rows, int sm_count, int64_t *grid_ctas) const
     {
         // (asking takes microseconds: the answers are kept, for each device, whose kernels have limits of their own)
         struct Known { const void *kernel; unsigned block; size_t shared; int device, ctas; };
         static thread_local Known known[32];
         static thread_local int n_known = 0, next = 0;
         int ctas = 0, device = -1;
-        if (cudaGetDevice(&device) != cudaSuccess) cudaGetLastError();
+        cudaError_t e = cudaGetDevice(&device);
+        if (e != cudaSuccess) return e;
         for (int i = 0; i < n_known && ctas == 0; ++i)
             if (known[i].device == device && known[i].kernel == kernel && known[i].block == shape.block() && known[i].shared == shared) ctas = known[i].ctas;
         if (ctas == 0) {
-            if ((shared > 40 * 1024 && cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMostShared) != cudaSuccess) ||
-                cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, (int)shape.block(), shared) != cudaSuccess || ctas < 1) {
-                cudaGetLastError();
-                ctas = 1;
-            }
+            if (shared > 40 * 1024) e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMostShared);
+            if (e == cudaSuccess) e = cudaOccupancyMaxActiveBlocksPerMultiprocessor(&ctas, kernel, (int)shape.block(), shared);
+            if (e == cudaSuccess && ctas < 1) e = cudaErrorLaunchOutOfResources;
+            if (e != cudaSuccess) return e;
             known[next] = Known{kernel, shape.block(), shared, device, ctas};
             next = (next + 1) % 32;
             if (n_known < 32) ++n_known;
         }
         const int64_t each = shape.rows_a_cta(), want = (rows + each - 1) / each, wave = (int64_t)sm_count * ctas;
-        return want < wave ? want : wave;
+        *grid_ctas = want < wave ? want : wave;
+        return cudaSuccess;
     }
 };
 
@@ -1052,15 +1058,18 @@ cudaError_t forward(const LayerNormArgs &a, int sm_count, cudaStream_t st)
         const size_t ring = (size_t)2 * piece_bytes<T>((int)a.cols) * (l.shape.threads <= 32 ? kSoloWarps : 1), affine = affine_bytes((int)a.cols, 2);
         // (staged where the registers, about 112 a thread, allow no more CTAs than then fit shared memory)
         const size_t by_registers = 65536 / (112 * (size_t)l.shape.threads);
-        const bool staged = l.shape.threads <= 32 || (a.rows >= 16 * (int64_t)sm_count && by_registers * (ring + affine) <= 224 * 1024);
+        const bool staged = l.shape.threads <= 32 || (a.rows >= 16 * (int64_t)sm_count && by_registers * (ring + affine) <= (size_t)kMostShared);
         l.kernel = forward_pieces<T, TW, 32>(l.shape, staged);
         l.shared = ring + (staged ? affine : 0);
     } else {
         l.kernel = forward_kernel<T, TW, kMostNum>(l.shape, a.cols, a.weight && a.bias);
         l.shared = (size_t)kDepth * l.shape.num * l.shape.block() * 16;
     }
+    int64_t ctas = 0;
+    const cudaError_t e = l.grid(a.rows, sm_count, &ctas);
+    if (e != cudaSuccess) return e;
     void *args[] = {const_cast<LayerNormArgs *>(&a), &l.shape.threads};
-    return cudaLaunchKernel(l.kernel, dim3((unsigned)l.grid(a.rows, sm_count)), dim3(l.shape.block()), args, l.shared, st);
+    return cudaLaunchKernel(l.kernel, dim3((unsigned)ctas), dim3(l.shape.block()), args, l.shared, st);
 }
 
 template <typename T, typename TW>
@@ -1119,19 +1128,24 @@ cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t
     return forward<uint16_t, uint16_t>(a, sm_count, st);
 }
 
-int layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count)
+cudaError_t layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count, int *slices)
 {
     const RowLaunch l = backward_launch(a, sm_count);
     if (l.kernel != nullptr) {
+        int64_t n = 0;
+        const cudaError_t e = l.grid(a.rows, sm_count, &n);
+        if (e != cudaSuccess) return e;
         // four rows or more for each thread of the vector form, where a wave would have less: what the CTAs gain by sharing
         // the rows the sum over their slices takes back (bf16 [2048, 896]: 10.5 against 13.1 us; larger ones do not change)
-        const int64_t n = l.grid(a.rows, sm_count), each = l.shape.rows_a_cta() * (l.shape.pieces ? 1 : 4), most = (a.rows + each - 1) / each;
-        return (int)(n < most ? n : most);
+        const int64_t each = l.shape.rows_a_cta() * (l.shape.pieces ? 1 : 4), most = (a.rows + each - 1) / each;
+        *slices = (int)(n < most ? n : most);
+        return cudaSuccess;
     }
     const int64_t strips = (a.cols + 31) / 32, most = (a.rows + 63) / 64;
     int64_t n = (4 * (int64_t)sm_count + strips - 1) / strips;
     n = n < most ? n : most;
-    return (int)(n < 1 ? 1 : n);
+    *slices = (int)(n < 1 ? 1 : n);
+    return cudaSuccess;
 }
 
 // So few rows for each warp of a CTA are summed by strips (33 rows of 896, four warps: 3.1 us on the GPU and 4.3 a call, against
@@ -1157,9 +1171,10 @@ cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int 
         if (sums && a.rows <= kFewRows * (int64_t)(l.shape.block() / 32)) {
             const int strips = (int)((a.cols + 31) / 32);
             const bool over = a.dx == a.x || a.dx == a.dy;       // (then the strips have to be done before dx is written)
-            const unsigned ctas = (unsigned)l.grid(a.rows, sm_count);
-            e = launch(a.dx && !over ? ctas : 0u, nullptr, strips);
-            return e == cudaSuccess && a.dx && over ? launch(ctas, nullptr, 0) : e;
+            int64_t ctas = 0;
+            e = l.grid(a.rows, sm_count, &ctas);
+            if (e == cudaSuccess) e = launch(a.dx && !over ? (unsigned)ctas : 0u, nullptr, strips);
+            return e == cudaSuccess && a.dx && over ? launch((unsigned)ctas, nullptr, 0) : e;
         }
         e = launch((unsigned)slices, part, 0);
     } else if (a.dtype == GG_F32 && a.w_dtype == GG_F32) {
