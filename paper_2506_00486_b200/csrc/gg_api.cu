@@ -586,10 +586,13 @@ gg_status gg_create(gg_ctx **out, int device)
         cudaError_t se = guard.ok ? cudaMalloc(reinterpret_cast<void **>(&ctx->seed), sizeof(double) * 2 * (kSeedCells + 1))
                                   : cudaErrorInvalidDevice;
         if (se == cudaSuccess) se = launch_fit_seed_table(ctx->seed, nullptr);
+        if (se == cudaSuccess) se = cudaMalloc(reinterpret_cast<void **>(&ctx->norm_ticket), sizeof(uint32_t));
+        if (se == cudaSuccess) se = cudaMemsetAsync(ctx->norm_ticket, 0, sizeof(uint32_t), nullptr);
         if (se == cudaSuccess) se = cudaStreamSynchronize(nullptr);
         if (se != cudaSuccess) {
             cudaGetLastError();
             if (ctx->seed) cudaFree(ctx->seed);
+            if (ctx->norm_ticket) cudaFree(ctx->norm_ticket);
             delete ctx;
             return se == cudaErrorMemoryAllocation ? GG_ERR_NOMEM : GG_ERR_CUDA;
         }
@@ -1654,10 +1657,6 @@ gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dty
         st = get_plan(ctx, g, n_seg, dtype, nullptr, 0, nullptr, &p, stream);
         if (st != GG_OK) return st;
         if (p->n_tiles > 0 && p->n_tiles <= kNormTiles) {
-            if (!ctx->norm_ticket) {
-                GG_CUDA(ctx, cudaMalloc(reinterpret_cast<void **>(&ctx->norm_ticket), sizeof(uint32_t)));
-                GG_CUDA(ctx, cudaMemset(ctx->norm_ticket, 0, sizeof(uint32_t)));
-            }
             GG_CUDA(ctx, launch_grad_norm_small(p->map, dtype, p->part.s2, p->part.bad, ctx->norm_ticket, max_norm, norm, scale, cs));
             ctx->launches += 1;
             mark_used(p, cs);

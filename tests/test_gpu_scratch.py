@@ -1,0 +1,62 @@
+"""Scratch of a context whose first use is on another stream or inside a stream capture."""
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture
+def ctx():
+    import __graft_entry__ as entry
+    entry.build()
+    from paper_2506_00486_b200 import Context
+    c = Context(0, guard=True)
+    yield c
+    c.check_guards()
+    c.close()
+
+
+def gradients(lens, seed=1):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    return [torch.randn(n, generator=gen, device="cuda") for n in lens]
+
+
+def norm_of(g):
+    return float(sum(t.double().square().sum() for t in g).sqrt())
+
+
+def test_the_first_gradient_norm_on_another_stream_behind_a_busy_default_stream(ctx):
+    g = gradients([5, 20000, 70001])
+    want = norm_of(g)
+    ctx.gg_fit(g)                       # the plan is known: the norm itself uploads nothing that could wait
+    out = dict(norm=torch.full((1,), -1.0, dtype=torch.float64, device="cuda"), scale=torch.full((1,), -1.0, device="cuda"))
+    busy = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(30):
+        busy = torch.tanh(busy @ busy)
+    with torch.cuda.stream(side):
+        ctx.gg_grad_norm(g, 1.0, out)
+        first = {k: t.clone() for k, t in out.items()}
+        ctx.gg_grad_norm(g, 1.0, out)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for got in (first, out):
+        assert abs(got["norm"].item() - want) <= 1e-6 * want and abs(got["scale"].item() * want - 1.0) <= 2e-6
+
+
+def test_the_first_gradient_norm_inside_a_capture(ctx):
+    g = gradients([300, 40000])
+    ctx.gg_fit(g)
+    out = dict(norm=torch.zeros(1, dtype=torch.float64, device="cuda"), scale=torch.zeros(1, device="cuda"))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctx.gg_grad_norm(g, 1.0, out)
+    for factor in (1.0, 3.0):
+        for t in g:
+            t.mul_(factor)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = norm_of(g)
+        assert abs(out["norm"].item() - want) <= 1e-6 * want
