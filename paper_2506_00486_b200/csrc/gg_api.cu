@@ -341,6 +341,9 @@ gg_status get_plan(gg_ctx *ctx, const gg_seg *segs, int32_t n_seg, int in_dtype,
     cudaError_t e = cudaMemcpy(p->dev, host.data(), table_bytes, cudaMemcpyHostToDevice);
     if (e == cudaSuccess && !groups.empty())
         e = cudaMemcpy(static_cast<char *>(p->dev) + o_grp, groups.data(), sizeof(int4) * groups.size(), cudaMemcpyHostToDevice);
+    // (a copy from pageable memory may return before its data has arrived, and a stream that does not wait for the legacy
+    // one could read the tables too early)
+    if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);
     if (e != cudaSuccess) { cudaFree(p->dev); return cuda_fail(ctx, e); }
     char *d = static_cast<char *>(p->dev);
     p->o_ptr = o_ptr; p->o_gptr = o_gptr;
@@ -437,6 +440,7 @@ gg_status ensure_entropy_scratch(gg_ctx *ctx, int32_t n_hist)
         GG_CUDA(ctx, cudaMalloc(reinterpret_cast<void **>(&ctx->ent_part), sizeof(double) * 2 * kEntSplit * (size_t)n_hist));
         GG_CUDA(ctx, cudaMalloc(reinterpret_cast<void **>(&ctx->ent_done), sizeof(uint32_t) * (size_t)n_hist));
         GG_CUDA(ctx, cudaMemset(ctx->ent_done, 0, sizeof(uint32_t) * (size_t)n_hist));
+        GG_CUDA(ctx, cudaStreamSynchronize(nullptr));      // (a memset does not wait, and the caller's stream need not wait for the legacy one)
         ctx->ent_hists = n_hist;
     }
     return GG_OK;

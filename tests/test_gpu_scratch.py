@@ -60,3 +60,26 @@ def test_the_first_gradient_norm_inside_a_capture(ctx):
         torch.cuda.synchronize()
         want = norm_of(g)
         assert abs(out["norm"].item() - want) <= 1e-6 * want
+
+
+def test_the_first_fused_pass_on_another_stream_behind_a_busy_default_stream(ctx):
+    # the tables of the plan and the counters of the entropy step are set up by this very call
+    from oracle import gg_oracle as o
+    g = [t.mul_(0.02) for t in gradients([70001, 20000, 5])]
+    step = torch.full((3,), 2.0 ** -10, device="cuda")
+    grad = [torch.empty_like(t) for t in g]
+    busy = torch.randn(4096, 4096, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for _ in range(30):
+        busy = torch.tanh(busy @ busy)
+    with torch.cuda.stream(side):
+        out = ctx.gg_fused(g, grad=grad, lam=1e-4, step=step)
+    side.synchronize()
+    torch.cuda.synchronize()
+    for s, t in enumerate(g):
+        x = t.cpu().numpy()
+        beta, alpha, *_ = o.fit(x)
+        assert abs(out["beta"][s].item() - beta) <= 1e-5 * beta and abs(out["alpha"][s].item() - alpha) <= 1e-5 * alpha
+        hist, _ = o.quantise_hist(x, 2.0 ** -10)
+        assert abs(o.entropy_bits(hist) - out["entropy_bits"][s].item()) <= 1e-9
