@@ -88,7 +88,11 @@ struct gg_ctx {
     uint32_t *small_counts = nullptr;   // scratch of the short-segment kernel: one slot of count cells per CTA
     void *chan_buf = nullptr;     // scratch of gg_fused_channels (partials per row block and column)
     int64_t chan_bytes = 0;
-    void *norm_part = nullptr;    // scratch of gg_layer_norm_grad (partial sums over the rows)
+    // scratch of gg_layer_norm_grad (partial sums over the rows): the last is the one in use.  The smaller ones before it stay,
+    // because a captured graph may hold their addresses; each is at most half the next, so all of them together are less than it
+    // (and 64 are never reached).
+    void *norm_part[64] = {};
+    int norm_parts = 0;
     int64_t norm_part_bytes = 0;
     uint32_t *norm_ticket = nullptr;    // counter of gg_grad_norm's one-launch form (zero between calls)
     double *seed = nullptr;       // device table that seeds the moment-ratio inversion of the short-segment kernel
@@ -626,7 +630,7 @@ gg_status gg_destroy(gg_ctx *ctx)
     if (ctx->seed) cudaFree(ctx->seed);
     if (ctx->small_counts) cudaFree(ctx->small_counts);
     if (ctx->chan_buf) cudaFree(ctx->chan_buf);
-    if (ctx->norm_part) cudaFree(ctx->norm_part);
+    for (int i = 0; i < ctx->norm_parts; ++i) cudaFree(ctx->norm_part[i]);
     if (ctx->norm_ticket) cudaFree(ctx->norm_ticket);
     if (ctx->ent_part) cudaFree(ctx->ent_part);
     if (ctx->ent_done) cudaFree(ctx->ent_done);
@@ -1633,12 +1637,19 @@ gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *a, void
     if (!guard.ok) return GG_ERR_CUDA;
     int slices = 0;
     GG_CUDA(ctx, layer_norm_grad_slices(*a, ctx->sm_count, &slices));
-    if (a->dweight || a->dbias) {
-        st = grow(ctx, &ctx->norm_part, &ctx->norm_part_bytes, (int64_t)sizeof(float) * 2 * slices * a->cols);
-        if (st != GG_OK) return st;
+    void *part = nullptr;
+    if ((a->dweight || a->dbias) && slices > 0) {
+        const int64_t need = (int64_t)sizeof(float) * 2 * slices * a->cols;
+        if (need > ctx->norm_part_bytes) {
+            const int64_t bytes = std::max(need, 2 * ctx->norm_part_bytes);
+            GG_CUDA(ctx, cudaMalloc(&part, (size_t)bytes));
+            ctx->norm_part[ctx->norm_parts++] = part;
+            ctx->norm_part_bytes = bytes;
+        }
+        part = ctx->norm_part[ctx->norm_parts - 1];
     }
     int launches = 0;
-    GG_CUDA(ctx, launch_layer_norm_grad(*a, static_cast<float *>(ctx->norm_part), slices, ctx->sm_count, &launches, static_cast<cudaStream_t>(stream)));
+    GG_CUDA(ctx, launch_layer_norm_grad(*a, static_cast<float *>(part), slices, ctx->sm_count, &launches, static_cast<cudaStream_t>(stream)));
     ctx->launches += launches;
     return GG_OK;
 }

@@ -251,7 +251,7 @@ cudaError_t launch_grad_norm_small(const TileMap &map, int dtype, double *s2, ui
 using LayerNormArgs = gg_layer_norm_args;
 using LayerNormGradArgs = gg_layer_norm_grad_args;
 cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t st);
-// part: 2 * slices * cols floats of scratch (layer_norm_grad_slices); launches: kernels launched
+// part: 2 * slices * cols floats of scratch (layer_norm_grad_slices: 0 if the sums need none); launches: kernels launched
 cudaError_t layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count, int *slices);
 cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int slices, int sm_count, int *launches, cudaStream_t st);
 

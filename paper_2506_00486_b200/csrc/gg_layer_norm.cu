@@ -1128,9 +1128,19 @@ cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t
     return forward<uint16_t, uint16_t>(a, sm_count, st);
 }
 
+// So few rows for each warp of a CTA are summed by strips (33 rows of 896, four warps: 3.1 us on the GPU and 4.3 a call, against
+// 4.0 and 6.1 with slices; 64 rows 4.3, but 128 rows 7.1 against 5.4.  128 rows of 4096, sixteen warps: 3.8 against 6.8).
+constexpr int64_t kFewRows = 16;
+static bool by_strips(const LayerNormGradArgs &a, const RowLaunch &l)
+{
+    return l.kernel != nullptr && (a.dweight != nullptr || a.dbias != nullptr) && a.rows <= kFewRows * (int64_t)(l.shape.block() / 32);
+}
+
 cudaError_t layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count, int *slices)
 {
     const RowLaunch l = backward_launch(a, sm_count);
+    *slices = 0;
+    if (by_strips(a, l)) return cudaSuccess;
     if (l.kernel != nullptr) {
         int64_t n = 0;
         const cudaError_t e = l.grid(a.rows, sm_count, &n);
@@ -1148,10 +1158,6 @@ cudaError_t layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count, int
     return cudaSuccess;
 }
 
-// So few rows for each warp of a CTA are summed by strips (33 rows of 896, four warps: 3.1 us on the GPU and 4.3 a call, against
-// 4.0 and 6.1 with slices; 64 rows 4.3, but 128 rows 7.1 against 5.4.  128 rows of 4096, sixteen warps: 3.8 against 6.8).
-constexpr int64_t kFewRows = 16;
-
 cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int slices, int sm_count, int *launches, cudaStream_t st)
 {
     *launches = 0;
@@ -1168,7 +1174,7 @@ cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int 
             const size_t shared = strips > 0 && l.shared < 8192 ? 8192 : l.shared;
             return cudaLaunchKernel(l.kernel, dim3(ctas + (unsigned)strips), dim3(l.shape.block()), args, shared, st);
         };
-        if (sums && a.rows <= kFewRows * (int64_t)(l.shape.block() / 32)) {
+        if (by_strips(a, l)) {
             const int strips = (int)((a.cols + 31) / 32);
             const bool over = a.dx == a.x || a.dx == a.dy;       // (then the strips have to be done before dx is written)
             int64_t ctas = 0;

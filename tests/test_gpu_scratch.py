@@ -83,3 +83,49 @@ def test_the_first_fused_pass_on_another_stream_behind_a_busy_default_stream(ctx
         assert abs(out["beta"][s].item() - beta) <= 1e-5 * beta and abs(out["alpha"][s].item() - alpha) <= 1e-5 * alpha
         hist, _ = o.quantise_hist(x, 2.0 ** -10)
         assert abs(o.entropy_bits(hist) - out["entropy_bits"][s].item()) <= 1e-9
+
+
+def norm_gradient(ctx, rows, cols, seed):
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x, dy = (torch.randn((rows, cols), generator=gen, device="cuda") for _ in range(2))
+    w = 1.0 + 0.1 * torch.randn(cols, generator=gen, device="cuda")
+    out = ctx.gg_layer_norm(x, w)
+    return ctx.make_layer_norm_grad(dy, x, out["mean"], out["rstd"], w)
+
+
+def test_a_captured_gradient_outlives_a_larger_one(ctx):
+    # the larger call needs more scratch for its sums; the graph still holds the smaller scratch
+    small = norm_gradient(ctx, 2000, 64, 1)
+    want = {k: t.clone() for k, t in small().items()}
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        small()
+    large = [norm_gradient(ctx, 3000, cols, 2) for cols in (520, 1024, 4096)]
+    for run in large:
+        run()
+    # whatever the driver hands out now must not be what the graph writes to
+    other = [torch.full((1 << 18,), 3.0, device="cuda") for _ in range(64)]
+    before = [{k: t.clone() for k, t in run().items()} for run in large]
+    for t in small.outputs.values():
+        t.zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(small.outputs[k], want[k]) for k in want)
+    assert all((t == 3.0).all() for t in other)
+    for run, old in zip(large, before):
+        assert all(torch.equal(run()[k], old[k]) for k in old)
+
+
+def test_sums_over_few_rows_need_no_scratch(ctx):
+    # so the first call of a context may be a captured one
+    run = norm_gradient(ctx, 20, 896, 3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run()
+    graph.replay()
+    torch.cuda.synchronize()
+    got = {k: t.clone() for k, t in run.outputs.items()}
+    run()
+    assert all(torch.equal(run.outputs[k], got[k]) and got[k].any() for k in got)
