@@ -113,3 +113,84 @@ def test_gradient_of_wide_rows_in_large_numbers(ctx, dtype, cols, pad):
     rstd = (1.0 / torch.sqrt((xd - mean.double()[:, None]).square().mean(1) + 1e-5)).float()
     del xd
     check_grad(dy, x, mean, rstd, w, ctx.gg_layer_norm_grad(dy, x, mean, rstd, w))
+
+
+# Several rows for every warp or CTA of every form.  Vectors: rows within a warp (24, 64, 520), CTAs of 1 to 4 vectors a thread.
+# Single elements: 8, 16 and 32 a thread within a warp (200, 511, 1023) and over a CTA (1100, 2001, 5001, 9001, 16383), weight and
+# bias staged (many rows) or not.
+SHAPES = [(20000, 24), (30011, 64), (20000, 520), (6000, 896), (5000, 2048), (16384, 4096), (4001, 8192), (3001, 16384), (2400, 11008),
+          (20011, 31), (15000, 200), (9001, 255), (9001, 511), (4099, 1023), (9001, 1023), (5003, 1100), (1500, 2001), (9000, 2001),
+          (3000, 5001), (2003, 9001), (2500, 16383)]
+
+
+@pytest.mark.parametrize("dtype,w_dtype", [("float32", "float32"), ("bfloat16", "bfloat16"), ("bfloat16", "float32"), ("float32", "bfloat16")])
+@pytest.mark.parametrize("rows,cols", SHAPES)
+def test_forward_and_gradient_of_many_rows(ctx, rows, cols, dtype, w_dtype):
+    dtype, w_dtype = getattr(torch, dtype), getattr(torch, w_dtype)
+    gen = torch.Generator(device="cuda").manual_seed(rows * 7919 + cols)
+    x, dy = matrix(gen, rows, cols, dtype, mean=0.2), matrix(gen, rows, cols, dtype, scale=0.01)
+    w, b = affine(gen, cols, w_dtype)
+    out = ctx.gg_layer_norm(x, w, b)
+    check_forward(x, w, b, 1e-5, out)
+    check_grad(dy, x, out["mean"], out["rstd"], w, ctx.gg_layer_norm_grad(dy, x, out["mean"], out["rstd"], w))
+
+
+@pytest.mark.parametrize("cols", [200, 896, 1023, 2049, 4096])
+@pytest.mark.parametrize("pad,shift", [(8, 0), (1, 0), (0, 1), (3, 5)])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_strides_alignment_and_in_place_with_many_rows(ctx, cols, pad, shift, dtype):
+    dtype, rows = getattr(torch, dtype), 5003
+    gen = torch.Generator(device="cuda").manual_seed(cols + 31 * pad + shift)
+    x, dy, y, dx = (matrix(gen, rows, cols, dtype, pad, shift) for _ in range(4))
+    w, b = affine(gen, cols, dtype)
+    out = ctx.gg_layer_norm(x, w, b, out=y)
+    check_forward(x, w, b, 1e-5, out)
+    grad = ctx.gg_layer_norm_grad(dy, x, out["mean"], out["rstd"], w, dx=dx)
+    check_grad(dy, x, out["mean"], out["rstd"], w, grad)
+    if pad:      # what lies between the rows is untouched
+        for t in (y, dx):
+            gap = t.as_strided((rows - 1, pad), (cols + pad, 1), t.storage_offset() + cols)
+            assert (gap == 7.0).all()
+    # over x, over dy
+    again = matrix(gen, rows, cols, dtype, pad, shift)
+    again.copy_(x)
+    assert torch.equal(ctx.gg_layer_norm(again, w, b, out=again)["y"], y)
+    for over in ("dy", "x"):
+        g, xx = (matrix(gen, rows, cols, dtype, pad, shift) for _ in range(2))
+        g.copy_(dy)
+        xx.copy_(x)
+        got = ctx.gg_layer_norm_grad(g, xx, out["mean"], out["rstd"], w, dx=g if over == "dy" else xx)
+        assert all(torch.equal(got[k], grad[k]) for k in grad), over
+
+
+@pytest.mark.parametrize("rows,cols", [(3000, 1023), (3000, 1024), (2500, 5001)])
+def test_sums_alone_accumulation_and_one_vector_with_many_rows(ctx, rows, cols):
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    x, dy = matrix(gen, rows, cols, torch.float32), matrix(gen, rows, cols, torch.float32)
+    w, b = affine(gen, cols, torch.float32)
+    for ww, bb in ((None, None), (w, None), (None, b)):
+        out = ctx.gg_layer_norm(x, ww, bb)
+        check_forward(x, ww, bb, 1e-5, out)
+    mean, rstd = out["mean"], out["rstd"]
+    check_grad(dy, x, mean, rstd, None, ctx.gg_layer_norm_grad(dy, x, mean, rstd, None))
+    check_grad(dy, x, mean, rstd, w, ctx.gg_layer_norm_grad(dy, x, mean, rstd, w, want_dx=False))
+    dw, db = (torch.randn(cols, generator=gen, device="cuda") for _ in range(2))
+    base = dw.double(), db.double()
+    got = ctx.gg_layer_norm_grad(dy, x, mean, rstd, w, dweight=dw, dbias=db, accumulate=True)
+    check_grad(dy, x, mean, rstd, w, got, base)
+
+
+@pytest.mark.parametrize("cols", [1000, 1023, 5001])
+def test_infinities_and_nan_stay_in_their_row_among_many(ctx, cols):
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    rows = 4000
+    x = matrix(gen, rows, cols, torch.float32)
+    w, b = affine(gen, cols, torch.float32)
+    clean = {k: t.clone() for k, t in ctx.gg_layer_norm(x, w, b).items()}
+    bad = torch.arange(7, rows, 97, device="cuda")
+    x[bad, torch.randint(cols, bad.shape, generator=gen, device="cuda")] = float("inf")
+    x[bad[::2], 0] = float("nan")
+    out = ctx.gg_layer_norm(x, w, b)
+    good = torch.ones(rows, dtype=torch.bool, device="cuda")
+    good[bad] = False
+    assert torch.isnan(out["y"][bad]).all() and all(torch.equal(out[k][good], clean[k][good]) for k in clean)
