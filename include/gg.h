@@ -418,7 +418,7 @@ gg_status gg_test_hook(gg_ctx *ctx, int32_t what, int64_t value);
 
 /* Bounds-checking build (no counterpart in the paper: a debugging aid that stands in for a memory checker).  A
  * library built with -DGG_BOUNDS (paper_2506_00486_b200/build.py --bounds) tests the index of every checked global
- * load and store of its streaming kernels against the extent of the segment or buffer it belongs to, counts the
+ * load and store of its streaming, layer norm and AdamW kernels against the extent of the segment, row or buffer it belongs to, counts the
  * ones that would have left it and skips them; nothing traps.  Returns the number of such accesses since the library
  * was loaded (after waiting for the device), or -1 from a normal build, which has no checks. */
 int64_t gg_debug_bounds_violations(void);

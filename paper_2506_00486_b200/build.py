@@ -29,7 +29,7 @@ def _stale(target, sources):
 
 def build(force=False, verbose=False, ptxas_info=False, bounds=False):
     """Builds the library.  bounds=True builds libgg_b200_bounds.so instead: the same sources with -DGG_BOUNDS, whose
-    streaming kernels count (and skip) every checked global access that would leave its buffer; run the GPU tests
+    streaming, layer norm and AdamW kernels count (and skip) every checked global access that would leave its buffer; run the GPU tests
     on it with GG_B200_LIB pointing at it."""
     build_dir = BUILD + ("_bounds" if bounds else "")
     lib = LIB.replace(".so", "_bounds.so") if bounds else LIB

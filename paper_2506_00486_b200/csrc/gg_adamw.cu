@@ -145,6 +145,9 @@ struct Place {
     uint16_t *copy;            // or null
     uint64_t block;            // of the tensor
     uint32_t id;
+#ifdef GG_BOUNDS
+    int64_t len;               // of the tensor
+#endif
 
     __device__ __forceinline__ void shift(int elements)
     {
@@ -187,7 +190,7 @@ __device__ __noinline__ float2 step_block_any(Place<TW, TG, kNarrow> at, int n, 
     for (int k = 0; k < kPerLane; ++k) {
         const int e = 32 * k + lane;
         mm[k] = rr[k] = 0.0f;
-        if (e >= n) continue;
+        if (e >= n || !GG_IN_BOUNDS((int64_t)at.block * kBlock + e, at.len)) continue;
         const float wf = widen<TW>(at.w[e]), gf = __fmul_rn(widen<TG>(at.g[e]), gscale);
         Element x;
         if constexpr (kNarrow) {
@@ -212,7 +215,7 @@ __device__ __noinline__ float2 step_block_any(Place<TW, TG, kNarrow> at, int n, 
 #pragma unroll
         for (int k = 0; k < kPerLane; ++k) {
             const int e = 32 * k + lane;
-            if (e >= n) continue;
+            if (e >= n || !GG_IN_BOUNDS((int64_t)at.block * kBlock + e, at.len)) continue;
             at.m[e] = e4m3_stochastic(mm[k], inv.x, u[e], false);
             at.v[e] = e4m3_stochastic(rr[k], inv.y, u[(e & ~7) + ((e + 4) & 7)], true);
         }
@@ -234,6 +237,7 @@ struct Operands {
     // the block `ahead` elements on, n elements of it
     static __device__ __forceinline__ void fetch(uint32_t slot, int lane, const Place<TW, TG, kNarrow> &at, int ahead, int n)
     {
+        if (n > 0 && !GG_IN_BOUNDS((int64_t)at.block * kBlock + ahead + min(n, kBlock) - 1, at.len)) return;
         if (n >= kBlock) fetch_from(slot, lane, at.g + ahead, at.w + ahead, at.m + ahead, at.v + ahead, kBlock);
         else if (n > 0) fetch_some(slot, lane, at.g + ahead, at.w + ahead, at.m + ahead, at.v + ahead, n);
     }
@@ -336,7 +340,7 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, false> &x, const P
         x.v.v[i] = pair(a.v, b.v);
     }
     const int mine = n - 8 * (int)(threadIdx.x & 31);
-    if (mine <= 0) return scale;
+    if (mine <= 0 || !GG_IN_BOUNDS((int64_t)at.block * kBlock + min(8 * (int)(threadIdx.x & 31) + 8, kRagged ? n : kBlock) - 1, at.len)) return scale;
     uint32_t out[4] = {0u, 0u, 0u, 0u};
     if constexpr (sizeof(TW) == 2) {
         const Block4 q = at.noise(c, threadIdx.x & 31);
@@ -474,7 +478,7 @@ __device__ __forceinline__ float2 step_eight(Operands<TW, TG, true> &x, const Pl
                 if ((vc[h] >> 8 * i & 0xFFu) == 0u && r[i] > kZeroRoot) vc[h] |= 1u << 8 * i;
         }
     }
-    if (8 * (int)(threadIdx.x & 31) >= n) return scale;
+    if (8 * (int)(threadIdx.x & 31) >= n || !GG_IN_BOUNDS((int64_t)at.block * kBlock + min(8 * (int)(threadIdx.x & 31) + 8, kRagged ? n : kBlock) - 1, at.len)) return scale;
     if constexpr (!kRagged) {
         Eight<uint8_t>::store(at.m, mc[0], mc[1]);
         Eight<uint8_t>::store(at.v, vc[0], vc[1]);
@@ -518,6 +522,9 @@ __global__ void __launch_bounds__(kThreads, 4) adamw_kernel(const __grid_constan
     Place<TW, TG, kNarrow> at;
     at.block = ((uint64_t)(blockIdx.x - tab.tile0[s]) * kStepWarps + warp) * (uint32_t)tab.per_warp;
     at.id = (uint32_t)(id & ~kAligned);
+#ifdef GG_BOUNDS
+    at.len = entry.len;
+#endif
     const int64_t first = (int64_t)at.block * kBlock;
     int left = (int)min((int64_t)tab.per_warp * kBlock, entry.len - first);      // elements of this warp
     if (left <= 0) return;

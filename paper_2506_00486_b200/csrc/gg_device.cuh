@@ -56,8 +56,17 @@ __device__ __forceinline__ bool gg_in_bounds(long long i, long long n)
     return false;
 }
 #define GG_IN_BOUNDS(i, n) gg_in_bounds((long long)(i), (long long)(n))
+// true if the n elements from p on lie in one row of a matrix at `base`; else counts the violation
+template <typename T>
+__device__ __forceinline__ bool gg_in_matrix(const T *p, long long n, const void *base, long long rows, long long cols, long long ld)
+{
+    const long long off = p - static_cast<const T *>(base);
+    return gg_in_bounds(off, rows * ld) && gg_in_bounds(off % ld + n - 1, cols);
+}
+#define GG_IN_MATRIX(p, n, base, rows, cols, ld) gg_in_matrix(p, n, base, rows, cols, ld)
 #else
 #define GG_IN_BOUNDS(i, n) true
+#define GG_IN_MATRIX(p, n, base, rows, cols, ld) true
 #endif
 
 // ---- gradient of lambda * R, R the mean k-th order Exponential-Golomb code length of the quantised symbols (Eq. 6-7),

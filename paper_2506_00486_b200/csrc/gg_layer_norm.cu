@@ -162,12 +162,12 @@ struct Rows {
     }
     __device__ __forceinline__ bool has(int k) const { return kWhole || (k * threads + tid) * kVec < cols; }
     __device__ __forceinline__ int column(int k) const { return (k * threads + tid) * kVec; }
-    // row: where this thread's first vector of it is
-    __device__ __forceinline__ void fetch(uint32_t slot, int operand, const T *row) const
+    // row: where this thread's first vector of it is, in the matrix at `base`
+    __device__ __forceinline__ void fetch(uint32_t slot, int operand, const T *row, const void *base, int64_t n_rows, int64_t ld) const
     {
 #pragma unroll
         for (int k = 0; k < kNum; ++k)
-            if (has(k)) copy16(slot + (operand * kNum + k) * step, row + k * threads * kVec);
+            if (has(k) && GG_IN_MATRIX(row + k * threads * kVec, kVec, base, n_rows, cols, ld)) copy16(slot + (operand * kNum + k) * step, row + k * threads * kVec);
     }
     __device__ __forceinline__ void read(uint32_t slot, int operand, Few<T> (&v)[kNum]) const
     {
@@ -197,6 +197,7 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(con
     if constexpr (kKnown == kKept)
 #pragma unroll
         for (int k = 0; k < kNum; ++k) {
+            if (!GG_IN_BOUNDS(rows.column(k) + rows.kVec - 1, a.cols)) continue;
             kept_w[k].read(weight + rows.column(k));
             kept_b[k].read(bias + rows.column(k));
         }
@@ -208,13 +209,13 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(con
     }
     int64_t r_ahead = rows.first;
     for (int d = 0; d < kDepth - 1; ++d) {
-        if (r_ahead < a.rows) rows.fetch(rows.base + d * rows.stage_bytes, 0, x_ahead);
+        if (r_ahead < a.rows) rows.fetch(rows.base + d * rows.stage_bytes, 0, x_ahead, a.x, a.rows, a.x_ld);
         copies_commit();
         x_ahead += x_step;
         r_ahead += rows.stride;
     }
     for (int64_t r = rows.first; rows.more(r, a.rows); r += rows.stride) {
-        if (r_ahead < a.rows) rows.fetch(rows.before(slot), 0, x_ahead);
+        if (r_ahead < a.rows) rows.fetch(rows.before(slot), 0, x_ahead, a.x, a.rows, a.x_ld);
         copies_commit();
         x_ahead += x_step;
         r_ahead += rows.stride;
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(con
                     if constexpr (kKnown == kKept) {
 #pragma unroll
                         for (int i = 0; i < kPairs; ++i) x[k][i] = fma2(x[k][i], kept_w[k].get(i), kept_b[k].get(i));
-                    } else if (weight && bias) {
+                    } else if (weight && bias && GG_IN_BOUNDS(c + rows.kVec - 1, a.cols)) {
                         f32x2 w[kPairs], b[kPairs];
                         read_vector(weight + c, w);
                         read_vector(bias + c, b);
@@ -273,9 +274,9 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_kernel(con
 #pragma unroll
                         for (int i = 0; i < kPairs; ++i) x[k][i] = weight ? mul2(x[k][i], o[i]) : add2(x[k][i], o[i]);
                     }
-                    Few<T>::store(y + k * threads * rows.kVec, x[k]);
+                    if (GG_IN_MATRIX(y + k * threads * rows.kVec, rows.kVec, a.y, a.rows, a.cols, a.y_ld)) Few<T>::store(y + k * threads * rows.kVec, x[k]);
                 }
-            if (rows.tid == 0) {
+            if (rows.tid == 0 && GG_IN_BOUNDS(r, a.rows)) {
                 if (a.mean) a.mean[r] = mean;
                 if (a.rstd) a.rstd[r] = rstd;
             }
@@ -320,8 +321,8 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
     int64_t r_ahead = rows.first;
     for (int d = 0; d < kDepth - 1; ++d) {
         if (r_ahead < a.rows) {
-            rows.fetch(rows.base + d * rows.stage_bytes, 0, dy_ahead);
-            rows.fetch(rows.base + d * rows.stage_bytes, 1, x_ahead);
+            rows.fetch(rows.base + d * rows.stage_bytes, 0, dy_ahead, a.dy, a.rows, a.dy_ld);
+            rows.fetch(rows.base + d * rows.stage_bytes, 1, x_ahead, a.x, a.rows, a.x_ld);
         }
         copies_commit();
         x_ahead += x_step;
@@ -337,8 +338,8 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
     for (int64_t r = rows.first; rows.more(r, a.rows); r += rows.stride) {
         if (r_ahead < a.rows) {
             const uint32_t to = rows.before(slot);
-            rows.fetch(to, 0, dy_ahead);
-            rows.fetch(to, 1, x_ahead);
+            rows.fetch(to, 0, dy_ahead, a.dy, a.rows, a.dy_ld);
+            rows.fetch(to, 1, x_ahead, a.x, a.rows, a.x_ld);
         }
         copies_commit();
         x_ahead += x_step;
@@ -370,7 +371,7 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
             }
         };
         auto weigh = [&](int k, f32x2 (&g)[kPairs]) {
-            if (weight) {
+            if (weight && GG_IN_BOUNDS(rows.column(k) + rows.kVec - 1, a.cols)) {
                 f32x2 w[kPairs];
                 read_vector(weight + rows.column(k), w);
 #pragma unroll
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
                     }
 #pragma unroll
                     for (int i = 0; i < kPairs; ++i) d[k][i] = fma2(xhat[k][i], c2, fma2(d[k][i], by, c1));
-                    Few<T>::store(dx + k * threads * rows.kVec, d[k]);
+                    if (GG_IN_MATRIX(dx + k * threads * rows.kVec, rows.kVec, a.dx, a.rows, a.cols, a.dx_ld)) Few<T>::store(dx + k * threads * rows.kVec, d[k]);
                 }
         }
         dx += dx_step;
@@ -456,6 +457,7 @@ __global__ void __launch_bounds__(kMostThreads<kNum>) layer_norm_rows_grad_kerne
 #pragma unroll
             for (int i = 0; i < kPairs; i += 2) {
                 const f32x2 w[2] = {dw[k][i], dw[k][i + 1]}, b[2] = {db[k][i], db[k][i + 1]};
+                if (!GG_IN_BOUNDS(blockIdx.x, row_ctas) || !GG_IN_BOUNDS(rows.column(k) + 2 * i + 3, cols)) continue;
                 Few<float>::store(out_w + rows.column(k) + 2 * i, w);
                 Few<float>::store(out_b + rows.column(k) + 2 * i, b);
             }
@@ -520,7 +522,8 @@ struct Pieces {
         const int pieces = (int)((uint32_t)(end - origin + 15u) / 16u);
         slot += 16u * tid;
         if (origin >= from && origin + 16u * (uint32_t)pieces <= to) {
-            for (int i = tid; i < pieces; i += threads, p += 16 * threads, slot += 16u * threads) copy16(slot, p);
+            for (int i = tid; i < pieces; i += threads, p += 16 * threads, slot += 16u * threads)
+                if (GG_IN_BOUNDS(reinterpret_cast<uintptr_t>(p) - from, to - from - 15)) copy16(slot, p);
             return;
         }
         for (int i = tid; i < pieces; i += threads, p += 16 * threads, slot += 16u * threads) {
@@ -643,14 +646,14 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 6 : 1) 
             const float2 o = halves(mul2(v[j], by));
             if (n > 0) {
                 const float2 w = kStaged ? affine[64 * j] : from_l1(64 * j);
-                y[64 * j] = narrow<T>(fmaf(o.x, w.x, w.y));
+                if (GG_IN_MATRIX(y + 64 * j, 1, a.y, a.rows, a.cols, a.y_ld)) y[64 * j] = narrow<T>(fmaf(o.x, w.x, w.y));
             }
             if (n > 1) {
                 const float2 w = kStaged ? affine[64 * j + 32] : from_l1(64 * j + 32);
-                y[64 * j + 32] = narrow<T>(fmaf(o.y, w.x, w.y));
+                if (GG_IN_MATRIX(y + 64 * j + 32, 1, a.y, a.rows, a.cols, a.y_ld)) y[64 * j + 32] = narrow<T>(fmaf(o.y, w.x, w.y));
             }
         });
-        if (rows.tid == 0) {
+        if (rows.tid == 0 && GG_IN_BOUNDS(r, a.rows)) {
             if (a.mean) a.mean[r] = mean;
             if (a.rstd) a.rstd[r] = rstd;
         }
@@ -734,8 +737,8 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) 
                 f32x2 g, xhat;
                 load(j, n, g, xhat);
                 const float2 o = halves(fma2(xhat, c2, fma2(weigh(j, n, g), by, c1)));
-                if (n > 0) dx[64 * j] = narrow<T>(o.x);
-                if (n > 1) dx[64 * j + 32] = narrow<T>(o.y);
+                if (n > 0 && GG_IN_MATRIX(dx + 64 * j, 1, a.dx, a.rows, a.cols, a.dx_ld)) dx[64 * j] = narrow<T>(o.x);
+                if (n > 1 && GG_IN_MATRIX(dx + 64 * j + 32, 1, a.dx, a.rows, a.cols, a.dx_ld)) dx[64 * j + 32] = narrow<T>(o.y);
             });
         }
         x += x_step;
@@ -771,6 +774,7 @@ __global__ void __launch_bounds__(kSolo ? kSoloWarps * 32 : 512, kSolo ? 4 : 1) 
         return;
     }
     rows.each([&](auto j, auto n) {
+        if (n > 0 && (!GG_IN_BOUNDS(blockIdx.x, row_ctas) || !GG_IN_BOUNDS(rows.column + 64 * j + (n > 1 ? 32 : 0), cols))) return;
         add(out_w + rows.column + 64 * j, dw[j], n, false);
         add(out_b + rows.column + 64 * j, db[j], n, false);
     });
