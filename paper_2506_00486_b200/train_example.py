@@ -11,26 +11,36 @@ weights with 32- or 8-bit states (gg_grad_norm, gg_adamw_step).
 import argparse
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from paper_2506_00486_b200 import Context, Segments, gg_init_alpha
 
 
 class LayerNorm(torch.autograd.Function):
-    """Layer norm over the last dimension for autograd: y = weight * xhat + bias."""
+    """Layer norm over the last dimension for autograd: y = weight * xhat + bias, each of the two may be None.
+
+    LayerNorm.apply(x, weight, bias, ctx, eps=1e-5).  Its gradient is that of the first order: it cannot be differentiated again.
+    Every call allocates its outputs; a loop over fixed buffers is faster with Context.make_layer_norm and make_layer_norm_grad."""
 
     @staticmethod
-    def forward(fctx, x, weight, bias, ctx):
+    def forward(fctx, x, weight, bias, ctx, eps=1e-5):
         rows = x.reshape(-1, x.shape[-1])
-        out = ctx.gg_layer_norm(rows, weight, bias)
+        if rows.stride(1) != 1 or rows.stride(0) < rows.shape[1]:      # strided columns, rows that overlap
+            rows = rows.contiguous()
+        out = ctx.gg_layer_norm(rows, weight, bias, eps=eps)
         fctx.save_for_backward(rows, weight, out["mean"], out["rstd"])
-        fctx.ctx = ctx
+        fctx.ctx, fctx.bias_dtype = ctx, None if bias is None else bias.dtype
         return out["y"].view(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(fctx, dy):
         rows, weight, mean, rstd = fctx.saved_tensors
-        out = fctx.ctx.gg_layer_norm_grad(dy.reshape(rows.shape).contiguous(), rows, mean, rstd, weight)
-        return out["dx"].view(dy.shape), out["dweight"].to(weight.dtype), out["dbias"].to(weight.dtype), None
+        want_dx, want_dweight, want_dbias = fctx.needs_input_grad[:3]
+        out = fctx.ctx.gg_layer_norm_grad(dy.reshape(rows.shape).contiguous(), rows, mean, rstd, weight, want_dx=want_dx,
+                                          want_dweight=want_dweight or want_dbias)
+        return (out["dx"].view(dy.shape) if want_dx else None, out["dweight"].to(weight.dtype) if want_dweight else None,
+                out["dbias"].to(fctx.bias_dtype) if want_dbias else None, None, None)
 
 
 class Mlp:
