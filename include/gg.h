@@ -296,7 +296,9 @@ gg_status gg_gct_step(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype g_dt
  *     y = weight * (x - mean) * rstd + bias,   rstd = 1 / sqrt(mean of (x - mean)^2 + eps)
  * with mean and rstd those of the row.  Element (r, c) of x lies at x[r * x_ld + c], that of y at
  * y[r * y_ld + c]; sums are taken in 32 bits or more and y is rounded once.  y may be x (the same address
- * and ld).  A row that holds an inf or a nan becomes nan; no other row does. */
+ * and ld).  A row that holds an inf or a nan becomes nan.  So may a row of finite elements whose sum passes the
+ * largest fp32 number (3.4e38); one whose sum of (x - mean)^2 does has rstd = 0 and y = bias.  No other row is affected.
+ * Without rows or columns nothing is written. */
 typedef struct {
     const void *x;               /* device, `dtype`                                           */
     int64_t     rows, cols, x_ld;/* ld >= cols, in elements                                   */
@@ -349,7 +351,8 @@ gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dty
  * in fp32 arithmetic whatever the types (a v below 2^-126 counts as 0).  A grad_scale that is inf or nan (as gg_grad_norm writes it for a
  * gradient that overflowed) makes the step a no-op: nothing is written.  Without it an inf or nan in g reaches its own
  * element's w, m and v and no other.  Needs no plan: tables travel with the launch, so addresses may differ from step
- * to step, and nothing is allocated.
+ * to step, and nothing is allocated.  A tensor whose arrays start at multiples of 8 elements' size (32 bytes for fp32, 16 for
+ * bf16, 8 for codes) is stepped by vectors, any other element by element (3 to 10 times slower).
  * Types: w fp32 or bf16, g fp32 or bf16, m and v fp32 (state_bits 32) or 8 bits (state_bits 8).  bf16 weights are
  * rounded stochastically: a step is mostly smaller than their spacing, and rounding to nearest would lose it.
  * 8-bit states: m and sqrt(v) as e4m3 codes (1 byte an element), each block of GG_ADAMW_BLOCK elements of a tensor,
@@ -357,9 +360,10 @@ gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dty
  * another, ceil(len / GG_ADAMW_BLOCK) for each in the order of the list.  The step updates w from m and v before they
  * are rounded; the codes are then rounded stochastically (sqrt(v) above 2^-62 never to 0).  A block of which the
  * largest |m| is below 2^-110, or the largest sqrt(v) below 2^-62, is stored as zeros.  Zeroed codes and scales are
- * the state before the first step.
- * The noise of the rounding is Philox4x32-10 at counter (j, j div 2^32, t, segment index) and key `seed`, 128 bits for
- * elements 8j .. 8j+7 of a segment: the same call gives the same bits. */
+ * the state before the first step.  With 8-bit states 2^-126 is added to v before its root, which shows below
+ * sqrt(v) = 2^-51 (4e-16; 2^-63 stands for 0): eps should be well above that.
+ * The noise of the rounding is Philox4x32-10 at counter (j mod 2^32, j div 2^32, t mod 2^32, segment index) and key
+ * `seed`, 128 bits for elements 8j .. 8j+7 of a segment: the same call gives the same bits. */
 #define GG_ADAMW_BLOCK 256
 typedef struct {
     int32_t       n_seg;

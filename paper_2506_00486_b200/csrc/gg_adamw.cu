@@ -225,7 +225,7 @@ __device__ __noinline__ float2 step_block_any(Place<TW, TG, kNarrow> at, int n, 
 
 // Blocks at vector boundaries: lane l takes the eight elements from 8 l on, in pairs.  Beyond the end of a tensor's last block
 // it computes on zeros and stores nothing.  kRagged: the end is within the eight elements of a lane, and every
-// lane stores one by one.  (A case of its own: within the other it takes 1.12 against 1.04 ms for a decoder with 8-bit
+// lane stores one by one (it is one block of a tensor at most).  (A case of its own: within the other it takes 1.12 against 1.04 ms for a decoder with 8-bit
 // states and bf16 weights.)
 template <typename TW, typename TG, bool kNarrow>
 struct Operands {
@@ -384,8 +384,8 @@ __device__ __forceinline__ float max3(float a, float b, float c)
 // sqrt of finite values >= 0 by one Newton step from an approximate reciprocal root y: g = v y, g + (v - g^2) y / 2, the
 // remainder v - g^2 exact.  That leaves the rounding of the last sum (and, once in about a million, the neighbour of the
 // nearest value; with g (1/2 - g y / 2) for the step, half of the rounding of g stays, one value in ten).  2^-126 is
-// added to v, so that y is finite: it changes no v above 2^-102, and the step divides by the root plus eps, so nothing
-// below that matters.  The root of 0 comes out as 2^-63, and roots up to kZeroRoot count as 0.
+// added to v, so that y is finite: it changes no v above 2^-102, and the step divides by the root plus eps, beside which
+// nothing below that shows (unless eps is below 2^-51 too).  The root of 0 comes out as 2^-63, and roots up to kZeroRoot count as 0.
 __device__ __forceinline__ f32x2 sqrt2(f32x2 v)
 {
     v = add2(v, both(0x1p-126f));

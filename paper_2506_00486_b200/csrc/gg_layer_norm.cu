@@ -4,7 +4,7 @@
 //     d = w dy:  dx = rstd (d - sum(d) / n - xhat sum(d xhat) / n),  dw = sum over rows of dy xhat,  db = sum over rows of dy
 //
 // n is the row length.  The variance is that of the differences from the mean (two passes over the row), so a large
-// mean costs no digits.  Both directions are bound by memory: the forward pass has to read x and write y once, the
+// mean costs it no digits beyond those of the mean itself, which is an fp32 sum.  Both directions are bound by memory: the forward pass has to read x and write y once, the
 // gradient has to read x and dy and write dx once.
 #include "gg_device.cuh"
 #include "gg_element.cuh"

@@ -194,3 +194,21 @@ def test_infinities_and_nan_stay_in_their_row_among_many(ctx, cols):
     good = torch.ones(rows, dtype=torch.bool, device="cuda")
     good[bad] = False
     assert torch.isnan(out["y"][bad]).all() and all(torch.equal(out[k][good], clean[k][good]) for k in clean)
+
+
+@pytest.mark.parametrize("cols", [64, 1000, 1023, 4096])
+def test_rows_of_very_large_and_very_small_elements(ctx, cols):
+    # squares from 1e-30 to 1e34: sums of both are normal fp32 numbers.  A row beyond that range changes nothing but itself
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    rows = 3000
+    x = matrix(gen, rows, cols, torch.float32)
+    x.mul_((10.0 ** (-15.0 + 32.0 * torch.rand((rows, 1), generator=gen, device="cuda", dtype=torch.float64))).float())
+    w, b = affine(gen, cols, torch.float32)
+    clean = {k: t.clone() for k, t in ctx.gg_layer_norm(x, w, b, eps=0.0).items()}
+    check_forward(x, w, b, 0.0, clean)
+    x[5::50] = 1e25 * torch.randn((60, cols), generator=gen, device="cuda")
+    out = ctx.gg_layer_norm(x, w, b, eps=0.0)
+    huge = torch.zeros(rows, dtype=torch.bool, device="cuda")
+    huge[5::50] = True
+    assert all(torch.equal(out[k][~huge], clean[k][~huge]) for k in clean)
+    assert not out["rstd"][huge].any() and torch.equal(out["y"][huge], b.expand(60, cols))
