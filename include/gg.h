@@ -28,7 +28,8 @@
  *    pinned memory, ordered on `stream`, no allocation and no wait for the device (also outside
  *    stream capture: a replayed upload would carry the addresses of capture time).  Only a new
  *    layout in a full context frees the oldest plan, after waiting for the work last enqueued
- *    with it (an event; the whole device if that work was captured in a graph); and a call that
+ *    with it (an event).  A plan that a captured call used stays as it is until gg_destroy, and
+ *    counts toward neither limit: the graph holds its tables.  And a call that
  *    needs more histogram or channel scratch than any before it reallocates that scratch after
  *    waiting for the device.  A context serves one stream at a time.
  *  - A segment is a contiguous run of `len` elements.  Pointers need only element alignment;

@@ -65,6 +65,7 @@ struct Plan {
     uint32_t *sync = nullptr;     // [2 * n_groups]
     uint64_t last_use = 0;
     cudaEvent_t used = nullptr;   // recorded after the last work enqueued with this plan: what an eviction waits for
+    bool captured = false;        // a graph may hold its tables: never evicted, never pointed at other addresses
     // a plan whose layout fits a call with other addresses is pointed at them: the two address tables are uploaded
     // again from this pinned staging block, in stream order
     size_t o_ptr = 0, o_gptr = 0;
@@ -232,6 +233,14 @@ gg_status repoint(gg_ctx *ctx, Plan *p, const gg_seg *segs, const gg_seg *grad, 
     return GG_OK;
 }
 
+// Plans that no captured graph holds: those the limits count.
+int open_plans(const gg_ctx *ctx)
+{
+    int n = 0;
+    for (auto &p : ctx->plans) n += !p->captured;
+    return n;
+}
+
 // Finds or builds the plan for this layout.  Building allocates and uploads with blocking calls; a layout that
 // already has kMaxPlansPerLayout plans (or any plan, once the cache is full) gets its least recently used plan
 // pointed at the new addresses instead, which neither allocates nor blocks.
@@ -248,24 +257,23 @@ gg_status get_plan(gg_ctx *ctx, const gg_seg *segs, int32_t n_seg, int in_dtype,
         Plan *lru = nullptr;
         int same = 0;
         for (auto &q : ctx->plans)
-            if (same_layout(*q, head, segs, n_seg, hist_id)) {
+            if (!q->captured && same_layout(*q, head, segs, n_seg, hist_id)) {
                 ++same;
                 if (lru == nullptr || q->last_use < lru->last_use) lru = q.get();
             }
-        if (lru != nullptr && (same >= kMaxPlansPerLayout || (int)ctx->plans.size() >= kMaxPlans)) {
+        if (lru != nullptr && (same >= kMaxPlansPerLayout || open_plans(ctx) >= kMaxPlans)) {
             gg_status st = repoint(ctx, lru, segs, grad, static_cast<cudaStream_t>(stream));
             if (st != GG_OK) return st;
             *out = lru;
             return GG_OK;
         }
     }
-    if ((int)ctx->plans.size() >= kMaxPlans) {
-        // Evict the least recently used plan.  Work that still uses its tables may be in flight: wait for the event
-        // recorded after its last use (not for the whole device; an event recorded inside a stream capture cannot
-        // be waited for, and then the device is).
-        size_t victim = 0;
-        for (size_t i = 1; i < ctx->plans.size(); ++i)
-            if (ctx->plans[i]->last_use < ctx->plans[victim]->last_use) victim = i;
+    if (open_plans(ctx) >= kMaxPlans) {
+        // Evict the least recently used plan that no graph holds.  Work that still uses its tables may be in flight: wait for
+        // the event recorded after its last use (not for the whole device, unless there is no event).
+        size_t victim = ctx->plans.size();
+        for (size_t i = 0; i < ctx->plans.size(); ++i)
+            if (!ctx->plans[i]->captured && (victim == ctx->plans.size() || ctx->plans[i]->last_use < ctx->plans[victim]->last_use)) victim = i;
         Plan *v = ctx->plans[victim].get();
         if (v->used == nullptr || cudaEventSynchronize(v->used) != cudaSuccess) {
             cudaGetLastError();
@@ -382,7 +390,11 @@ gg_status get_plan(gg_ctx *ctx, const gg_seg *segs, int32_t n_seg, int in_dtype,
 // After the last launch that uses the plan's tables.
 void mark_used(Plan *p, cudaStream_t cs)
 {
-    if (p != nullptr && p->used != nullptr && cudaEventRecord(p->used, cs) != cudaSuccess) cudaGetLastError();
+    if (p == nullptr) return;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    if (cudaStreamIsCapturing(cs, &capture) != cudaSuccess) cudaGetLastError();
+    if (capture != cudaStreamCaptureStatusNone) p->captured = true;
+    else if (p->used != nullptr && cudaEventRecord(p->used, cs) != cudaSuccess) cudaGetLastError();
 }
 
 // Brackets one sweep of a fused call: an NVTX range (visible to a profiler that is attached, free otherwise) and,

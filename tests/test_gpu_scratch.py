@@ -129,3 +129,34 @@ def test_sums_over_few_rows_need_no_scratch(ctx):
     got = {k: t.clone() for k, t in run.outputs.items()}
     run()
     assert all(torch.equal(run.outputs[k], got[k]) and got[k].any() for k in got)
+
+
+def test_a_captured_call_keeps_its_plan(ctx):
+    # afterwards come enough layouts to fill the context, and one layout at more addresses than it has plans for
+    g = gradients([3000, 70001])
+    w = [torch.ones_like(t) for t in g]
+    st = ctx.adamw_state(w)
+    step = ctx.make_adamw_step(w, g, **st, max_norm=1.0, weight_decay=0.0)
+    step(1, 1e-3)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(2, 1e-3)
+    others = [gradients([100 + i, 50], seed=i) for i in range(80)] + [gradients([3000, 70001], seed=100 + i) for i in range(20)]
+    norms = [ctx.gg_grad_norm(t) for t in others]
+    for t, out in zip(others, norms):
+        assert abs(out["norm"].item() - norm_of(t)) <= 1e-6 * norm_of(t)
+    for factor in (1.0, 5.0):
+        for t in g:
+            t.mul_(factor)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = norm_of(g)
+        assert abs(step.outputs["norm"].item() - want) <= 1e-6 * want
+        assert abs(step.outputs["scale"].item() * want - 1.0) <= 2e-6
+    # the plans that no graph holds are still limited and recycled
+    built, repointed = ctx.plan_stats
+    for t in others[80:]:
+        ctx.gg_grad_norm(t)
+    again = ctx.plan_stats
+    assert again[0] == built and again[1] > repointed
