@@ -29,9 +29,10 @@
  *    stream capture: a replayed upload would carry the addresses of capture time).  Only a new
  *    layout in a full context frees the oldest plan, after waiting for the work last enqueued
  *    with it (an event).  A plan that a captured call used stays as it is until gg_destroy, and
- *    counts toward neither limit: the graph holds its tables.  And a call that
- *    needs more histogram or channel scratch than any before it reallocates that scratch after
- *    waiting for the device.  A context serves one stream at a time.
+ *    counts toward neither limit: the graph holds its tables.  And a call that needs more
+ *    histogram, channel or layer norm scratch than any before it allocates it, outside stream
+ *    capture too; what it had before stays until gg_destroy, for graphs captured earlier.  A
+ *    context serves one stream at a time.
  *  - A segment is a contiguous run of `len` elements.  Pointers need only element alignment;
  *    16-byte aligned segments take the vectorised path.  Long segments stream fastest when input
  *    and gradient sit at the same element offset from a 1 KB boundary (slices of aligned buffers
@@ -319,8 +320,7 @@ gg_status gg_layer_norm(gg_ctx *ctx, const gg_layer_norm_args *args, void *strea
  *     dweight = sum over the rows of dy * xhat,     dbias = sum over the rows of dy
  * The sums over the rows are reduced in a fixed order (no atomics): the same call gives the same bits.  dx may be
  * dy or x (the same address and ld).  The first call that needs more scratch for the sums than any before
- * allocates it (outside stream capture); what it had before stays until gg_destroy, so graphs captured earlier
- * remain valid.  Up to 32 rows of up to 16384 bf16 or 11456 fp32 elements need none. */
+ * allocates it.  Up to 32 rows of up to 16384 bf16 or 11456 fp32 elements need none. */
 typedef struct {
     const void  *dy, *x;         /* device, `dtype`                                           */
     int64_t      rows, cols, dy_ld, x_ld;

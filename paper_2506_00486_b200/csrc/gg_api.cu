@@ -89,12 +89,12 @@ struct gg_ctx {
     uint32_t *small_counts = nullptr;   // scratch of the short-segment kernel: one slot of count cells per CTA
     void *chan_buf = nullptr;     // scratch of gg_fused_channels (partials per row block and column)
     int64_t chan_bytes = 0;
-    // scratch of gg_layer_norm_grad (partial sums over the rows): the last is the one in use.  The smaller ones before it stay,
-    // because a captured graph may hold their addresses; each is at most half the next, so all of them together are less than it
-    // (and 64 are never reached).
-    void *norm_part[64] = {};
-    int norm_parts = 0;
+    void *norm_part = nullptr;    // scratch of gg_layer_norm_grad (partial sums over the rows)
     int64_t norm_part_bytes = 0;
+    // scratch that was outgrown: kept until the end, because a captured graph may hold its address.  Each buffer is at most half of the
+    // one that replaced it, so that all of them together are less than what is in use, and there are never so many of them.
+    void *outgrown[192] = {};
+    int n_outgrown = 0;
     uint32_t *norm_ticket = nullptr;    // counter of gg_grad_norm's one-launch form (zero between calls)
     double *seed = nullptr;       // device table that seeds the moment-ratio inversion of the short-segment kernel
     int resident_grid[2][8];      // CTAs the one-launch pass may use, by gradient type and sweep flags (-1: not asked yet)
@@ -444,20 +444,41 @@ cudaError_t launch_sweep(gg_ctx *ctx, int flags, gg_dtype in_dtype, gg_dtype gra
     return launch_stream(flags, in_dtype, grad_dtype, has_grad_out, sa, cs);
 }
 
+// Keeps scratch that has been replaced until the context ends.
+void keep(gg_ctx *ctx, void *outgrown)
+{
+    if (outgrown != nullptr && ctx->n_outgrown < (int)(sizeof(ctx->outgrown) / sizeof(void *))) ctx->outgrown[ctx->n_outgrown++] = outgrown;
+}
+
+// Grows scratch that captured work may use: what it replaces is kept, so nothing has to be waited for.
+gg_status grow_kept(gg_ctx *ctx, void **buf, int64_t *have, int64_t need)
+{
+    if (need <= *have) return GG_OK;
+    const int64_t bytes = std::max(need, 2 * *have);
+    void *p = nullptr;
+    GG_CUDA(ctx, cudaMalloc(&p, (size_t)bytes));
+    keep(ctx, *buf);
+    *buf = p;
+    *have = bytes;
+    return GG_OK;
+}
+
 // Entropy of n_hist count tables; grows the context's scratch (blocking) the first time a call needs more.
 gg_status ensure_entropy_scratch(gg_ctx *ctx, int32_t n_hist)
 {
     if (n_hist > ctx->ent_hists) {
-        if (ctx->ent_part) {
-            GG_CUDA(ctx, cudaDeviceSynchronize());
-            cudaFree(ctx->ent_part); cudaFree(ctx->ent_done);
-            ctx->ent_part = nullptr; ctx->ent_done = nullptr; ctx->ent_hists = 0;
-        }
-        GG_CUDA(ctx, cudaMalloc(reinterpret_cast<void **>(&ctx->ent_part), sizeof(double) * 2 * kEntSplit * (size_t)n_hist));
-        GG_CUDA(ctx, cudaMalloc(reinterpret_cast<void **>(&ctx->ent_done), sizeof(uint32_t) * (size_t)n_hist));
-        GG_CUDA(ctx, cudaMemset(ctx->ent_done, 0, sizeof(uint32_t) * (size_t)n_hist));
-        GG_CUDA(ctx, cudaStreamSynchronize(nullptr));      // (a memset does not wait, and the caller's stream need not wait for the legacy one)
-        ctx->ent_hists = n_hist;
+        const int64_t n = std::max((int64_t)n_hist, 2 * ctx->ent_hists);
+        void *part = nullptr, *done = nullptr;
+        GG_CUDA(ctx, cudaMalloc(&part, sizeof(double) * 2 * kEntSplit * (size_t)n));
+        cudaError_t e = cudaMalloc(&done, sizeof(uint32_t) * (size_t)n);
+        if (e == cudaSuccess) e = cudaMemset(done, 0, sizeof(uint32_t) * (size_t)n);
+        if (e == cudaSuccess) e = cudaStreamSynchronize(nullptr);      // (a memset does not wait, and the caller's stream need not wait for the legacy one)
+        if (e != cudaSuccess) { cudaFree(part); cudaFree(done); return cuda_fail(ctx, e); }
+        keep(ctx, ctx->ent_part);
+        keep(ctx, ctx->ent_done);
+        ctx->ent_part = static_cast<double *>(part);
+        ctx->ent_done = static_cast<uint32_t *>(done);
+        ctx->ent_hists = n;
     }
     return GG_OK;
 }
@@ -642,7 +663,8 @@ gg_status gg_destroy(gg_ctx *ctx)
     if (ctx->seed) cudaFree(ctx->seed);
     if (ctx->small_counts) cudaFree(ctx->small_counts);
     if (ctx->chan_buf) cudaFree(ctx->chan_buf);
-    for (int i = 0; i < ctx->norm_parts; ++i) cudaFree(ctx->norm_part[i]);
+    if (ctx->norm_part) cudaFree(ctx->norm_part);
+    for (int i = 0; i < ctx->n_outgrown; ++i) cudaFree(ctx->outgrown[i]);
     if (ctx->norm_ticket) cudaFree(ctx->norm_ticket);
     if (ctx->ent_part) cudaFree(ctx->ent_part);
     if (ctx->ent_done) cudaFree(ctx->ent_done);
@@ -1124,7 +1146,7 @@ gg_status gg_fused_channels(gg_ctx *ctx, const gg_channel_args *a, void *stream)
         const size_t n_strips = 2 * ((nc + kChanStrip - 1) / kChanStrip);
         const size_t n_dbl = 2 * nm + 2 * nc + ns, n_w32 = 3 * nm + 2 * nc + n_strips * (kChanTabFloats / 2 + 1) + 8;
         void *buf = ctx->chan_buf;
-        gg_status st = grow(ctx, &buf, &ctx->chan_bytes, (int64_t)(n_dbl * 8 + n_w32 * 4));
+        gg_status st = grow_kept(ctx, &buf, &ctx->chan_bytes, (int64_t)(n_dbl * 8 + n_w32 * 4));
         ctx->chan_buf = buf;
         if (st != GG_OK) return st;
         double *d = static_cast<double *>(ctx->chan_buf);
@@ -1649,19 +1671,12 @@ gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *a, void
     if (!guard.ok) return GG_ERR_CUDA;
     int slices = 0;
     GG_CUDA(ctx, layer_norm_grad_slices(*a, ctx->sm_count, &slices));
-    void *part = nullptr;
     if ((a->dweight || a->dbias) && slices > 0) {
-        const int64_t need = (int64_t)sizeof(float) * 2 * slices * a->cols;
-        if (need > ctx->norm_part_bytes) {
-            const int64_t bytes = std::max(need, 2 * ctx->norm_part_bytes);
-            GG_CUDA(ctx, cudaMalloc(&part, (size_t)bytes));
-            ctx->norm_part[ctx->norm_parts++] = part;
-            ctx->norm_part_bytes = bytes;
-        }
-        part = ctx->norm_part[ctx->norm_parts - 1];
+        st = grow_kept(ctx, &ctx->norm_part, &ctx->norm_part_bytes, (int64_t)sizeof(float) * 2 * slices * a->cols);
+        if (st != GG_OK) return st;
     }
     int launches = 0;
-    GG_CUDA(ctx, launch_layer_norm_grad(*a, static_cast<float *>(part), slices, ctx->sm_count, &launches, static_cast<cudaStream_t>(stream)));
+    GG_CUDA(ctx, launch_layer_norm_grad(*a, static_cast<float *>(ctx->norm_part), slices, ctx->sm_count, &launches, static_cast<cudaStream_t>(stream)));
     ctx->launches += launches;
     return GG_OK;
 }

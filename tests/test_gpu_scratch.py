@@ -160,3 +160,35 @@ def test_a_captured_call_keeps_its_plan(ctx):
         ctx.gg_grad_norm(t)
     again = ctx.plan_stats
     assert again[0] == built and again[1] > repointed
+
+
+def test_captured_passes_outlive_larger_scratch(ctx):
+    # the entropy step's and the channel-wise pass's scratch, outgrown by later calls
+    gen = torch.Generator(device="cuda").manual_seed(7)
+    segs = [t.mul_(0.02) for t in gradients([70001, 5000])]
+    few = torch.zeros(2, dtype=torch.int32)
+    fused = ctx.make_fused(segs, grad=[torch.empty_like(t) for t in segs], lam=1e-4, step=torch.full((2,), 2.0 ** -10, device="cuda"), hist_id=few, n_hist=1)
+    matrix = 0.02 * torch.randn((300, 64), generator=gen, device="cuda")
+    channels = ctx.make_fused_channels(matrix, grad=torch.empty_like(matrix), step=2.0 ** -10)
+    # (the step among the results is the one that was passed in)
+    want = [{k: t.clone() for k, t in run().items() if torch.is_tensor(t) and k != "step"} for run in (fused, channels)]
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        fused()
+        channels()
+    many = [t.mul_(0.02) for t in gradients([3000] * 40, seed=3)]
+    ctx.gg_fused(many, grad=[torch.empty_like(t) for t in many], lam=1e-4, step=torch.full((40,), 2.0 ** -10, device="cuda"))
+    for cols in (700, 5000):
+        wide = 0.02 * torch.randn((2000, cols), generator=gen, device="cuda")
+        ctx.gg_fused_channels(wide, grad=torch.empty_like(wide), step=2.0 ** -10)
+    other = [torch.full((1 << 16,), 3.0, device="cuda") for _ in range(64)]
+    for run, old in zip((fused, channels), want):
+        for k in old:
+            run.outputs[k].zero_()
+    graph.replay()
+    torch.cuda.synchronize()
+    for run, old in zip((fused, channels), want):
+        for k in old:
+            assert torch.equal(run.outputs[k], old[k]), k
+    assert all((t == 3.0).all() for t in other)
