@@ -335,6 +335,113 @@ typedef struct {
 } gg_layer_norm_grad_args;
 gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *args, void *stream);
 
+/* Softmax cross entropy of a linear output layer, without its logits: with l = h w^T,
+ *     lse[r]  = log sum over v of exp(l[r][v]),     loss[r] = lse[r] - l[r][target[r]]
+ * A negative target marks a position without one: its loss is 0 and its gradient too.  A target of `vocab` or more makes
+ * the row's loss and gradient nan.  The product takes bf16 operands and sums in fp32; the logits stay fp32 and never reach memory.  A row
+ * whose logits hold an inf or nan gets a lse and a loss that are not finite; other rows do not see it. */
+typedef struct {
+    const void    *h;            /* device, bf16 [rows][width]: the features                  */
+    int64_t        rows, width, h_ld;
+    const void    *w;            /* device, bf16 [vocab][width]                               */
+    int64_t        vocab, w_ld;
+    int32_t        dtype;        /* gg_dtype of h and w: GG_BF16                              */
+    const int64_t *target;       /* device [rows]                                             */
+    float         *loss, *lse;   /* device [rows]; each may be NULL                           */
+} gg_cross_entropy_args;
+gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *args, void *stream);
+
+/* Its gradient for dloss = dL/dloss and the lse that gg_cross_entropy wrote.  With
+ *     d[r][v] = dloss[r] (exp(l[r][v] - lse[r]) - [v = target[r]]):     dh = d w,     dw = d^T h
+ * The logits are computed again, a piece of the vocabulary at a time; d of the piece lies in scratch, rounded to bf16 as the
+ * products take it.  Sums are fp32, in a fixed order.  Where a target is negative, d is 0 whatever the logits are, but h has to be finite
+ * there (dw adds 0 * h).  Scratch: up to 512 MB for d, and 4 bytes for each element of dh. */
+typedef struct {
+    const float   *dloss;        /* device [rows]                                             */
+    const void    *h;            /* device, bf16 [rows][width]                                */
+    int64_t        rows, width, h_ld;
+    const void    *w;            /* device, bf16 [vocab][width]                               */
+    int64_t        vocab, w_ld;
+    int32_t        dtype;        /* gg_dtype of h, w, dh and dw: GG_BF16                      */
+    const int64_t *target;       /* device [rows]                                             */
+    const float   *lse;          /* device [rows]                                             */
+    void          *dh;           /* device or NULL (not wanted); not h                        */
+    int64_t        dh_ld;
+    void          *dw;           /* device or NULL; not w                                     */
+    int64_t        dw_ld;
+    int32_t        accumulate;   /* 0: dw = the sum; 1: += (dh is always written)             */
+} gg_cross_entropy_grad_args;
+gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *args, void *stream);
+
+/* The gated half of a feed-forward block, both projections and their product in one kernel:
+ *     gate = x w_gate^T,     up = x w_up^T,     h = act(gate) * up
+ * The operands are bf16, the sums, the activation and the product fp32; h is rounded once.  gate and up (bf16) are what
+ * the gradient needs. */
+enum {
+    GG_ACT_SILU = 0,             /* a / (1 + exp(-a))                                         */
+    GG_ACT_GELU = 1,             /* a (1 + erf(a / sqrt 2)) / 2                               */
+    GG_ACT_GELU_TANH = 2,        /* a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2         */
+    GG_ACT_RELU = 3              /* max(a, 0); its derivative at 0 is 0                       */
+};
+typedef struct {
+    const void *x;               /* device, bf16 [rows][width]                                */
+    int64_t     rows, width, x_ld;
+    const void *w_gate, *w_up;   /* device, bf16 [hidden][width]                              */
+    int64_t     hidden, w_gate_ld, w_up_ld;
+    int32_t     dtype;           /* gg_dtype of every matrix: GG_BF16                         */
+    int32_t     act;             /* GG_ACT_*                                                  */
+    void       *h;               /* device [rows][hidden]                                     */
+    int64_t     h_ld;
+    void       *gate, *up;       /* device [rows][hidden], each may be NULL (not wanted)      */
+    int64_t     gate_ld, up_ld;
+} gg_gated_linear_args;
+gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *args, void *stream);
+
+/* Its gradient, for dh = dL/dh and the gate and up that gg_gated_linear wrote:
+ *     dgate = dh * up * act'(gate),     dup = dh * act(gate)
+ *     dx = dgate w_gate + dup w_up,     dw_gate = dgate^T x,     dw_up = dup^T x
+ * dgate and dup lie in scratch (4 bytes for each element of h), rounded to bf16 as the products take them.  Sums are fp32, in
+ * a fixed order. */
+typedef struct {
+    const void *dh, *gate, *up;  /* device, bf16 [rows][hidden]                               */
+    int64_t     dh_ld, gate_ld, up_ld;
+    const void *x;               /* device, bf16 [rows][width]                                */
+    int64_t     rows, width, x_ld;
+    const void *w_gate, *w_up;   /* device, bf16 [hidden][width]                              */
+    int64_t     hidden, w_gate_ld, w_up_ld;
+    int32_t     dtype;           /* gg_dtype of every matrix: GG_BF16                         */
+    int32_t     act;             /* GG_ACT_*                                                  */
+    void       *dx;              /* device or NULL (not wanted); not x                        */
+    int64_t     dx_ld;
+    void       *dw_gate, *dw_up; /* device, both or neither NULL; not w_gate, w_up            */
+    int64_t     dw_gate_ld, dw_up_ld;
+    int32_t     accumulate;      /* 0: dw_gate, dw_up = the sums; 1: += (dx is always written)*/
+} gg_gated_linear_grad_args;
+gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *args, void *stream);
+
+/* Dropout with a mask that is never stored: y = [residual +] x * m / (1 - q), where an element is kept (m = 1) if its 16
+ * random bits are q * 65536 or more and q is p rounded to a multiple of 2^-16.  The bits are Philox4x32-10 at counter
+ * (j mod 2^32, j div 2^32, t mod 2^32, tensor_id) and key `seed`, 128 bits for elements 8i .. 8i+7 of a row, j = row * ceil(cols / 8) + i
+ * (the low half of a word first): whatever the strides and types, the same call makes the same mask.  So the gradient
+ * is the same call on dy, without the residual.  A dropped element counts as 0 whatever it was, inf and nan included.  Arithmetic is fp32.
+ * y may be x or residual (the same address and ld).
+ *   t_dev   device int64[1] or NULL: added to t (a captured graph advances it from replay to replay) */
+typedef struct {
+    const void    *x;            /* device, `dtype` [rows][cols]                              */
+    int64_t        rows, cols, x_ld;
+    int32_t        dtype;        /* gg_dtype of x, residual and y                             */
+    const void    *residual;     /* device or NULL (0)                                        */
+    int64_t        residual_ld;
+    void          *y;
+    int64_t        y_ld;
+    double         p;            /* 0 <= p, and q < 1                                         */
+    uint64_t       seed;
+    int64_t        t;
+    const int64_t *t_dev;
+    uint32_t       tensor_id;
+} gg_dropout_args;
+gg_status gg_dropout(gg_ctx *ctx, const gg_dropout_args *args, void *stream);
+
 /* Global norm of a gradient that lies in many tensors, and the factor that clips it, both left on the
  * device: norm = sqrt(sum over all segments of g^2), scale = min(1, max_norm / norm).  An inf or nan anywhere
  * makes both nan.  gg_adamw_step takes `scale` as its grad_scale.

@@ -22,6 +22,7 @@ FLAG_DEGENERATE, FLAG_BETA_CLAMPED_LO, FLAG_BETA_CLAMPED_HI, FLAG_NONFINITE, FLA
 FLAG_TIMEOUT = 32
 HOOK_RESIDENT_MODE, HOOK_EXTRA_ARRIVALS, HOOK_WAIT_CAP, HOOK_CLUSTER_MODE = 0, 1, 2, 3
 BETA_LO, BETA_HI = 0.05, 20.0
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 ADAMW_BLOCK = 256          # elements that share one scale of an 8-bit AdamW state
 
 _SEG_DTYPE = np.dtype([("ptr", np.uint64), ("len", np.int64)])
@@ -87,6 +88,53 @@ class AdamwArgs(ctypes.Structure):
     ]
 
 
+class CrossEntropyArgs(ctypes.Structure):
+    """Mirror of gg_cross_entropy_args."""
+    _fields_ = [
+        ("h", _P), ("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("h_ld", ctypes.c_int64), ("w", _P),
+        ("vocab", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("target", _P), ("loss", _P), ("lse", _P),
+    ]
+
+
+class CrossEntropyGradArgs(ctypes.Structure):
+    """Mirror of gg_cross_entropy_grad_args."""
+    _fields_ = [
+        ("dloss", _P), ("h", _P), ("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("h_ld", ctypes.c_int64), ("w", _P),
+        ("vocab", ctypes.c_int64), ("w_ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("target", _P), ("lse", _P),
+        ("dh", _P), ("dh_ld", ctypes.c_int64), ("dw", _P), ("dw_ld", ctypes.c_int64), ("accumulate", ctypes.c_int32),
+    ]
+
+
+class GatedLinearArgs(ctypes.Structure):
+    """Mirror of gg_gated_linear_args."""
+    _fields_ = [
+        ("x", _P), ("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("x_ld", ctypes.c_int64), ("w_gate", _P), ("w_up", _P),
+        ("hidden", ctypes.c_int64), ("w_gate_ld", ctypes.c_int64), ("w_up_ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+        ("act", ctypes.c_int32), ("h", _P), ("h_ld", ctypes.c_int64), ("gate", _P), ("up", _P), ("gate_ld", ctypes.c_int64),
+        ("up_ld", ctypes.c_int64),
+    ]
+
+
+class GatedLinearGradArgs(ctypes.Structure):
+    """Mirror of gg_gated_linear_grad_args."""
+    _fields_ = [
+        ("dh", _P), ("gate", _P), ("up", _P), ("dh_ld", ctypes.c_int64), ("gate_ld", ctypes.c_int64), ("up_ld", ctypes.c_int64),
+        ("x", _P), ("rows", ctypes.c_int64), ("width", ctypes.c_int64), ("x_ld", ctypes.c_int64), ("w_gate", _P), ("w_up", _P),
+        ("hidden", ctypes.c_int64), ("w_gate_ld", ctypes.c_int64), ("w_up_ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+        ("act", ctypes.c_int32), ("dx", _P), ("dx_ld", ctypes.c_int64), ("dw_gate", _P), ("dw_up", _P),
+        ("dw_gate_ld", ctypes.c_int64), ("dw_up_ld", ctypes.c_int64), ("accumulate", ctypes.c_int32),
+    ]
+
+
+class DropoutArgs(ctypes.Structure):
+    """Mirror of gg_dropout_args."""
+    _fields_ = [
+        ("x", _P), ("rows", ctypes.c_int64), ("cols", ctypes.c_int64), ("x_ld", ctypes.c_int64), ("dtype", ctypes.c_int32),
+        ("residual", _P), ("residual_ld", ctypes.c_int64), ("y", _P), ("y_ld", ctypes.c_int64), ("p", ctypes.c_double),
+        ("seed", ctypes.c_uint64), ("t", ctypes.c_int64), ("t_dev", _P), ("tensor_id", ctypes.c_uint32),
+    ]
+
+
 class GGError(RuntimeError):
     def __init__(self, status, text):
         super().__init__(f"gg status {status}: {text}")
@@ -148,7 +196,13 @@ def lib():
         L.gg_layer_norm_grad.argtypes = [_P, ctypes.POINTER(LayerNormGradArgs), _P]
         L.gg_grad_norm.argtypes = [_P, _P, i32, ctypes.c_int, d, _P, _P, _P]
         L.gg_adamw_step.argtypes = [_P, ctypes.POINTER(AdamwArgs), _P]
-        for name in ("gg_layer_norm", "gg_layer_norm_grad", "gg_grad_norm", "gg_adamw_step"):
+        L.gg_cross_entropy.argtypes = [_P, ctypes.POINTER(CrossEntropyArgs), _P]
+        L.gg_cross_entropy_grad.argtypes = [_P, ctypes.POINTER(CrossEntropyGradArgs), _P]
+        L.gg_gated_linear.argtypes = [_P, ctypes.POINTER(GatedLinearArgs), _P]
+        L.gg_gated_linear_grad.argtypes = [_P, ctypes.POINTER(GatedLinearGradArgs), _P]
+        L.gg_dropout.argtypes = [_P, ctypes.POINTER(DropoutArgs), _P]
+        for name in ("gg_layer_norm", "gg_layer_norm_grad", "gg_grad_norm", "gg_adamw_step", "gg_cross_entropy", "gg_cross_entropy_grad",
+                     "gg_gated_linear", "gg_gated_linear_grad", "gg_dropout"):
             getattr(L, name).restype = ctypes.c_int
         L.gg_compression_ratio.argtypes = [d, d]
         L.gg_compression_ratio.restype = d
@@ -814,6 +868,161 @@ class Context:
     def gg_adamw_step(self, w, g, m, v, t, lr, **kw):
         """One-shot form of make_adamw_step(...)(t, lr)."""
         return self.make_adamw_step(w, g, m, v, **kw)(t, lr)
+
+    # --------------------------------------------------------- vocabulary loss
+    def make_cross_entropy(self, h, w, target):
+        """Softmax cross entropy of the logits h @ w.t(), which are never stored.
+
+        h: bfloat16 [rows, width], w: bfloat16 [vocab, width] (rows may be strided), target: int64 [rows], negative where a
+        position has none.  Allocates the outputs once and returns a callable that enqueues the pass and returns
+        dict(loss, lse) (float32 [rows]); lse is what the gradient needs."""
+        a = CrossEntropyArgs()
+        self._features(a, h, w, target)
+        res = dict(loss=self._new(h.shape[0], torch.float32), lse=self._new(h.shape[0], torch.float32))
+        a.loss, a.lse = _ptr(res["loss"]), _ptr(res["lse"])
+        return self._callable("gg_cross_entropy", a, res, [h, w, target])
+
+    def gg_cross_entropy(self, h, w, target):
+        """One-shot form of make_cross_entropy(...)()."""
+        return self.make_cross_entropy(h, w, target)()
+
+    def make_cross_entropy_grad(self, dloss, h, w, target, lse, dh=None, dw=None, want_dh=True, want_dw=True, accumulate=False):
+        """Gradient of cross_entropy for dloss (float32 [rows]) and the lse that it returned.
+
+        Allocates dh and dw (bfloat16, like h and w, unless given) once and returns a callable that enqueues the pass and returns
+        dict(dh, dw).  accumulate adds to dw instead of overwriting it."""
+        a = CrossEntropyGradArgs()
+        rows, width = self._features(a, h, w, target)
+        self._vector("dloss", dloss, rows)
+        self._vector("lse", lse, rows)
+        if accumulate and want_dw and dw is None:
+            raise ValueError("accumulate adds to dw: give it")
+        dh, dw = self._result("dh", dh, h, want_dh), self._result("dw", dw, w, want_dw)
+        a.dloss, a.lse = _ptr(dloss), _ptr(lse)
+        a.dh, a.dh_ld = _ptr(dh), width if dh is None else _ld(dh)
+        a.dw, a.dw_ld = _ptr(dw), width if dw is None else _ld(dw)
+        a.accumulate = int(bool(accumulate))
+        return self._callable("gg_cross_entropy_grad", a, dict(dh=dh, dw=dw), [dloss, h, w, target, lse])
+
+    def gg_cross_entropy_grad(self, dloss, h, w, target, lse, **kw):
+        """One-shot form of make_cross_entropy_grad(...)()."""
+        return self.make_cross_entropy_grad(dloss, h, w, target, lse, **kw)()
+
+    def _features(self, a, h, w, target):
+        rows, width = self._operand(h, "h")
+        vocab, _ = self._operand(w, "w", cols=width)
+        self._vector("target", target, rows, torch.int64)
+        a.h, a.rows, a.width, a.h_ld, a.dtype = _ptr(h), rows, width, _ld(h), GG_BF16
+        a.w, a.vocab, a.w_ld, a.target = _ptr(w), vocab, _ld(w), _ptr(target)
+        return rows, width
+
+    def _operand(self, t, name, rows=None, cols=None):
+        """A matrix of a product: bfloat16, what the tensor cores take."""
+        shape = self._rows(t, name)
+        if t.dtype != torch.bfloat16:
+            raise TypeError(f"{name} must be bfloat16 (AdamW keeps a bfloat16 copy of float32 weights: w_copy)")
+        if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
+            raise ValueError(f"{name} must be [{'rows' if rows is None else rows}, {'cols' if cols is None else cols}], not {list(shape)}")
+        return shape
+
+    def _result(self, name, t, like, want=True):
+        if not want:
+            return None
+        if t is None:
+            return self._new(like.shape, like.dtype)
+        self._rows(t, name, like)
+        return t
+
+    # ------------------------------------------------------------- gated block
+    def make_gated_linear(self, x, w_gate, w_up, act="silu", out=None, keep=False):
+        """h = act(x @ w_gate.t()) * (x @ w_up.t()), both products and the activation in one kernel.
+
+        x: bfloat16 [rows, width], w_gate, w_up: bfloat16 [hidden, width] (rows may be strided; halves of one matrix will do),
+        act: "silu", "gelu", "gelu_tanh" or "relu".  Allocates h (unless `out` is given) once and returns a callable that
+        enqueues the pass and returns dict(h, gate, up); gate and up, the products that the gradient needs, only with `keep`."""
+        rows, width = self._operand(x, "x")
+        hidden, _ = self._operand(w_gate, "w_gate", cols=width)
+        self._operand(w_up, "w_up", hidden, width)
+        if out is None:
+            out = self._new((rows, hidden), torch.bfloat16)
+        self._operand(out, "out", rows, hidden)
+        res = dict(h=out, gate=self._new((rows, hidden), torch.bfloat16) if keep else None,
+                   up=self._new((rows, hidden), torch.bfloat16) if keep else None)
+        a = GatedLinearArgs()
+        a.x, a.rows, a.width, a.x_ld, a.dtype, a.act = _ptr(x), rows, width, _ld(x), GG_BF16, self._act(act)
+        a.w_gate, a.w_up, a.hidden, a.w_gate_ld, a.w_up_ld = _ptr(w_gate), _ptr(w_up), hidden, _ld(w_gate), _ld(w_up)
+        a.h, a.h_ld, a.gate, a.up, a.gate_ld, a.up_ld = _ptr(out), _ld(out), _ptr(res["gate"]), _ptr(res["up"]), hidden, hidden
+        return self._callable("gg_gated_linear", a, res, [x, w_gate, w_up])
+
+    def gg_gated_linear(self, x, w_gate, w_up, **kw):
+        """One-shot form of make_gated_linear(...)()."""
+        return self.make_gated_linear(x, w_gate, w_up, **kw)()
+
+    def make_gated_linear_grad(self, dh, x, w_gate, w_up, gate, up, act="silu", dx=None, dw_gate=None, dw_up=None, want_dx=True,
+                               want_dweight=True, accumulate=False):
+        """Gradient of gated_linear for dh, its operands and the gate and up that it kept.
+
+        Allocates dx, dw_gate and dw_up (bfloat16, like x and the weights, unless given) once and returns a callable that enqueues
+        the pass and returns dict(dx, dw_gate, dw_up).  accumulate adds to dw_gate and dw_up instead of overwriting them."""
+        rows, width = self._operand(x, "x")
+        hidden, _ = self._operand(w_gate, "w_gate", cols=width)
+        self._operand(w_up, "w_up", hidden, width)
+        for name, t in (("dh", dh), ("gate", gate), ("up", up)):
+            self._operand(t, name, rows, hidden)
+        if accumulate and want_dweight and (dw_gate is None or dw_up is None):
+            raise ValueError("accumulate adds to dw_gate and dw_up: give both")
+        res = dict(dx=self._result("dx", dx, x, want_dx), dw_gate=self._result("dw_gate", dw_gate, w_gate, want_dweight),
+                   dw_up=self._result("dw_up", dw_up, w_up, want_dweight))
+        a = GatedLinearGradArgs()
+        a.dh, a.gate, a.up, a.dh_ld, a.gate_ld, a.up_ld = _ptr(dh), _ptr(gate), _ptr(up), _ld(dh), _ld(gate), _ld(up)
+        a.x, a.rows, a.width, a.x_ld, a.dtype, a.act = _ptr(x), rows, width, _ld(x), GG_BF16, self._act(act)
+        a.w_gate, a.w_up, a.hidden, a.w_gate_ld, a.w_up_ld = _ptr(w_gate), _ptr(w_up), hidden, _ld(w_gate), _ld(w_up)
+        for name, t in res.items():
+            setattr(a, name, _ptr(t))
+            setattr(a, name + "_ld", width if t is None else _ld(t))
+        a.accumulate = int(bool(accumulate))
+        return self._callable("gg_gated_linear_grad", a, res, [dh, x, w_gate, w_up, gate, up])
+
+    def gg_gated_linear_grad(self, dh, x, w_gate, w_up, gate, up, **kw):
+        """One-shot form of make_gated_linear_grad(...)()."""
+        return self.make_gated_linear_grad(dh, x, w_gate, w_up, gate, up, **kw)()
+
+    @staticmethod
+    def _act(act):
+        if act not in ACTIVATIONS:
+            raise ValueError(f"act must be one of {', '.join(ACTIVATIONS)}, not {act!r}")
+        return ACTIVATIONS[act]
+
+    # ----------------------------------------------------------------- dropout
+    def make_dropout(self, x, p, residual=None, out=None, seed=0, tensor_id=0, t_dev=None):
+        """Dropout of the 2-D tensor x (rows may be strided) with a mask that is drawn, not stored.
+
+        Returns drop(t), which enqueues y = [residual +] x * mask / (1 - p) and returns dict(y); y is allocated once unless
+        `out` is given (it may be x or residual).  The mask depends on seed, tensor_id, t and the shape alone: the gradient is drop(t) of
+        another make_dropout on dy.  t_dev: an int64 device tensor of one value that is added to t, for captured graphs."""
+        rows, cols = self._rows(x, "x")
+        if residual is not None:
+            self._rows(residual, "residual", x)
+        y = self._result("out", out, x)
+        if t_dev is not None:
+            self._vector("t_dev", t_dev, 1, torch.int64)
+        a = DropoutArgs()
+        a.x, a.rows, a.cols, a.x_ld, a.dtype = _ptr(x), rows, cols, _ld(x), _dtype_code(x.dtype)
+        a.residual, a.residual_ld = _ptr(residual), cols if residual is None else _ld(residual)
+        a.y, a.y_ld, a.p, a.seed, a.t_dev = _ptr(y), _ld(y), float(p), int(seed) & (2 ** 64 - 1), _ptr(t_dev)
+        a.tensor_id = int(tensor_id) & 0xFFFFFFFF
+        enqueue = self._callable("gg_dropout", a, dict(y=y), [x, residual, t_dev])
+
+        def drop(t=0):
+            a.t = int(t)
+            return enqueue()
+
+        drop.outputs, drop.args = enqueue.outputs, a
+        return drop
+
+    def gg_dropout(self, x, p, t=0, **kw):
+        """One-shot form of make_dropout(...)(t)."""
+        return self.make_dropout(x, p, **kw)(t)
 
     # ------------------------------------------------------------------ timing
     def timing_enable(self, on=True):

@@ -17,6 +17,7 @@
 #include "gg_adamw.cuh"
 #include "gg_internal.h"
 #include "gg_philox.cuh"
+#include "gg_products.cuh"
 
 using namespace gg;
 
@@ -91,6 +92,9 @@ struct gg_ctx {
     int64_t chan_bytes = 0;
     void *norm_part = nullptr;    // scratch of gg_layer_norm_grad (partial sums over the rows)
     int64_t norm_part_bytes = 0;
+    void *product_buf = nullptr;  // scratch of the vocabulary loss, the gated block and their gradients
+    int64_t product_bytes = 0;
+    uint32_t *gave_up = nullptr;  // pinned host word that a product kernel sets when one of its waits runs out
     // scratch that was outgrown: kept until the end, because a captured graph may hold its address.  Each buffer is at most half of the
     // one that replaced it, so that all of them together are less than what is in use, and there are never so many of them.
     void *outgrown[192] = {};
@@ -630,8 +634,11 @@ gg_status gg_create(gg_ctx **out, int device)
         if (se == cudaSuccess) se = cudaMalloc(reinterpret_cast<void **>(&ctx->norm_ticket), sizeof(uint32_t));
         if (se == cudaSuccess) se = cudaMemsetAsync(ctx->norm_ticket, 0, sizeof(uint32_t), nullptr);
         if (se == cudaSuccess) se = cudaStreamSynchronize(nullptr);
+        if (se == cudaSuccess) se = cudaHostAlloc(reinterpret_cast<void **>(&ctx->gave_up), sizeof(uint32_t), cudaHostAllocMapped);
+        if (se == cudaSuccess) *ctx->gave_up = 0;
         if (se != cudaSuccess) {
             cudaGetLastError();
+            if (ctx->gave_up) cudaFreeHost(ctx->gave_up);
             if (ctx->seed) cudaFree(ctx->seed);
             if (ctx->norm_ticket) cudaFree(ctx->norm_ticket);
             delete ctx;
@@ -664,6 +671,8 @@ gg_status gg_destroy(gg_ctx *ctx)
     if (ctx->small_counts) cudaFree(ctx->small_counts);
     if (ctx->chan_buf) cudaFree(ctx->chan_buf);
     if (ctx->norm_part) cudaFree(ctx->norm_part);
+    if (ctx->product_buf) cudaFree(ctx->product_buf);
+    if (ctx->gave_up) cudaFreeHost(ctx->gave_up);
     for (int i = 0; i < ctx->n_outgrown; ++i) cudaFree(ctx->outgrown[i]);
     if (ctx->norm_ticket) cudaFree(ctx->norm_ticket);
     if (ctx->ent_part) cudaFree(ctx->ent_part);
@@ -1754,6 +1763,334 @@ gg_status gg_adamw_step(gg_ctx *ctx, const gg_adamw_args *a, void *stream)
     const int per_warp = (int)(share < 1 ? 1 : share > most ? most : share);
     cudaStream_t cs = static_cast<cudaStream_t>(stream);
     return full <= kTableSmall ? run_adamw<kTableSmall>(ctx, *a, per_warp, c, cs) : run_adamw<kTableLarge>(ctx, *a, per_warp, c, cs);
+}
+
+}  // extern "C"
+
+// ---- the operators around matrix products
+namespace {
+
+constexpr int64_t kMostSize = 0x7FFFFF00;      // rows and columns of a product's matrices: tensor copies count in 32 bits
+constexpr int64_t kLossRows = 32768;           // positions of the loss that are taken at a time (bounds the scratch for their partials)
+constexpr int64_t kPieceBytes = 512ll << 20;   // of the logits' gradient in scratch
+
+bool product_size(int64_t n) { return n >= 0 && n <= kMostSize; }
+gg_status check_bf16(const void *p, int64_t rows, int64_t cols, int64_t ld) { return check_matrix(p, rows, cols, ld, GG_BF16); }
+Bf16Matrix matrix_of(const void *p, int64_t rows, int64_t cols, int64_t ld)
+{
+    return Bf16Matrix{static_cast<const uint16_t *>(p), rows, cols, ld};
+}
+
+// The scratch of one call: places first, then one buffer for all of them.
+struct ProductScratch {
+    gg_ctx *ctx;
+    cudaStream_t st;
+    int64_t bytes = 0;
+    int64_t place(int64_t n) { const int64_t at = bytes; bytes += (n + 1023) & ~(int64_t)1023; return at; }
+    // (a stream capture may be under way: the allocation is no part of it)
+    gg_status grow()
+    {
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+        if (bytes > ctx->product_bytes) cudaThreadExchangeStreamCaptureMode(&mode);
+        const int64_t before = ctx->product_bytes;
+        gg_status s = grow_kept(ctx, &ctx->product_buf, &ctx->product_bytes, bytes);
+        if (bytes > before) cudaThreadExchangeStreamCaptureMode(&mode);
+        return s;
+    }
+    template <typename T> T *at(int64_t place) const { return reinterpret_cast<T *>(static_cast<char *>(ctx->product_buf) + place); }
+};
+
+// An operand that tensor copies read where it lies, or a copy of it in scratch with rows at multiples of 16 bytes.
+struct Operand {
+    Bf16Matrix m;
+    int64_t copy = -1;
+    Operand(const Bf16Matrix &from, ProductScratch &s) : m(from)
+    {
+        if (!tma_reads(m)) copy = s.place(m.rows * ((m.cols + 7) / 8 * 8) * 2);
+    }
+    gg_status lay(ProductScratch &s)
+    {
+        if (copy < 0) return GG_OK;
+        const int64_t ld = (m.cols + 7) / 8 * 8;
+        uint16_t *to = s.at<uint16_t>(copy);
+        GG_CUDA(s.ctx, launch_realign(m, to, ld, s.st));
+        s.ctx->launches += 1;
+        m.p = to;
+        m.ld = ld;
+        copy = -1;
+        return GG_OK;
+    }
+};
+
+// A wait that ran out in an earlier call is this call's error: its results were not finished.
+gg_status product_alive(gg_ctx *ctx)
+{
+    volatile uint32_t *word = ctx->gave_up;
+    if (*word == 0) return GG_OK;
+    *word = 0;
+    ctx->cuda_error = "a wait inside a product kernel of an earlier call ran out";
+    return GG_ERR_CUDA;
+}
+
+gg_status zero_matrix(gg_ctx *ctx, void *p, int64_t rows, int64_t cols, int64_t ld, cudaStream_t st)
+{
+    if (p != nullptr && rows > 0 && cols > 0) GG_CUDA(ctx, cudaMemset2DAsync(p, (size_t)ld * 2, 0, (size_t)cols * 2, (size_t)rows, st));
+    return GG_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *stream)
+{
+    if (!ctx || !a || !product_size(a->rows) || !product_size(a->width) || !product_size(a->vocab) || a->width < 1 || a->vocab < 1) return GG_ERR_INVALID_ARG;
+    if (a->dtype != GG_BF16) return GG_ERR_DTYPE;
+    gg_status st = check_bf16(a->h, a->rows, a->width, a->h_ld);
+    if (st == GG_OK) st = check_bf16(a->w, a->vocab, a->width, a->w_ld);
+    if (st == GG_OK && a->rows > 0 && !a->target) st = GG_ERR_INVALID_ARG;
+    if (st == GG_OK && !on_boundary(a->target, 8)) st = GG_ERR_ALIGNMENT;
+    if (st == GG_OK) st = check_f32(a->loss);
+    if (st == GG_OK) st = check_f32(a->lse);
+    if (st != GG_OK) return st;
+    if (a->rows == 0 || (!a->loss && !a->lse)) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    if ((st = product_alive(ctx)) != GG_OK) return st;
+    ProductScratch s{ctx, static_cast<cudaStream_t>(stream)};
+    const int64_t most = std::min(a->rows, kLossRows);
+    Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
+    const int64_t part_at = s.place(most * product_partials(most, a->vocab) * (int64_t)sizeof(float2)), logit_at = s.place(most * 4);
+    if ((st = s.grow()) != GG_OK || (st = h.lay(s)) != GG_OK || (st = w.lay(s)) != GG_OK) return st;
+    for (int64_t r = 0; r < a->rows; r += kLossRows) {
+        const int64_t rows = std::min(a->rows - r, kLossRows);
+        ProductArgs p{};
+        p.a[0] = matrix_of(h.m.p + r * h.m.ld, rows, a->width, h.m.ld);
+        p.b[0] = w.m;
+        p.m = rows; p.n = a->vocab; p.k = a->width;
+        p.segments = p.batches = p.splits = 1;
+        p.part = s.at<float2>(part_at);
+        p.target_logit = s.at<float>(logit_at);
+        p.target = a->target + r;
+        p.vocab = a->vocab;
+        p.gave_up = ctx->gave_up;
+        GG_CUDA(ctx, launch_product_rows(kLse, p, ctx->sm_count, s.st));
+        GG_CUDA(ctx, launch_lse_finish(p.part, product_partials(rows, a->vocab), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
+                                       a->loss ? a->loss + r : nullptr, s.st));
+        ctx->launches += 2;
+    }
+    return GG_OK;
+}
+
+gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a, void *stream)
+{
+    if (!ctx || !a || !product_size(a->rows) || !product_size(a->width) || !product_size(a->vocab) || a->width < 1 || a->vocab < 1) return GG_ERR_INVALID_ARG;
+    if (a->dtype != GG_BF16) return GG_ERR_DTYPE;
+    gg_status st = check_bf16(a->h, a->rows, a->width, a->h_ld);
+    if (st == GG_OK) st = check_bf16(a->w, a->vocab, a->width, a->w_ld);
+    if (st == GG_OK && a->dh) st = check_bf16(a->dh, a->rows, a->width, a->dh_ld);
+    if (st == GG_OK && a->dw) st = check_bf16(a->dw, a->vocab, a->width, a->dw_ld);
+    if (st == GG_OK && ((a->rows > 0 && (!a->target || !a->dloss || !a->lse)) || (a->dh && a->dh == a->h) || (a->dw && a->dw == a->w))) st = GG_ERR_INVALID_ARG;
+    if (st == GG_OK && !on_boundary(a->target, 8)) st = GG_ERR_ALIGNMENT;
+    if (st == GG_OK) st = check_f32(a->dloss);
+    if (st == GG_OK) st = check_f32(a->lse);
+    if (st != GG_OK) return st;
+    if (!a->dh && !a->dw) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    ProductScratch s{ctx, static_cast<cudaStream_t>(stream)};
+    if (a->rows == 0) return a->accumulate ? GG_OK : zero_matrix(ctx, a->dw, a->vocab, a->width, a->dw_ld, s.st);
+    if ((st = product_alive(ctx)) != GG_OK) return st;
+    // pieces of the vocabulary of one size, a multiple of the tile
+    const int64_t all = (a->vocab + 255) / 256, fit = std::max<int64_t>(1, kPieceBytes / (512 * a->rows)), pieces = (all + fit - 1) / fit;
+    const int64_t piece = (all + pieces - 1) / pieces * 256, last = a->vocab - (a->vocab - 1) / piece * piece, n_pieces = (a->vocab + piece - 1) / piece;
+    const int splits = a->dh ? product_splits(a->rows, a->width, last, 1, ctx->sm_count) : 1;
+    const int64_t f32_ld = (a->width + 31) / 32 * 32;
+    Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
+    const int64_t d_at = s.place(a->rows * piece * 2);
+    const int64_t f32_at = s.place(a->dh && (splits > 1 || n_pieces > 1) ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
+    if ((st = s.grow()) != GG_OK || (st = h.lay(s)) != GG_OK || (st = w.lay(s)) != GG_OK) return st;
+    for (int64_t i = 0; i < n_pieces; ++i) {
+        const int64_t first = i * piece, n = std::min(piece, a->vocab - first);
+        const Bf16Matrix d{s.at<uint16_t>(d_at), a->rows, n, piece}, rows_of_w{w.m.p + first * w.m.ld, n, a->width, w.m.ld};
+        ProductArgs p{};
+        p.segments = p.batches = p.splits = 1;
+        p.gave_up = ctx->gave_up;
+        p.a[0] = h.m;
+        p.b[0] = rows_of_w;
+        p.m = a->rows; p.n = n; p.k = a->width;
+        p.target = a->target; p.vocab = a->vocab; p.first = first;
+        p.lse = a->lse; p.dloss = a->dloss;
+        p.out[0] = s.at<uint16_t>(d_at);
+        p.out_ld[0] = piece;
+        GG_CUDA(ctx, launch_product_rows(kDlogits, p, ctx->sm_count, s.st));
+        ctx->launches += 1;
+        if (a->dw) {
+            ProductArgs q = p;
+            q.a[0] = d;
+            q.b[0] = h.m;
+            q.m = n; q.n = a->width; q.k = a->rows;
+            q.out[0] = static_cast<uint16_t *>(a->dw) + first * a->dw_ld;
+            q.out_ld[0] = a->dw_ld;
+            q.mode = a->accumulate ? kAddBf16 : kStoreBf16;
+            GG_CUDA(ctx, launch_product_dweight(q, ctx->sm_count, s.st));
+            ctx->launches += 1;
+        }
+        if (a->dh) {
+            ProductArgs q = p;
+            q.a[0] = d;
+            q.b[0] = rows_of_w;
+            q.m = a->rows; q.n = a->width; q.k = n;
+            q.splits = splits;
+            q.out[0] = static_cast<uint16_t *>(a->dh);
+            q.out_ld[0] = a->dh_ld;
+            q.f32 = s.at<float>(f32_at);
+            q.f32_ld = f32_ld;
+            const bool ends = i == n_pieces - 1 && splits == 1;
+            q.mode = i == 0 ? (ends ? kStoreBf16 : kStoreF32) : (ends ? kStoreBf16OfSum : kAddF32);
+            GG_CUDA(ctx, launch_product_drows(q, ctx->sm_count, s.st));
+            ctx->launches += 1;
+        }
+    }
+    if (a->dh && splits > 1) {
+        GG_CUDA(ctx, launch_sum_splits(s.at<float>(f32_at), splits, a->rows, a->width, f32_ld, static_cast<uint16_t *>(a->dh), a->dh_ld, s.st));
+        ctx->launches += 1;
+    }
+    return GG_OK;
+}
+
+gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *a, void *stream)
+{
+    if (!ctx || !a || !product_size(a->rows) || !product_size(a->width) || !product_size(a->hidden) || a->width < 1) return GG_ERR_INVALID_ARG;
+    if (a->act < GG_ACT_SILU || a->act > GG_ACT_RELU) return GG_ERR_INVALID_ARG;
+    if (a->dtype != GG_BF16) return GG_ERR_DTYPE;
+    gg_status st = check_bf16(a->x, a->rows, a->width, a->x_ld);
+    if (st == GG_OK) st = check_bf16(a->w_gate, a->hidden, a->width, a->w_gate_ld);
+    if (st == GG_OK) st = check_bf16(a->w_up, a->hidden, a->width, a->w_up_ld);
+    if (st == GG_OK) st = check_bf16(a->h, a->rows, a->hidden, a->h_ld);
+    if (st == GG_OK && a->gate) st = check_bf16(a->gate, a->rows, a->hidden, a->gate_ld);
+    if (st == GG_OK && a->up) st = check_bf16(a->up, a->rows, a->hidden, a->up_ld);
+    if (st == GG_OK && a->rows > 0 && a->hidden > 0 && a->h == a->x) st = GG_ERR_INVALID_ARG;
+    if (st != GG_OK) return st;
+    if (a->rows == 0 || a->hidden == 0) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    if ((st = product_alive(ctx)) != GG_OK) return st;
+    ProductScratch s{ctx, static_cast<cudaStream_t>(stream)};
+    Operand x(matrix_of(a->x, a->rows, a->width, a->x_ld), s), wg(matrix_of(a->w_gate, a->hidden, a->width, a->w_gate_ld), s),
+        wu(matrix_of(a->w_up, a->hidden, a->width, a->w_up_ld), s);
+    if ((st = s.grow()) != GG_OK || (st = x.lay(s)) != GG_OK || (st = wg.lay(s)) != GG_OK || (st = wu.lay(s)) != GG_OK) return st;
+    ProductArgs p{};
+    p.a[0] = x.m;
+    p.b[0] = wg.m;
+    p.b[1] = wu.m;
+    p.m = a->rows; p.n = a->hidden; p.k = a->width;
+    p.segments = p.batches = p.splits = 1;
+    p.h = static_cast<uint16_t *>(a->h); p.gate = static_cast<uint16_t *>(a->gate); p.up = static_cast<uint16_t *>(a->up);
+    p.h_ld = a->h_ld; p.gate_ld = a->gate_ld; p.up_ld = a->up_ld;
+    p.act = a->act;
+    p.gave_up = ctx->gave_up;
+    GG_CUDA(ctx, launch_product_rows(kGated, p, ctx->sm_count, s.st));
+    ctx->launches += 1;
+    return GG_OK;
+}
+
+gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, void *stream)
+{
+    if (!ctx || !a || !product_size(a->rows) || !product_size(a->width) || !product_size(a->hidden) || a->width < 1) return GG_ERR_INVALID_ARG;
+    if (a->act < GG_ACT_SILU || a->act > GG_ACT_RELU || !a->dw_gate != !a->dw_up) return GG_ERR_INVALID_ARG;
+    if (a->dtype != GG_BF16) return GG_ERR_DTYPE;
+    gg_status st = check_bf16(a->x, a->rows, a->width, a->x_ld);
+    if (st == GG_OK) st = check_bf16(a->w_gate, a->hidden, a->width, a->w_gate_ld);
+    if (st == GG_OK) st = check_bf16(a->w_up, a->hidden, a->width, a->w_up_ld);
+    if (st == GG_OK) st = check_bf16(a->dh, a->rows, a->hidden, a->dh_ld);
+    if (st == GG_OK) st = check_bf16(a->gate, a->rows, a->hidden, a->gate_ld);
+    if (st == GG_OK) st = check_bf16(a->up, a->rows, a->hidden, a->up_ld);
+    if (st == GG_OK && a->dx) st = check_bf16(a->dx, a->rows, a->width, a->dx_ld);
+    if (st == GG_OK && a->dw_gate) st = check_bf16(a->dw_gate, a->hidden, a->width, a->dw_gate_ld);
+    if (st == GG_OK && a->dw_up) st = check_bf16(a->dw_up, a->hidden, a->width, a->dw_up_ld);
+    if (st == GG_OK && ((a->dx && a->dx == a->x) || (a->dw_gate && (a->dw_gate == a->w_gate || a->dw_gate == a->w_up || a->dw_up == a->w_gate ||
+                                                                   a->dw_up == a->w_up || a->dw_gate == a->dw_up)))) st = GG_ERR_INVALID_ARG;
+    if (st != GG_OK) return st;
+    if (!a->dx && !a->dw_gate) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    ProductScratch s{ctx, static_cast<cudaStream_t>(stream)};
+    if (a->rows == 0 || a->hidden == 0) {
+        st = zero_matrix(ctx, a->dx, a->rows, a->width, a->dx_ld, s.st);
+        if (st == GG_OK && !a->accumulate) st = zero_matrix(ctx, a->dw_gate, a->hidden, a->width, a->dw_gate_ld, s.st);
+        if (st == GG_OK && !a->accumulate) st = zero_matrix(ctx, a->dw_up, a->hidden, a->width, a->dw_up_ld, s.st);
+        return st;
+    }
+    if ((st = product_alive(ctx)) != GG_OK) return st;
+    const int64_t ld = (a->hidden + 63) / 64 * 64, f32_ld = (a->width + 31) / 32 * 32;
+    const int splits = a->dx ? product_splits(a->rows, a->width, a->hidden, 2, ctx->sm_count) : 1;
+    Operand x(matrix_of(a->x, a->rows, a->width, a->x_ld), s), wg(matrix_of(a->w_gate, a->hidden, a->width, a->w_gate_ld), s),
+        wu(matrix_of(a->w_up, a->hidden, a->width, a->w_up_ld), s);
+    const int64_t dgate_at = s.place(a->rows * ld * 2), dup_at = s.place(a->rows * ld * 2), f32_at = s.place(splits > 1 ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
+    if ((st = s.grow()) != GG_OK) return st;
+    if (a->dw_gate && (st = x.lay(s)) != GG_OK) return st;
+    if (a->dx && ((st = wg.lay(s)) != GG_OK || (st = wu.lay(s)) != GG_OK)) return st;
+    uint16_t *dgate = s.at<uint16_t>(dgate_at), *dup = s.at<uint16_t>(dup_at);
+    GG_CUDA(ctx, launch_gated_slopes(matrix_of(a->dh, a->rows, a->hidden, a->dh_ld), matrix_of(a->gate, a->rows, a->hidden, a->gate_ld),
+                                     matrix_of(a->up, a->rows, a->hidden, a->up_ld), a->act, dgate, dup, ld, s.st));
+    ctx->launches += 1;
+    ProductArgs p{};
+    p.segments = p.batches = p.splits = 1;
+    p.gave_up = ctx->gave_up;
+    p.a[0] = matrix_of(dgate, a->rows, a->hidden, ld);
+    p.a[1] = matrix_of(dup, a->rows, a->hidden, ld);
+    if (a->dx) {
+        ProductArgs q = p;
+        q.b[0] = wg.m;
+        q.b[1] = wu.m;
+        q.m = a->rows; q.n = a->width; q.k = a->hidden;
+        q.segments = 2;
+        q.splits = splits;
+        q.out[0] = static_cast<uint16_t *>(a->dx);
+        q.out_ld[0] = a->dx_ld;
+        q.f32 = s.at<float>(f32_at);
+        q.f32_ld = f32_ld;
+        q.mode = splits > 1 ? kStoreF32 : kStoreBf16;
+        GG_CUDA(ctx, launch_product_drows(q, ctx->sm_count, s.st));
+        ctx->launches += 1;
+        if (splits > 1) {
+            GG_CUDA(ctx, launch_sum_splits(q.f32, splits, a->rows, a->width, f32_ld, q.out[0], a->dx_ld, s.st));
+            ctx->launches += 1;
+        }
+    }
+    if (a->dw_gate) {
+        p.b[0] = p.b[1] = x.m;
+        p.m = a->hidden; p.n = a->width; p.k = a->rows;
+        p.batches = 2;
+        p.out[0] = static_cast<uint16_t *>(a->dw_gate);
+        p.out[1] = static_cast<uint16_t *>(a->dw_up);
+        p.out_ld[0] = a->dw_gate_ld;
+        p.out_ld[1] = a->dw_up_ld;
+        p.mode = a->accumulate ? kAddBf16 : kStoreBf16;
+        GG_CUDA(ctx, launch_product_dweight(p, ctx->sm_count, s.st));
+        ctx->launches += 1;
+    }
+    return GG_OK;
+}
+
+gg_status gg_dropout(gg_ctx *ctx, const gg_dropout_args *a, void *stream)
+{
+    if (!ctx || !a || a->rows < 0 || a->cols < 0 || !(a->p >= 0.0 && a->p < 1.0)) return GG_ERR_INVALID_ARG;
+    const uint32_t least = (uint32_t)(a->p * 65536.0 + 0.5);
+    if (least > 65535) return GG_ERR_INVALID_ARG;
+    if (!dtype_ok(a->dtype)) return GG_ERR_DTYPE;
+    gg_status st = check_matrix(a->x, a->rows, a->cols, a->x_ld, a->dtype);
+    if (st == GG_OK && a->residual) st = check_matrix(a->residual, a->rows, a->cols, a->residual_ld, a->dtype);
+    if (st == GG_OK) st = check_matrix(a->y, a->rows, a->cols, a->y_ld, a->dtype);
+    if (st == GG_OK && !on_boundary(a->t_dev, 8)) st = GG_ERR_ALIGNMENT;
+    if (st != GG_OK) return st;
+    if (a->rows == 0 || a->cols == 0) return GG_OK;
+    DeviceGuard guard(ctx->device);
+    if (!guard.ok) return GG_ERR_CUDA;
+    GG_CUDA(ctx, launch_dropout(*a, least, ctx->sm_count, static_cast<cudaStream_t>(stream)));
+    ctx->launches += 1;
+    return GG_OK;
 }
 
 }  // extern "C"

@@ -255,4 +255,8 @@ cudaError_t launch_layer_norm(const LayerNormArgs &a, int sm_count, cudaStream_t
 cudaError_t layer_norm_grad_slices(const LayerNormGradArgs &a, int sm_count, int *slices);
 cudaError_t launch_layer_norm_grad(const LayerNormGradArgs &a, float *part, int slices, int sm_count, int *launches, cudaStream_t st);
 
+// Dropout (gg_dropout.cu): the arguments of the interface, checked; an element with fewer than `least` of 65536 is dropped.
+using DropoutArgs = gg_dropout_args;
+cudaError_t launch_dropout(const DropoutArgs &a, uint32_t least, int sm_count, cudaStream_t st);
+
 }  // namespace gg
