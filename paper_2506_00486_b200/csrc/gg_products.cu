@@ -657,33 +657,35 @@ cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-constexpr int kCtasOf = 1, kTileN = 256;      // the tile of C: 128 rows for each CTA, so many columns
+constexpr int kTileN = 256;      // columns of C in a tile
+// Two CTAs for a tile of 256 rows, where there are more than one CTA's.
+int ctas_of(int64_t m) { return m > 128 ? 2 : 1; }
+
+template <bool kAT, bool kBT, int kEnd>
+cudaError_t launch_tiles(const ProductArgs &a, int sm_count, cudaStream_t st)
+{
+    return ctas_of(a.m) == 2 ? launch_product<2, kTileN, kAT, kBT, kEnd>(a, sm_count, st) : launch_product<1, kTileN, kAT, kBT, kEnd>(a, sm_count, st);
+}
 
 }  // namespace
 
 cudaError_t launch_product_rows(ProductEnd end, const ProductArgs &a, int sm_count, cudaStream_t st)
 {
-    if (end == kGated) return launch_product<kCtasOf, kTileN, false, false, kGated>(a, sm_count, st);
-    if (end == kLse) return launch_product<kCtasOf, kTileN, false, false, kLse>(a, sm_count, st);
-    if (end == kDlogits) return launch_product<kCtasOf, kTileN, false, false, kDlogits>(a, sm_count, st);
+    if (end == kGated) return launch_tiles<false, false, kGated>(a, sm_count, st);
+    if (end == kLse) return launch_tiles<false, false, kLse>(a, sm_count, st);
+    if (end == kDlogits) return launch_tiles<false, false, kDlogits>(a, sm_count, st);
     return cudaErrorInvalidValue;
 }
-cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st)
-{
-    return launch_product<kCtasOf, kTileN, false, true, kStore>(a, sm_count, st);
-}
-cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st)
-{
-    return launch_product<kCtasOf, kTileN, true, true, kStore>(a, sm_count, st);
-}
+cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st) { return launch_tiles<false, true, kStore>(a, sm_count, st); }
+cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st) { return launch_tiles<true, true, kStore>(a, sm_count, st); }
 
 int product_partials(int64_t, int64_t n) { return (int)(2 * ((n + kTileN - 1) / kTileN)); }
 
 int product_splits(int64_t m, int64_t n, int64_t k, int segments, int sm_count)
 {
     // as many as give every SM a tile, but at least 16 stages for each
-    const int64_t tiles = ((m + 128 * kCtasOf - 1) / (128 * kCtasOf)) * ((n + kTileN - 1) / kTileN);
-    const int64_t most = (k + kBlockK - 1) / kBlockK * segments / 16, want = sm_count / kCtasOf / (tiles > 0 ? tiles : 1);
+    const int64_t ctas = ctas_of(m), tiles = ((m + 128 * ctas - 1) / (128 * ctas)) * ((n + kTileN - 1) / kTileN);
+    const int64_t most = (k + kBlockK - 1) / kBlockK * segments / 16, want = sm_count / ctas / (tiles > 0 ? tiles : 1);
     const int64_t s = want < most ? want : most;
     return (int)(s < 1 ? 1 : s);
 }
