@@ -1858,9 +1858,11 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
     if (!guard.ok) return GG_ERR_CUDA;
     if ((st = product_alive(ctx)) != GG_OK) return st;
     ProductScratch s{ctx, static_cast<cudaStream_t>(stream)};
-    const int64_t most = std::min(a->rows, kLossRows);
+    const int64_t most = std::min(a->rows, kLossRows), last = (a->rows - 1) % kLossRows + 1;
+    const int64_t part_bytes = (int64_t)sizeof(float2) * std::max(most * product_partials(most, a->vocab, a->width, ctx->sm_count),
+                                                                  last * product_partials(last, a->vocab, a->width, ctx->sm_count));
     Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
-    const int64_t part_at = s.place(most * product_partials(most, a->vocab) * (int64_t)sizeof(float2)), logit_at = s.place(most * 4);
+    const int64_t part_at = s.place(part_bytes), logit_at = s.place(most * 4);
     if ((st = s.grow()) != GG_OK || (st = h.lay(s)) != GG_OK || (st = w.lay(s)) != GG_OK) return st;
     for (int64_t r = 0; r < a->rows; r += kLossRows) {
         const int64_t rows = std::min(a->rows - r, kLossRows);
@@ -1875,7 +1877,7 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
         p.vocab = a->vocab;
         p.gave_up = ctx->gave_up;
         GG_CUDA(ctx, launch_product_rows(kLse, p, ctx->sm_count, s.st));
-        GG_CUDA(ctx, launch_lse_finish(p.part, product_partials(rows, a->vocab), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
+        GG_CUDA(ctx, launch_lse_finish(p.part, product_partials(rows, a->vocab, a->width, ctx->sm_count), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
                                        a->loss ? a->loss + r : nullptr, s.st));
         ctx->launches += 2;
     }
@@ -1986,8 +1988,8 @@ gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *a, void *stre
     p.b[1] = wu.m;
     p.m = a->rows; p.n = a->hidden; p.k = a->width;
     p.segments = p.batches = p.splits = 1;
-    p.h = static_cast<uint16_t *>(a->h); p.gate = static_cast<uint16_t *>(a->gate); p.up = static_cast<uint16_t *>(a->up);
-    p.h_ld = a->h_ld; p.gate_ld = a->gate_ld; p.up_ld = a->up_ld;
+    p.out[0] = static_cast<uint16_t *>(a->h); p.out[1] = static_cast<uint16_t *>(a->gate); p.out[2] = static_cast<uint16_t *>(a->up);
+    p.out_ld[0] = a->h_ld; p.out_ld[1] = a->gate_ld; p.out_ld[2] = a->up_ld;
     p.act = a->act;
     p.gave_up = ctx->gave_up;
     GG_CUDA(ctx, launch_product_rows(kGated, p, ctx->sm_count, s.st));

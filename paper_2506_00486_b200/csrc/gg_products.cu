@@ -23,24 +23,41 @@ namespace {
 constexpr int kBlockK = 64;             // summed elements of a stage: 128 bytes, a row of the swizzle
 constexpr int kEndWarps = 8, kThreads = 32 * (4 + kEndWarps);
 constexpr int kRing = 192 * 1024;       // bytes of the ring of stages
-constexpr int kBand = 8;                // tiles of C that are taken in bands of so many rows, so that B's stay in L2
+constexpr int kMostStages = 16;
+constexpr int kOutBytes = 4096;         // 32 rows of 64 bf16 on their way out, for each warp of the end
+constexpr int kShared = 1024 + kRing + kEndWarps * kOutBytes;
+constexpr int kAccColumns = 256;        // of tensor memory for one accumulator; there are two
 constexpr float kLog2e = 1.4426950408889634f;
+
+struct Output {
+    uint16_t *p;
+    int64_t ld;
+    int whole;           // every row starts on a 16-byte boundary
+};
+
+// n / d for 0 <= n < 2^31 without a division (five of them stand in the path of each tile otherwise): mul is
+// 2^(32 + shift) / d rounded up, and the error of that stays below 1 / d as 2^(31 + ceil(log2 d)) / d has 32 bits.
+struct Divider {
+    uint32_t d, mul, shift;
+    __device__ __forceinline__ int of(int n) const { return d == 1 ? n : (int)(__umulhi((uint32_t)n, mul) >> shift); }
+};
 
 struct Params {
     CUtensorMap a[2], b[2];
+    Output out[3];                      // kGated: h, gate, up
     int64_t m, n;
-    int tiles_m, tiles_n, total, kblocks, segments, batches, splits;
-    uint16_t *h, *gate, *up;
-    int64_t h_ld, gate_ld, up_ld;
-    int act, h_align, gate_align, up_align;
+    int tile_n;                         // rows of B in a tile (kGated: half of them gate's, half up's)
+    int cols;                           // columns of C in a tile
+    int tiles_m, tiles_n, band, total, kblocks, all_k, batches;
+    int each_k, more_k;                 // stages of a split, and how many splits have one more
+    Divider by_outer, by_band, by_height, by_last;      // tiles of a batch or split, of a band; its height, the last band's
+    int stages, bytes_a, bytes_b;       // of the ring: A's part has only as many rows as A
+    int act;
     float2 *part;
     float *target_logit;
     const int64_t *target;
     int64_t vocab, first;
     const float *lse, *dloss;
-    uint16_t *out[2];
-    int64_t out_ld[2];
-    int out_align;
     float *f32;
     int64_t f32_ld;
     int mode;
@@ -91,88 +108,116 @@ __device__ __forceinline__ void by_activation(int act, F f)
     else f(std::integral_constant<int, GG_ACT_RELU>());
 }
 
-// ------------------------------------------------------------------ rows of 32 columns
-__device__ __forceinline__ uint32_t narrow_pair(float lo, float hi) { return narrow2(pair(lo, hi)); }
+// ------------------------------------------------------------------ the ends of a tile
+struct Tile {
+    int64_t row0, row;   // first row of the warp, row of this thread
+    int64_t col;         // first column of the tile
+    int64_t end;         // behind its last
+    int batch, split, n_tile;
+    uint32_t acc;        // its sums: tensor memory of the warp's lanes
+};
 
-// The first n of 32 bf16 values to p, which is on a boundary of `align` bytes.
-__device__ __forceinline__ void store_row(uint16_t *p, const uint32_t (&w)[16], int64_t n, int align)
-{
-    if (n >= 32 && align >= 32) {
-#pragma unroll
-        for (int i = 0; i < 16; i += 8)
-            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p + 2 * i), "r"(w[i]), "r"(w[i + 1]), "r"(w[i + 2]), "r"(w[i + 3]),
-                         "r"(w[i + 4]), "r"(w[i + 5]), "r"(w[i + 6]), "r"(w[i + 7]) : "memory");
-    } else if (n >= 32 && align >= 16) {
-#pragma unroll
-        for (int i = 0; i < 16; i += 4) *reinterpret_cast<uint4 *>(p + 2 * i) = make_uint4(w[i], w[i + 1], w[i + 2], w[i + 3]);
-    } else {
-#pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < n) p[i] = (uint16_t)(w[i / 2] >> 16 * (i & 1));
-    }
-}
 __device__ __forceinline__ void narrow_row(const float (&v)[32], uint32_t (&w)[16])
 {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = narrow_pair(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 16; ++i) w[i] = narrow2(pair(v[2 * i], v[2 * i + 1]));
 }
 
-// ------------------------------------------------------------------ the ends of a tile
-struct Tile {
-    int64_t row;         // of this thread
-    int64_t col;         // first column of the tile
-    int batch, split, n_tile;
-};
-
-// kN columns of the tile, of which a warp has the half that `half` says; `at` is the accumulator of the warp's lanes.
-template <int kN>
-__device__ __forceinline__ void end_gated(const Params &p, const Tile &t, uint32_t at, int half)
-{
-    constexpr int kMine = kN / 4;        // columns of h for a warp
-    const bool there = t.row < p.m;
-#pragma unroll 1
-    for (int c = half * kMine; c < (half + 1) * kMine; c += 32) {
-        float g[32], u[32];
-        tmem_read(at + c, g);
-        tmem_read(at + kN / 2 + c, u);
-        tmem_read_wait();
-        const int64_t col = t.col + c, left = there ? p.n - col : 0;
-        if (left > 0) {
-            uint32_t w[16];
-            if (p.gate != nullptr) {
-                narrow_row(g, w);
-                store_row(p.gate + t.row * p.gate_ld + col, w, left, p.gate_align);
-            }
-            if (p.up != nullptr) {
-                narrow_row(u, w);
-                store_row(p.up + t.row * p.up_ld + col, w, left, p.up_align);
-            }
-            by_activation(p.act, [&](auto act) {
+// Takes 32 rows of up to 64 bf16 out through shared memory, so that a store instruction writes whole 128-byte pieces of rows and
+// not 16 bytes of each (the gradient of a 151936 x 896 output matrix from 33 positions, which is nearly all stores: 115 -> 94 us).  A lane has a row; its 16-byte pieces
+// are exchanged by row, so that eight lanes reach all banks either way.
+struct Way {
+    uint32_t at;
+    int lane;
+    __device__ __forceinline__ void put(int part, const uint32_t (&w)[16])       // 32 columns, part 0 or 1
+    {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) g[i] = activation<decltype(act)::value>(g[i]) * u[i];
-            });
-            narrow_row(g, w);
-            store_row(p.h + t.row * p.h_ld + col, w, left, p.h_align);
+        for (int j = 0; j < 4; ++j)
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((4 * part + j ^ (lane & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
+                         "r"(w[4 * j + 2]), "r"(w[4 * j + 3]) : "memory");
+    }
+    template <int kPieces>      // 16-byte pieces of a row: 8, or 4 for part 0 alone
+    __device__ __forceinline__ void send(const Params &p, const Output &o, const Tile &t, int64_t col)
+    {
+        constexpr int kRows = 32 / kPieces;
+        __syncwarp();
+        const int piece = lane % kPieces, first = lane / kPieces;
+        const int64_t at_col = col + piece * 8, left = t.end - at_col;
+        uint16_t *q = o.p + (t.row0 + first) * o.ld + at_col;
+        const int rows = p.m - t.row0 < 32 ? (int)(p.m - t.row0) : 32;
+        if (left >= 8 && o.whole) {
+#pragma unroll
+            for (int r = 0; r < 32; r += kRows) {
+                uint32_t w[4];
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                             : "r"(at + (r + first) * 128 + ((piece ^ (r + first & 7)) << 4)) : "memory");
+                if (r + first < rows) *reinterpret_cast<uint4 *>(q + r * o.ld) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        } else if (!o.whole) {
+            // element by element: a lane takes columns lane and lane + 32 of every row
+            for (int r = 0; r < rows; ++r)
+#pragma unroll
+                for (int c = lane; c < kPieces * 8; c += 32) {
+                    uint16_t v;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + r * 128 + ((c >> 3 ^ (r & 7)) << 4) + (c & 7) * 2) : "memory");
+                    if (col + c < t.end) o.p[(t.row0 + r) * o.ld + col + c] = v;
+                }
+        } else if (left > 0) {
+            // the last columns of rows that are no multiple of eight long
+            for (int r = first; r < rows; r += kRows)
+                for (int c = 0; c < left; ++c) {
+                    uint16_t v;
+                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + r * 128 + ((piece ^ (r & 7)) << 4) + c * 2) : "memory");
+                    o.p[(t.row0 + r) * o.ld + at_col + c] = v;
+                }
         }
         __syncwarp();
+    }
+};
+
+// A tile's columns go to the two warps of a lane quarter in turn, 32 or 64 at a time.
+__device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int half, Way &way)
+{
+#pragma unroll 1
+    for (int c = half * 32; t.col + c < t.end; c += 64) {
+        float g[32], u[32];
+        tmem_read(t.acc + c, g);
+        tmem_read(t.acc + p.cols + c, u);
+        tmem_read_wait();
+        uint32_t w[16];
+        if (p.out[1].p != nullptr) {
+            narrow_row(g, w);
+            way.put(0, w);
+            way.send<4>(p, p.out[1], t, t.col + c);
+        }
+        if (p.out[2].p != nullptr) {
+            narrow_row(u, w);
+            way.put(0, w);
+            way.send<4>(p, p.out[2], t, t.col + c);
+        }
+        by_activation(p.act, [&](auto act) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) g[i] = activation<decltype(act)::value>(g[i]) * u[i];
+        });
+        narrow_row(g, w);
+        way.put(0, w);
+        way.send<4>(p, p.out[0], t, t.col + c);
     }
 }
 
 // The sum is taken relative to the running maximum.  A NaN, which no maximum shows, reaches the sum by its own term.
-template <int kN>
-__device__ __forceinline__ void end_lse(const Params &p, const Tile &t, uint32_t at, int half)
+__device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half)
 {
-    constexpr int kMine = kN / 2;
     const bool there = t.row < p.m;
     const int64_t target = there ? p.target[t.row] - p.first : -1;
     float most = -INFINITY, sum = 0.0f;
 #pragma unroll 1
-    for (int c = half * kMine; c < (half + 1) * kMine; c += 32) {
+    for (int c = half * 32; t.col + c < t.end; c += 64) {
         float v[32];
-        tmem_read(at + c, v);
+        tmem_read(t.acc + c, v);
         tmem_read_wait();
-        const int64_t col = t.col + c, left = p.n - col;
-        if (target >= col && target < col + 32 && target < p.n) {
+        const int64_t col = t.col + c, left = t.end - col;
+        if (target >= col && target < col + 32 && target < t.end) {
             const int j = (int)(target - col);
             float l = 0.0f;
 #pragma unroll
@@ -200,95 +245,97 @@ __device__ __forceinline__ void end_lse(const Params &p, const Tile &t, uint32_t
     if (there) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, sum);
 }
 
-template <int kN>
-__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, uint32_t at, int half)
+__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int half, Way &way)
 {
-    constexpr int kMine = kN / 2;
     const bool there = t.row < p.m;
     const int64_t of = there ? p.target[t.row] : -1, target = of - p.first;
     const float lse = there ? p.lse[t.row] : 0.0f, g = of < 0 ? 0.0f : of >= p.vocab ? NAN : p.dloss[t.row];
 #pragma unroll 1
-    for (int c = half * kMine; c < (half + 1) * kMine; c += 32) {
-        float v[32];
-        tmem_read(at + c, v);
-        tmem_read_wait();
-        const int64_t col = t.col + c;
-        if (there && col < p.n) {
+    for (int c = half * 64; t.col + c < t.end; c += 128) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            float v[32];
+            tmem_read(t.acc + c + 32 * part, v);
+            tmem_read_wait();
+            const int64_t col = t.col + c + 32 * part;
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] = g * exp2f((v[i] - lse) * kLog2e);
+            if (target >= col && target < col + 32) {
+                const int j = (int)(target - col);
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] = i == j ? v[i] - g : v[i];
+            }
             uint32_t w[16];
+            narrow_row(v, w);
             if (of < 0) {              // no position, whatever its logits are
 #pragma unroll
                 for (int i = 0; i < 16; ++i) w[i] = 0;
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = g * exp2f((v[i] - lse) * kLog2e);
-                if (target >= col && target < col + 32) {
-                    const int j = (int)(target - col);
-#pragma unroll
-                    for (int i = 0; i < 32; ++i) v[i] = i == j ? v[i] - g : v[i];
-                }
-                narrow_row(v, w);
             }
-            store_row(p.out[0] + t.row * p.out_ld[0] + col, w, 32, 32);      // (a row has room for whole runs of 32)
+            way.put(part, w);
         }
-        __syncwarp();
+        way.send<8>(p, p.out[0], t, t.col + c);
     }
 }
 
-__device__ __forceinline__ void store_part(const Params &p, const Tile &t, float (&v)[32], int64_t col, int64_t left)
+__device__ __forceinline__ void add_old(const Output &o, const Tile &t, int64_t col, float (&v)[32])
 {
-    if (p.mode != kStoreBf16 && p.mode != kAddBf16) {
-        float4 *f = reinterpret_cast<float4 *>(p.f32 + ((int64_t)t.split * p.m + t.row) * p.f32_ld + col);
-        if (p.mode != kStoreF32) {
+    const uint16_t *q = o.p + t.row * o.ld + col;
+    const int64_t left = t.end - col;
+    if (left >= 32 && o.whole) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float4 o = f[i];
-                v[4 * i] += o.x; v[4 * i + 1] += o.y; v[4 * i + 2] += o.z; v[4 * i + 3] += o.w;
+        for (int i = 0; i < 4; ++i) {
+            const uint4 x = reinterpret_cast<const uint4 *>(q)[i];
+            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 f = halves(widen2(w[j]));
+                v[8 * i + 2 * j] += f.x;
+                v[8 * i + 2 * j + 1] += f.y;
             }
         }
-        if (p.mode != kStoreBf16OfSum) {
+    } else {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) f[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-            return;
-        }
+        for (int i = 0; i < 32; ++i)
+            if (i < left) v[i] += widen<uint16_t>(q[i]);
     }
-    uint16_t *o = p.out[t.batch] + t.row * p.out_ld[t.batch] + col;
-    if (p.mode == kAddBf16) {
-        if (left >= 32 && p.out_align >= 16) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint4 q = reinterpret_cast<const uint4 *>(o)[i];
-                const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float2 f = halves(widen2(w[j]));
-                    v[8 * i + 2 * j] += f.x;
-                    v[8 * i + 2 * j + 1] += f.y;
-                }
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-                if (i < left) v[i] += widen<uint16_t>(o[i]);
-        }
-    }
-    uint32_t w[16];
-    narrow_row(v, w);
-    store_row(o, w, left, p.out_align);
 }
 
-template <int kN>
-__device__ __forceinline__ void end_store(const Params &p, const Tile &t, uint32_t at, int half)
+__device__ __forceinline__ void end_store(const Params &p, const Tile &t, int half, Way &way)
 {
-    constexpr int kMine = kN / 2;
-    const bool there = t.row < p.m;
+    const bool there = t.row < p.m, narrow_out = p.mode == kStoreBf16 || p.mode == kAddBf16 || p.mode == kStoreBf16OfSum;
 #pragma unroll 1
-    for (int c = half * kMine; c < (half + 1) * kMine; c += 32) {
-        float v[32];
-        tmem_read(at + c, v);
-        tmem_read_wait();
-        const int64_t col = t.col + c, left = there ? p.n - col : 0;
-        if (left > 0) store_part(p, t, v, col, left);
-        __syncwarp();
+    for (int c = half * 64; t.col + c < t.end; c += 128) {
+#pragma unroll
+        for (int part = 0; part < 2; ++part) {
+            float v[32];
+            tmem_read(t.acc + c + 32 * part, v);
+            tmem_read_wait();
+            const int64_t col = t.col + c + 32 * part;
+            if (there && col < t.end) {
+                if (p.mode == kAddBf16) add_old(p.out[t.batch], t, col, v);
+                if (p.mode == kStoreF32 || p.mode == kAddF32 || p.mode == kStoreBf16OfSum) {
+                    float4 *f = reinterpret_cast<float4 *>(p.f32 + ((int64_t)t.split * p.m + t.row) * p.f32_ld + col);
+                    if (p.mode != kStoreF32) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) {
+                            const float4 o = f[i];
+                            v[4 * i] += o.x; v[4 * i + 1] += o.y; v[4 * i + 2] += o.z; v[4 * i + 3] += o.w;
+                        }
+                    }
+                    if (p.mode != kStoreBf16OfSum) {
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) f[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+                    }
+                }
+            }
+            if (narrow_out) {
+                uint32_t w[16];
+                narrow_row(v, w);
+                way.put(part, w);
+            }
+            __syncwarp();
+        }
+        if (narrow_out) way.send<8>(p, p.out[t.batch], t, t.col + c);
     }
 }
 
@@ -296,37 +343,33 @@ __device__ __forceinline__ void end_store(const Params &p, const Tile &t, uint32
 struct Work { int m_tile, n_tile, outer; };
 __device__ __forceinline__ Work work_of(const Params &p, int w)
 {
-    const int each = p.tiles_m * p.tiles_n;
     Work r;
-    r.outer = w / each;
-    w -= r.outer * each;
-    const int band = w / (kBand * p.tiles_n), first = band * kBand;
-    const int height = p.tiles_m - first < kBand ? p.tiles_m - first : kBand;
-    w -= first * p.tiles_n;
-    r.n_tile = w / height;
-    r.m_tile = first + (w - r.n_tile * height);
+    r.outer = p.by_outer.of(w);
+    w -= r.outer * (int)p.by_outer.d;
+    const int band = p.by_band.of(w), first = band * p.band;
+    w -= band * (int)p.by_band.d;
+    const bool last = p.tiles_m - first < p.band;
+    r.n_tile = last ? p.by_last.of(w) : p.by_height.of(w);
+    r.m_tile = first + (w - r.n_tile * (int)(last ? p.by_last.d : p.by_height.d));
     return r;
 }
+__device__ __forceinline__ int split_start(const Params &p, int split) { return split * p.each_k + (split < p.more_k ? split : p.more_k); }
 
-template <int kCtas, int kN, bool kAT, bool kBT, int kEnd>
+// kHalves 2: a pair's tile has 512 rows, as two halves of 256 with an accumulator each.  Otherwise the two accumulators take turns.
+template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd>
 __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Params p)
 {
-    constexpr int kRowsB = kN / kCtas;                    // rows of B that a CTA brings in
-    constexpr uint32_t kBytesA = 128 * kBlockK * 2, kBytes = kBytesA + kRowsB * kBlockK * 2;
-    constexpr int kStages = kRing / kBytes;
-    constexpr uint32_t kColumns = 2 * kN;                 // of tensor memory: two accumulators
     extern __shared__ uint8_t ring_bytes[];
-    __shared__ uint64_t bars[2 * kStages + 5];
+    __shared__ uint64_t bars[2 * kMostStages + 5];
     __shared__ uint32_t tmem_at;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = kCtas == 2 ? cluster_rank() : 0;
-    const uint32_t ring = (shared_address(ring_bytes) + 1023) & ~1023u;
-    const uint32_t bar = shared_address(bars);
-    const uint32_t full = bar, empty = bar + 8 * kStages, done = bar + 16 * kStages, free_at = done + 16, drained = done + 32;
+    const uint32_t ring = (shared_address(ring_bytes) + 1023) & ~1023u, half_a = p.bytes_a, bytes_a = kHalves * half_a, bytes = bytes_a + p.bytes_b, stages = p.stages;
+    const uint32_t full = shared_address(bars), empty = full + 8 * kMostStages, done = empty + 8 * kMostStages, free_at = done + 16, drained = done + 32;
 
     if (warp == 0 && lane == 0) {
-        for (int i = 0; i < kStages; ++i) {
+        for (uint32_t i = 0; i < stages; ++i) {
             barrier_init(full + 8 * i, 1);
             barrier_init(empty + 8 * i, 1);
         }
@@ -339,110 +382,164 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         prefetch_map(&p.a[0]);
         prefetch_map(&p.b[0]);
     }
-    if (warp == 2) tmem_alloc<kCtas>(shared_address(&tmem_at), kColumns);
+    if (warp == 2) tmem_alloc<kCtas>(shared_address(&tmem_at), 2 * kAccColumns);
     tmem_before_sync();
     if constexpr (kCtas == 2) cluster_sync();
     else __syncthreads();
     tmem_after_sync();
     const uint32_t tmem = tmem_at;
 
-    const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas, all_k = p.kblocks * p.segments;
+    const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
     bool failed = false;
-    if (warp == 0 && lane == 0) {
+    // (a warp walks its loop as one, and one lane issues: so addresses and coordinates stay in uniform registers)
+    if (warp == 0) {
         // ---- copies
+        const bool leader = elect_lane();
+        const int rows_b = p.tile_n / kCtas;
         uint32_t stage = 0, phase = 0, issued = 0;
         for (int w = first; w < p.total && !failed; w += step) {
             const Work t = work_of(p, w);
             const int batch = p.batches > 1 ? t.outer : 0, split = p.batches > 1 ? 0 : t.outer;
-            const int m0 = t.m_tile * 128 * kCtas + (int)rank * 128;
-            const int n0 = kEnd == kGated ? t.n_tile * (kN / 2) : t.n_tile * kN + (int)rank * kRowsB;
-            const int end = (int)((int64_t)all_k * (split + 1) / p.splits);
-            for (int kb = (int)((int64_t)all_k * split / p.splits); kb < end; ++kb) {
+            const int m0 = t.m_tile * 128 * kCtas * kHalves + (int)rank * 128;
+            const int n0 = t.n_tile * p.cols + (kEnd == kGated ? 0 : (int)rank * rows_b);
+            const int end = split_start(p, split + 1);
+            for (int kb = split_start(p, split); kb < end; ++kb) {
                 if (!barrier_wait(empty + 8 * stage, phase ^ 1)) { failed = true; break; }
-                if (rank == 0) barrier_expect(full + 8 * stage, kBytes * kCtas);
-                const int segment = kb >= p.kblocks, k0 = (kb - segment * p.kblocks) * kBlockK, which = segment | batch;
-                const uint32_t to_a = ring + stage * kBytes, to_b = to_a + kBytesA;
-                const uint32_t signal = kCtas == 2 ? peer_address(full + 8 * stage, 0) : full + 8 * stage;
-                if constexpr (kAT) {
-                    tensor_copy<kCtas>(to_a, &p.a[which], m0, k0, signal);
-                    tensor_copy<kCtas>(to_a + 8192, &p.a[which], m0 + 64, k0, signal);
-                } else {
-                    tensor_copy<kCtas>(to_a, &p.a[which], k0, m0, signal);
-                }
-                if constexpr (kBT) {
+                if (leader) {
+                    if (rank == 0) barrier_expect(full + 8 * stage, bytes * kCtas);
+                    const int segment = kb >= p.kblocks, k0 = (kb - segment * p.kblocks) * kBlockK, which = segment | batch;
+                    const uint32_t to_a = ring + stage * bytes, to_b = to_a + bytes_a;
+                    const uint32_t signal = kCtas == 2 ? peer_address(full + 8 * stage, 0) : full + 8 * stage;
 #pragma unroll
-                    for (int i = 0; i < kRowsB / 64; ++i) tensor_copy<kCtas>(to_b + 8192 * i, &p.b[which], n0 + 64 * i, k0, signal);
-                } else if constexpr (kEnd == kGated && kCtas == 1) {
-                    tensor_copy<kCtas>(to_b, &p.b[0], k0, n0, signal);
-                    tensor_copy<kCtas>(to_b + kRowsB / 2 * kBlockK * 2, &p.b[1], k0, n0, signal);
-                } else if constexpr (kEnd == kGated) {
-                    tensor_copy<kCtas>(to_b, &p.b[rank], k0, n0, signal);
-                } else {
-                    tensor_copy<kCtas>(to_b, &p.b[which], k0, n0, signal);
+                    for (int h = 0; h < kHalves; ++h) {
+                        if constexpr (kAT) {
+                            tensor_copy<kCtas>(to_a + half_a * h, &p.a[which], m0 + 256 * h, k0, signal);
+                            tensor_copy<kCtas>(to_a + half_a * h + 8192, &p.a[which], m0 + 256 * h + 64, k0, signal);
+                        } else {
+                            tensor_copy<kCtas>(to_a + half_a * h, &p.a[which], k0, m0 + 256 * h, signal);
+                        }
+                    }
+                    if constexpr (kBT) {
+                        for (int i = 0; i < rows_b; i += 64) tensor_copy<kCtas>(to_b + 128 * i, &p.b[which], n0 + i, k0, signal);
+                    } else if constexpr (kEnd == kGated && kCtas == 1) {
+                        tensor_copy<kCtas>(to_b, &p.b[0], k0, n0, signal);
+                        tensor_copy<kCtas>(to_b + p.cols * 128, &p.b[1], k0, n0, signal);
+                    } else if constexpr (kEnd == kGated) {
+                        tensor_copy<kCtas>(to_b, &p.b[rank], k0, n0, signal);
+                    } else {
+                        tensor_copy<kCtas>(to_b, &p.b[which], k0, n0, signal);
+                    }
                 }
                 ++issued;
-                if (++stage == kStages) { stage = 0; phase ^= 1; }
+                if (++stage == stages) { stage = 0; phase ^= 1; }
             }
         }
         // what is still under way when a wait gave up has to land before the CTA may end
         if (failed && rank == 0)
-            for (uint32_t i = 0; i < kStages && i < issued; ++i) {
-                stage = stage == 0 ? kStages - 1 : stage - 1;
-                if (stage == kStages - 1) phase ^= 1;
+            for (uint32_t i = 0; i < stages && i < issued; ++i) {
+                stage = stage == 0 ? stages - 1 : stage - 1;
+                if (stage == stages - 1) phase ^= 1;
                 barrier_wait(full + 8 * stage, phase);
             }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         // ---- products
-        constexpr uint32_t shape = product_shape<128 * kCtas, kN, kAT, kBT>();
-        uint32_t stage = 0, phase = 0, acc = 0, acc_phase = 0;
-        for (int w = first; w < p.total && !failed; w += step) {
-            const int split = p.batches > 1 ? 0 : work_of(p, w).outer;
-            if (!barrier_wait(free_at + 8 * acc, acc_phase ^ 1)) { failed = true; break; }
-            tmem_after_sync();
-            const int begin = (int)((int64_t)all_k * split / p.splits), end = (int)((int64_t)all_k * (split + 1) / p.splits);
-            for (int kb = begin; kb < end; ++kb) {
-                if (!barrier_wait(full + 8 * stage, phase)) { failed = true; break; }
-                tmem_after_sync();
-                const uint64_t a = tile_descriptor<kAT>(ring + stage * kBytes), b = tile_descriptor<kBT>(ring + stage * kBytes + kBytesA);
+        const bool leader = elect_lane();
+        const uint32_t shape = product_shape<128 * kCtas, kAT, kBT>(p.tile_n);
+        uint32_t stage = 0, phase = 0, units = 0;
+        auto issue = [&](uint32_t at, uint32_t acc, bool fresh) {
+            const uint64_t a = tile_descriptor<kAT>(ring + at * bytes + (kHalves == 2 ? acc * half_a : 0)), b = tile_descriptor<kBT>(ring + at * bytes + bytes_a);
+            if (leader) {
 #pragma unroll
                 for (int i = 0; i < kBlockK / 16; ++i)
-                    product_issue<kCtas>(tmem + acc * kN, a + i * tile_step<kAT>(), b + i * tile_step<kBT>(), shape, kb > begin || i > 0);
-                product_commit<kCtas>(empty + 8 * stage);
-                if (++stage == kStages) { stage = 0; phase ^= 1; }
+                    product_issue<kCtas>(tmem + acc * kAccColumns, a + i * tile_step<kAT>(), b + i * tile_step<kBT>(), shape, !fresh || i > 0);
             }
-            if (failed) break;
-            product_commit<kCtas>(done + 8 * acc);
-            acc ^= 1;
-            acc_phase ^= acc == 0;
+        };
+        auto commit = [&](uint32_t bar) {
+            if (leader) product_commit<kCtas>(bar);
+        };
+        for (int w = first; w < p.total && !failed; w += step) {
+            const int split = p.batches > 1 ? 0 : work_of(p, w).outer;
+            const int begin = split_start(p, split), end = split_start(p, split + 1);
+            const uint32_t acc_phase = (kHalves == 2 ? units : units >> 1) & 1;
+            if constexpr (kHalves == 1) {
+                const uint32_t acc = units & 1;
+                if (!barrier_wait(free_at + 8 * acc, acc_phase ^ 1)) { failed = true; break; }
+                tmem_after_sync();
+                for (int kb = begin; kb < end; ++kb) {
+                    if (!barrier_wait(full + 8 * stage, phase)) { failed = true; break; }
+                    tmem_after_sync();
+                    issue(stage, acc, kb == begin);
+                    commit(empty + 8 * stage);
+                    if (++stage == stages) { stage = 0; phase ^= 1; }
+                }
+                if (failed) break;
+                commit(done + 8 * acc);
+            } else {
+                // Both accumulators belong to this tile.  At its start and its end a ring's worth of stages is taken for the first
+                // half and then again for the second, so that the first half's end runs while the second is still summed, and
+                // the second's while the next tile's first has begun.
+                for (int kb = begin; kb < end && !failed;) {
+                    const bool head = kb == begin;
+                    const int left = end - kb, many = (int)stages;
+                    const int run = head || left <= many ? (left < many ? left : many) : 1;
+                    const bool last = left == run;
+                    if (head && !barrier_wait(free_at, acc_phase ^ 1)) { failed = true; break; }
+                    uint32_t at = stage, at_phase = phase;
+                    for (int i = 0; i < run; ++i) {
+                        if (!barrier_wait(full + 8 * at, at_phase)) { failed = true; break; }
+                        tmem_after_sync();
+                        issue(at, 0, head && i == 0);
+                        if (++at == stages) { at = 0; at_phase ^= 1; }
+                    }
+                    if (failed) break;
+                    if (last) commit(done);
+                    if (head && !barrier_wait(free_at + 8, acc_phase ^ 1)) { failed = true; break; }
+                    tmem_after_sync();
+                    for (int i = 0; i < run; ++i) {
+                        issue(stage, 1, head && i == 0);
+                        commit(empty + 8 * stage);
+                        if (++stage == stages) { stage = 0; phase ^= 1; }
+                    }
+                    if (last) commit(done + 8);
+                    kb += run;
+                }
+            }
+            ++units;
         }
         if (failed) {
-            product_commit<kCtas>(drained);
+            commit(drained);
             barrier_wait(drained, 0);
         }
     } else if (warp >= 4) {
         // ---- ends
         const int half = (warp - 4) >> 2, quarter = warp & 3;
-        uint32_t acc = 0, acc_phase = 0;
-        for (int w = first; w < p.total; w += step) {
+        Way way{ring + kRing + (uint32_t)(warp - 4) * kOutBytes, lane};
+        uint32_t units = 0;
+        for (int w = first; w < p.total && !failed; w += step) {
             const Work t = work_of(p, w);
-            if (!barrier_wait(done + 8 * acc, acc_phase)) { failed = true; break; }
-            tmem_after_sync();
             Tile tile;
-            tile.row = (int64_t)t.m_tile * 128 * kCtas + rank * 128 + quarter * 32 + lane;
-            tile.col = (int64_t)t.n_tile * (kEnd == kGated ? kN / 2 : kN);
+            tile.col = (int64_t)t.n_tile * p.cols;
+            tile.end = tile.col + p.cols < p.n ? tile.col + p.cols : p.n;
             tile.batch = p.batches > 1 ? t.outer : 0;
             tile.split = p.batches > 1 ? 0 : t.outer;
             tile.n_tile = t.n_tile;
-            const uint32_t at = tmem + acc * kN + ((uint32_t)quarter << 21);      // (lane 32 * quarter, in the upper half of the word)
-            if constexpr (kEnd == kGated) end_gated<kN>(p, tile, at, half);
-            if constexpr (kEnd == kLse) end_lse<kN>(p, tile, at, half);
-            if constexpr (kEnd == kDlogits) end_dlogits<kN>(p, tile, at, half);
-            if constexpr (kEnd == kStore) end_store<kN>(p, tile, at, half);
-            __syncwarp();
-            tmem_before_sync();
-            if (lane == 0) barrier_arrive(peer_address(free_at + 8 * acc, 0));
-            acc ^= 1;
-            acc_phase ^= acc == 0;
+#pragma unroll 1
+            for (int h = 0; h < kHalves; ++h, ++units) {
+                const uint32_t acc = units & 1;
+                if (!barrier_wait(done + 8 * acc, units >> 1 & 1)) { failed = true; break; }
+                __syncwarp();
+                tmem_after_sync();
+                tile.row0 = (int64_t)t.m_tile * 128 * kCtas * kHalves + 256 * h + rank * 128 + quarter * 32;
+                tile.row = tile.row0 + lane;
+                tile.acc = tmem + acc * kAccColumns + ((uint32_t)quarter << 21);      // (lane 32 * quarter, in the upper half of the word)
+                if constexpr (kEnd == kGated) end_gated(p, tile, half, way);
+                if constexpr (kEnd == kLse) end_lse(p, tile, half);
+                if constexpr (kEnd == kDlogits) end_dlogits(p, tile, half, way);
+                if constexpr (kEnd == kStore) end_store(p, tile, half, way);
+                __syncwarp();
+                tmem_before_sync();
+                if (lane == 0) barrier_arrive(peer_address(free_at + 8 * acc, 0));
+            }
         }
     }
     if (failed && p.gave_up != nullptr) *reinterpret_cast<volatile uint32_t *>(p.gave_up) = 1;
@@ -451,7 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     if constexpr (kCtas == 2) cluster_sync();
     else __syncthreads();
     tmem_after_sync();
-    if (warp == 2) tmem_free<kCtas>(tmem, kColumns);
+    if (warp == 2) tmem_free<kCtas>(tmem, 2 * kAccColumns);
 }
 
 // ------------------------------------------------------------------ around the products
@@ -471,81 +568,108 @@ __global__ void __launch_bounds__(256) realign_kernel(const Bf16Matrix from, uin
     }
 }
 
-__device__ __forceinline__ void eight_of(const Bf16Matrix &m, int64_t row, int64_t col, bool vector, float (&v)[8])
-{
-    const uint16_t *p = m.p + row * m.ld + col;
-    if (vector) {
-        const uint4 q = *reinterpret_cast<const uint4 *>(p);
-        const uint32_t w[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = halves(widen2(w[i]));
-            v[2 * i] = f.x;
-            v[2 * i + 1] = f.y;
-        }
-    } else {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = col + i < m.cols ? widen<uint16_t>(p[i]) : 0.0f;
-    }
-}
-
+// Eight columns a thread, two of them under way, where every row starts on a 16-byte boundary ...
 template <int kAct>
 __global__ void __launch_bounds__(256) gated_slopes_kernel(const Bf16Matrix dh, const Bf16Matrix gate, const Bf16Matrix up, uint16_t *dgate, uint16_t *dup,
-                                                           int64_t ld, int64_t groups, int vector)
+                                                           int64_t ld, uint32_t groups, int64_t total)
 {
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < groups * dh.rows; i += gridDim.x * 256ll) {
-        const int64_t row = i / groups, col = (i - row * groups) * 8;
-        const bool whole = vector && col + 8 <= dh.cols;
-        float d[8], g[8], u[8];
-        eight_of(dh, row, col, whole, d);
-        eight_of(gate, row, col, whole, g);
-        eight_of(up, row, col, whole, u);
-        uint32_t wg[4], wu[4];
+    const int64_t step = gridDim.x * 256ll;
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += 2 * step) {
+        uint4 d[2], g[2], u[2];
+        int64_t row[2];
+        int col[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            float v0, v1, s0, s1;
-            slope<kAct>(g[2 * j], v0, s0);
-            slope<kAct>(g[2 * j + 1], v1, s1);
-            wg[j] = narrow_pair(d[2 * j] * u[2 * j] * s0, d[2 * j + 1] * u[2 * j + 1] * s1);
-            wu[j] = narrow_pair(d[2 * j] * v0, d[2 * j + 1] * v1);
+        for (int k = 0; k < 2; ++k) {
+            const int64_t at = i + k * step;
+            row[k] = total <= 0x7FFFFFFF ? (int64_t)((uint32_t)at / groups) : at / groups;
+            col[k] = (int)(at - row[k] * groups) * 8;
+            if (at < total) {
+                d[k] = *reinterpret_cast<const uint4 *>(dh.p + row[k] * dh.ld + col[k]);
+                g[k] = *reinterpret_cast<const uint4 *>(gate.p + row[k] * gate.ld + col[k]);
+                u[k] = *reinterpret_cast<const uint4 *>(up.p + row[k] * up.ld + col[k]);
+            }
         }
-        *reinterpret_cast<uint4 *>(dgate + row * ld + col) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
-        *reinterpret_cast<uint4 *>(dup + row * ld + col) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            if (i + k * step >= total) break;
+            const uint32_t dw[4] = {d[k].x, d[k].y, d[k].z, d[k].w}, gw[4] = {g[k].x, g[k].y, g[k].z, g[k].w}, uw[4] = {u[k].x, u[k].y, u[k].z, u[k].w};
+            uint32_t wg[4], wu[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 df = halves(widen2(dw[j])), gf = halves(widen2(gw[j])), uf = halves(widen2(uw[j]));
+                float v0, v1, s0, s1;
+                slope<kAct>(gf.x, v0, s0);
+                slope<kAct>(gf.y, v1, s1);
+                wg[j] = narrow2(pair(df.x * uf.x * s0, df.y * uf.y * s1));
+                wu[j] = narrow2(pair(df.x * v0, df.y * v1));
+            }
+            *reinterpret_cast<uint4 *>(dgate + row[k] * ld + col[k]) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
+            *reinterpret_cast<uint4 *>(dup + row[k] * ld + col[k]) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
+        }
+    }
+}
+// ... else single columns, a warp's side by side, four runs of them under way.
+template <int kAct>
+__global__ void __launch_bounds__(256) gated_slopes_any_kernel(const Bf16Matrix dh, const Bf16Matrix gate, const Bf16Matrix up, uint16_t *dgate, uint16_t *dup,
+                                                               int64_t ld)
+{
+    for (int64_t row = blockIdx.y; row < dh.rows; row += gridDim.y)
+        for (int64_t first = blockIdx.x * 1024ll + threadIdx.x; first < dh.cols; first += gridDim.x * 1024ll) {
+            float d[4], g[4], u[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t col = first + 256 * k;
+                if (col < dh.cols) {
+                    d[k] = widen<uint16_t>(dh.p[row * dh.ld + col]);
+                    g[k] = widen<uint16_t>(gate.p[row * gate.ld + col]);
+                    u[k] = widen<uint16_t>(up.p[row * up.ld + col]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const int64_t col = first + 256 * k;
+                if (col < dh.cols) {
+                    float v, s;
+                    slope<kAct>(g[k], v, s);
+                    dgate[row * ld + col] = narrow<uint16_t>(d[k] * u[k] * s);
+                    dup[row * ld + col] = narrow<uint16_t>(d[k] * v);
+                }
+            }
+        }
+}
+
+// The largest logit and the sum of exp(l - that) of two parts of a row.
+__device__ __forceinline__ float2 join(float2 a, float2 b)
+{
+    const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
+    return make_float2(top, a.y * exp2f((a.x - base) * kLog2e) + b.y * exp2f((b.x - base) * kLog2e));
+}
+__device__ __forceinline__ void finish_row(float2 v, int64_t row, const float *target_logit, const int64_t *target, int64_t vocab, float *lse, float *loss)
+{
+    const float l = v.x + logf(v.y);
+    if (lse != nullptr) lse[row] = l;
+    if (loss != nullptr) {
+        const int64_t t = target[row];
+        loss[row] = t < 0 ? 0.0f : t >= vocab ? NAN : l - target_logit[row];
     }
 }
 
-// 32 rows a CTA, a warp for every 32nd partial of each; the warps' results are joined in their order.
-__global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, int n_part, int64_t rows, const float *target_logit, const int64_t *target,
-                                                          int64_t vocab, float *lse, float *loss)
+// `rows_a_cta` (a power of two up to 32) rows a CTA, 1024 / that threads for each: joined in a fixed order.
+__global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, int n_part, int64_t rows, int rows_a_cta, const float *target_logit,
+                                                          const int64_t *target, int64_t vocab, float *lse, float *loss)
 {
-    __shared__ float2 of[32][33];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int64_t row = blockIdx.x * 32ll + lane;
-    auto join = [](float2 a, float2 b) {
-        const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
-        return make_float2(top, a.y * exp2f((a.x - base) * kLog2e) + b.y * exp2f((b.x - base) * kLog2e));
-    };
+    __shared__ float2 of[1024];
+    const int mine = threadIdx.x & (rows_a_cta - 1), lanes = 1024 / rows_a_cta, of_row = threadIdx.x / rows_a_cta;
+    const int64_t row = (int64_t)blockIdx.x * rows_a_cta + mine;
     float2 v = make_float2(-INFINITY, 0.0f);
     if (row < rows)
-        for (int i = warp; i < n_part; i += 32) v = join(v, part[(int64_t)i * rows + row]);
-    of[warp][lane] = v;
-    __syncthreads();
-    // (a warp has a row now, its lanes the 32 parts)
-    v = of[lane][warp];
-#pragma unroll
-    for (int d = 1; d < 32; d *= 2) {
-        const float2 o = make_float2(__shfl_xor_sync(~0u, v.x, d), __shfl_xor_sync(~0u, v.y, d));
-        v = lane & d ? join(o, v) : join(v, o);
+        for (int i = of_row; i < n_part; i += lanes) v = join(v, part[(int64_t)i * rows + row]);
+    of[threadIdx.x] = v;
+    for (int n = lanes / 2; n >= 1; n /= 2) {
+        __syncthreads();
+        if (of_row < n) of[threadIdx.x] = v = join(v, of[threadIdx.x + n * rows_a_cta]);
     }
-    const int64_t r = blockIdx.x * 32ll + warp;
-    if (lane == 0 && r < rows) {
-        const float l = v.x + logf(v.y);
-        if (lse != nullptr) lse[r] = l;
-        if (loss != nullptr) {
-            const int64_t t = target[r];
-            loss[r] = t < 0 ? 0.0f : t >= vocab ? NAN : l - target_logit[r];
-        }
-    }
+    if (of_row == 0 && row < rows) finish_row(v, row, target_logit, target, vocab, lse, loss);
 }
 
 __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld)
@@ -554,6 +678,7 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int s
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < groups * rows; i += gridDim.x * 256ll) {
         const int64_t row = i / groups, col = (i - row * groups) * 4;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll 8
         for (int j = 0; j < splits; ++j) {
             const float4 v = *reinterpret_cast<const float4 *>(f32 + (j * rows + row) * f32_ld + col);
             s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
@@ -593,48 +718,95 @@ cudaError_t encode(CUtensorMap *map, const Bf16Matrix &m, int box_rows)
     return r == CUDA_SUCCESS ? cudaSuccess : cudaErrorInvalidValue;
 }
 
-// Bytes of which both the address and every row's start are multiples, as far as stores care.
-int row_align(const void *p, int64_t ld, int esize)
-{
-    const uint64_t both = reinterpret_cast<uintptr_t>(p) | (uint64_t)(ld * esize);
-    return both % 32 == 0 ? 32 : both % 16 == 0 ? 16 : esize;
-}
-
 int grid_of(int64_t threads) { const int64_t n = (threads + 255) / 256; return (int)(n < 148 * 16 ? (n > 0 ? n : 1) : 148 * 16); }
 
-template <int kCtas, int kN, bool kAT, bool kBT, int kEnd>
-cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
+Divider divider(int d)
+{
+    Divider r{(uint32_t)d, 0, 0};
+    if (d > 1) {
+        uint32_t up = 0;
+        while ((1u << up) < (uint32_t)d) ++up;
+        r.mul = (uint32_t)(((1ull << (31 + up)) + (uint32_t)d - 1) / (uint32_t)d);
+        r.shift = up - 1;
+    }
+    return r;
+}
+
+// How C is cut into tiles.  All units (CTAs, or pairs of them) take tiles in turn, so the time is that of the unit with the
+// most, and a width is chosen that leaves the last round full: 517 rows against 32003 are 6 rounds of 3 x 126 tiles of 256 x 256, and 6 of
+// 3 x 143 of 224 columns, which are shorter (53.3 and 52.2 us; 128 columns 68.8).  Clocks of a stage of 64 summed elements for 128 rows, from a product of
+// 16384 x 4096 x 32000: 512 for 256 columns, 457 for 224, 421 for 192, 405 for 128, 302 for 64, 272 for 32; a single CTA, which brings in more bytes
+// for its products, takes 25 % longer (517 rows: 77 and 52 us), two halves of 256 rows, which bring in fewer, 7 % less.
+struct Tiling {
+    int ctas = 1, halves = 1, tile_n = 256, cols = 256, splits = 1;
+    int64_t tiles_m = 1, tiles_n = 1;
+};
+Tiling tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t stages, int batches, bool may_split, int sm_count)
+{
+    Tiling best;
+    double least = 0.0;
+    // (halves only where the end is short: that of the loss is not hidden behind them, 3.00 against 2.86 ms)
+    for (int form = m > 256 && end == kStore ? 2 : m > 128 ? 1 : 0; form >= 0; --form) {
+        const int ctas = form > 0 ? 2 : 1, halves = form == 2 ? 2 : 1, rows = 128 * ctas * halves;
+        const double factor = form == 2 ? 0.93 : form == 1 ? 1.0 : 1.25;
+        // columns of C: the tensor cores take multiples of 16, of a pair of 32; kGated halves them
+        const int step = ctas == 1 && end != kDlogits && end != kStore ? 16 : 32, widest = end == kGated ? 128 : 256;
+        for (int cols = widest; cols >= step; cols -= step) {
+            const int width = end == kGated ? 2 * cols : cols;
+            const int64_t tiles_m = (m + rows - 1) / rows, tiles_n = (n + cols - 1) / cols, tiles = tiles_m * tiles_n * batches, units = sm_count / ctas;
+            int64_t splits = 1;
+            if (may_split && tiles < units) splits = units / tiles < stages / 8 ? units / tiles : stages / 8;
+            if (splits < 1) splits = 1;
+            const int64_t rounds = (tiles * splits + units - 1) / units, each = (stages + splits - 1) / splits;
+            const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage, store = 8.0 * width;
+            double cost = rounds * ((main > store ? main : store) + 200.0) * halves + store;
+            if (splits > 1) cost += 4000.0 + (double)splits * m * n * 8.0 / 3600.0;       // the sums of the splits, written and read
+            if (least == 0.0 || cost < least) {
+                least = cost;
+                best = Tiling{ctas, halves, width, cols, (int)splits, tiles_m, tiles_n};
+            }
+        }
+    }
+    return best;
+}
+
+template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd>
+cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, cudaStream_t st)
 {
     Params p{};
-    constexpr int kColumns = kEnd == kGated ? kN / 2 : kN;
     const int maps_a = a.segments > 1 || a.batches > 1 ? 2 : 1, maps_b = kEnd == kGated || maps_a == 2 ? 2 : 1;
+    const int rows_a = kAT || a.m > 128 ? 128 : (int)((a.m + 7) / 8 * 8);
     cudaError_t e = cudaSuccess;
-    for (int i = 0; i < maps_a && e == cudaSuccess; ++i) e = encode(&p.a[i], a.a[i], kAT ? 64 : 128);
-    for (int i = 0; i < maps_b && e == cudaSuccess; ++i) e = encode(&p.b[i], a.b[i], kBT ? 64 : kEnd == kGated && kCtas == 1 ? kN / 2 : kN / kCtas);
+    for (int i = 0; i < maps_a && e == cudaSuccess; ++i) e = encode(&p.a[i], a.a[i], kAT ? 64 : rows_a);
+    for (int i = 0; i < maps_b && e == cudaSuccess; ++i) e = encode(&p.b[i], a.b[i], kBT ? 64 : kEnd == kGated ? t.cols : t.tile_n / kCtas);
+    const int outs = kEnd == kGated ? 3 : kEnd == kDlogits ? 1 : kEnd == kStore ? a.batches : 0;
+    for (int i = 0; i < outs; ++i) p.out[i] = Output{a.out[i], a.out_ld[i], tma_reads(Bf16Matrix{a.out[i], a.m, a.n, a.out_ld[i]})};
     if (e != cudaSuccess) return e;
     p.m = a.m; p.n = a.n;
-    p.tiles_m = (int)((a.m + 128 * kCtas - 1) / (128 * kCtas));
-    p.tiles_n = (int)((a.n + kColumns - 1) / kColumns);
+    p.tile_n = t.tile_n; p.cols = t.cols;
+    p.tiles_m = (int)t.tiles_m; p.tiles_n = (int)t.tiles_n;
     p.kblocks = (int)((a.k + kBlockK - 1) / kBlockK);
-    p.segments = a.segments; p.batches = a.batches; p.splits = a.splits;
-    const int64_t total = (int64_t)p.tiles_m * p.tiles_n * a.batches * a.splits;
-    if (total > 0x3FFFFFFF) return cudaErrorInvalidValue;
+    p.all_k = p.kblocks * a.segments; p.batches = a.batches;
+    p.each_k = p.all_k / a.splits; p.more_k = p.all_k % a.splits;
+    const int64_t total = t.tiles_m * t.tiles_n * a.batches * a.splits;
+    if (total > 0x3FFFFFFF || (t.tiles_m + 16) * t.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidValue;
     p.total = (int)total;
-    p.h = a.h; p.gate = a.gate; p.up = a.up;
-    p.h_ld = a.h_ld; p.gate_ld = a.gate_ld; p.up_ld = a.up_ld;
+    p.band = 16 / kHalves;
+    const int last = p.tiles_m % p.band;
+    p.by_outer = divider(p.tiles_m * p.tiles_n);
+    p.by_band = divider(p.band * p.tiles_n);
+    p.by_height = divider(p.band);
+    p.by_last = divider(last == 0 ? p.band : last);
+    // (a product reads 128 rows of A from the ring, also where A has fewer and other bytes follow: rows of C that nobody stores)
+    p.bytes_a = rows_a * 128;
+    p.bytes_b = (kBT ? (t.tile_n / kCtas + 63) / 64 * 64 : t.tile_n / kCtas) * 128;
+    p.stages = (kRing - (16384 - p.bytes_a)) / (kHalves * p.bytes_a + p.bytes_b);
+    if (p.stages > kMostStages) p.stages = kMostStages;
     p.act = a.act;
-    p.h_align = row_align(a.h, a.h_ld, 2); p.gate_align = row_align(a.gate, a.gate_ld, 2); p.up_align = row_align(a.up, a.up_ld, 2);
     p.part = a.part; p.target_logit = a.target_logit; p.target = a.target; p.vocab = a.vocab; p.first = a.first;
     p.lse = a.lse; p.dloss = a.dloss;
-    p.out_align = 32;
-    for (int i = 0; i < a.batches; ++i) {
-        p.out[i] = a.out[i]; p.out_ld[i] = a.out_ld[i];
-        const int align = row_align(a.out[i], a.out_ld[i], 2);
-        p.out_align = align < p.out_align ? align : p.out_align;
-    }
     p.f32 = a.f32; p.f32_ld = a.f32_ld; p.mode = a.mode; p.gave_up = a.gave_up;
-    auto kernel = product_kernel<kCtas, kN, kAT, kBT, kEnd>;
-    constexpr int kShared = kRing + 1024;
+    auto kernel = product_kernel<kCtas, kHalves, kAT, kBT, kEnd>;
     static std::atomic<uint64_t> known{0};      // devices on which the kernel has its shared memory
     int device = 0;
     e = cudaGetDevice(&device);
@@ -657,37 +829,42 @@ cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
-constexpr int kTileN = 256;      // columns of C in a tile
-// Two CTAs for a tile of 256 rows, where there are more than one CTA's.
-int ctas_of(int64_t m) { return m > 128 ? 2 : 1; }
-
 template <bool kAT, bool kBT, int kEnd>
-cudaError_t launch_tiles(const ProductArgs &a, int sm_count, cudaStream_t st)
+cudaError_t launch_tiles(const ProductArgs &a, const Tiling &t, int sm_count, cudaStream_t st)
 {
-    return ctas_of(a.m) == 2 ? launch_product<2, kTileN, kAT, kBT, kEnd>(a, sm_count, st) : launch_product<1, kTileN, kAT, kBT, kEnd>(a, sm_count, st);
+    if constexpr (kEnd == kStore)
+        if (t.halves == 2) return launch_product<2, 2, kAT, kBT, kEnd>(a, t, sm_count, st);
+    return t.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd>(a, t, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd>(a, t, sm_count, st);
 }
+
+int64_t stages_of(int64_t k) { return (k + kBlockK - 1) / kBlockK; }
 
 }  // namespace
 
 cudaError_t launch_product_rows(ProductEnd end, const ProductArgs &a, int sm_count, cudaStream_t st)
 {
-    if (end == kGated) return launch_tiles<false, false, kGated>(a, sm_count, st);
-    if (end == kLse) return launch_tiles<false, false, kLse>(a, sm_count, st);
-    if (end == kDlogits) return launch_tiles<false, false, kDlogits>(a, sm_count, st);
+    const Tiling t = tiling(end, false, a.m, a.n, stages_of(a.k), 1, false, sm_count);
+    if (end == kGated) return launch_tiles<false, false, kGated>(a, t, sm_count, st);
+    if (end == kLse) return launch_tiles<false, false, kLse>(a, t, sm_count, st);
+    if (end == kDlogits) return launch_tiles<false, false, kDlogits>(a, t, sm_count, st);
     return cudaErrorInvalidValue;
 }
-cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st) { return launch_tiles<false, true, kStore>(a, sm_count, st); }
-cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st) { return launch_tiles<true, true, kStore>(a, sm_count, st); }
+cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st)
+{
+    return launch_tiles<false, true, kStore>(a, tiling(kStore, true, a.m, a.n, stages_of(a.k) * a.segments, 1, true, sm_count), sm_count, st);
+}
+cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st)
+{
+    return launch_tiles<true, true, kStore>(a, tiling(kStore, true, a.m, a.n, stages_of(a.k), a.batches, false, sm_count), sm_count, st);
+}
 
-int product_partials(int64_t, int64_t n) { return (int)(2 * ((n + kTileN - 1) / kTileN)); }
-
+int product_partials(int64_t m, int64_t n, int64_t k, int sm_count)
+{
+    return (int)(2 * tiling(kLse, false, m, n, stages_of(k), 1, false, sm_count).tiles_n);
+}
 int product_splits(int64_t m, int64_t n, int64_t k, int segments, int sm_count)
 {
-    // as many as give every SM a tile, but at least 16 stages for each
-    const int64_t ctas = ctas_of(m), tiles = ((m + 128 * ctas - 1) / (128 * ctas)) * ((n + kTileN - 1) / kTileN);
-    const int64_t most = (k + kBlockK - 1) / kBlockK * segments / 16, want = sm_count / ctas / (tiles > 0 ? tiles : 1);
-    const int64_t s = want < most ? want : most;
-    return (int)(s < 1 ? 1 : s);
+    return tiling(kStore, true, m, n, stages_of(k) * segments, 1, true, sm_count).splits;
 }
 
 bool tma_reads(const Bf16Matrix &m)
@@ -705,7 +882,9 @@ cudaError_t launch_realign(const Bf16Matrix &from, uint16_t *to, int64_t ld, cud
 cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, const float *target_logit, const int64_t *target, int64_t vocab, float *lse,
                               float *loss, cudaStream_t st)
 {
-    lse_finish_kernel<<<(unsigned)((rows + 31) / 32), 1024, 0, st>>>(part, n_part, rows, target_logit, target, vocab, lse, loss);
+    int each = 1;
+    while (each < 32 && rows > 256 * each) each *= 2;
+    lse_finish_kernel<<<(unsigned)((rows + each - 1) / each), 1024, 0, st>>>(part, n_part, rows, each, target_logit, target, vocab, lse, loss);
     return cudaGetLastError();
 }
 
@@ -718,13 +897,18 @@ cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,
                                 cudaStream_t st)
 {
-    const int64_t groups = (dh.cols + 7) / 8;
-    const int grid = grid_of(groups * dh.rows), vector = tma_reads(dh) && tma_reads(gate) && tma_reads(up);
-    auto go = [&](auto kernel) { kernel<<<grid, 256, 0, st>>>(dh, gate, up, dgate, dup, ld, groups, vector); };
-    if (act == GG_ACT_SILU) go(gated_slopes_kernel<GG_ACT_SILU>);
-    else if (act == GG_ACT_GELU) go(gated_slopes_kernel<GG_ACT_GELU>);
-    else if (act == GG_ACT_GELU_TANH) go(gated_slopes_kernel<GG_ACT_GELU_TANH>);
-    else go(gated_slopes_kernel<GG_ACT_RELU>);
+    auto go = [&](auto kernel, auto any) {
+        if (dh.cols % 8 == 0 && tma_reads(dh) && tma_reads(gate) && tma_reads(up)) {
+            const int64_t groups = dh.cols / 8, total = groups * dh.rows, want = (total + 511) / 512;
+            kernel<<<(unsigned)(want < 0x7FFFFFFF ? want : 0x7FFFFFFF), 256, 0, st>>>(dh, gate, up, dgate, dup, ld, (uint32_t)groups, total);
+        } else {
+            any<<<dim3((unsigned)((dh.cols + 1023) / 1024), (unsigned)(dh.rows < 65535 ? dh.rows : 65535)), 256, 0, st>>>(dh, gate, up, dgate, dup, ld);
+        }
+    };
+    if (act == GG_ACT_SILU) go(gated_slopes_kernel<GG_ACT_SILU>, gated_slopes_any_kernel<GG_ACT_SILU>);
+    else if (act == GG_ACT_GELU) go(gated_slopes_kernel<GG_ACT_GELU>, gated_slopes_any_kernel<GG_ACT_GELU>);
+    else if (act == GG_ACT_GELU_TANH) go(gated_slopes_kernel<GG_ACT_GELU_TANH>, gated_slopes_any_kernel<GG_ACT_GELU_TANH>);
+    else go(gated_slopes_kernel<GG_ACT_RELU>, gated_slopes_any_kernel<GG_ACT_RELU>);
     return cudaGetLastError();
 }
 

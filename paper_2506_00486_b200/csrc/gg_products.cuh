@@ -27,20 +27,17 @@ struct ProductArgs {
     Bf16Matrix a[2], b[2];      // of a segment, or of a batch (one of the two); kGated: b[0] gate, b[1] up
     int64_t m, n, k;            // kGated: n counts the columns of h
     int segments, batches, splits;
-    // kGated
-    uint16_t *h, *gate, *up;    // gate and up may be null
-    int64_t h_ld, gate_ld, up_ld;
-    int act;
-    // kLse: [n_tiles * 2][m] partials; target[m], the logits of the targets.  kDlogits: target, lse, dloss, out.
+    int act;                    // kGated
+    // kLse: [product_partials][m] partials; target[m], the logits of the targets.  kDlogits: target, lse, dloss, out.
     float2 *part;
     float *target_logit;
     const int64_t *target;
     int64_t vocab;              // targets count from 0 to vocab - 1 ...
     int64_t first;              // ... and this call's columns begin there
     const float *lse, *dloss;
-    // kDlogits (out[0], a multiple of 32 from row to row), kStore
-    uint16_t *out[2];           // of a batch
-    int64_t out_ld[2];
+    // kGated: h, gate, up (each of the last two may be null); kDlogits: out[0]; kStore: of a batch
+    uint16_t *out[3];
+    int64_t out_ld[3];
     float *f32;                 // kStore: [splits][m][f32_ld], f32_ld a multiple of 32
     int64_t f32_ld;
     int mode;
@@ -52,9 +49,9 @@ cudaError_t launch_product_rows(ProductEnd end, const ProductArgs &a, int sm_cou
 // ... with A K-major and B [k, n] (the gradient of the rows), and with A [k, m] and B [k, n] (that of a weight); kStore
 cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st);
 cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st);
-// columns of C in a tile of launch_product_rows, and the partials of a row that kLse leaves for n columns
-int product_partials(int64_t m, int64_t n);
-// how many pieces the long axis of launch_product_drows is cut into, so that all SMs have work
+// the partials of a row that kLse leaves
+int product_partials(int64_t m, int64_t n, int64_t k, int sm_count);
+// how many pieces the long axis of launch_product_drows is best cut into, so that all SMs have work
 int product_splits(int64_t m, int64_t n, int64_t k, int segments, int sm_count);
 
 // Can TMA read the matrix where it is?  If not, realign_rows copies it to rows of `ld` elements (a multiple of 8).

@@ -13,12 +13,14 @@ __device__ __forceinline__ void barrier_expect(uint32_t bar, uint32_t bytes)
 {
     asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
-// (an address of the cluster's shared memory, such as peer_address gives)
-__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
+// (an address of the cluster's shared memory, such as peer_address gives.  What it says is that the caller has read tensor memory, and
+// tmem_before_sync orders that; a release of the whole cluster would also wait for the caller's stores to memory, which took half of
+// the time of a product that is mostly stores)
+__device__ __forceinline__ void barrier_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory"); }
 __device__ __forceinline__ bool barrier_test(uint32_t bar, uint32_t parity)
 {
     uint32_t done;
-    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}"
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
@@ -42,6 +44,13 @@ __device__ __forceinline__ uint32_t cluster_rank()
     uint32_t r;
     asm volatile("mov.u32 %0, %%cluster_ctarank;" : "=r"(r));
     return r;
+}
+// One lane of a whole warp, always the same.
+__device__ __forceinline__ bool elect_lane()
+{
+    uint32_t is;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(is));
+    return is != 0;
 }
 __device__ __forceinline__ void cluster_sync()
 {
@@ -100,11 +109,12 @@ __device__ __forceinline__ void tmem_read(uint32_t at, float (&v)[32])
 __device__ __forceinline__ void tmem_read_wait() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 
 // ---- products
-// bf16 operands, fp32 sums; kAT, kBT: the operand lies with the rows of the product (not the summed axis) side by side
-template <int kM, int kN, bool kAT, bool kBT>
-__host__ __device__ constexpr uint32_t product_shape()
+// bf16 operands, fp32 sums; kAT, kBT: the operand lies with the rows of the product (not the summed axis) side by side; n: a
+// multiple of 16 up to 256
+template <int kM, bool kAT, bool kBT>
+__device__ __forceinline__ uint32_t product_shape(int n)
 {
-    return 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)kAT << 15 | (uint32_t)kBT << 16 | (uint32_t)(kN >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
+    return 1u << 4 | 1u << 7 | 1u << 10 | (uint32_t)kAT << 15 | (uint32_t)kBT << 16 | (uint32_t)(n >> 3) << 17 | (uint32_t)(kM >> 4) << 24;
 }
 // A tile in shared memory as 128-byte rows in the 128-byte swizzle, at a multiple of 1024 bytes.  Along the summed axis: a row
 // is 64 summed elements of one product row, 8 rows lie 1024 bytes from the next 8.  Otherwise: a row is 64 product rows of
