@@ -1992,7 +1992,8 @@ gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *a, void *stre
     p.out_ld[0] = a->h_ld; p.out_ld[1] = a->gate_ld; p.out_ld[2] = a->up_ld;
     p.act = a->act;
     p.gave_up = ctx->gave_up;
-    GG_CUDA(ctx, launch_product_rows(kGated, p, ctx->sm_count, s.st));
+    if (gated_row(a->rows, a->width)) GG_CUDA(ctx, launch_gated_row(p, ctx->sm_count, s.st));
+    else GG_CUDA(ctx, launch_product_rows(kGated, p, ctx->sm_count, s.st));
     ctx->launches += 1;
     return GG_OK;
 }

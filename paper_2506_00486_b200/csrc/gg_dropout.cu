@@ -3,6 +3,7 @@
 // Eight elements of a row share one block of 128 random bits.  A warp takes runs of 256 elements of a row: each lane draws the
 // eight keep bits of one group, and the lanes then read and write the run side by side, in whatever pieces its alignment allows,
 // fetching the bits of their elements from the lane that drew them.
+#include "gg_after.cuh"
 #include "gg_element.cuh"
 #include "gg_internal.h"
 #include "gg_philox.cuh"
@@ -66,6 +67,7 @@ __global__ void __launch_bounds__(kWarps * 32) dropout_runs_kernel(const Dropout
     constexpr int kPieces = kRun / (32 * kEach);         // of a lane in a run
     constexpr int kTogether = kPieces > kAtOnce ? 1 : kAtOnce / kPieces;
     const int lane = threadIdx.x & 31;
+    wait_for_the_one_before();
     const uint32_t t = (uint32_t)(a.t + (a.t_dev ? *a.t_dev : 0));
     const int64_t groups = (a.cols + 7) / 8, first = (blockIdx.x * (int64_t)kWarps + (threadIdx.x >> 5)) * kTogether;
     Piece<T, kEach> x[kTogether][kPieces], r[kResidual ? kTogether : 1][kPieces];
@@ -109,6 +111,7 @@ __global__ void __launch_bounds__(kWarps * 32) dropout_runs_kernel(const Dropout
 template <typename T>
 __global__ void __launch_bounds__(kWarps * 32) dropout_groups_kernel(const DropoutArgs a, const Keys keys, uint32_t least, float scale)
 {
+    wait_for_the_one_before();
     const int64_t groups = (a.cols + 7) / 8;
     const uint32_t t = (uint32_t)(a.t + (a.t_dev ? *a.t_dev : 0));
     for (int64_t i = blockIdx.x * (int64_t)(kWarps * 32) + threadIdx.x; i < groups * a.rows; i += gridDim.x * (int64_t)(kWarps * 32)) {
@@ -143,8 +146,7 @@ cudaError_t launch(DropoutArgs a, const Keys &keys, uint32_t least, float scale,
     }
     if (a.rows > 1 && a.cols < 96) {
         const int64_t want = ((a.cols + 7) / 8 * a.rows + kWarps * 32 - 1) / (kWarps * 32), most = (int64_t)sm_count * 8;
-        dropout_groups_kernel<T><<<(unsigned)(want < most ? want : most), kWarps * 32, 0, st>>>(a, keys, least, scale);
-        return cudaGetLastError();
+        return launch_after(st, dim3((unsigned)(want < most ? want : most)), kWarps * 32, 0, dropout_groups_kernel<T>, a, keys, least, scale);
     }
     const bool whole = a.cols % kEach == 0 && whole_pieces(a.x, a.rows, a.x_ld, kEach) && whole_pieces(a.y, a.rows, a.y_ld, kEach) &&
                        (!a.residual || whole_pieces(a.residual, a.rows, a.residual_ld, kEach));
@@ -152,8 +154,7 @@ cudaError_t launch(DropoutArgs a, const Keys &keys, uint32_t least, float scale,
     auto go = [&](auto kernel, int pieces) {
         const int64_t together = (int64_t)kWarps * (pieces > kAtOnce ? 1 : kAtOnce / pieces), ctas = (total + together - 1) / together;
         if (ctas > 0x7FFFFFFF) return cudaErrorInvalidValue;
-        kernel<<<(unsigned)ctas, kWarps * 32, 0, st>>>(a, keys, least, scale, runs, total);
-        return cudaGetLastError();
+        return launch_after(st, dim3((unsigned)ctas), kWarps * 32, 0, kernel, a, keys, least, scale, runs, total);
     };
     if (whole) return a.residual ? go(dropout_runs_kernel<T, kEach, true>, kRun / (32 * kEach)) : go(dropout_runs_kernel<T, kEach, false>, kRun / (32 * kEach));
     return a.residual ? go(dropout_runs_kernel<T, 1, true>, kRun / 32) : go(dropout_runs_kernel<T, 1, false>, kRun / 32);

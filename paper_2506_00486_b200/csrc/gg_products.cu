@@ -13,6 +13,7 @@
 #include <type_traits>
 
 #include "gg.h"
+#include "gg_after.cuh"
 #include "gg_element.cuh"
 #include "gg_products.cuh"
 #include "gg_tensor.cuh"
@@ -388,6 +389,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     else __syncthreads();
     tmem_after_sync();
     const uint32_t tmem = tmem_at;
+    wait_for_the_one_before();
 
     const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
     bool failed = false;
@@ -555,6 +557,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 // One thread for eight columns of a row.
 __global__ void __launch_bounds__(256) realign_kernel(const Bf16Matrix from, uint16_t *to, int64_t ld, int64_t groups)
 {
+    wait_for_the_one_before();
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < groups * from.rows; i += gridDim.x * 256ll) {
         const int64_t row = i / groups, col = (i - row * groups) * 8;
         const uint16_t *f = from.p + row * from.ld + col;
@@ -573,6 +576,7 @@ template <int kAct>
 __global__ void __launch_bounds__(256) gated_slopes_kernel(const Bf16Matrix dh, const Bf16Matrix gate, const Bf16Matrix up, uint16_t *dgate, uint16_t *dup,
                                                            int64_t ld, uint32_t groups, int64_t total)
 {
+    wait_for_the_one_before();
     const int64_t step = gridDim.x * 256ll;
     for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < total; i += 2 * step) {
         uint4 d[2], g[2], u[2];
@@ -613,6 +617,7 @@ template <int kAct>
 __global__ void __launch_bounds__(256) gated_slopes_any_kernel(const Bf16Matrix dh, const Bf16Matrix gate, const Bf16Matrix up, uint16_t *dgate, uint16_t *dup,
                                                                int64_t ld)
 {
+    wait_for_the_one_before();
     for (int64_t row = blockIdx.y; row < dh.rows; row += gridDim.y)
         for (int64_t first = blockIdx.x * 1024ll + threadIdx.x; first < dh.cols; first += gridDim.x * 1024ll) {
             float d[4], g[4], u[4];
@@ -644,13 +649,13 @@ __device__ __forceinline__ float2 join(float2 a, float2 b)
     const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
     return make_float2(top, a.y * exp2f((a.x - base) * kLog2e) + b.y * exp2f((b.x - base) * kLog2e));
 }
-__device__ __forceinline__ void finish_row(float2 v, int64_t row, const float *target_logit, const int64_t *target, int64_t vocab, float *lse, float *loss)
+__device__ __forceinline__ void finish_row(float2 v, int64_t row, float target_logit, const int64_t *target, int64_t vocab, float *lse, float *loss)
 {
     const float l = v.x + logf(v.y);
     if (lse != nullptr) lse[row] = l;
     if (loss != nullptr) {
         const int64_t t = target[row];
-        loss[row] = t < 0 ? 0.0f : t >= vocab ? NAN : l - target_logit[row];
+        loss[row] = t < 0 ? 0.0f : t >= vocab ? NAN : l - target_logit;
     }
 }
 
@@ -659,6 +664,7 @@ __global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, in
                                                           const int64_t *target, int64_t vocab, float *lse, float *loss)
 {
     __shared__ float2 of[1024];
+    wait_for_the_one_before();
     const int mine = threadIdx.x & (rows_a_cta - 1), lanes = 1024 / rows_a_cta, of_row = threadIdx.x / rows_a_cta;
     const int64_t row = (int64_t)blockIdx.x * rows_a_cta + mine;
     float2 v = make_float2(-INFINITY, 0.0f);
@@ -669,25 +675,167 @@ __global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, in
         __syncthreads();
         if (of_row < n) of[threadIdx.x] = v = join(v, of[threadIdx.x + n * rows_a_cta]);
     }
-    if (of_row == 0 && row < rows) finish_row(v, row, target_logit, target, vocab, lse, loss);
+    if (of_row == 0 && row < rows) finish_row(v, row, target_logit[row], target, vocab, lse, loss);
 }
 
+// 32 runs of four columns a CTA, eight threads for each, which take every eighth split and are added in order.
 __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld)
 {
+    __shared__ float4 of[8][33];
     const int64_t groups = (cols + 3) / 4;
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < groups * rows; i += gridDim.x * 256ll) {
-        const int64_t row = i / groups, col = (i - row * groups) * 4;
+    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    wait_for_the_one_before();
+    for (int64_t first = blockIdx.x * 32ll; first < groups * rows; first += gridDim.x * 32ll) {
+        const int64_t i = first + lane, row = i / groups, col = (i - row * groups) * 4;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll 8
-        for (int j = 0; j < splits; ++j) {
-            const float4 v = *reinterpret_cast<const float4 *>(f32 + (j * rows + row) * f32_ld + col);
-            s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        if (row < rows) {
+#pragma unroll 4
+            for (int j = part; j < splits; j += 8) {
+                const float4 v = *reinterpret_cast<const float4 *>(f32 + (j * rows + row) * f32_ld + col);
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
         }
-        const float v[4] = {s.x, s.y, s.z, s.w};
-        uint16_t *o = out + row * out_ld + col;
+        of[part][lane] = s;
+        __syncthreads();
+        if (part == 0 && row < rows) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            if (col + j < cols) o[j] = narrow<uint16_t>(v[j]);
+            for (int j = 1; j < 8; ++j) {
+                const float4 v = of[j][lane];
+                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+            }
+            const float v[4] = {s.x, s.y, s.z, s.w};
+            uint16_t *o = out + row * out_ld + col;
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (col + j < cols) o[j] = narrow<uint16_t>(v[j]);
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ one row
+// One row of A: a pass over both weights with nothing to fill a tile.  A warp takes two rows of gate and the same two of up, its
+// lanes side by side in pieces of 16 bytes, the next 512 columns on their way while these are added; A lies in shared memory.
+// Less to start and to drain than the tensor cores' kernel: 1 x 896 against 2 x 4864 rows 6.2 and 7.1 us a call, 256 against 2 x 512 3.4 and 4.2,
+// 4096 against 2 x 11008 32.0 and 33.1 (2048 against 2 x 8192 12.2 and 11.3); with two rows there is nothing left of that.
+struct RowArgs {
+    const uint16_t *x, *w[2];
+    int64_t w_ld[2], n;
+    int k;
+    uint16_t *h, *gate, *up;
+    int act;
+};
+constexpr int kRowWarps = 8;
+
+// 512 columns of four rows: two pieces of eight for each lane.  Beyond column k they are 0, as A is there.
+struct RowPiece {
+    uint4 w[4][2];
+    __device__ __forceinline__ void read(const uint16_t *const (&row)[4], int c, int lane, int k)
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int col = c + 256 * h + lane * 8;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                w[r][h] = make_uint4(0, 0, 0, 0);
+                if (col + 8 <= k) w[r][h] = __ldcs(reinterpret_cast<const uint4 *>(row[r] + col));
+                else if (col < k) w[r][h] = some(row[r] + col, k - col);
+            }
+        }
+    }
+    static __device__ __noinline__ uint4 some(const uint16_t *p, int n)
+    {
+        uint32_t h[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) h[e] = e < n ? p[e] : 0;
+        return make_uint4(h[0] | h[1] << 16, h[2] | h[3] << 16, h[4] | h[5] << 16, h[6] | h[7] << 16);
+    }
+    __device__ __forceinline__ void add(uint32_t x_at, int c, f32x2 (&sum)[4]) const
+    {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            uint32_t x[4];
+            asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(x[0]), "=r"(x[1]), "=r"(x[2]), "=r"(x[3]) : "r"(x_at + (uint32_t)(c + 256 * h) * 2u));
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const uint4 &q = w[r][h];
+                    sum[r] = fma2(widen2(j == 0 ? q.x : j == 1 ? q.y : j == 2 ? q.z : q.w), widen2(x[j]), sum[r]);
+                }
+        }
+    }
+};
+
+// Where a warp is: four rows and a run of 512 columns.
+struct RowPlace {
+    int64_t unit;
+    int c;
+    const uint16_t *row[4];
+    __device__ __forceinline__ void go(const RowArgs &a, int64_t to)
+    {
+        unit = to;
+        c = 0;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int64_t of = 2 * unit + (r >> 1), there = of < a.n ? of : a.n - 1;
+            row[r] = a.w[r & 1] + there * a.w_ld[r & 1];
+        }
+    }
+    __device__ __forceinline__ void next(const RowArgs &a, int64_t step)
+    {
+        c += 512;
+        if (c >= a.k) go(a, unit + step);
+    }
+};
+
+__global__ void __launch_bounds__(kRowWarps * 32, 2) gated_row_kernel(const RowArgs a)
+{
+    extern __shared__ uint4 row_shared[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, padded = (a.k + 511) / 512 * 512;
+    const int64_t units = (a.n + 1) / 2, step = (int64_t)gridDim.x * kRowWarps;
+    wait_for_the_one_before();
+    RowPlace now, then;
+    RowPiece piece[2];
+    now.go(a, blockIdx.x * (int64_t)kRowWarps + warp);
+    if (now.unit < units) piece[0].read(now.row, now.c, lane, a.k);
+    for (int c = threadIdx.x * 8; c < padded; c += kRowWarps * 256) {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (c < a.k) q = c + 8 <= a.k ? *reinterpret_cast<const uint4 *>(a.x + c) : RowPiece::some(a.x + c, a.k - c);
+        row_shared[c / 8] = q;
+    }
+    __syncthreads();
+    const uint32_t at = shared_address(row_shared) + lane * 16;
+    f32x2 sum[4] = {both(0.0f), both(0.0f), both(0.0f), both(0.0f)};
+    while (now.unit < units) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            then = now;
+            then.next(a, step);
+            if (then.unit < units) piece[i ^ 1].read(then.row, then.c, lane, a.k);
+            piece[i].add(at, now.c, sum);
+            if (then.unit != now.unit) {
+                float v[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const float2 f = halves(sum[r]);
+                    v[r] = f.x + f.y;
+                    sum[r] = both(0.0f);
+#pragma unroll
+                    for (int d = 16; d > 0; d >>= 1) v[r] += __shfl_xor_sync(~0u, v[r], d);
+                }
+                const float gate = lane == 0 ? v[0] : v[2], up = lane == 0 ? v[1] : v[3];
+                const int64_t of = 2 * now.unit + lane;
+                if (lane < 2 && of < a.n) {
+                    by_activation(a.act, [&](auto act) { a.h[of] = narrow<uint16_t>(activation<decltype(act)::value>(gate) * up); });
+                    if (a.gate != nullptr) a.gate[of] = narrow<uint16_t>(gate);
+                    if (a.up != nullptr) a.up[of] = narrow<uint16_t>(up);
+                }
+                __syncwarp();
+            }
+            now = then;
+            if (now.unit >= units) break;
+        }
     }
 }
 
@@ -821,11 +969,13 @@ cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, 
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = kShared;
     cfg.stream = st;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = kCtas; attr[0].val.clusterDim.y = 1; attr[0].val.clusterDim.z = 1;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = kCtas; attr[1].val.clusterDim.y = 1; attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = 1;
+    cfg.numAttrs = 2;
     return cudaLaunchKernelEx(&cfg, kernel, p);
 }
 
@@ -836,6 +986,8 @@ cudaError_t launch_tiles(const ProductArgs &a, const Tiling &t, int sm_count, cu
         if (t.halves == 2) return launch_product<2, 2, kAT, kBT, kEnd>(a, t, sm_count, st);
     return t.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd>(a, t, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd>(a, t, sm_count, st);
 }
+
+int64_t row_shared_bytes(int64_t k) { return (k + 511) / 512 * 512 * 2; }
 
 int64_t stages_of(int64_t k) { return (k + kBlockK - 1) / kBlockK; }
 
@@ -875,8 +1027,7 @@ bool tma_reads(const Bf16Matrix &m)
 cudaError_t launch_realign(const Bf16Matrix &from, uint16_t *to, int64_t ld, cudaStream_t st)
 {
     const int64_t groups = (from.cols + 7) / 8;
-    realign_kernel<<<grid_of(groups * from.rows), 256, 0, st>>>(from, to, ld, groups);
-    return cudaGetLastError();
+    return launch_after(st, dim3(grid_of(groups * from.rows)), 256, 0, realign_kernel, from, to, ld, groups);
 }
 
 cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, const float *target_logit, const int64_t *target, int64_t vocab, float *lse,
@@ -884,14 +1035,12 @@ cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, cons
 {
     int each = 1;
     while (each < 32 && rows > 256 * each) each *= 2;
-    lse_finish_kernel<<<(unsigned)((rows + each - 1) / each), 1024, 0, st>>>(part, n_part, rows, each, target_logit, target, vocab, lse, loss);
-    return cudaGetLastError();
+    return launch_after(st, dim3((unsigned)((rows + each - 1) / each)), 1024, 0, lse_finish_kernel, part, n_part, rows, each, target_logit, target, vocab, lse, loss);
 }
 
 cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, cudaStream_t st)
 {
-    sum_splits_kernel<<<grid_of((cols + 3) / 4 * rows), 256, 0, st>>>(f32, splits, rows, cols, f32_ld, out, out_ld);
-    return cudaGetLastError();
+    return launch_after(st, dim3(grid_of((cols + 3) / 4 * rows * 8)), 256, 0, sum_splits_kernel, f32, splits, rows, cols, f32_ld, out, out_ld);
 }
 
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,
@@ -900,16 +1049,32 @@ cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, co
     auto go = [&](auto kernel, auto any) {
         if (dh.cols % 8 == 0 && tma_reads(dh) && tma_reads(gate) && tma_reads(up)) {
             const int64_t groups = dh.cols / 8, total = groups * dh.rows, want = (total + 511) / 512;
-            kernel<<<(unsigned)(want < 0x7FFFFFFF ? want : 0x7FFFFFFF), 256, 0, st>>>(dh, gate, up, dgate, dup, ld, (uint32_t)groups, total);
-        } else {
-            any<<<dim3((unsigned)((dh.cols + 1023) / 1024), (unsigned)(dh.rows < 65535 ? dh.rows : 65535)), 256, 0, st>>>(dh, gate, up, dgate, dup, ld);
+            return launch_after(st, dim3((unsigned)(want < 0x7FFFFFFF ? want : 0x7FFFFFFF)), 256, 0, kernel, dh, gate, up, dgate, dup, ld, (uint32_t)groups, total);
         }
+        return launch_after(st, dim3((unsigned)((dh.cols + 1023) / 1024), (unsigned)(dh.rows < 65535 ? dh.rows : 65535)), 256, 0, any, dh, gate, up, dgate, dup, ld);
     };
-    if (act == GG_ACT_SILU) go(gated_slopes_kernel<GG_ACT_SILU>, gated_slopes_any_kernel<GG_ACT_SILU>);
-    else if (act == GG_ACT_GELU) go(gated_slopes_kernel<GG_ACT_GELU>, gated_slopes_any_kernel<GG_ACT_GELU>);
-    else if (act == GG_ACT_GELU_TANH) go(gated_slopes_kernel<GG_ACT_GELU_TANH>, gated_slopes_any_kernel<GG_ACT_GELU_TANH>);
-    else go(gated_slopes_kernel<GG_ACT_RELU>, gated_slopes_any_kernel<GG_ACT_RELU>);
-    return cudaGetLastError();
+    if (act == GG_ACT_SILU) return go(gated_slopes_kernel<GG_ACT_SILU>, gated_slopes_any_kernel<GG_ACT_SILU>);
+    if (act == GG_ACT_GELU) return go(gated_slopes_kernel<GG_ACT_GELU>, gated_slopes_any_kernel<GG_ACT_GELU>);
+    if (act == GG_ACT_GELU_TANH) return go(gated_slopes_kernel<GG_ACT_GELU_TANH>, gated_slopes_any_kernel<GG_ACT_GELU_TANH>);
+    return go(gated_slopes_kernel<GG_ACT_RELU>, gated_slopes_any_kernel<GG_ACT_RELU>);
+}
+
+bool gated_row(int64_t m, int64_t k) { return m == 1 && row_shared_bytes(k) <= 48 * 1024; }
+
+cudaError_t launch_gated_row(const ProductArgs &a, int sm_count, cudaStream_t st)
+{
+    RowArgs r{};
+    r.x = a.a[0].p;
+    for (int i = 0; i < 2; ++i) {
+        r.w[i] = a.b[i].p;
+        r.w_ld[i] = a.b[i].ld;
+    }
+    r.n = a.n; r.k = (int)a.k;
+    r.h = a.out[0]; r.gate = a.out[1]; r.up = a.out[2];
+    r.act = a.act;
+    // two CTAs an SM, or a unit of work for each warp
+    const int64_t want = (a.n + 2 * kRowWarps - 1) / (2 * kRowWarps), most = 2 * (int64_t)sm_count;
+    return launch_after(st, dim3((unsigned)(want < most ? want : most)), kRowWarps * 32, (size_t)row_shared_bytes(a.k), gated_row_kernel, r);
 }
 
 }  // namespace gg

@@ -54,6 +54,10 @@ int product_partials(int64_t m, int64_t n, int64_t k, int sm_count);
 // how many pieces the long axis of launch_product_drows is best cut into, so that all SMs have work
 int product_splits(int64_t m, int64_t n, int64_t k, int segments, int sm_count);
 
+// kGated for a single row, without the tensor cores
+bool gated_row(int64_t m, int64_t k);
+cudaError_t launch_gated_row(const ProductArgs &a, int sm_count, cudaStream_t st);
+
 // Can TMA read the matrix where it is?  If not, realign_rows copies it to rows of `ld` elements (a multiple of 8).
 bool tma_reads(const Bf16Matrix &m);
 cudaError_t launch_realign(const Bf16Matrix &from, uint16_t *to, int64_t ld, cudaStream_t st);
