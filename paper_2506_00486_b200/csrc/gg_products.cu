@@ -68,11 +68,32 @@ struct Params {
 // ------------------------------------------------------------------ activations
 // a / (1 + e^-a): an e^-a that overflows gives 0, as the product does.
 __device__ __forceinline__ float sigmoid(float a) { return __fdividef(1.0f, 1.0f + __expf(-a)); }
+// The normal distribution function of a and e = exp(-a^2 / 2).  Its tail at -z is e R(z), R falling slowly from 1/2; R is a polynomial in
+// t = 1 / (1 + 0.3 z) without a constant term, fitted for least relative error over [0, 20] (6.5e-7 in fp32; erfcf takes three times the
+// instructions, and its 1 - erf is no good for negative a).
+__device__ __forceinline__ float normal(float a, float &e)
+{
+    const float z = fabsf(a), t = __fdividef(1.0f, 1.0f + 0.3f * z);
+    float r = 0.0330343359f;
+    r = r * t - 0.1463946f;
+    r = r * t + 0.188128167f;
+    r = r * t - 0.0373476765f;
+    r = r * t + 0.120195597f;
+    r = r * t + 0.102349824f;
+    r = r * t + 0.120381962f;
+    r = r * t + 0.119652203f;
+    e = __expf(-0.5f * z * z);
+    const float tail = e * (r * t);
+    return a > 0.0f ? 1.0f - tail : tail;
+}
 template <int kAct>
 __device__ __forceinline__ float activation(float a)
 {
     if constexpr (kAct == GG_ACT_SILU) return a * sigmoid(a);
-    if constexpr (kAct == GG_ACT_GELU) return 0.5f * a * erfcf(-0.70710678118654752f * a);      // (erfc: 1 + erf cancels)
+    if constexpr (kAct == GG_ACT_GELU) {
+        float e;
+        return a * normal(a, e);
+    }
     if constexpr (kAct == GG_ACT_GELU_TANH) {           // (1 + tanh z) / 2 = sigmoid(2 z), which is 0 or 1 beyond 30
         const float b = fminf(fmaxf(a, -30.0f), 30.0f);
         return a * sigmoid(1.5957691216057308f * (b + 0.044715f * b * b * b));
@@ -88,9 +109,10 @@ __device__ __forceinline__ void slope(float a, float &value, float &d)
         value = a * s;
         d = s + value * (1.0f - s);
     } else if constexpr (kAct == GG_ACT_GELU) {
-        const float c = 0.5f * erfcf(-0.70710678118654752f * a);
+        float e;
+        const float c = normal(a, e);
         value = a * c;
-        d = c + a * 0.3989422804014327f * __expf(-0.5f * a * a);
+        d = c + a * 0.3989422804014327f * e;
     } else if constexpr (kAct == GG_ACT_GELU_TANH) {
         const float b = fminf(fmaxf(a, -30.0f), 30.0f), s = sigmoid(1.5957691216057308f * (b + 0.044715f * b * b * b));
         value = a * s;
@@ -906,7 +928,7 @@ Tiling tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t stages, int
             if (may_split && tiles < units) splits = units / tiles < stages / 8 ? units / tiles : stages / 8;
             if (splits < 1) splits = 1;
             const int64_t rounds = (tiles * splits + units - 1) / units, each = (stages + splits - 1) / splits;
-            const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage, store = 8.0 * width;
+            const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage, store = (cols % 64 == 0 ? 15.0 : 20.0) * width;
             double cost = rounds * ((main > store ? main : store) + 200.0) * halves + store;
             if (splits > 1) cost += 4000.0 + (double)splits * m * n * 8.0 / 3600.0;       // the sums of the splits, written and read
             if (least == 0.0 || cost < least) {
