@@ -1922,7 +1922,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
         p.b[0] = rows_of_w;
         p.m = a->rows; p.n = n; p.k = a->width;
         p.target = a->target; p.vocab = a->vocab; p.first = first;
-        p.lse = a->lse; p.dloss = a->dloss;
+        p.lse = a->lse; p.dloss = a->dloss; p.positions = a->rows;
         p.out[0] = s.at<uint16_t>(d_at);
         p.out_ld[0] = piece;
         GG_CUDA(ctx, launch_product_rows(kDlogits, p, ctx->sm_count, s.st));
@@ -1955,7 +1955,8 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
         }
     }
     if (a->dh && splits > 1) {
-        GG_CUDA(ctx, launch_sum_splits(s.at<float>(f32_at), splits, a->rows, a->width, f32_ld, static_cast<uint16_t *>(a->dh), a->dh_ld, s.st));
+        GG_CUDA(ctx, launch_sum_splits(s.at<float>(f32_at), splits, a->rows, a->width, f32_ld, static_cast<uint16_t *>(a->dh), a->dh_ld, a->dloss, a->target,
+                                       s.st));
         ctx->launches += 1;
     }
     return GG_OK;
@@ -2058,7 +2059,7 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
         GG_CUDA(ctx, launch_product_drows(q, ctx->sm_count, s.st));
         ctx->launches += 1;
         if (splits > 1) {
-            GG_CUDA(ctx, launch_sum_splits(q.f32, splits, a->rows, a->width, f32_ld, q.out[0], a->dx_ld, s.st));
+            GG_CUDA(ctx, launch_sum_splits(q.f32, splits, a->rows, a->width, f32_ld, q.out[0], a->dx_ld, nullptr, nullptr, s.st));
             ctx->launches += 1;
         }
     }

@@ -28,6 +28,7 @@ constexpr int kMostStages = 16;
 constexpr int kOutBytes = 4096;         // 32 rows of 64 bf16 on their way out, for each warp of the end
 constexpr int kShared = 1024 + kRing + kEndWarps * kOutBytes;
 constexpr int kAccColumns = 256;        // of tensor memory for one accumulator; there are two
+constexpr int kLseRun = 16;             // stages after which the sums of a logit are taken out of the tensor cores
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Output {
@@ -59,11 +60,20 @@ struct Params {
     const int64_t *target;
     int64_t vocab, first;
     const float *lse, *dloss;
+    int64_t positions;
     float *f32;
     int64_t f32_ld;
     int mode;
     uint32_t *gave_up;
 };
+
+// 2^x in one instruction (2 units off at most; what would be subnormal is 0).
+__device__ __forceinline__ float power2(float x)
+{
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 // ------------------------------------------------------------------ activations
 // a / (1 + e^-a): an e^-a that overflows gives 0, as the product does.
@@ -198,6 +208,22 @@ struct Way {
     }
 };
 
+// The weights of the positions are mostly one number, 1 / their count, and d = weight * (p - 1) is then mostly that number too: rounded
+// to bf16 it may be off by 2^-8 in all of them alike (the gradient of 33 positions: 0.4 % off as a whole).  So d is kept relative to the
+// mantissa, 1 .. 2, of the first weight that is not 0, and the sums are multiplied by it: p - 1 itself is rounded (0.2 %, and
+// no longer alike).  A whole warp asks; only so many rows are looked at, beyond them it is 1.
+__device__ __forceinline__ float weight_mantissa(const float *dloss, const int64_t *target, int64_t rows)
+{
+    const int lane = threadIdx.x & 31;
+    for (int64_t r = 0; r < rows && r < 4096; r += 32) {
+        float g = 0.0f;
+        if (r + lane < rows && target[r + lane] >= 0) g = fabsf(dloss[r + lane]);
+        const uint32_t some = __ballot_sync(~0u, g > 1e-30f && g < 1e30f);
+        if (some != 0) return __uint_as_float((__float_as_uint(__shfl_sync(~0u, g, __ffs(some) - 1)) & 0x7FFFFFu) | 0x3F800000u);
+    }
+    return 1.0f;
+}
+
 // A tile's columns go to the two warps of a lane quarter in turn, 32 or 64 at a time.
 __device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int half, Way &way)
 {
@@ -228,51 +254,75 @@ __device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int ha
     }
 }
 
-// The sum is taken relative to the running maximum.  A NaN, which no maximum shows, reaches the sum by its own term.
-__device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half)
+// The logits of a warp's half of the tile, four runs of 32 columns: the tensor cores cut every sum at 24 bits, always towards 0, so a
+// long one comes out too small by (steps of 16) * 2^-25 (the loss of 16384 positions of width 4096 was 2.5e-6 off); after every
+// kLseRun stages what they have is added here, rounded, and they begin anew.
+struct Logits {
+    float v[8][16];
+    __device__ __forceinline__ void clear()
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) v[i][j] = 0.0f;
+    }
+    __device__ __forceinline__ void take(const Tile &t, int half)
+    {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int c = half * 32 + (i >> 1) * 64 + (i & 1) * 16;
+            if (t.col + c < t.end) {
+                float x[16];
+                tmem_read(t.acc + c, x);
+                tmem_read_wait();
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[i][j] += x[j];
+            }
+        }
+    }
+};
+
+// The sum is taken relative to the largest.  A NaN, which no maximum shows, reaches the sum by its own term.
+__device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half, Logits &l)
 {
     const bool there = t.row < p.m;
     const int64_t target = there ? p.target[t.row] - p.first : -1;
-    float most = -INFINITY, sum = 0.0f;
-#pragma unroll 1
-    for (int c = half * 32; t.col + c < t.end; c += 64) {
-        float v[32];
-        tmem_read(t.acc + c, v);
-        tmem_read_wait();
-        const int64_t col = t.col + c, left = t.end - col;
-        if (target >= col && target < col + 32 && target < t.end) {
-            const int j = (int)(target - col);
-            float l = 0.0f;
+    float most = -INFINITY, s0 = 0.0f, s1 = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) l = i == j ? v[i] : l;
-            p.target_logit[t.row] = l;
+    for (int i = 0; i < 8; ++i) {
+        const int64_t col = t.col + half * 32 + (i >> 1) * 64 + (i & 1) * 16, left = t.end - col;
+        if (left < 16) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) l.v[i][j] = j < left ? l.v[i][j] : -INFINITY;
         }
-        if (left < 32) {
+        if (target >= col && target < col + 16 && target < t.end) {
+            const int at = (int)(target - col);
+            float x = 0.0f;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = i < left ? v[i] : -INFINITY;
+            for (int j = 0; j < 16; ++j) x = j == at ? l.v[i][j] : x;
+            p.target_logit[t.row] = x;
         }
-        float top = most;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) top = fmaxf(top, v[i]);
-        const float base = top == -INFINITY ? 0.0f : top;
-        float s0 = sum * exp2f((most - base) * kLog2e), s1 = 0.0f;
-#pragma unroll
-        for (int i = 0; i < 32; i += 2) {
-            s0 += exp2f((v[i] - base) * kLog2e);
-            s1 += exp2f((v[i + 1] - base) * kLog2e);
-        }
-        sum = s0 + s1;
-        most = top;
-        __syncwarp();
+        for (int j = 0; j < 16; ++j) most = fmaxf(most, l.v[i][j]);
     }
-    if (there) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, sum);
+    const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+        if (t.col + half * 32 + (i >> 1) * 64 + (i & 1) * 16 < t.end) {
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) {
+                s0 += power2((l.v[i][j] - base) * kLog2e);
+                s1 += power2((l.v[i][j + 1] - base) * kLog2e);
+            }
+        }
+    if (there) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, s0 + s1);
 }
 
-__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int half, Way &way)
+__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int half, Way &way, float scale)
 {
     const bool there = t.row < p.m;
     const int64_t of = there ? p.target[t.row] : -1, target = of - p.first;
-    const float lse = there ? p.lse[t.row] : 0.0f, g = of < 0 ? 0.0f : of >= p.vocab ? NAN : p.dloss[t.row];
+    const float lse = there ? p.lse[t.row] : 0.0f, g = of < 0 ? 0.0f : of >= p.vocab ? NAN : p.dloss[t.row] / scale;
 #pragma unroll 1
     for (int c = half * 64; t.col + c < t.end; c += 128) {
 #pragma unroll
@@ -282,7 +332,7 @@ __device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int 
             tmem_read_wait();
             const int64_t col = t.col + c + 32 * part;
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = g * exp2f((v[i] - lse) * kLog2e);
+            for (int i = 0; i < 32; ++i) v[i] = g * power2((v[i] - lse) * kLog2e);
             if (target >= col && target < col + 32) {
                 const int j = (int)(target - col);
 #pragma unroll
@@ -323,7 +373,7 @@ __device__ __forceinline__ void add_old(const Output &o, const Tile &t, int64_t 
     }
 }
 
-__device__ __forceinline__ void end_store(const Params &p, const Tile &t, int half, Way &way)
+__device__ __forceinline__ void end_store(const Params &p, const Tile &t, int half, Way &way, float scale)
 {
     const bool there = t.row < p.m, narrow_out = p.mode == kStoreBf16 || p.mode == kAddBf16 || p.mode == kStoreBf16OfSum;
 #pragma unroll 1
@@ -334,6 +384,10 @@ __device__ __forceinline__ void end_store(const Params &p, const Tile &t, int ha
             tmem_read(t.acc + c + 32 * part, v);
             tmem_read_wait();
             const int64_t col = t.col + c + 32 * part;
+            if (p.mode == kStoreBf16 || p.mode == kAddBf16) {
+#pragma unroll
+                for (int i = 0; i < 32; ++i) v[i] *= scale;
+            }
             if (there && col < t.end) {
                 if (p.mode == kAddBf16) add_old(p.out[t.batch], t, col, v);
                 if (p.mode == kStoreF32 || p.mode == kAddF32 || p.mode == kStoreBf16OfSum) {
@@ -345,7 +399,10 @@ __device__ __forceinline__ void end_store(const Params &p, const Tile &t, int ha
                             v[4 * i] += o.x; v[4 * i + 1] += o.y; v[4 * i + 2] += o.z; v[4 * i + 3] += o.w;
                         }
                     }
-                    if (p.mode != kStoreBf16OfSum) {
+                    if (p.mode == kStoreBf16OfSum) {
+#pragma unroll
+                        for (int i = 0; i < 32; ++i) v[i] *= scale;
+                    } else {
 #pragma unroll
                         for (int i = 0; i < 8; ++i) f[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
                     }
@@ -484,24 +541,27 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         for (int w = first; w < p.total && !failed; w += step) {
             const int split = p.batches > 1 ? 0 : work_of(p, w).outer;
             const int begin = split_start(p, split), end = split_start(p, split + 1);
-            const uint32_t acc_phase = (kHalves == 2 ? units : units >> 1) & 1;
             if constexpr (kHalves == 1) {
-                const uint32_t acc = units & 1;
-                if (!barrier_wait(free_at + 8 * acc, acc_phase ^ 1)) { failed = true; break; }
-                tmem_after_sync();
-                for (int kb = begin; kb < end; ++kb) {
-                    if (!barrier_wait(full + 8 * stage, phase)) { failed = true; break; }
+                const int run = kEnd == kLse ? kLseRun : end - begin;
+                for (int from = begin; from < end && !failed; from += run, ++units) {
+                    const uint32_t acc = units & 1;
+                    if (!barrier_wait(free_at + 8 * acc, (units >> 1 & 1) ^ 1)) { failed = true; break; }
                     tmem_after_sync();
-                    issue(stage, acc, kb == begin);
-                    commit(empty + 8 * stage);
-                    if (++stage == stages) { stage = 0; phase ^= 1; }
+                    const int to = from + run < end ? from + run : end;
+                    for (int kb = from; kb < to; ++kb) {
+                        if (!barrier_wait(full + 8 * stage, phase)) { failed = true; break; }
+                        tmem_after_sync();
+                        issue(stage, acc, kb == from);
+                        commit(empty + 8 * stage);
+                        if (++stage == stages) { stage = 0; phase ^= 1; }
+                    }
+                    if (!failed) commit(done + 8 * acc);
                 }
-                if (failed) break;
-                commit(done + 8 * acc);
             } else {
                 // Both accumulators belong to this tile.  At its start and its end a ring's worth of stages is taken for the first
                 // half and then again for the second, so that the first half's end runs while the second is still summed, and
                 // the second's while the next tile's first has begun.
+                const uint32_t acc_phase = units & 1;
                 for (int kb = begin; kb < end && !failed;) {
                     const bool head = kb == begin;
                     const int left = end - kb, many = (int)stages;
@@ -527,8 +587,8 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                     if (last) commit(done + 8);
                     kb += run;
                 }
+                ++units;
             }
-            ++units;
         }
         if (failed) {
             commit(drained);
@@ -538,6 +598,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         // ---- ends
         const int half = (warp - 4) >> 2, quarter = warp & 3;
         Way way{ring + kRing + (uint32_t)(warp - 4) * kOutBytes, lane};
+        const float scale = (kEnd == kDlogits || kEnd == kStore) && p.dloss != nullptr ? weight_mantissa(p.dloss, p.target, p.positions) : 1.0f;
         uint32_t units = 0;
         for (int w = first; w < p.total && !failed; w += step) {
             const Work t = work_of(p, w);
@@ -547,23 +608,28 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             tile.batch = p.batches > 1 ? t.outer : 0;
             tile.split = p.batches > 1 ? 0 : t.outer;
             tile.n_tile = t.n_tile;
+            const int runs = kEnd == kLse ? (p.kblocks + kLseRun - 1) / kLseRun : kHalves;
+            Logits logits;
+            if constexpr (kEnd == kLse) logits.clear();
 #pragma unroll 1
-            for (int h = 0; h < kHalves; ++h, ++units) {
+            for (int h = 0; h < runs; ++h, ++units) {
                 const uint32_t acc = units & 1;
                 if (!barrier_wait(done + 8 * acc, units >> 1 & 1)) { failed = true; break; }
                 __syncwarp();
                 tmem_after_sync();
-                tile.row0 = (int64_t)t.m_tile * 128 * kCtas * kHalves + 256 * h + rank * 128 + quarter * 32;
+                tile.row0 = (int64_t)t.m_tile * 128 * kCtas * kHalves + (kHalves == 2 ? 256 * h : 0) + rank * 128 + quarter * 32;
                 tile.row = tile.row0 + lane;
                 tile.acc = tmem + acc * kAccColumns + ((uint32_t)quarter << 21);      // (lane 32 * quarter, in the upper half of the word)
                 if constexpr (kEnd == kGated) end_gated(p, tile, half, way);
-                if constexpr (kEnd == kLse) end_lse(p, tile, half);
-                if constexpr (kEnd == kDlogits) end_dlogits(p, tile, half, way);
-                if constexpr (kEnd == kStore) end_store(p, tile, half, way);
+                if constexpr (kEnd == kLse) logits.take(tile, half);
+                if constexpr (kEnd == kDlogits) end_dlogits(p, tile, half, way, scale);
+                if constexpr (kEnd == kStore) end_store(p, tile, half, way, scale);
                 __syncwarp();
                 tmem_before_sync();
                 if (lane == 0) barrier_arrive(peer_address(free_at + 8 * acc, 0));
             }
+            if constexpr (kEnd == kLse)
+                if (!failed) end_lse(p, tile, half, logits);
         }
     }
     if (failed && p.gave_up != nullptr) *reinterpret_cast<volatile uint32_t *>(p.gave_up) = 1;
@@ -669,7 +735,7 @@ __global__ void __launch_bounds__(256) gated_slopes_any_kernel(const Bf16Matrix 
 __device__ __forceinline__ float2 join(float2 a, float2 b)
 {
     const float top = fmaxf(a.x, b.x), base = top == -INFINITY ? 0.0f : top;
-    return make_float2(top, a.y * exp2f((a.x - base) * kLog2e) + b.y * exp2f((b.x - base) * kLog2e));
+    return make_float2(top, a.y * power2((a.x - base) * kLog2e) + b.y * power2((b.x - base) * kLog2e));
 }
 __device__ __forceinline__ void finish_row(float2 v, int64_t row, float target_logit, const int64_t *target, int64_t vocab, float *lse, float *loss)
 {
@@ -701,12 +767,14 @@ __global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, in
 }
 
 // 32 runs of four columns a CTA, eight threads for each, which take every eighth split and are added in order.
-__global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld)
+__global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld,
+                                                         const float *dloss, const int64_t *target)
 {
     __shared__ float4 of[8][33];
     const int64_t groups = (cols + 3) / 4;
     const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
     wait_for_the_one_before();
+    const float scale = dloss != nullptr ? weight_mantissa(dloss, target, rows) : 1.0f;
     for (int64_t first = blockIdx.x * 32ll; first < groups * rows; first += gridDim.x * 32ll) {
         const int64_t i = first + lane, row = i / groups, col = (i - row * groups) * 4;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -725,7 +793,7 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int s
                 const float4 v = of[j][lane];
                 s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
-            const float v[4] = {s.x, s.y, s.z, s.w};
+            const float v[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
             uint16_t *o = out + row * out_ld + col;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
@@ -974,7 +1042,7 @@ cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, 
     if (p.stages > kMostStages) p.stages = kMostStages;
     p.act = a.act;
     p.part = a.part; p.target_logit = a.target_logit; p.target = a.target; p.vocab = a.vocab; p.first = a.first;
-    p.lse = a.lse; p.dloss = a.dloss;
+    p.lse = a.lse; p.dloss = a.dloss; p.positions = a.positions;
     p.f32 = a.f32; p.f32_ld = a.f32_ld; p.mode = a.mode; p.gave_up = a.gave_up;
     auto kernel = product_kernel<kCtas, kHalves, kAT, kBT, kEnd>;
     static std::atomic<uint64_t> known{0};      // devices on which the kernel has its shared memory
@@ -1060,9 +1128,10 @@ cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, cons
     return launch_after(st, dim3((unsigned)((rows + each - 1) / each)), 1024, 0, lse_finish_kernel, part, n_part, rows, each, target_logit, target, vocab, lse, loss);
 }
 
-cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, cudaStream_t st)
+cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *dloss,
+                              const int64_t *target, cudaStream_t st)
 {
-    return launch_after(st, dim3(grid_of((cols + 3) / 4 * rows * 8)), 256, 0, sum_splits_kernel, f32, splits, rows, cols, f32_ld, out, out_ld);
+    return launch_after(st, dim3(grid_of((cols + 3) / 4 * rows * 8)), 256, 0, sum_splits_kernel, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target);
 }
 
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,
