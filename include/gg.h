@@ -335,10 +335,17 @@ typedef struct {
 } gg_layer_norm_grad_args;
 gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *args, void *stream);
 
+/* The operators around matrix products that follow take their operands in bf16 (what the tensor cores multiply; gg_adamw_step keeps
+ * such a copy of fp32 weights) and sum in fp32.  A matrix whose rows do not all start on a 16-byte boundary is copied into
+ * scratch first.  Scratch is the context's: a call that needs more than any before it allocates, during a stream
+ * capture too, and what it had stays until gg_destroy for graphs captured earlier.  Outputs may not overlap the operands.
+ * The kernels wait for copies and for one another's warps inside a pair of CTAs; every such wait is bounded, and one that
+ * ran out is reported by the next of these calls as GG_ERR_CUDA. */
+
 /* Softmax cross entropy of a linear output layer, without its logits: with l = h w^T,
  *     lse[r]  = log sum over v of exp(l[r][v]),     loss[r] = lse[r] - l[r][target[r]]
  * A negative target marks a position without one: its loss is 0 and its gradient too.  A target of `vocab` or more makes
- * the row's loss and gradient nan.  The product takes bf16 operands and sums in fp32; the logits stay fp32 and never reach memory.  A row
+ * the row's loss and gradient nan.  The logits stay fp32 and never reach memory.  A row
  * whose logits hold an inf or nan gets a lse and a loss that are not finite; other rows do not see it. */
 typedef struct {
     const void    *h;            /* device, bf16 [rows][width]: the features                  */
@@ -354,7 +361,8 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *args, void 
 /* Its gradient for dloss = dL/dloss and the lse that gg_cross_entropy wrote.  With
  *     d[r][v] = dloss[r] (exp(l[r][v] - lse[r]) - [v = target[r]]):     dh = d w,     dw = d^T h
  * The logits are computed again, a piece of the vocabulary at a time; d of the piece lies in scratch, rounded to bf16 as the
- * products take it.  Sums are fp32, in a fixed order.  Where a target is negative, d is 0 whatever the logits are, but h has to be finite
+ * products take it (relative to the mantissa of the first weight, so that the rounding is that of exp(l - lse) - 1 and not one
+ * error that all positions share).  Sums are fp32, in a fixed order.  Where a target is negative, d is 0 whatever the logits are, but h has to be finite
  * there (dw adds 0 * h).  Scratch: up to 512 MB for d, and 4 bytes for each element of dh. */
 typedef struct {
     const float   *dloss;        /* device [rows]                                             */
@@ -513,9 +521,11 @@ gg_status gg_timing_read(gg_ctx *ctx, double *ms_first, int64_t *n_first, double
  *   GG_HOOK_RESIDENT_MODE   0 (default): two launches; 1: the one-launch form whenever it can run
  *   GG_HOOK_EXTRA_ARRIVALS  arrivals the fitting CTA waits for beyond the CTAs that exist (default 0); a positive
  *                           value makes its wait run out: the way to test the time-out path without any fault (the
- *                           one-cluster-per-segment form then expects 16 bytes per unit more than it copies, with
- *                           the same effect on its wait)
- *   GG_HOOK_WAIT_CAP        polls (about half a microsecond each) after which a wait gives up (default 2^18) */
+ *                           one-cluster-per-segment form, and the products of gg_cross_entropy, gg_gated_linear and
+ *                           their gradients, then expect 16 bytes per unit more than they copy, with the same effect
+ *                           on their waits; the next such call reports it as GG_ERR_CUDA)
+ *   GG_HOOK_WAIT_CAP        polls (about half a microsecond each) after which a wait gives up (default 2^18; the products
+ *                           take 2^22 and more for long sums unless another value is set) */
 #define GG_HOOK_RESIDENT_MODE  0
 #define GG_HOOK_EXTRA_ARRIVALS 1
 #define GG_HOOK_WAIT_CAP       2

@@ -1822,6 +1822,16 @@ struct Operand {
     }
 };
 
+ProductArgs product_args(gg_ctx *ctx)
+{
+    ProductArgs p{};
+    p.segments = p.batches = p.splits = 1;
+    p.gave_up = ctx->gave_up;
+    p.polls = ctx->wait_cap != kWaitCap ? ctx->wait_cap : 0;
+    p.extra_bytes = ctx->expect_delta > 0 ? 16u * (uint32_t)ctx->expect_delta : 0u;
+    return p;
+}
+
 // A wait that ran out in an earlier call is this call's error: its results were not finished.
 gg_status product_alive(gg_ctx *ctx)
 {
@@ -1866,16 +1876,14 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
     if ((st = s.grow()) != GG_OK || (st = h.lay(s)) != GG_OK || (st = w.lay(s)) != GG_OK) return st;
     for (int64_t r = 0; r < a->rows; r += kLossRows) {
         const int64_t rows = std::min(a->rows - r, kLossRows);
-        ProductArgs p{};
+        ProductArgs p = product_args(ctx);
         p.a[0] = matrix_of(h.m.p + r * h.m.ld, rows, a->width, h.m.ld);
         p.b[0] = w.m;
         p.m = rows; p.n = a->vocab; p.k = a->width;
-        p.segments = p.batches = p.splits = 1;
         p.part = s.at<float2>(part_at);
         p.target_logit = s.at<float>(logit_at);
         p.target = a->target + r;
         p.vocab = a->vocab;
-        p.gave_up = ctx->gave_up;
         GG_CUDA(ctx, launch_product_rows(kLse, p, ctx->sm_count, s.st));
         GG_CUDA(ctx, launch_lse_finish(p.part, product_partials(rows, a->vocab, a->width, ctx->sm_count), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
                                        a->loss ? a->loss + r : nullptr, s.st));
@@ -1915,9 +1923,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
     for (int64_t i = 0; i < n_pieces; ++i) {
         const int64_t first = i * piece, n = std::min(piece, a->vocab - first);
         const Bf16Matrix d{s.at<uint16_t>(d_at), a->rows, n, piece}, rows_of_w{w.m.p + first * w.m.ld, n, a->width, w.m.ld};
-        ProductArgs p{};
-        p.segments = p.batches = p.splits = 1;
-        p.gave_up = ctx->gave_up;
+        ProductArgs p = product_args(ctx);
         p.a[0] = h.m;
         p.b[0] = rows_of_w;
         p.m = a->rows; p.n = n; p.k = a->width;
@@ -1983,16 +1989,14 @@ gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *a, void *stre
     Operand x(matrix_of(a->x, a->rows, a->width, a->x_ld), s), wg(matrix_of(a->w_gate, a->hidden, a->width, a->w_gate_ld), s),
         wu(matrix_of(a->w_up, a->hidden, a->width, a->w_up_ld), s);
     if ((st = s.grow()) != GG_OK || (st = x.lay(s)) != GG_OK || (st = wg.lay(s)) != GG_OK || (st = wu.lay(s)) != GG_OK) return st;
-    ProductArgs p{};
+    ProductArgs p = product_args(ctx);
     p.a[0] = x.m;
     p.b[0] = wg.m;
     p.b[1] = wu.m;
     p.m = a->rows; p.n = a->hidden; p.k = a->width;
-    p.segments = p.batches = p.splits = 1;
     p.out[0] = static_cast<uint16_t *>(a->h); p.out[1] = static_cast<uint16_t *>(a->gate); p.out[2] = static_cast<uint16_t *>(a->up);
     p.out_ld[0] = a->h_ld; p.out_ld[1] = a->gate_ld; p.out_ld[2] = a->up_ld;
     p.act = a->act;
-    p.gave_up = ctx->gave_up;
     if (gated_row(a->rows, a->width)) GG_CUDA(ctx, launch_gated_row(p, ctx->sm_count, s.st));
     else GG_CUDA(ctx, launch_product_rows(kGated, p, ctx->sm_count, s.st));
     ctx->launches += 1;
@@ -2039,9 +2043,7 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
     GG_CUDA(ctx, launch_gated_slopes(matrix_of(a->dh, a->rows, a->hidden, a->dh_ld), matrix_of(a->gate, a->rows, a->hidden, a->gate_ld),
                                      matrix_of(a->up, a->rows, a->hidden, a->up_ld), a->act, dgate, dup, ld, s.st));
     ctx->launches += 1;
-    ProductArgs p{};
-    p.segments = p.batches = p.splits = 1;
-    p.gave_up = ctx->gave_up;
+    ProductArgs p = product_args(ctx);
     p.a[0] = matrix_of(dgate, a->rows, a->hidden, ld);
     p.a[1] = matrix_of(dup, a->rows, a->hidden, ld);
     if (a->dx) {

@@ -64,6 +64,7 @@ struct Params {
     float *f32;
     int64_t f32_ld;
     int mode;
+    uint32_t polls, extra_bytes;        // after so many a wait gives up; test hook: bytes that are expected and never come
     uint32_t *gave_up;
 };
 
@@ -485,9 +486,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             const int n0 = t.n_tile * p.cols + (kEnd == kGated ? 0 : (int)rank * rows_b);
             const int end = split_start(p, split + 1);
             for (int kb = split_start(p, split); kb < end; ++kb) {
-                if (!barrier_wait(empty + 8 * stage, phase ^ 1)) { failed = true; break; }
+                if (!barrier_wait(empty + 8 * stage, phase ^ 1, p.polls)) { failed = true; break; }
                 if (leader) {
-                    if (rank == 0) barrier_expect(full + 8 * stage, bytes * kCtas);
+                    if (rank == 0) barrier_expect(full + 8 * stage, bytes * kCtas + p.extra_bytes);
                     const int segment = kb >= p.kblocks, k0 = (kb - segment * p.kblocks) * kBlockK, which = segment | batch;
                     const uint32_t to_a = ring + stage * bytes, to_b = to_a + bytes_a;
                     const uint32_t signal = kCtas == 2 ? peer_address(full + 8 * stage, 0) : full + 8 * stage;
@@ -520,7 +521,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             for (uint32_t i = 0; i < stages && i < issued; ++i) {
                 stage = stage == 0 ? stages - 1 : stage - 1;
                 if (stage == stages - 1) phase ^= 1;
-                barrier_wait(full + 8 * stage, phase);
+                barrier_wait(full + 8 * stage, phase, p.polls / 16 + 1);
             }
     } else if (warp == 1 && rank == 0) {
         // ---- products
@@ -545,11 +546,11 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 const int run = kEnd == kLse ? kLseRun : end - begin;
                 for (int from = begin; from < end && !failed; from += run, ++units) {
                     const uint32_t acc = units & 1;
-                    if (!barrier_wait(free_at + 8 * acc, (units >> 1 & 1) ^ 1)) { failed = true; break; }
+                    if (!barrier_wait(free_at + 8 * acc, (units >> 1 & 1) ^ 1, p.polls)) { failed = true; break; }
                     tmem_after_sync();
                     const int to = from + run < end ? from + run : end;
                     for (int kb = from; kb < to; ++kb) {
-                        if (!barrier_wait(full + 8 * stage, phase)) { failed = true; break; }
+                        if (!barrier_wait(full + 8 * stage, phase, p.polls)) { failed = true; break; }
                         tmem_after_sync();
                         issue(stage, acc, kb == from);
                         commit(empty + 8 * stage);
@@ -567,17 +568,17 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                     const int left = end - kb, many = (int)stages;
                     const int run = head || left <= many ? (left < many ? left : many) : 1;
                     const bool last = left == run;
-                    if (head && !barrier_wait(free_at, acc_phase ^ 1)) { failed = true; break; }
+                    if (head && !barrier_wait(free_at, acc_phase ^ 1, p.polls)) { failed = true; break; }
                     uint32_t at = stage, at_phase = phase;
                     for (int i = 0; i < run; ++i) {
-                        if (!barrier_wait(full + 8 * at, at_phase)) { failed = true; break; }
+                        if (!barrier_wait(full + 8 * at, at_phase, p.polls)) { failed = true; break; }
                         tmem_after_sync();
                         issue(at, 0, head && i == 0);
                         if (++at == stages) { at = 0; at_phase ^= 1; }
                     }
                     if (failed) break;
                     if (last) commit(done);
-                    if (head && !barrier_wait(free_at + 8, acc_phase ^ 1)) { failed = true; break; }
+                    if (head && !barrier_wait(free_at + 8, acc_phase ^ 1, p.polls)) { failed = true; break; }
                     tmem_after_sync();
                     for (int i = 0; i < run; ++i) {
                         issue(stage, 1, head && i == 0);
@@ -592,7 +593,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         }
         if (failed) {
             commit(drained);
-            barrier_wait(drained, 0);
+            barrier_wait(drained, 0, p.polls);
         }
     } else if (warp >= 4) {
         // ---- ends
@@ -614,7 +615,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 #pragma unroll 1
             for (int h = 0; h < runs; ++h, ++units) {
                 const uint32_t acc = units & 1;
-                if (!barrier_wait(done + 8 * acc, units >> 1 & 1)) { failed = true; break; }
+                if (!barrier_wait(done + 8 * acc, units >> 1 & 1, p.polls)) { failed = true; break; }
                 __syncwarp();
                 tmem_after_sync();
                 tile.row0 = (int64_t)t.m_tile * 128 * kCtas * kHalves + (kHalves == 2 ? 256 * h : 0) + rank * 128 + quarter * 32;
@@ -1044,6 +1045,10 @@ cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, 
     p.part = a.part; p.target_logit = a.target_logit; p.target = a.target; p.vocab = a.vocab; p.first = a.first;
     p.lse = a.lse; p.dloss = a.dloss; p.positions = a.positions;
     p.f32 = a.f32; p.f32_ld = a.f32_ld; p.mode = a.mode; p.gave_up = a.gave_up;
+    // (the longest wait, for the sums of a tile, grows with the stages: about 0.3 us each)
+    const int64_t polls = (int64_t)(1 << 22) + 8 * (int64_t)p.all_k;
+    p.polls = a.polls != 0 ? a.polls : polls < 0xFFFFFFFF ? (uint32_t)polls : 0xFFFFFFFF;
+    p.extra_bytes = a.extra_bytes;
     auto kernel = product_kernel<kCtas, kHalves, kAT, kBT, kEnd>;
     static std::atomic<uint64_t> known{0};      // devices on which the kernel has its shared memory
     int device = 0;

@@ -43,6 +43,8 @@ struct ProductArgs {
     int64_t f32_ld;
     int mode;
     uint32_t *gave_up;          // host-visible word: set if a wait inside the kernel ran out
+    uint32_t polls;             // after which one does (0: the default)
+    uint32_t extra_bytes;       // test hook: bytes a stage expects beyond what is copied (the waits then run out)
 };
 
 // C = A B^T with both operands K-major ...

@@ -24,11 +24,10 @@ __device__ __forceinline__ bool barrier_test(uint32_t bar, uint32_t parity)
                  : "=r"(done) : "r"(bar), "r"(parity) : "memory");
     return done != 0;
 }
-// Every wait ends: try_wait itself sleeps for a while, and after so many of them the caller gives up.
-constexpr uint32_t kBarrierPolls = 1u << 22;
-__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity)
+// Every wait ends: after so many polls, of half a microsecond or so, the caller gives up.
+__device__ __forceinline__ bool barrier_wait(uint32_t bar, uint32_t parity, uint32_t polls)
 {
-    for (uint32_t i = 0; i < kBarrierPolls; ++i)
+    for (uint32_t i = 0; i < polls; ++i)
         if (barrier_test(bar, parity)) return true;
     return false;
 }

@@ -248,3 +248,30 @@ def test_refusals(ctx):
         assert e.value.status == status, field
         setattr(run.args, field, keep)
     assert ctx.launch_count == before
+
+
+@pytest.mark.parametrize("rows", [70, 300, 700])
+def test_a_wait_that_runs_out_is_reported_and_leaves_the_context_usable(rows):
+    # the barriers of the copies expect more bytes than come: every wait of the kernel runs out, none faults
+    from paper_2506_00486_b200 import Context, GGError
+    from paper_2506_00486_b200.binding import HOOK_EXTRA_ARRIVALS, HOOK_WAIT_CAP
+    mine = Context(0)
+    x, wg, wu, dh = problem(11, rows, 200, 300)
+    want = mine.gg_gated_linear(x, wg, wu, keep=True)
+    wantg = mine.gg_gated_linear_grad(dh, x, wg, wu, want["gate"], want["up"])
+    mine.gg_test_hook(HOOK_EXTRA_ARRIVALS, 1)
+    mine.gg_test_hook(HOOK_WAIT_CAP, 256)
+    mine.gg_gated_linear(x, wg, wu)
+    torch.cuda.synchronize()
+    with pytest.raises(GGError, match="ran out"):
+        mine.gg_gated_linear(x, wg, wu)
+    mine.gg_gated_linear_grad(dh, x, wg, wu, want["gate"], want["up"])
+    torch.cuda.synchronize()
+    mine.gg_test_hook(HOOK_EXTRA_ARRIVALS, 0)
+    mine.gg_test_hook(HOOK_WAIT_CAP, 1 << 18)
+    with pytest.raises(GGError, match="ran out"):
+        mine.gg_gated_linear(x, wg, wu)
+    again = mine.gg_gated_linear(x, wg, wu, keep=True)
+    grad = mine.gg_gated_linear_grad(dh, x, wg, wu, want["gate"], want["up"])
+    assert all(torch.equal(again[k], want[k]) for k in want) and all(torch.equal(grad[k], wantg[k]) for k in wantg)
+    mine.close()
