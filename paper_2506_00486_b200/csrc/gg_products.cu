@@ -77,60 +77,88 @@ __device__ __forceinline__ float power2(float x)
 }
 
 // ------------------------------------------------------------------ activations
-// a / (1 + e^-a): an e^-a that overflows gives 0, as the product does.
-__device__ __forceinline__ float sigmoid(float a) { return __fdividef(1.0f, 1.0f + __expf(-a)); }
-// The normal distribution function of a and e = exp(-a^2 / 2).  Its tail at -z is e R(z), R falling slowly from 1/2; R is a polynomial in
-// t = 1 / (1 + 0.3 z) without a constant term, fitted for least relative error over [0, 20] (6.5e-7 in fp32; erfcf takes three times the
-// instructions, and its 1 - erf is no good for negative a).
-__device__ __forceinline__ float normal(float a, float &e)
+// Two at a time: the ends of a narrow product are bound by them (gelu at width 896: 97 us a call with erfcf, 75 one by one, 67 so; silu 52 to 65).
+__device__ __forceinline__ float reciprocal(float x)
 {
-    const float z = fabsf(a), t = __fdividef(1.0f, 1.0f + 0.3f * z);
-    float r = 0.0330343359f;
-    r = r * t - 0.1463946f;
-    r = r * t + 0.188128167f;
-    r = r * t - 0.0373476765f;
-    r = r * t + 0.120195597f;
-    r = r * t + 0.102349824f;
-    r = r * t + 0.120381962f;
-    r = r * t + 0.119652203f;
-    e = __expf(-0.5f * z * z);
-    const float tail = e * (r * t);
-    return a > 0.0f ? 1.0f - tail : tail;
+    float y;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ f32x2 power2(f32x2 x)
+{
+    const float2 f = halves(x);
+    return pair(power2(f.x), power2(f.y));
+}
+__device__ __forceinline__ f32x2 reciprocal(f32x2 x)
+{
+    const float2 f = halves(x);
+    return pair(reciprocal(f.x), reciprocal(f.y));
+}
+// 1 / (1 + e^-a): an e^-a that overflows gives 0.
+__device__ __forceinline__ f32x2 sigmoid(f32x2 a) { return reciprocal(add2(power2(mul2(a, both(-kLog2e))), both(1.0f))); }
+// The normal distribution function of a and e = exp(-a^2 / 2).  Its tail at -z is e R(z), R falling slowly from 1/2; R is a polynomial in
+// t = 1 / (1 + 0.3 z) without a constant term, fitted for least relative error over [0, 20] (6.5e-7 in fp32).  (1 + erf is no good for negative a.)
+__device__ __forceinline__ f32x2 normal(f32x2 a, f32x2 &e)
+{
+    const f32x2 z = a & 0x7FFFFFFF7FFFFFFFull, t = reciprocal(fma2(z, both(0.3f), both(1.0f)));
+    f32x2 r = both(0.0330343359f);
+    r = fma2(r, t, both(-0.1463946f));
+    r = fma2(r, t, both(0.188128167f));
+    r = fma2(r, t, both(-0.0373476765f));
+    r = fma2(r, t, both(0.120195597f));
+    r = fma2(r, t, both(0.102349824f));
+    r = fma2(r, t, both(0.120381962f));
+    r = fma2(r, t, both(0.119652203f));
+    e = power2(mul2(mul2(z, z), both(-0.5f * kLog2e)));
+    const float2 tail = halves(mul2(e, mul2(r, t))), x = halves(a);
+    return pair(x.x > 0.0f ? 1.0f - tail.x : tail.x, x.y > 0.0f ? 1.0f - tail.y : tail.y);
+}
+// The sigmoid of 2 sqrt(2 / pi) (a + 0.044715 a^3), which is (1 + tanh) / 2, and the derivative of that argument.  Beyond 30 it is 0 or 1.
+__device__ __forceinline__ f32x2 cubic_sigmoid(f32x2 a, f32x2 &inner)
+{
+    const float2 f = halves(a);
+    const f32x2 b = pair(fminf(fmaxf(f.x, -30.0f), 30.0f), fminf(fmaxf(f.y, -30.0f), 30.0f)), q = mul2(b, b);
+    inner = fma2(q, both(1.5957691216057308f * 0.134145f), both(1.5957691216057308f));
+    return sigmoid(mul2(b, fma2(q, both(1.5957691216057308f * 0.044715f), both(1.5957691216057308f))));
+}
+// max(a, 0), NaN for NaN
+__device__ __forceinline__ float positive(float a)
+{
+    float y;
+    asm("max.NaN.f32 %0, %1, 0f00000000;" : "=f"(y) : "f"(a));
+    return y;
 }
 template <int kAct>
-__device__ __forceinline__ float activation(float a)
+__device__ __forceinline__ f32x2 activation(f32x2 a)
 {
-    if constexpr (kAct == GG_ACT_SILU) return a * sigmoid(a);
-    if constexpr (kAct == GG_ACT_GELU) {
-        float e;
-        return a * normal(a, e);
-    }
-    if constexpr (kAct == GG_ACT_GELU_TANH) {           // (1 + tanh z) / 2 = sigmoid(2 z), which is 0 or 1 beyond 30
-        const float b = fminf(fmaxf(a, -30.0f), 30.0f);
-        return a * sigmoid(1.5957691216057308f * (b + 0.044715f * b * b * b));
-    }
-    return a > 0.0f ? a : (a != a ? a : 0.0f);
+    f32x2 more;
+    if constexpr (kAct == GG_ACT_SILU) return mul2(a, sigmoid(a));
+    if constexpr (kAct == GG_ACT_GELU) return mul2(a, normal(a, more));
+    if constexpr (kAct == GG_ACT_GELU_TANH) return mul2(a, cubic_sigmoid(a, more));
+    const float2 f = halves(a);
+    return pair(positive(f.x), positive(f.y));
 }
 // act(a) and its derivative
 template <int kAct>
-__device__ __forceinline__ void slope(float a, float &value, float &d)
+__device__ __forceinline__ void slope(f32x2 a, f32x2 &value, f32x2 &d)
 {
+    f32x2 more;
     if constexpr (kAct == GG_ACT_SILU) {
-        const float s = sigmoid(a);
-        value = a * s;
-        d = s + value * (1.0f - s);
+        const f32x2 s = sigmoid(a);
+        value = mul2(a, s);
+        d = fma2(value, fma2(s, both(-1.0f), both(1.0f)), s);
     } else if constexpr (kAct == GG_ACT_GELU) {
-        float e;
-        const float c = normal(a, e);
-        value = a * c;
-        d = c + a * 0.3989422804014327f * e;
+        const f32x2 c = normal(a, more);
+        value = mul2(a, c);
+        d = fma2(mul2(a, both(0.3989422804014327f)), more, c);
     } else if constexpr (kAct == GG_ACT_GELU_TANH) {
-        const float b = fminf(fmaxf(a, -30.0f), 30.0f), s = sigmoid(1.5957691216057308f * (b + 0.044715f * b * b * b));
-        value = a * s;
-        d = s + value * (1.0f - s) * 1.5957691216057308f * (1.0f + 0.134145f * b * b);
+        const f32x2 s = cubic_sigmoid(a, more);
+        value = mul2(a, s);
+        d = fma2(mul2(value, fma2(s, both(-1.0f), both(1.0f))), more, s);
     } else {
+        const float2 f = halves(a);
         value = activation<GG_ACT_RELU>(a);
-        d = a > 0.0f ? 1.0f : (a != a ? a : 0.0f);
+        d = pair(f.x > 0.0f ? 1.0f : f.x != f.x ? f.x : 0.0f, f.y > 0.0f ? 1.0f : f.y != f.y ? f.y : 0.0f);
     }
 }
 template <typename F>
@@ -247,9 +275,8 @@ __device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int ha
         }
         by_activation(p.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < 32; ++i) g[i] = activation<decltype(act)::value>(g[i]) * u[i];
+            for (int i = 0; i < 16; ++i) w[i] = narrow2(mul2(activation<decltype(act)::value>(pair(g[2 * i], g[2 * i + 1])), pair(u[2 * i], u[2 * i + 1])));
         });
-        narrow_row(g, w);
         way.put(0, w);
         way.send<4>(p, p.out[0], t, t.col + c);
     }
@@ -689,12 +716,11 @@ __global__ void __launch_bounds__(256) gated_slopes_kernel(const Bf16Matrix dh, 
             uint32_t wg[4], wu[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const float2 df = halves(widen2(dw[j])), gf = halves(widen2(gw[j])), uf = halves(widen2(uw[j]));
-                float v0, v1, s0, s1;
-                slope<kAct>(gf.x, v0, s0);
-                slope<kAct>(gf.y, v1, s1);
-                wg[j] = narrow2(pair(df.x * uf.x * s0, df.y * uf.y * s1));
-                wu[j] = narrow2(pair(df.x * v0, df.y * v1));
+                const f32x2 d2 = widen2(dw[j]);
+                f32x2 value, s;
+                slope<kAct>(widen2(gw[j]), value, s);
+                wg[j] = narrow2(mul2(mul2(d2, widen2(uw[j])), s));
+                wu[j] = narrow2(mul2(d2, value));
             }
             *reinterpret_cast<uint4 *>(dgate + row[k] * ld + col[k]) = make_uint4(wg[0], wg[1], wg[2], wg[3]);
             *reinterpret_cast<uint4 *>(dup + row[k] * ld + col[k]) = make_uint4(wu[0], wu[1], wu[2], wu[3]);
@@ -713,6 +739,7 @@ __global__ void __launch_bounds__(256) gated_slopes_any_kernel(const Bf16Matrix 
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int64_t col = first + 256 * k;
+                d[k] = g[k] = u[k] = 0.0f;
                 if (col < dh.cols) {
                     d[k] = widen<uint16_t>(dh.p[row * dh.ld + col]);
                     g[k] = widen<uint16_t>(gate.p[row * gate.ld + col]);
@@ -720,13 +747,19 @@ __global__ void __launch_bounds__(256) gated_slopes_any_kernel(const Bf16Matrix 
                 }
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t col = first + 256 * k;
-                if (col < dh.cols) {
-                    float v, s;
-                    slope<kAct>(g[k], v, s);
-                    dgate[row * ld + col] = narrow<uint16_t>(d[k] * u[k] * s);
-                    dup[row * ld + col] = narrow<uint16_t>(d[k] * v);
+            for (int k = 0; k < 4; k += 2) {
+                f32x2 value, s;
+                slope<kAct>(pair(g[k], g[k + 1]), value, s);
+                const f32x2 d2 = pair(d[k], d[k + 1]);
+                const uint32_t wg = narrow2(mul2(mul2(d2, pair(u[k], u[k + 1])), s)), wu = narrow2(mul2(d2, value));
+                const int64_t at = row * ld + first + 256 * k;
+                if (first + 256 * k < dh.cols) {
+                    dgate[at] = (uint16_t)wg;
+                    dup[at] = (uint16_t)wu;
+                }
+                if (first + 256 * k + 256 < dh.cols) {
+                    dgate[at + 256] = (uint16_t)(wg >> 16);
+                    dup[at + 256] = (uint16_t)(wu >> 16);
                 }
             }
         }
@@ -918,7 +951,7 @@ __global__ void __launch_bounds__(kRowWarps * 32, 2) gated_row_kernel(const RowA
                 const float gate = lane == 0 ? v[0] : v[2], up = lane == 0 ? v[1] : v[3];
                 const int64_t of = 2 * now.unit + lane;
                 if (lane < 2 && of < a.n) {
-                    by_activation(a.act, [&](auto act) { a.h[of] = narrow<uint16_t>(activation<decltype(act)::value>(gate) * up); });
+                    by_activation(a.act, [&](auto act) { a.h[of] = narrow<uint16_t>(halves(activation<decltype(act)::value>(both(gate))).x * up); });
                     if (a.gate != nullptr) a.gate[of] = narrow<uint16_t>(gate);
                     if (a.up != nullptr) a.up[of] = narrow<uint16_t>(up);
                 }
