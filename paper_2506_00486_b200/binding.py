@@ -895,6 +895,7 @@ class Context:
         rows, width = self._features(a, h, w, target)
         self._vector("dloss", dloss, rows)
         self._vector("lse", lse, rows)
+        self._here(dloss=dloss, lse=lse)
         if accumulate and want_dw and dw is None:
             raise ValueError("accumulate adds to dw: give it")
         dh, dw = self._result("dh", dh, h, want_dh), self._result("dw", dw, w, want_dw)
@@ -912,13 +913,20 @@ class Context:
         rows, width = self._operand(h, "h")
         vocab, _ = self._operand(w, "w", cols=width)
         self._vector("target", target, rows, torch.int64)
+        self._here(target=target)
         a.h, a.rows, a.width, a.h_ld, a.dtype = _ptr(h), rows, width, _ld(h), GG_BF16
         a.w, a.vocab, a.w_ld, a.target = _ptr(w), vocab, _ld(w), _ptr(target)
         return rows, width
 
+    def _here(self, **tensors):
+        for name, t in tensors.items():
+            if t is not None and t.is_cuda and t.device.index != (self.device.index or 0):
+                raise ValueError(f"{name} is on {t.device}, the context on cuda:{self.device.index or 0}")
+
     def _operand(self, t, name, rows=None, cols=None):
         """A matrix of a product: bfloat16, what the tensor cores take."""
         shape = self._rows(t, name)
+        self._here(**{name: t})
         if t.dtype != torch.bfloat16:
             raise TypeError(f"{name} must be bfloat16 (AdamW keeps a bfloat16 copy of float32 weights: w_copy)")
         if (rows is not None and shape[0] != rows) or (cols is not None and shape[1] != cols):
@@ -931,6 +939,7 @@ class Context:
         if t is None:
             return self._new(like.shape, like.dtype)
         self._rows(t, name, like)
+        self._here(**{name: t})
         return t
 
     # ------------------------------------------------------------- gated block
@@ -1006,6 +1015,7 @@ class Context:
         y = self._result("out", out, x)
         if t_dev is not None:
             self._vector("t_dev", t_dev, 1, torch.int64)
+        self._here(x=x, residual=residual, t_dev=t_dev)
         a = DropoutArgs()
         a.x, a.rows, a.cols, a.x_ld, a.dtype = _ptr(x), rows, cols, _ld(x), _dtype_code(x.dtype)
         a.residual, a.residual_ld = _ptr(residual), cols if residual is None else _ld(residual)
