@@ -174,66 +174,81 @@ __device__ __forceinline__ void by_activation(int act, F f)
 struct Tile {
     int64_t row0, row;   // first row of the warp, row of this thread
     int64_t col;         // first column of the tile
-    int64_t end;         // behind its last
+    int width;           // its columns that C has
     int batch, split, n_tile;
     uint32_t acc;        // its sums: tensor memory of the warp's lanes
 };
-
-__device__ __forceinline__ void narrow_row(const float (&v)[32], uint32_t (&w)[16])
-{
-#pragma unroll
-    for (int i = 0; i < 16; ++i) w[i] = narrow2(pair(v[2 * i], v[2 * i + 1]));
-}
 
 // Takes 32 rows of up to 64 bf16 out through shared memory, so that a store instruction writes whole 128-byte pieces of rows and
 // not 16 bytes of each.  (The gradient of a 151936 x 896 matrix from 33 positions, which is nearly all stores: 114 us by tensor copies of
 // 32 x 32, 95 so.)  A lane has a row; its 16-byte pieces are exchanged by row, so that eight lanes reach all banks either way.
 struct Way {
-    uint32_t at;
+    uint32_t at, mine;   // the warp's place; the lane's row in it, its first piece where the exchange puts it
     int lane;
-    __device__ __forceinline__ void put(int part, const uint32_t (&w)[16])       // 32 columns, part 0 or 1
+    __device__ __forceinline__ Way(uint32_t place, int lane_) : at(place), mine(place + lane_ * 128 + ((lane_ & 7) << 4)), lane(lane_) {}
+    __device__ __forceinline__ void put(int part, const uint32_t (&w)[16]) const       // 32 columns, part 0 or 1
     {
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at + lane * 128 + ((4 * part + j ^ (lane & 7)) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
+            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(mine ^ (uint32_t)((4 * part + j) << 4)), "r"(w[4 * j]), "r"(w[4 * j + 1]),
                          "r"(w[4 * j + 2]), "r"(w[4 * j + 3]) : "memory");
     }
-    template <int kPieces>      // 16-byte pieces of a row: 8, or 4 for part 0 alone
-    __device__ __forceinline__ void send(const Params &p, const Output &o, const Tile &t, int64_t col)
+    // The rows from column c of the tile on; kPieces 16-byte pieces of each: 8, or 4 for part 0 alone.
+    template <int kPieces>
+    __device__ __forceinline__ void send(const Params &p, const Output &o, const Tile &t, int c) const
     {
         constexpr int kRows = 32 / kPieces;
         __syncwarp();
-        const int piece = lane % kPieces, first = lane / kPieces;
-        const int64_t at_col = col + piece * 8, left = t.end - at_col;
-        uint16_t *q = o.p + (t.row0 + first) * o.ld + at_col;
-        const int rows = p.m - t.row0 < 32 ? (int)(p.m - t.row0) : 32;
-        if (left >= 8 && o.whole) {
+        const int piece = lane % kPieces, first = lane / kPieces, rows = p.m - t.row0 < 32 ? (int)(p.m - t.row0) : 32;
+        uint16_t *q = o.p + (t.row0 + first) * o.ld + t.col + c + piece * 8;
+        if (o.whole && rows == 32 && t.width - c >= kPieces * 8) {
+            // (rows `first`, first + kRows, ...: the exchange has two turns, or one)
+            const uint32_t from = at + first * 128 + ((piece ^ first) << 4), turned = kPieces == 8 ? from ^ 64u : from;
+            uint32_t w[kPieces][4];
 #pragma unroll
-            for (int r = 0; r < 32; r += kRows) {
-                uint32_t w[4];
-                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
-                             : "r"(at + (r + first) * 128 + ((piece ^ (r + first & 7)) << 4)) : "memory");
-                if (r + first < rows) *reinterpret_cast<uint4 *>(q + r * o.ld) = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int i = 0; i < kPieces; ++i)
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[i][0]), "=r"(w[i][1]), "=r"(w[i][2]), "=r"(w[i][3])
+                             : "r"((i & 1 ? turned : from) + i * kRows * 128) : "memory");
+            const int64_t down = kRows * o.ld;
+#pragma unroll
+            for (int i = 0; i < kPieces; ++i) {
+                *reinterpret_cast<uint4 *>(q) = make_uint4(w[i][0], w[i][1], w[i][2], w[i][3]);
+                q += down;
             }
-        } else if (!o.whole) {
+        } else {
+            send_some<kPieces>(o, t, c, q, piece, first, rows);
+        }
+        __syncwarp();
+    }
+    template <int kPieces>
+    __device__ __forceinline__ void send_some(const Output &o, const Tile &t, int c, uint16_t *q, int piece, int first, int rows) const
+    {
+        constexpr int kRows = 32 / kPieces;
+        const int left = t.width - c - piece * 8;
+        if (!o.whole) {
             // element by element: a lane takes columns lane and lane + 32 of every row
             for (int r = 0; r < rows; ++r)
 #pragma unroll
-                for (int c = lane; c < kPieces * 8; c += 32) {
-                    uint16_t v;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + r * 128 + ((c >> 3 ^ (r & 7)) << 4) + (c & 7) * 2) : "memory");
-                    if (col + c < t.end) o.p[(t.row0 + r) * o.ld + col + c] = v;
-                }
-        } else if (left > 0) {
+                for (int e = lane; e < kPieces * 8; e += 32)
+                    if (c + e < t.width) o.p[(t.row0 + r) * o.ld + t.col + c + e] = element(r, e);
+        } else if (left >= 8) {
+            for (int r = first; r < rows; r += kRows) {
+                uint32_t w[4];
+                asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3])
+                             : "r"(at + r * 128 + ((piece ^ (r & 7)) << 4)) : "memory");
+                *reinterpret_cast<uint4 *>(q + (r - first) * o.ld) = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+        } else {
             // the last columns of rows that are no multiple of eight long
             for (int r = first; r < rows; r += kRows)
-                for (int c = 0; c < left; ++c) {
-                    uint16_t v;
-                    asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + r * 128 + ((piece ^ (r & 7)) << 4) + c * 2) : "memory");
-                    o.p[(t.row0 + r) * o.ld + at_col + c] = v;
-                }
+                for (int e = 0; e < left; ++e) q[(r - first) * o.ld + e] = element(r, piece * 8 + e);
         }
-        __syncwarp();
+    }
+    __device__ __forceinline__ uint16_t element(int r, int e) const
+    {
+        uint16_t v;
+        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"(at + r * 128 + ((e >> 3 ^ (r & 7)) << 4) + (e & 7) * 2) : "memory");
+        return v;
     }
 };
 
@@ -253,32 +268,52 @@ __device__ __forceinline__ float weight_mantissa(const float *dloss, const int64
     return 1.0f;
 }
 
+// 32 columns as pairs.
+__device__ __forceinline__ void read_pairs(uint32_t at, f32x2 (&v)[16])
+{
+    float x[32];
+    tmem_read(at, x);
+    tmem_read_wait();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) v[i] = pair(x[2 * i], x[2 * i + 1]);
+}
+
 // A tile's columns go to the two warps of a lane quarter in turn, 32 or 64 at a time.
-__device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int half, Way &way)
+__device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int half, const Way &way)
 {
 #pragma unroll 1
-    for (int c = half * 32; t.col + c < t.end; c += 64) {
-        float g[32], u[32];
-        tmem_read(t.acc + c, g);
-        tmem_read(t.acc + p.cols + c, u);
-        tmem_read_wait();
+    for (int c = half * 32; c < t.width; c += 64) {
+        f32x2 g[16], u[16];
+        {
+            float x[32], y[32];
+            tmem_read(t.acc + c, x);
+            tmem_read(t.acc + p.cols + c, y);
+            tmem_read_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                g[i] = pair(x[2 * i], x[2 * i + 1]);
+                u[i] = pair(y[2 * i], y[2 * i + 1]);
+            }
+        }
         uint32_t w[16];
         if (p.out[1].p != nullptr) {
-            narrow_row(g, w);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = narrow2(g[i]);
             way.put(0, w);
-            way.send<4>(p, p.out[1], t, t.col + c);
+            way.send<4>(p, p.out[1], t, c);
         }
         if (p.out[2].p != nullptr) {
-            narrow_row(u, w);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = narrow2(u[i]);
             way.put(0, w);
-            way.send<4>(p, p.out[2], t, t.col + c);
+            way.send<4>(p, p.out[2], t, c);
         }
         by_activation(p.act, [&](auto act) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) w[i] = narrow2(mul2(activation<decltype(act)::value>(pair(g[2 * i], g[2 * i + 1])), pair(u[2 * i], u[2 * i + 1])));
+            for (int i = 0; i < 16; ++i) w[i] = narrow2(mul2(activation<decltype(act)::value>(g[i]), u[i]));
         });
         way.put(0, w);
-        way.send<4>(p, p.out[0], t, t.col + c);
+        way.send<4>(p, p.out[0], t, c);
     }
 }
 
@@ -286,165 +321,180 @@ __device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int ha
 // comes out too small (the loss of 16384 positions of width 4096 was 2.5e-6 off; it is 6e-7 now, at the same speed).  So after every kLseRun stages
 // what they have is added here, rounded, and they begin anew, in the other accumulator.
 struct Logits {
-    float v[8][16];
+    f32x2 v[8][8];
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
 #pragma unroll
-            for (int j = 0; j < 16; ++j) v[i][j] = 0.0f;
+            for (int j = 0; j < 8; ++j) v[i][j] = both(0.0f);
     }
+    static __device__ __forceinline__ int column(int half, int i) { return half * 32 + (i >> 1) * 64 + (i & 1) * 16; }
     __device__ __forceinline__ void take(const Tile &t, int half)
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int c = half * 32 + (i >> 1) * 64 + (i & 1) * 16;
-            if (t.col + c < t.end) {
+        for (int i = 0; i < 8; ++i)
+            if (column(half, i) < t.width) {
                 float x[16];
-                tmem_read(t.acc + c, x);
+                tmem_read(t.acc + column(half, i), x);
                 tmem_read_wait();
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[i][j] += x[j];
+                for (int j = 0; j < 8; ++j) v[i][j] = add2(v[i][j], pair(x[2 * j], x[2 * j + 1]));
             }
-        }
     }
 };
+
+// Where in the tile the row's target is, or -1.
+__device__ __forceinline__ int target_column(const Params &p, const Tile &t, int64_t target)
+{
+    const int64_t at = target - p.first - t.col;
+    return target >= 0 && at >= 0 && at < t.width ? (int)at : -1;
+}
 
 // The sum is taken relative to the largest.  A NaN, which no maximum shows, reaches the sum by its own term.
 __device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half, Logits &l)
 {
     const bool there = t.row < p.m;
-    const int64_t target = there ? p.target[t.row] - p.first : -1;
-    float most = -INFINITY, s0 = 0.0f, s1 = 0.0f;
+    const int target = target_column(p, t, there ? p.target[t.row] : -1);
+    float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int64_t col = t.col + half * 32 + (i >> 1) * 64 + (i & 1) * 16, left = t.end - col;
+        const int c = Logits::column(half, i), left = t.width - c;
         if (left < 16) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) l.v[i][j] = j < left ? l.v[i][j] : -INFINITY;
+            for (int j = 0; j < 8; ++j) {
+                const float2 x = halves(l.v[i][j]);
+                l.v[i][j] = pair(2 * j < left ? x.x : -INFINITY, 2 * j + 1 < left ? x.y : -INFINITY);
+            }
         }
-        if (target >= col && target < col + 16 && target < t.end) {
-            const int at = (int)(target - col);
+        if ((unsigned)(target - c) < 16u) {
             float x = 0.0f;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) x = j == at ? l.v[i][j] : x;
+            for (int j = 0; j < 8; ++j) {
+                const float2 y = halves(l.v[i][j]);
+                x = target - c == 2 * j ? y.x : target - c == 2 * j + 1 ? y.y : x;
+            }
             p.target_logit[t.row] = x;
         }
 #pragma unroll
-        for (int j = 0; j < 16; ++j) most = fmaxf(most, l.v[i][j]);
+        for (int j = 0; j < 8; ++j) {
+            const float2 x = halves(l.v[i][j]);
+            most = fmaxf(most, fmaxf(x.x, x.y));
+        }
     }
-    const float base = most == -INFINITY ? 0.0f : most;
+    const f32x2 base = both(most == -INFINITY ? 0.0f : -most);
+    f32x2 sum[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-        if (t.col + half * 32 + (i >> 1) * 64 + (i & 1) * 16 < t.end) {
+        if (Logits::column(half, i) < t.width) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 2) {
-                s0 += power2((l.v[i][j] - base) * kLog2e);
-                s1 += power2((l.v[i][j + 1] - base) * kLog2e);
-            }
+            for (int j = 0; j < 8; ++j) sum[j & 1] = add2(sum[j & 1], power2(mul2(add2(l.v[i][j], base), both(kLog2e))));
         }
-    if (there) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, s0 + s1);
+    const float2 s = halves(add2(sum[0], sum[1]));
+    if (there) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, s.x + s.y);
 }
 
-__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int half, Way &way, float scale)
+__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int half, const Way &way, float scale)
 {
     const bool there = t.row < p.m;
-    const int64_t of = there ? p.target[t.row] : -1, target = of - p.first;
-    const float lse = there ? p.lse[t.row] : 0.0f, g = of < 0 ? 0.0f : of >= p.vocab ? NAN : p.dloss[t.row] / scale;
+    const int64_t of = there ? p.target[t.row] : -1;
+    const int target = target_column(p, t, of);
+    const float g = of < 0 ? 0.0f : of >= p.vocab ? NAN : p.dloss[t.row] / scale;
+    const f32x2 lse = both(there ? -p.lse[t.row] : 0.0f);
 #pragma unroll 1
-    for (int c = half * 64; t.col + c < t.end; c += 128) {
+    for (int c = half * 64; c < t.width; c += 128) {
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            float v[32];
-            tmem_read(t.acc + c + 32 * part, v);
-            tmem_read_wait();
-            const int64_t col = t.col + c + 32 * part;
+            f32x2 v[16];
+            read_pairs(t.acc + c + 32 * part, v);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] = g * power2((v[i] - lse) * kLog2e);
-            if (target >= col && target < col + 32) {
-                const int j = (int)(target - col);
+            for (int i = 0; i < 16; ++i) v[i] = mul2(both(g), power2(mul2(add2(v[i], lse), both(kLog2e))));
+            const int at = target - c - 32 * part;
+            if ((unsigned)at < 32u) {
 #pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] = i == j ? v[i] - g : v[i];
+                for (int i = 0; i < 16; ++i) {
+                    const float2 x = halves(v[i]);
+                    v[i] = pair(at == 2 * i ? x.x - g : x.x, at == 2 * i + 1 ? x.y - g : x.y);
+                }
             }
             uint32_t w[16];
-            narrow_row(v, w);
-            if (of < 0) {              // no position, whatever its logits are
 #pragma unroll
-                for (int i = 0; i < 16; ++i) w[i] = 0;
-            }
+            for (int i = 0; i < 16; ++i) w[i] = of < 0 ? 0u : narrow2(v[i]);       // (no position: 0, whatever its logits are)
             way.put(part, w);
             __syncwarp();
         }
-        way.send<8>(p, p.out[0], t, t.col + c);
+        way.send<8>(p, p.out[0], t, c);
     }
 }
 
-__device__ __forceinline__ void add_old(const Output &o, const Tile &t, int64_t col, float (&v)[32])
+__device__ __forceinline__ void add_old(const Output &o, const Tile &t, int c, f32x2 (&v)[16])
 {
-    const uint16_t *q = o.p + t.row * o.ld + col;
-    const int64_t left = t.end - col;
+    const uint16_t *q = o.p + t.row * o.ld + t.col + c;
+    const int left = t.width - c;
     if (left >= 32 && o.whole) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4 x = reinterpret_cast<const uint4 *>(q)[i];
-            const uint32_t w[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 f = halves(widen2(w[j]));
-                v[8 * i + 2 * j] += f.x;
-                v[8 * i + 2 * j + 1] += f.y;
-            }
+            v[4 * i] = add2(v[4 * i], widen2(x.x));
+            v[4 * i + 1] = add2(v[4 * i + 1], widen2(x.y));
+            v[4 * i + 2] = add2(v[4 * i + 2], widen2(x.z));
+            v[4 * i + 3] = add2(v[4 * i + 3], widen2(x.w));
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i)
-            if (i < left) v[i] += widen<uint16_t>(q[i]);
+        for (int i = 0; i < 16; ++i)
+            v[i] = add2(v[i], pair(2 * i < left ? widen<uint16_t>(q[2 * i]) : 0.0f, 2 * i + 1 < left ? widen<uint16_t>(q[2 * i + 1]) : 0.0f));
     }
 }
 
-__device__ __forceinline__ void end_store(const Params &p, const Tile &t, int half, Way &way, float scale)
+// fp32 sums: into memory, added to what is there, or what is there added to them.
+__device__ __forceinline__ void fp32_sums(const Params &p, const Tile &t, int c, f32x2 (&v)[16])
 {
-    const bool there = t.row < p.m, narrow_out = p.mode == kStoreBf16 || p.mode == kAddBf16 || p.mode == kStoreBf16OfSum;
+    float4 *f = reinterpret_cast<float4 *>(p.f32 + ((int64_t)t.split * p.m + t.row) * p.f32_ld + t.col + c);
+    if (p.mode != kStoreF32) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float4 o = f[i];
+            v[2 * i] = add2(v[2 * i], pair(o.x, o.y));
+            v[2 * i + 1] = add2(v[2 * i + 1], pair(o.z, o.w));
+        }
+    }
+    if (p.mode != kStoreBf16OfSum) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float2 x = halves(v[2 * i]), y = halves(v[2 * i + 1]);
+            f[i] = make_float4(x.x, x.y, y.x, y.y);
+        }
+    }
+}
+
+__device__ __forceinline__ void end_store(const Params &p, const Tile &t, int half, const Way &way, float scale)
+{
+    const bool there = t.row < p.m;
+    const f32x2 scales = both(scale);
 #pragma unroll 1
-    for (int c = half * 64; t.col + c < t.end; c += 128) {
+    for (int c = half * 64; c < t.width; c += 128) {
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
-            float v[32];
-            tmem_read(t.acc + c + 32 * part, v);
-            tmem_read_wait();
-            const int64_t col = t.col + c + 32 * part;
-            if (p.mode == kStoreBf16 || p.mode == kAddBf16) {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) v[i] *= scale;
+            f32x2 v[16];
+            read_pairs(t.acc + c + 32 * part, v);
+            if (p.mode != kStoreBf16 && p.mode != kAddBf16) {
+                if (there && c + 32 * part < t.width) fp32_sums(p, t, c + 32 * part, v);
+                __syncwarp();
+                if (p.mode != kStoreBf16OfSum) continue;
             }
-            if (there && col < t.end) {
-                if (p.mode == kAddBf16) add_old(p.out[t.batch], t, col, v);
-                if (p.mode == kStoreF32 || p.mode == kAddF32 || p.mode == kStoreBf16OfSum) {
-                    float4 *f = reinterpret_cast<float4 *>(p.f32 + ((int64_t)t.split * p.m + t.row) * p.f32_ld + col);
-                    if (p.mode != kStoreF32) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const float4 o = f[i];
-                            v[4 * i] += o.x; v[4 * i + 1] += o.y; v[4 * i + 2] += o.z; v[4 * i + 3] += o.w;
-                        }
-                    }
-                    if (p.mode == kStoreBf16OfSum) {
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) v[i] *= scale;
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-                    }
-                }
+            for (int i = 0; i < 16; ++i) v[i] = mul2(v[i], scales);
+            if (p.mode == kAddBf16) {
+                if (there && c + 32 * part < t.width) add_old(p.out[t.batch], t, c + 32 * part, v);
+                __syncwarp();
             }
-            if (narrow_out) {
-                uint32_t w[16];
-                narrow_row(v, w);
-                way.put(part, w);
-            }
-            __syncwarp();
+            uint32_t w[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) w[i] = narrow2(v[i]);
+            way.put(part, w);
         }
-        if (narrow_out) way.send<8>(p, p.out[t.batch], t, t.col + c);
+        if (p.mode != kStoreF32 && p.mode != kAddF32) way.send<8>(p, p.out[t.batch], t, c);
     }
 }
 
@@ -626,14 +676,14 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
     } else if (warp >= 4) {
         // ---- ends
         const int half = (warp - 4) >> 2, quarter = warp & 3;
-        Way way{ring + kRing + (uint32_t)(warp - 4) * kOutBytes, lane};
+        const Way way(ring + kRing + (uint32_t)(warp - 4) * kOutBytes, lane);
         const float scale = (kEnd == kDlogits || kEnd == kStore) && p.dloss != nullptr ? weight_mantissa(p.dloss, p.target, p.positions) : 1.0f;
         uint32_t units = 0;
         for (int w = first; w < p.total && !failed; w += step) {
             const Work t = work_of(p, w);
             Tile tile;
             tile.col = (int64_t)t.n_tile * p.cols;
-            tile.end = tile.col + p.cols < p.n ? tile.col + p.cols : p.n;
+            tile.width = p.n - tile.col < p.cols ? (int)(p.n - tile.col) : p.cols;
             tile.batch = p.batches > 1 ? t.outer : 0;
             tile.split = p.batches > 1 ? 0 : t.outer;
             tile.n_tile = t.n_tile;
