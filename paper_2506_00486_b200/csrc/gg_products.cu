@@ -778,39 +778,40 @@ __global__ void __launch_bounds__(256) gated_slopes_kernel(const Bf16Matrix dh, 
         }
     }
 }
-// ... else single columns, a warp's side by side, four runs of them under way.
+// ... else single columns, a warp's side by side, eight runs of them under way.
 template <int kAct>
-__global__ void __launch_bounds__(256) gated_slopes_any_kernel(const Bf16Matrix dh, const Bf16Matrix gate, const Bf16Matrix up, uint16_t *dgate, uint16_t *dup,
+__global__ void __launch_bounds__(128) gated_slopes_any_kernel(const Bf16Matrix dh, const Bf16Matrix gate, const Bf16Matrix up, uint16_t *dgate, uint16_t *dup,
                                                                int64_t ld)
 {
     wait_for_the_one_before();
     for (int64_t row = blockIdx.y; row < dh.rows; row += gridDim.y)
         for (int64_t first = blockIdx.x * 1024ll + threadIdx.x; first < dh.cols; first += gridDim.x * 1024ll) {
-            float d[4], g[4], u[4];
+            const int left = dh.cols - first < 1024 ? (int)(dh.cols - first) : 1024;
+            const uint16_t *dp = dh.p + row * dh.ld + first, *gp = gate.p + row * gate.ld + first, *up_ = up.p + row * up.ld + first;
+            uint16_t d[8], g[8], u[8];
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const int64_t col = first + 256 * k;
-                d[k] = g[k] = u[k] = 0.0f;
-                if (col < dh.cols) {
-                    d[k] = widen<uint16_t>(dh.p[row * dh.ld + col]);
-                    g[k] = widen<uint16_t>(gate.p[row * gate.ld + col]);
-                    u[k] = widen<uint16_t>(up.p[row * up.ld + col]);
+            for (int k = 0; k < 8; ++k) {
+                d[k] = g[k] = u[k] = 0;
+                if (128 * k < left) {
+                    d[k] = dp[128 * k];
+                    g[k] = gp[128 * k];
+                    u[k] = up_[128 * k];
                 }
             }
+            uint16_t *dg = dgate + row * ld + first, *du = dup + row * ld + first;
 #pragma unroll
-            for (int k = 0; k < 4; k += 2) {
+            for (int k = 0; k < 8; k += 2) {
                 f32x2 value, s;
-                slope<kAct>(pair(g[k], g[k + 1]), value, s);
-                const f32x2 d2 = pair(d[k], d[k + 1]);
-                const uint32_t wg = narrow2(mul2(mul2(d2, pair(u[k], u[k + 1])), s)), wu = narrow2(mul2(d2, value));
-                const int64_t at = row * ld + first + 256 * k;
-                if (first + 256 * k < dh.cols) {
-                    dgate[at] = (uint16_t)wg;
-                    dup[at] = (uint16_t)wu;
+                slope<kAct>(pair(widen<uint16_t>(g[k]), widen<uint16_t>(g[k + 1])), value, s);
+                const f32x2 d2 = pair(widen<uint16_t>(d[k]), widen<uint16_t>(d[k + 1]));
+                const uint32_t wg = narrow2(mul2(mul2(d2, pair(widen<uint16_t>(u[k]), widen<uint16_t>(u[k + 1]))), s)), wu = narrow2(mul2(d2, value));
+                if (128 * k < left) {
+                    dg[128 * k] = (uint16_t)wg;
+                    du[128 * k] = (uint16_t)wu;
                 }
-                if (first + 256 * k + 256 < dh.cols) {
-                    dgate[at + 256] = (uint16_t)(wg >> 16);
-                    dup[at + 256] = (uint16_t)(wu >> 16);
+                if (128 * k + 128 < left) {
+                    dg[128 * k + 128] = (uint16_t)(wg >> 16);
+                    du[128 * k + 128] = (uint16_t)(wu >> 16);
                 }
             }
         }
@@ -851,40 +852,51 @@ __global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, in
     if (of_row == 0 && row < rows) finish_row(v, row, target_logit[row], target, vocab, lse, loss);
 }
 
-// 32 runs of four columns a CTA, eight threads for each, which take every eighth split and are added in order.
+// A thread for four columns; or, where there are many splits, kParts of them, which take every kParts-th split and are added in order.
+template <int kParts>
 __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld,
                                                          const float *dloss, const int64_t *target)
 {
-    __shared__ float4 of[8][33];
+    constexpr int kRuns = 256 / kParts;
+    __shared__ float4 of[kParts][kRuns];
     const int64_t groups = (cols + 3) / 4;
-    const int lane = threadIdx.x & 31, part = threadIdx.x >> 5;
+    const int lane = threadIdx.x % kRuns, part = threadIdx.x / kRuns;
     wait_for_the_one_before();
     const float scale = dloss != nullptr ? weight_mantissa(dloss, target, rows) : 1.0f;
-    for (int64_t first = blockIdx.x * 32ll; first < groups * rows; first += gridDim.x * 32ll) {
+    for (int64_t first = blockIdx.x * (int64_t)kRuns; first < groups * rows; first += gridDim.x * (int64_t)kRuns) {
         const int64_t i = first + lane, row = i / groups, col = (i - row * groups) * 4;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
         if (row < rows) {
 #pragma unroll 4
-            for (int j = part; j < splits; j += 8) {
+            for (int j = part; j < splits; j += kParts) {
                 const float4 v = *reinterpret_cast<const float4 *>(f32 + (j * rows + row) * f32_ld + col);
                 s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
             }
         }
-        of[part][lane] = s;
-        __syncthreads();
-        if (part == 0 && row < rows) {
+        if constexpr (kParts > 1) {
+            of[part][lane] = s;
+            __syncthreads();
+            if (part == 0) {
 #pragma unroll
-            for (int j = 1; j < 8; ++j) {
-                const float4 v = of[j][lane];
-                s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+                for (int j = 1; j < kParts; ++j) {
+                    const float4 v = of[j][lane];
+                    s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+                }
             }
-            const float v[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
-            uint16_t *o = out + row * out_ld + col;
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-                if (col + j < cols) o[j] = narrow<uint16_t>(v[j]);
         }
-        __syncthreads();
+        if (part == 0 && row < rows) {
+            const f32x2 lo = pair(s.x * scale, s.y * scale), hi = pair(s.z * scale, s.w * scale);
+            const uint32_t w[2] = {narrow2(lo), narrow2(hi)};
+            uint16_t *o = out + row * out_ld + col;
+            if (col + 4 <= cols && reinterpret_cast<uintptr_t>(o) % 8 == 0) {
+                *reinterpret_cast<uint2 *>(o) = make_uint2(w[0], w[1]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (col + j < cols) o[j] = (uint16_t)(w[j / 2] >> 16 * (j & 1));
+            }
+        }
+        if constexpr (kParts > 1) __syncthreads();
     }
 }
 
@@ -1220,7 +1232,9 @@ cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, cons
 cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *dloss,
                               const int64_t *target, cudaStream_t st)
 {
-    return launch_after(st, dim3(grid_of((cols + 3) / 4 * rows * 8)), 256, 0, sum_splits_kernel, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target);
+    const int64_t threads = (cols + 3) / 4 * rows;
+    if (splits < 8) return launch_after(st, dim3(grid_of(threads)), 256, 0, sum_splits_kernel<1>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target);
+    return launch_after(st, dim3(grid_of(threads * 8)), 256, 0, sum_splits_kernel<8>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target);
 }
 
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,
@@ -1231,7 +1245,7 @@ cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, co
             const int64_t groups = dh.cols / 8, total = groups * dh.rows, want = (total + 511) / 512;
             return launch_after(st, dim3((unsigned)(want < 0x7FFFFFFF ? want : 0x7FFFFFFF)), 256, 0, kernel, dh, gate, up, dgate, dup, ld, (uint32_t)groups, total);
         }
-        return launch_after(st, dim3((unsigned)((dh.cols + 1023) / 1024), (unsigned)(dh.rows < 65535 ? dh.rows : 65535)), 256, 0, any, dh, gate, up, dgate, dup, ld);
+        return launch_after(st, dim3((unsigned)((dh.cols + 1023) / 1024), (unsigned)(dh.rows < 65535 ? dh.rows : 65535)), 128, 0, any, dh, gate, up, dgate, dup, ld);
     };
     if (act == GG_ACT_SILU) return go(gated_slopes_kernel<GG_ACT_SILU>, gated_slopes_any_kernel<GG_ACT_SILU>);
     if (act == GG_ACT_GELU) return go(gated_slopes_kernel<GG_ACT_GELU>, gated_slopes_any_kernel<GG_ACT_GELU>);
