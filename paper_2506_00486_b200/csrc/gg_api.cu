@@ -1842,6 +1842,19 @@ gg_status product_alive(gg_ctx *ctx)
     return GG_ERR_CUDA;
 }
 
+// The gradient of weights into out[] of each batch, by way of fp32 sums where the long axis is split.
+gg_status store_weights(gg_ctx *ctx, ProductArgs &q, bool add, cudaStream_t st)
+{
+    q.mode = q.splits > 1 ? kStoreF32 : add ? kAddBf16 : kStoreBf16;
+    GG_CUDA(ctx, launch_product_dweight(q, ctx->sm_count, st));
+    ctx->launches += 1;
+    for (int i = 0; q.splits > 1 && i < q.batches; ++i) {
+        GG_CUDA(ctx, launch_sum_splits(q.f32 + (int64_t)i * q.splits * q.m * q.f32_ld, q.splits, q.m, q.n, q.f32_ld, q.out[i], q.out_ld[i], q.dloss, q.target, q.positions, add, st));
+        ctx->launches += 1;
+    }
+    return GG_OK;
+}
+
 gg_status zero_matrix(gg_ctx *ctx, void *p, int64_t rows, int64_t cols, int64_t ld, cudaStream_t st)
 {
     if (p != nullptr && rows > 0 && cols > 0) GG_CUDA(ctx, cudaMemset2DAsync(p, (size_t)ld * 2, 0, (size_t)cols * 2, (size_t)rows, st));
@@ -1914,11 +1927,14 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
     // pieces of the vocabulary of one size, a multiple of the tile
     const int64_t all = (a->vocab + 255) / 256, fit = std::max<int64_t>(1, kPieceBytes / (512 * a->rows)), pieces = (all + fit - 1) / fit;
     const int64_t piece = (all + pieces - 1) / pieces * 256, last = a->vocab - (a->vocab - 1) / piece * piece, n_pieces = (a->vocab + piece - 1) / piece;
-    const int splits = a->dh ? product_splits(a->rows, a->width, last, 1, ctx->sm_count) : 1;
+    const int splits = a->dh ? product_splits(a->rows, a->width, last, 1, 1, ctx->sm_count) : 1;
+    auto weight_splits = [&](int64_t n) { return a->dw ? product_splits(n, a->width, a->rows, 1, 1, ctx->sm_count) : 1; };
     const int64_t f32_ld = (a->width + 31) / 32 * 32;
     Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
     const int64_t d_at = s.place(a->rows * piece * 2);
     const int64_t f32_at = s.place(a->dh && (splits > 1 || n_pieces > 1) ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
+    const int64_t first_sums = weight_splits(piece) > 1 ? weight_splits(piece) * piece : 0, last_sums = weight_splits(last) > 1 ? weight_splits(last) * last : 0;
+    const int64_t f32w_at = s.place(4 * std::max(first_sums, last_sums) * f32_ld);
     if ((st = s.grow()) != GG_OK || (st = h.lay(s)) != GG_OK || (st = w.lay(s)) != GG_OK) return st;
     for (int64_t i = 0; i < n_pieces; ++i) {
         const int64_t first = i * piece, n = std::min(piece, a->vocab - first);
@@ -1940,9 +1956,10 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
             q.m = n; q.n = a->width; q.k = a->rows;
             q.out[0] = static_cast<uint16_t *>(a->dw) + first * a->dw_ld;
             q.out_ld[0] = a->dw_ld;
-            q.mode = a->accumulate ? kAddBf16 : kStoreBf16;
-            GG_CUDA(ctx, launch_product_dweight(q, ctx->sm_count, s.st));
-            ctx->launches += 1;
+            q.splits = weight_splits(n);
+            q.f32 = s.at<float>(f32w_at);
+            q.f32_ld = f32_ld;
+            if ((st = store_weights(ctx, q, a->accumulate != 0, s.st)) != GG_OK) return st;
         }
         if (a->dh) {
             ProductArgs q = p;
@@ -1962,7 +1979,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
     }
     if (a->dh && splits > 1) {
         GG_CUDA(ctx, launch_sum_splits(s.at<float>(f32_at), splits, a->rows, a->width, f32_ld, static_cast<uint16_t *>(a->dh), a->dh_ld, a->dloss, a->target,
-                                       s.st));
+                                       a->rows, false, s.st));
         ctx->launches += 1;
     }
     return GG_OK;
@@ -2032,10 +2049,12 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
     }
     if ((st = product_alive(ctx)) != GG_OK) return st;
     const int64_t ld = (a->hidden + 63) / 64 * 64, f32_ld = (a->width + 31) / 32 * 32;
-    const int splits = a->dx ? product_splits(a->rows, a->width, a->hidden, 2, ctx->sm_count) : 1;
+    const int splits = a->dx ? product_splits(a->rows, a->width, a->hidden, 2, 1, ctx->sm_count) : 1;
+    const int weight_splits = a->dw_gate ? product_splits(a->hidden, a->width, a->rows, 1, 2, ctx->sm_count) : 1;
     Operand x(matrix_of(a->x, a->rows, a->width, a->x_ld), s), wg(matrix_of(a->w_gate, a->hidden, a->width, a->w_gate_ld), s),
         wu(matrix_of(a->w_up, a->hidden, a->width, a->w_up_ld), s);
     const int64_t dgate_at = s.place(a->rows * ld * 2), dup_at = s.place(a->rows * ld * 2), f32_at = s.place(splits > 1 ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
+    const int64_t f32w_at = s.place(weight_splits > 1 ? 8 * (int64_t)weight_splits * a->hidden * f32_ld : 0);
     if ((st = s.grow()) != GG_OK) return st;
     if (a->dw_gate && (st = x.lay(s)) != GG_OK) return st;
     if (a->dx && ((st = wg.lay(s)) != GG_OK || (st = wu.lay(s)) != GG_OK)) return st;
@@ -2061,7 +2080,7 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
         GG_CUDA(ctx, launch_product_drows(q, ctx->sm_count, s.st));
         ctx->launches += 1;
         if (splits > 1) {
-            GG_CUDA(ctx, launch_sum_splits(q.f32, splits, a->rows, a->width, f32_ld, q.out[0], a->dx_ld, nullptr, nullptr, s.st));
+            GG_CUDA(ctx, launch_sum_splits(q.f32, splits, a->rows, a->width, f32_ld, q.out[0], a->dx_ld, nullptr, nullptr, 0, false, s.st));
             ctx->launches += 1;
         }
     }
@@ -2073,9 +2092,10 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
         p.out[1] = static_cast<uint16_t *>(a->dw_up);
         p.out_ld[0] = a->dw_gate_ld;
         p.out_ld[1] = a->dw_up_ld;
-        p.mode = a->accumulate ? kAddBf16 : kStoreBf16;
-        GG_CUDA(ctx, launch_product_dweight(p, ctx->sm_count, s.st));
-        ctx->launches += 1;
+        p.splits = weight_splits;
+        p.f32 = s.at<float>(f32w_at);
+        p.f32_ld = f32_ld;
+        if ((st = store_weights(ctx, p, a->accumulate != 0, s.st)) != GG_OK) return st;
     }
     return GG_OK;
 }

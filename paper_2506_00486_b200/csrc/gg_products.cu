@@ -50,7 +50,7 @@ struct Params {
     int64_t m, n;
     int tile_n;                         // rows of B in a tile (kGated: half of them gate's, half up's)
     int cols;                           // columns of C in a tile
-    int tiles_m, tiles_n, band, total, kblocks, all_k, batches;
+    int tiles_m, tiles_n, band, total, kblocks, all_k, splits;      // (up to two batches of so many splits)
     int each_k, more_k;                 // stages of a split, and how many splits have one more
     Divider by_outer, by_band, by_height, by_last;      // tiles of a batch or split, of a band; its height, the last band's
     int stages, bytes_a, bytes_b;       // of the ring: A's part has only as many rows as A
@@ -175,8 +175,16 @@ struct Tile {
     int64_t row0, row;   // first row of the warp, row of this thread
     int64_t col;         // first column of the tile
     int width;           // its columns that C has
-    int batch, split, n_tile;
+    int batch, sums, n_tile;      // sums: which of the fp32 matrices (kStore)
     uint32_t acc;        // its sums: tensor memory of the warp's lanes
+    // of this thread's row (kLse, kDlogits)
+    int64_t of;          // its target
+    float lse, weight;
+    __device__ __forceinline__ int target(int64_t first) const      // where in the tile that is, or -1
+    {
+        const int64_t at = of - first - col;
+        return of >= 0 && at >= 0 && at < width ? (int)at : -1;
+    }
 };
 
 // Takes 32 rows of up to 64 bf16 out through shared memory, so that a store instruction writes whole 128-byte pieces of rows and
@@ -226,7 +234,8 @@ struct Way {
         constexpr int kRows = 32 / kPieces;
         const int left = t.width - c - piece * 8;
         if (!o.whole) {
-            // element by element: a lane takes columns lane and lane + 32 of every row
+            // element by element: a lane takes columns lane and lane + 32 of every row (pairs from the first even element on measured
+            // twice as long)
             for (int r = 0; r < rows; ++r)
 #pragma unroll
                 for (int e = lane; e < kPieces * 8; e += 32)
@@ -344,18 +353,10 @@ struct Logits {
     }
 };
 
-// Where in the tile the row's target is, or -1.
-__device__ __forceinline__ int target_column(const Params &p, const Tile &t, int64_t target)
-{
-    const int64_t at = target - p.first - t.col;
-    return target >= 0 && at >= 0 && at < t.width ? (int)at : -1;
-}
-
 // The sum is taken relative to the largest.  A NaN, which no maximum shows, reaches the sum by its own term.
 __device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half, Logits &l)
 {
-    const bool there = t.row < p.m;
-    const int target = target_column(p, t, there ? p.target[t.row] : -1);
+    const int target = t.target(p.first);
     float most = -INFINITY;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -391,16 +392,15 @@ __device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half
             for (int j = 0; j < 8; ++j) sum[j & 1] = add2(sum[j & 1], power2(mul2(add2(l.v[i][j], base), both(kLog2e))));
         }
     const float2 s = halves(add2(sum[0], sum[1]));
-    if (there) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, s.x + s.y);
+    if (t.row < p.m) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, s.x + s.y);
 }
 
 __device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int half, const Way &way, float scale)
 {
-    const bool there = t.row < p.m;
-    const int64_t of = there ? p.target[t.row] : -1;
-    const int target = target_column(p, t, of);
-    const float g = of < 0 ? 0.0f : of >= p.vocab ? NAN : p.dloss[t.row] / scale;
-    const f32x2 lse = both(there ? -p.lse[t.row] : 0.0f);
+    const int64_t of = t.of;
+    const int target = t.target(p.first);
+    const float g = of < 0 ? 0.0f : of >= p.vocab ? NAN : t.weight / scale;
+    const f32x2 lse = both(-t.lse);
 #pragma unroll 1
     for (int c = half * 64; c < t.width; c += 128) {
 #pragma unroll
@@ -450,7 +450,7 @@ __device__ __forceinline__ void add_old(const Output &o, const Tile &t, int c, f
 // fp32 sums: into memory, added to what is there, or what is there added to them.
 __device__ __forceinline__ void fp32_sums(const Params &p, const Tile &t, int c, f32x2 (&v)[16])
 {
-    float4 *f = reinterpret_cast<float4 *>(p.f32 + ((int64_t)t.split * p.m + t.row) * p.f32_ld + t.col + c);
+    float4 *f = reinterpret_cast<float4 *>(p.f32 + ((int64_t)t.sums * p.m + t.row) * p.f32_ld + t.col + c);
     if (p.mode != kStoreF32) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -559,7 +559,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
         uint32_t stage = 0, phase = 0, issued = 0;
         for (int w = first; w < p.total && !failed; w += step) {
             const Work t = work_of(p, w);
-            const int batch = p.batches > 1 ? t.outer : 0, split = p.batches > 1 ? 0 : t.outer;
+            const int batch = t.outer >= p.splits, split = t.outer - batch * p.splits;
             const int m0 = t.m_tile * 128 * kCtas * kHalves + (int)rank * 128;
             const int n0 = t.n_tile * p.cols + (kEnd == kGated ? 0 : (int)rank * rows_b);
             const int end = split_start(p, split + 1);
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             if (leader) product_commit<kCtas>(bar);
         };
         for (int w = first; w < p.total && !failed; w += step) {
-            const int split = p.batches > 1 ? 0 : work_of(p, w).outer;
+            const int outer = work_of(p, w).outer, split = outer - (outer >= p.splits ? p.splits : 0);
             const int begin = split_start(p, split), end = split_start(p, split + 1);
             if constexpr (kHalves == 1) {
                 const int run = kEnd == kLse ? kLseRun : end - begin;
@@ -684,9 +684,17 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             Tile tile;
             tile.col = (int64_t)t.n_tile * p.cols;
             tile.width = p.n - tile.col < p.cols ? (int)(p.n - tile.col) : p.cols;
-            tile.batch = p.batches > 1 ? t.outer : 0;
-            tile.split = p.batches > 1 ? 0 : t.outer;
+            tile.batch = t.outer >= p.splits;
+            tile.sums = t.outer;
             tile.n_tile = t.n_tile;
+            if constexpr (kEnd == kLse || kEnd == kDlogits) {      // (read while the tile is being summed)
+                const int64_t row = (int64_t)t.m_tile * 128 * kCtas + rank * 128 + quarter * 32 + lane;
+                tile.of = row < p.m ? p.target[row] : -1;
+                if constexpr (kEnd == kDlogits) {
+                    tile.lse = row < p.m ? p.lse[row] : 0.0f;
+                    tile.weight = row < p.m ? p.dloss[row] : 0.0f;
+                }
+            }
             const int runs = kEnd == kLse ? (p.kblocks + kLseRun - 1) / kLseRun : kHalves;
             Logits logits;
             if constexpr (kEnd == kLse) logits.clear();
@@ -855,14 +863,14 @@ __global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, in
 // A thread for four columns; or, where there are many splits, kParts of them, which take every kParts-th split and are added in order.
 template <int kParts>
 __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld,
-                                                         const float *dloss, const int64_t *target)
+                                                         const float *dloss, const int64_t *target, int64_t positions, int add)
 {
     constexpr int kRuns = 256 / kParts;
     __shared__ float4 of[kParts][kRuns];
     const int64_t groups = (cols + 3) / 4;
     const int lane = threadIdx.x % kRuns, part = threadIdx.x / kRuns;
     wait_for_the_one_before();
-    const float scale = dloss != nullptr ? weight_mantissa(dloss, target, rows) : 1.0f;
+    const float scale = dloss != nullptr ? weight_mantissa(dloss, target, positions) : 1.0f;
     for (int64_t first = blockIdx.x * (int64_t)kRuns; first < groups * rows; first += gridDim.x * (int64_t)kRuns) {
         const int64_t i = first + lane, row = i / groups, col = (i - row * groups) * 4;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -885,9 +893,14 @@ __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int s
             }
         }
         if (part == 0 && row < rows) {
-            const f32x2 lo = pair(s.x * scale, s.y * scale), hi = pair(s.z * scale, s.w * scale);
-            const uint32_t w[2] = {narrow2(lo), narrow2(hi)};
             uint16_t *o = out + row * out_ld + col;
+            float v[4] = {s.x * scale, s.y * scale, s.z * scale, s.w * scale};
+            if (add) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (col + j < cols) v[j] += widen<uint16_t>(o[j]);
+            }
+            const uint32_t w[2] = {narrow2(pair(v[0], v[1])), narrow2(pair(v[2], v[3]))};
             if (col + 4 <= cols && reinterpret_cast<uintptr_t>(o) % 8 == 0) {
                 *reinterpret_cast<uint2 *>(o) = make_uint2(w[0], w[1]);
             } else {
@@ -1095,7 +1108,7 @@ Tiling tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t stages, int
             const int64_t rounds = (tiles * splits + units - 1) / units, each = (stages + splits - 1) / splits;
             const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage, store = (cols % 64 == 0 ? 15.0 : 20.0) * width;
             double cost = rounds * ((main > store ? main : store) + 200.0) * halves + store;
-            if (splits > 1) cost += 4000.0 + (double)splits * m * n * 8.0 / 3600.0;       // the sums of the splits, written and read
+            if (splits > 1) cost += 4000.0 + (double)splits * batches * m * n * 8.0 / 3600.0;       // the sums of the splits, written and read
             if (least == 0.0 || cost < least) {
                 least = cost;
                 best = Tiling{ctas, halves, width, cols, (int)splits, tiles_m, tiles_n};
@@ -1121,7 +1134,7 @@ cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, 
     p.tile_n = t.tile_n; p.cols = t.cols;
     p.tiles_m = (int)t.tiles_m; p.tiles_n = (int)t.tiles_n;
     p.kblocks = (int)((a.k + kBlockK - 1) / kBlockK);
-    p.all_k = p.kblocks * a.segments; p.batches = a.batches;
+    p.all_k = p.kblocks * a.segments; p.splits = a.splits;
     p.each_k = p.all_k / a.splits; p.more_k = p.all_k % a.splits;
     const int64_t total = t.tiles_m * t.tiles_n * a.batches * a.splits;
     if (total > 0x3FFFFFFF || (t.tiles_m + 16) * t.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidValue;
@@ -1198,16 +1211,16 @@ cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_
 }
 cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st)
 {
-    return launch_tiles<true, true, kStore>(a, tiling(kStore, true, a.m, a.n, stages_of(a.k), a.batches, false, sm_count), sm_count, st);
+    return launch_tiles<true, true, kStore>(a, tiling(kStore, true, a.m, a.n, stages_of(a.k), a.batches, true, sm_count), sm_count, st);
 }
 
 int product_partials(int64_t m, int64_t n, int64_t k, int sm_count)
 {
     return (int)(2 * tiling(kLse, false, m, n, stages_of(k), 1, false, sm_count).tiles_n);
 }
-int product_splits(int64_t m, int64_t n, int64_t k, int segments, int sm_count)
+int product_splits(int64_t m, int64_t n, int64_t k, int segments, int batches, int sm_count)
 {
-    return tiling(kStore, true, m, n, stages_of(k) * segments, 1, true, sm_count).splits;
+    return tiling(kStore, true, m, n, stages_of(k) * segments, batches, true, sm_count).splits;
 }
 
 bool tma_reads(const Bf16Matrix &m)
@@ -1230,11 +1243,11 @@ cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, cons
 }
 
 cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *dloss,
-                              const int64_t *target, cudaStream_t st)
+                              const int64_t *target, int64_t positions, bool add, cudaStream_t st)
 {
     const int64_t threads = (cols + 3) / 4 * rows;
-    if (splits < 8) return launch_after(st, dim3(grid_of(threads)), 256, 0, sum_splits_kernel<1>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target);
-    return launch_after(st, dim3(grid_of(threads * 8)), 256, 0, sum_splits_kernel<8>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target);
+    if (splits < 8) return launch_after(st, dim3(grid_of(threads)), 256, 0, sum_splits_kernel<1>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target, positions, (int)add);
+    return launch_after(st, dim3(grid_of(threads * 8)), 256, 0, sum_splits_kernel<8>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target, positions, (int)add);
 }
 
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,

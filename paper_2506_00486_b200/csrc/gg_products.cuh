@@ -39,7 +39,7 @@ struct ProductArgs {
     // kGated: h, gate, up (each of the last two may be null); kDlogits: out[0]; kStore: of a batch
     uint16_t *out[3];
     int64_t out_ld[3];
-    float *f32;                 // kStore: [splits][m][f32_ld], f32_ld a multiple of 32
+    float *f32;                 // kStore: [batches][splits][m][f32_ld], f32_ld a multiple of 32
     int64_t f32_ld;
     int mode;
     uint32_t *gave_up;          // host-visible word: set if a wait inside the kernel ran out
@@ -54,9 +54,8 @@ cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_
 cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st);
 // the partials of a row that kLse leaves
 int product_partials(int64_t m, int64_t n, int64_t k, int sm_count);
-// how many pieces the long axis of launch_product_drows is best cut into, so that all SMs have work
-int product_splits(int64_t m, int64_t n, int64_t k, int segments, int sm_count);
-
+// how many pieces the long axis of launch_product_drows and launch_product_dweight is best cut into, so that all SMs have work
+int product_splits(int64_t m, int64_t n, int64_t k, int segments, int batches, int sm_count);
 // kGated for a single row, without the tensor cores
 bool gated_row(int64_t m, int64_t k);
 cudaError_t launch_gated_row(const ProductArgs &a, int sm_count, cudaStream_t st);
@@ -68,9 +67,9 @@ cudaError_t launch_realign(const Bf16Matrix &from, uint16_t *to, int64_t ld, cud
 // lse and loss of a row from its partials; a negative target has loss 0, one beyond the vocabulary NaN
 cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, const float *target_logit, const int64_t *target, int64_t vocab, float *lse,
                               float *loss, cudaStream_t st);
-// out = bf16 of the sum of `splits` fp32 matrices (dloss, target as in ProductArgs)
+// out = bf16 of the sum of `splits` fp32 matrices (dloss, target, positions as in ProductArgs), and of what is there with `add`
 cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *dloss,
-                              const int64_t *target, cudaStream_t st);
+                              const int64_t *target, int64_t positions, bool add, cudaStream_t st);
 // dgate = dh * up * act'(gate), dup = dh * act(gate)
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,
                                 cudaStream_t st);
