@@ -6,6 +6,7 @@
 #include <string.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <memory>
 #include <new>
 #include <string>
@@ -1808,19 +1809,29 @@ struct Operand {
     {
         if (!tma_reads(m)) copy = s.place(m.rows * ((m.cols + 7) / 8 * 8) * 2);
     }
-    gg_status lay(ProductScratch &s)
-    {
-        if (copy < 0) return GG_OK;
-        const int64_t ld = (m.cols + 7) / 8 * 8;
-        uint16_t *to = s.at<uint16_t>(copy);
-        GG_CUDA(s.ctx, launch_realign(m, to, ld, s.st));
-        s.ctx->launches += 1;
-        m.p = to;
-        m.ld = ld;
-        copy = -1;
-        return GG_OK;
-    }
 };
+// Copies those that need it, in one launch.
+gg_status lay(ProductScratch &s, std::initializer_list<Operand *> operands)
+{
+    Copies c{};
+    int n = 0;
+    for (Operand *o : operands) {
+        if (o->copy < 0) continue;
+        const int64_t ld = (o->m.cols + 7) / 8 * 8;
+        uint16_t *to = s.at<uint16_t>(o->copy);
+        c.from[n] = o->m;
+        c.to[n] = to;
+        c.ld[n] = ld;
+        ++n;
+        o->m.p = to;
+        o->m.ld = ld;
+        o->copy = -1;
+    }
+    if (n == 0) return GG_OK;
+    GG_CUDA(s.ctx, launch_realign(c, s.st));
+    s.ctx->launches += 1;
+    return GG_OK;
+}
 
 ProductArgs product_args(gg_ctx *ctx)
 {
@@ -1886,7 +1897,7 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
                                                                   last * product_partials(last, a->vocab, a->width, ctx->sm_count));
     Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
     const int64_t part_at = s.place(part_bytes), logit_at = s.place(most * 4);
-    if ((st = s.grow()) != GG_OK || (st = h.lay(s)) != GG_OK || (st = w.lay(s)) != GG_OK) return st;
+    if ((st = s.grow()) != GG_OK || (st = lay(s, {&h, &w})) != GG_OK) return st;
     for (int64_t r = 0; r < a->rows; r += kLossRows) {
         const int64_t rows = std::min(a->rows - r, kLossRows);
         ProductArgs p = product_args(ctx);
@@ -1935,7 +1946,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
     const int64_t f32_at = s.place(a->dh && (splits > 1 || n_pieces > 1) ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
     const int64_t first_sums = weight_splits(piece) > 1 ? weight_splits(piece) * piece : 0, last_sums = weight_splits(last) > 1 ? weight_splits(last) * last : 0;
     const int64_t f32w_at = s.place(4 * std::max(first_sums, last_sums) * f32_ld);
-    if ((st = s.grow()) != GG_OK || (st = h.lay(s)) != GG_OK || (st = w.lay(s)) != GG_OK) return st;
+    if ((st = s.grow()) != GG_OK || (st = lay(s, {&h, &w})) != GG_OK) return st;
     for (int64_t i = 0; i < n_pieces; ++i) {
         const int64_t first = i * piece, n = std::min(piece, a->vocab - first);
         const Bf16Matrix d{s.at<uint16_t>(d_at), a->rows, n, piece}, rows_of_w{w.m.p + first * w.m.ld, n, a->width, w.m.ld};
@@ -2005,7 +2016,7 @@ gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *a, void *stre
     ProductScratch s{ctx, static_cast<cudaStream_t>(stream)};
     Operand x(matrix_of(a->x, a->rows, a->width, a->x_ld), s), wg(matrix_of(a->w_gate, a->hidden, a->width, a->w_gate_ld), s),
         wu(matrix_of(a->w_up, a->hidden, a->width, a->w_up_ld), s);
-    if ((st = s.grow()) != GG_OK || (st = x.lay(s)) != GG_OK || (st = wg.lay(s)) != GG_OK || (st = wu.lay(s)) != GG_OK) return st;
+    if ((st = s.grow()) != GG_OK || (st = lay(s, {&x, &wg, &wu})) != GG_OK) return st;
     ProductArgs p = product_args(ctx);
     p.a[0] = x.m;
     p.b[0] = wg.m;
@@ -2056,8 +2067,8 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
     const int64_t dgate_at = s.place(a->rows * ld * 2), dup_at = s.place(a->rows * ld * 2), f32_at = s.place(splits > 1 ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
     const int64_t f32w_at = s.place(weight_splits > 1 ? 8 * (int64_t)weight_splits * a->hidden * f32_ld : 0);
     if ((st = s.grow()) != GG_OK) return st;
-    if (a->dw_gate && (st = x.lay(s)) != GG_OK) return st;
-    if (a->dx && ((st = wg.lay(s)) != GG_OK || (st = wu.lay(s)) != GG_OK)) return st;
+    st = a->dx && a->dw_gate ? lay(s, {&x, &wg, &wu}) : a->dx ? lay(s, {&wg, &wu}) : lay(s, {&x});
+    if (st != GG_OK) return st;
     uint16_t *dgate = s.at<uint16_t>(dgate_at), *dup = s.at<uint16_t>(dup_at);
     GG_CUDA(ctx, launch_gated_slopes(matrix_of(a->dh, a->rows, a->hidden, a->dh_ld), matrix_of(a->gate, a->rows, a->hidden, a->gate_ld),
                                      matrix_of(a->up, a->rows, a->hidden, a->up_ld), a->act, dgate, dup, ld, s.st));

@@ -729,20 +729,39 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
 }
 
 // ------------------------------------------------------------------ around the products
-// One thread for eight columns of a row.
-__global__ void __launch_bounds__(256) realign_kernel(const Bf16Matrix from, uint16_t *to, int64_t ld, int64_t groups)
+// Copies of up to three matrices, a thread for eight columns of a row: by words of two elements, shifted where the row starts on an odd
+// one; single elements at a row's ends.
+__device__ __forceinline__ uint4 eight_anywhere(const uint16_t *p, int64_t col, int64_t cols)
 {
-    wait_for_the_one_before();
-    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < groups * from.rows; i += gridDim.x * 256ll) {
-        const int64_t row = i / groups, col = (i - row * groups) * 8;
-        const uint16_t *f = from.p + row * from.ld + col;
-        uint32_t w[4];
+    uint32_t w[5];
+    const int odd = (int)(reinterpret_cast<uintptr_t>(p) >> 1 & 1);
+    if (col >= odd && col + 8 + odd <= cols) {
+        const uint32_t *q = reinterpret_cast<const uint32_t *>(p - odd);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[j] = q[j];
+        if (odd) {
+            w[4] = q[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = __funnelshift_r(w[j], w[j + 1], 16);
+        }
+    } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const uint32_t lo = col + 2 * j < from.cols ? f[2 * j] : 0, hi = col + 2 * j + 1 < from.cols ? f[2 * j + 1] : 0;
+            const uint32_t lo = col + 2 * j < cols ? p[2 * j] : 0, hi = col + 2 * j + 1 < cols ? p[2 * j + 1] : 0;
             w[j] = lo | hi << 16;
         }
-        *reinterpret_cast<uint4 *>(to + row * ld + col) = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+__global__ void __launch_bounds__(256) realign_kernel(const Copies c)
+{
+    wait_for_the_one_before();
+    for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < c.end[2]; i += gridDim.x * 256ll) {
+        const int which = (i >= c.end[0]) + (i >= c.end[1]);
+        const int64_t at = i - (which == 0 ? 0 : c.end[which - 1]), groups = (c.from[which].cols + 7) / 8;
+        const int64_t row = at <= 0x7FFFFFFF ? (int64_t)((uint32_t)at / (uint32_t)groups) : at / groups, col = (at - row * groups) * 8;
+        const Bf16Matrix &m = c.from[which];
+        *reinterpret_cast<uint4 *>(c.to[which] + row * c.ld[which] + col) = eight_anywhere(m.p + row * m.ld + col, col, m.cols);
     }
 }
 
@@ -1228,10 +1247,14 @@ bool tma_reads(const Bf16Matrix &m)
     return reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.ld % 8 == 0;
 }
 
-cudaError_t launch_realign(const Bf16Matrix &from, uint16_t *to, int64_t ld, cudaStream_t st)
+cudaError_t launch_realign(Copies c, cudaStream_t st)
 {
-    const int64_t groups = (from.cols + 7) / 8;
-    return launch_after(st, dim3(grid_of(groups * from.rows)), 256, 0, realign_kernel, from, to, ld, groups);
+    int64_t n = 0;
+    for (int i = 0; i < 3; ++i) {
+        n += (c.from[i].cols + 7) / 8 * c.from[i].rows;
+        c.end[i] = n;
+    }
+    return n == 0 ? cudaSuccess : launch_after(st, dim3(grid_of(n)), 256, 0, realign_kernel, c);
 }
 
 cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, const float *target_logit, const int64_t *target, int64_t vocab, float *lse,

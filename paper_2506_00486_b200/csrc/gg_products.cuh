@@ -60,9 +60,16 @@ int product_splits(int64_t m, int64_t n, int64_t k, int segments, int batches, i
 bool gated_row(int64_t m, int64_t k);
 cudaError_t launch_gated_row(const ProductArgs &a, int sm_count, cudaStream_t st);
 
-// Can TMA read the matrix where it is?  If not, realign_rows copies it to rows of `ld` elements (a multiple of 8).
+// Can TMA read the matrix where it is?  If not, launch_realign copies it (up to three in one launch) to rows of `ld` elements, a multiple
+// of 8; what a row has beyond the matrix becomes 0.
 bool tma_reads(const Bf16Matrix &m);
-cudaError_t launch_realign(const Bf16Matrix &from, uint16_t *to, int64_t ld, cudaStream_t st);
+struct Copies {
+    Bf16Matrix from[3];         // (rows 0: none)
+    uint16_t *to[3];
+    int64_t ld[3];
+    int64_t end[3];             // (set by launch_realign)
+};
+cudaError_t launch_realign(Copies c, cudaStream_t st);
 
 // lse and loss of a row from its partials; a negative target has loss 0, one beyond the vocabulary NaN
 cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, const float *target_logit, const int64_t *target, int64_t vocab, float *lse,

@@ -98,12 +98,12 @@ def gated_problem(seed, rows, width, hidden, pad=0, shift=0):
 
 
 # positions beyond one block; pieces of the vocabulary (more than 512 MB of logits' gradient); a long sum over few and over many rows
-@pytest.mark.parametrize("rows,width,vocab", [(33001, 16, 300), (33000, 40, 9000), (20, 64, 40000), (5000, 520, 700), (1030, 4104, 1100), (300, 2048, 3000)])
+@pytest.mark.parametrize("rows,width,vocab", [(33001, 16, 300), (33000, 40, 9000), (20, 64, 40000), (5000, 520, 700), (1030, 4104, 1100), (300, 2048, 3000), (9000, 72, 500)])
 def test_loss_forms(ctx, rows, width, vocab):
     check_loss(ctx, *loss_problem(rows, rows, width, vocab))
 
 
-@pytest.mark.parametrize("rows,width,hidden", [(20000, 520, 300), (3000, 1100, 2056), (600, 4104, 520), (40, 300, 9000), (1, 5000, 70), (1, 30000, 6)])
+@pytest.mark.parametrize("rows,width,hidden", [(20000, 520, 300), (3000, 1100, 2056), (600, 4104, 520), (40, 300, 9000), (1, 5000, 70), (1, 30000, 6), (9000, 65, 300)])
 def test_gated_forms(ctx, rows, width, hidden):
     check_gated(ctx, *gated_problem(rows, rows, width, hidden), "silu")
 
@@ -119,6 +119,27 @@ def test_random_shapes(ctx, seed):
     check_loss(ctx, *loss_problem(seed, size(3000), size(1500), size(6000), pad=pad, shift=shift))
     act = ("silu", "gelu", "gelu_tanh", "relu")[seed % 4]
     check_gated(ctx, *gated_problem(seed, size(3000), size(1500), size(2500), pad=shift, shift=pad), act)
+
+
+@pytest.mark.parametrize("width", [72, 65])
+def test_gradients_of_weights_that_are_split_and_added(ctx, width):
+    # few columns, many rows: the sums are cut into splits, joined, and added to what is there
+    x, wg, wu, dh = gated_problem(3, 9000, width, 300)
+    f = ctx.gg_gated_linear(x, wg, wu, keep=True)
+    args = (dh, x, wg, wu, f["gate"], f["up"])
+    fresh = ctx.gg_gated_linear_grad(*args)
+    base = [torch.randn_like(wg), torch.randn_like(wg)]
+    out = ctx.gg_gated_linear_grad(*args, dw_gate=base[0].clone(), dw_up=base[1].clone(), accumulate=True)
+    for name, b in zip(("dw_gate", "dw_up"), base):
+        want = fresh[name].double() + b.double()       # (fresh is rounded once, the sum once)
+        near(out[name], want, BF16 * (fresh[name].double().abs() + want.abs() * (1 + BF16)) + 1e-37)
+    h, w, target, dloss = loss_problem(4, 9000, width, 500)
+    lse = ctx.gg_cross_entropy(h, w, target)["lse"]
+    fresh = ctx.gg_cross_entropy_grad(dloss, h, w, target, lse)["dw"]
+    base = torch.randn_like(w)
+    out = ctx.gg_cross_entropy_grad(dloss, h, w, target, lse, dw=base.clone(), accumulate=True)["dw"]
+    want = fresh.double() + base.double()
+    near(out, want, BF16 * (fresh.double().abs() + want.abs() * (1 + BF16)) + 1e-37)
 
 
 def test_elements_past_32_bits(ctx):
