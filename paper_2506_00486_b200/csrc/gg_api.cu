@@ -1836,7 +1836,7 @@ gg_status lay(ProductScratch &s, std::initializer_list<Operand *> operands)
 ProductArgs product_args(gg_ctx *ctx)
 {
     ProductArgs p{};
-    p.segments = p.batches = p.splits = 1;
+    p.segments = p.batches = 1;
     p.gave_up = ctx->gave_up;
     p.polls = ctx->wait_cap != kWaitCap ? ctx->wait_cap : 0;
     p.extra_bytes = ctx->expect_delta > 0 ? 16u * (uint32_t)ctx->expect_delta : 0u;
@@ -1856,11 +1856,12 @@ gg_status product_alive(gg_ctx *ctx)
 // The gradient of weights into out[] of each batch, by way of fp32 sums where the long axis is split.
 gg_status store_weights(gg_ctx *ctx, ProductArgs &q, bool add, cudaStream_t st)
 {
-    q.mode = q.splits > 1 ? kStoreF32 : add ? kAddBf16 : kStoreBf16;
+    const int splits = q.tiling.splits;
+    q.mode = splits > 1 ? kStoreF32 : add ? kAddBf16 : kStoreBf16;
     GG_CUDA(ctx, launch_product_dweight(q, ctx->sm_count, st));
     ctx->launches += 1;
-    for (int i = 0; q.splits > 1 && i < q.batches; ++i) {
-        GG_CUDA(ctx, launch_sum_splits(q.f32 + (int64_t)i * q.splits * q.m * q.f32_ld, q.splits, q.m, q.n, q.f32_ld, q.out[i], q.out_ld[i], q.dloss, q.target, q.positions, add, st));
+    for (int i = 0; splits > 1 && i < q.batches; ++i) {
+        GG_CUDA(ctx, launch_sum_splits(q.f32 + (int64_t)i * splits * q.m * q.f32_ld, splits, q.m, q.n, q.f32_ld, q.out[i], q.out_ld[i], q.dloss, q.target, q.positions, add, st));
         ctx->launches += 1;
     }
     return GG_OK;
@@ -1893,8 +1894,9 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
     if ((st = product_alive(ctx)) != GG_OK) return st;
     ProductScratch s{ctx, static_cast<cudaStream_t>(stream)};
     const int64_t most = std::min(a->rows, kLossRows), last = (a->rows - 1) % kLossRows + 1;
-    const int64_t part_bytes = (int64_t)sizeof(float2) * std::max(most * product_partials(most, a->vocab, a->width, ctx->sm_count),
-                                                                  last * product_partials(last, a->vocab, a->width, ctx->sm_count));
+    auto cut = [&](int64_t rows) { return product_tiling(kLse, false, rows, a->vocab, a->width, 1, 1, false, ctx->sm_count); };
+    const Tiling most_cut = cut(most), last_cut = last == most ? most_cut : cut(last);
+    const int64_t part_bytes = 2 * (int64_t)sizeof(float2) * std::max(most * most_cut.tiles_n, last * last_cut.tiles_n);
     Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
     const int64_t part_at = s.place(part_bytes), logit_at = s.place(most * 4);
     if ((st = s.grow()) != GG_OK || (st = lay(s, {&h, &w})) != GG_OK) return st;
@@ -1908,8 +1910,9 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
         p.target_logit = s.at<float>(logit_at);
         p.target = a->target + r;
         p.vocab = a->vocab;
+        p.tiling = rows == most ? most_cut : last_cut;
         GG_CUDA(ctx, launch_product_rows(kLse, p, ctx->sm_count, s.st));
-        GG_CUDA(ctx, launch_lse_finish(p.part, product_partials(rows, a->vocab, a->width, ctx->sm_count), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
+        GG_CUDA(ctx, launch_lse_finish(p.part, (int)(2 * p.tiling.tiles_n), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
                                        a->loss ? a->loss + r : nullptr, s.st));
         ctx->launches += 2;
     }
@@ -1938,14 +1941,24 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
     // pieces of the vocabulary of one size, a multiple of the tile
     const int64_t all = (a->vocab + 255) / 256, fit = std::max<int64_t>(1, kPieceBytes / (512 * a->rows)), pieces = (all + fit - 1) / fit;
     const int64_t piece = (all + pieces - 1) / pieces * 256, last = a->vocab - (a->vocab - 1) / piece * piece, n_pieces = (a->vocab + piece - 1) / piece;
-    const int splits = a->dh ? product_splits(a->rows, a->width, last, 1, 1, ctx->sm_count) : 1;
-    auto weight_splits = [&](int64_t n) { return a->dw ? product_splits(n, a->width, a->rows, 1, 1, ctx->sm_count) : 1; };
+    // (dh's sums are those of all pieces: one cut for it, and others for a last piece that is shorter)
+    auto logits_cut = [&](int64_t n) { return product_tiling(kDlogits, false, a->rows, n, a->width, 1, 1, false, ctx->sm_count); };
+    auto weights_cut = [&](int64_t n) { return product_tiling(kStore, true, n, a->width, a->rows, 1, 1, true, ctx->sm_count); };
+    Tiling cuts[3][2] = {};
+    cuts[0][0] = logits_cut(piece);
+    cuts[0][1] = last == piece ? cuts[0][0] : logits_cut(last);
+    if (a->dw) {
+        cuts[1][0] = weights_cut(piece);
+        cuts[1][1] = last == piece ? cuts[1][0] : weights_cut(last);
+    }
+    if (a->dh) cuts[2][0] = product_tiling(kStore, true, a->rows, a->width, last, 1, 1, true, ctx->sm_count);
+    const int splits = a->dh ? cuts[2][0].splits : 1;
     const int64_t f32_ld = (a->width + 31) / 32 * 32;
     Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
     const int64_t d_at = s.place(a->rows * piece * 2);
     const int64_t f32_at = s.place(a->dh && (splits > 1 || n_pieces > 1) ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
-    const int64_t first_sums = weight_splits(piece) > 1 ? weight_splits(piece) * piece : 0, last_sums = weight_splits(last) > 1 ? weight_splits(last) * last : 0;
-    const int64_t f32w_at = s.place(4 * std::max(first_sums, last_sums) * f32_ld);
+    const int64_t sums[2] = {cuts[1][0].splits > 1 ? cuts[1][0].splits * piece : 0, cuts[1][1].splits > 1 ? cuts[1][1].splits * last : 0};
+    const int64_t f32w_at = s.place(4 * std::max(sums[0], sums[1]) * f32_ld);
     if ((st = s.grow()) != GG_OK || (st = lay(s, {&h, &w})) != GG_OK) return st;
     for (int64_t i = 0; i < n_pieces; ++i) {
         const int64_t first = i * piece, n = std::min(piece, a->vocab - first);
@@ -1958,6 +1971,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
         p.lse = a->lse; p.dloss = a->dloss; p.positions = a->rows;
         p.out[0] = s.at<uint16_t>(d_at);
         p.out_ld[0] = piece;
+        p.tiling = cuts[0][n != piece];
         GG_CUDA(ctx, launch_product_rows(kDlogits, p, ctx->sm_count, s.st));
         ctx->launches += 1;
         if (a->dw) {
@@ -1967,7 +1981,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
             q.m = n; q.n = a->width; q.k = a->rows;
             q.out[0] = static_cast<uint16_t *>(a->dw) + first * a->dw_ld;
             q.out_ld[0] = a->dw_ld;
-            q.splits = weight_splits(n);
+            q.tiling = cuts[1][n != piece];
             q.f32 = s.at<float>(f32w_at);
             q.f32_ld = f32_ld;
             if ((st = store_weights(ctx, q, a->accumulate != 0, s.st)) != GG_OK) return st;
@@ -1977,7 +1991,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
             q.a[0] = d;
             q.b[0] = rows_of_w;
             q.m = a->rows; q.n = a->width; q.k = n;
-            q.splits = splits;
+            q.tiling = cuts[2][0];
             q.out[0] = static_cast<uint16_t *>(a->dh);
             q.out_ld[0] = a->dh_ld;
             q.f32 = s.at<float>(f32_at);
@@ -2025,8 +2039,12 @@ gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *a, void *stre
     p.out[0] = static_cast<uint16_t *>(a->h); p.out[1] = static_cast<uint16_t *>(a->gate); p.out[2] = static_cast<uint16_t *>(a->up);
     p.out_ld[0] = a->h_ld; p.out_ld[1] = a->gate_ld; p.out_ld[2] = a->up_ld;
     p.act = a->act;
-    if (gated_row(a->rows, a->width)) GG_CUDA(ctx, launch_gated_row(p, ctx->sm_count, s.st));
-    else GG_CUDA(ctx, launch_product_rows(kGated, p, ctx->sm_count, s.st));
+    if (gated_row(a->rows, a->width)) {
+        GG_CUDA(ctx, launch_gated_row(p, ctx->sm_count, s.st));
+    } else {
+        p.tiling = product_tiling(kGated, false, p.m, p.n, p.k, 1, 1, false, ctx->sm_count);
+        GG_CUDA(ctx, launch_product_rows(kGated, p, ctx->sm_count, s.st));
+    }
     ctx->launches += 1;
     return GG_OK;
 }
@@ -2060,12 +2078,14 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
     }
     if ((st = product_alive(ctx)) != GG_OK) return st;
     const int64_t ld = (a->hidden + 63) / 64 * 64, f32_ld = (a->width + 31) / 32 * 32;
-    const int splits = a->dx ? product_splits(a->rows, a->width, a->hidden, 2, 1, ctx->sm_count) : 1;
-    const int weight_splits = a->dw_gate ? product_splits(a->hidden, a->width, a->rows, 1, 2, ctx->sm_count) : 1;
+    Tiling rows_cut{}, weights_cut{};
+    if (a->dx) rows_cut = product_tiling(kStore, true, a->rows, a->width, a->hidden, 2, 1, true, ctx->sm_count);
+    if (a->dw_gate) weights_cut = product_tiling(kStore, true, a->hidden, a->width, a->rows, 1, 2, true, ctx->sm_count);
+    const int splits = rows_cut.splits;
     Operand x(matrix_of(a->x, a->rows, a->width, a->x_ld), s), wg(matrix_of(a->w_gate, a->hidden, a->width, a->w_gate_ld), s),
         wu(matrix_of(a->w_up, a->hidden, a->width, a->w_up_ld), s);
     const int64_t dgate_at = s.place(a->rows * ld * 2), dup_at = s.place(a->rows * ld * 2), f32_at = s.place(splits > 1 ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
-    const int64_t f32w_at = s.place(weight_splits > 1 ? 8 * (int64_t)weight_splits * a->hidden * f32_ld : 0);
+    const int64_t f32w_at = s.place(weights_cut.splits > 1 ? 8 * (int64_t)weights_cut.splits * a->hidden * f32_ld : 0);
     if ((st = s.grow()) != GG_OK) return st;
     st = a->dx && a->dw_gate ? lay(s, {&x, &wg, &wu}) : a->dx ? lay(s, {&wg, &wu}) : lay(s, {&x});
     if (st != GG_OK) return st;
@@ -2082,7 +2102,7 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
         q.b[1] = wu.m;
         q.m = a->rows; q.n = a->width; q.k = a->hidden;
         q.segments = 2;
-        q.splits = splits;
+        q.tiling = rows_cut;
         q.out[0] = static_cast<uint16_t *>(a->dx);
         q.out_ld[0] = a->dx_ld;
         q.f32 = s.at<float>(f32_at);
@@ -2103,7 +2123,7 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
         p.out[1] = static_cast<uint16_t *>(a->dw_up);
         p.out_ld[0] = a->dw_gate_ld;
         p.out_ld[1] = a->dw_up_ld;
-        p.splits = weight_splits;
+        p.tiling = weights_cut;
         p.f32 = s.at<float>(f32w_at);
         p.f32_ld = f32_ld;
         if ((st = store_weights(ctx, p, a->accumulate != 0, s.st)) != GG_OK) return st;

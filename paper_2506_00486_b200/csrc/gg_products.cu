@@ -1104,27 +1104,28 @@ Divider divider(int d)
 // 3 x 143 of 224 columns, which are shorter (53.3 and 52.2 us; 128 columns 68.8).  Clocks of a stage of 64 summed elements for 128 rows, from a product of
 // 16384 x 4096 x 32000: 512 for 256 columns, 457 for 224, 421 for 192, 405 for 128, 302 for 64, 272 for 32; a single CTA, which brings in more bytes
 // for its products, takes 25 % longer (517 rows: 77 and 52 us), two halves of 256 rows, which bring in fewer, 7 % less.
-struct Tiling {
-    int ctas = 1, halves = 1, tile_n = 256, cols = 256, splits = 1;
-    int64_t tiles_m = 1, tiles_n = 1;
-};
-Tiling tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t stages, int batches, bool may_split, int sm_count)
+}  // namespace
+Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, int segments, int batches, bool may_split, int sm_count)
 {
+    const int64_t stages = (k + kBlockK - 1) / kBlockK * segments;
     Tiling best;
     double least = 0.0;
     // (halves only where the end is short: that of the loss is not hidden behind them, 3.00 against 2.86 ms)
     for (int form = m > 256 && end == kStore ? 2 : m > 128 ? 1 : 0; form >= 0; --form) {
         const int ctas = form > 0 ? 2 : 1, halves = form == 2 ? 2 : 1, rows = 128 * ctas * halves;
         const double factor = form == 2 ? 0.93 : form == 1 ? 1.0 : 1.25;
+        const int64_t tiles_m = (m + rows - 1) / rows, units = sm_count / ctas;
         // columns of C: the tensor cores take multiples of 16, of a pair of 32; kGated halves them
         const int step = ctas == 1 && end != kDlogits && end != kStore ? 16 : 32, widest = end == kGated ? 128 : 256;
         for (int cols = widest; cols >= step; cols -= step) {
             const int width = end == kGated ? 2 * cols : cols;
-            const int64_t tiles_m = (m + rows - 1) / rows, tiles_n = (n + cols - 1) / cols, tiles = tiles_m * tiles_n * batches, units = sm_count / ctas;
-            int64_t splits = 1;
-            if (may_split && tiles < units) splits = units / tiles < stages / 8 ? units / tiles : stages / 8;
-            if (splits < 1) splits = 1;
-            const int64_t rounds = (tiles * splits + units - 1) / units, each = (stages + splits - 1) / splits;
+            const int64_t tiles_n = (n + cols - 1) / cols, tiles = tiles_m * tiles_n * batches;
+            int64_t splits = 1, each = stages;
+            if (may_split && tiles < units && stages >= 16) {
+                splits = units / tiles < stages / 8 ? units / tiles : stages / 8;
+                each = (stages + splits - 1) / splits;
+            }
+            const int64_t rounds = (tiles * splits + units - 1) / units;
             const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage, store = (cols % 64 == 0 ? 15.0 : 20.0) * width;
             double cost = rounds * ((main > store ? main : store) + 200.0) * halves + store;
             if (splits > 1) cost += 4000.0 + (double)splits * batches * m * n * 8.0 / 3600.0;       // the sums of the splits, written and read
@@ -1136,11 +1137,13 @@ Tiling tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t stages, int
     }
     return best;
 }
+namespace {
 
 template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd>
-cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, cudaStream_t st)
+cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
 {
     Params p{};
+    const Tiling &t = a.tiling;
     const int maps_a = a.segments > 1 || a.batches > 1 ? 2 : 1, maps_b = kEnd == kGated || maps_a == 2 ? 2 : 1;
     const int rows_a = kAT || a.m > 128 ? 128 : (int)((a.m + 7) / 8 * 8);
     cudaError_t e = cudaSuccess;
@@ -1153,9 +1156,9 @@ cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, 
     p.tile_n = t.tile_n; p.cols = t.cols;
     p.tiles_m = (int)t.tiles_m; p.tiles_n = (int)t.tiles_n;
     p.kblocks = (int)((a.k + kBlockK - 1) / kBlockK);
-    p.all_k = p.kblocks * a.segments; p.splits = a.splits;
-    p.each_k = p.all_k / a.splits; p.more_k = p.all_k % a.splits;
-    const int64_t total = t.tiles_m * t.tiles_n * a.batches * a.splits;
+    p.all_k = p.kblocks * a.segments; p.splits = t.splits;
+    p.each_k = p.all_k / t.splits; p.more_k = p.all_k % t.splits;
+    const int64_t total = t.tiles_m * t.tiles_n * a.batches * t.splits;
     if (total > 0x3FFFFFFF || (t.tiles_m + 16) * t.tiles_n > 0x3FFFFFFF) return cudaErrorInvalidValue;
     p.total = (int)total;
     p.band = 16 / kHalves;
@@ -1203,44 +1206,26 @@ cudaError_t launch_product(const ProductArgs &a, const Tiling &t, int sm_count, 
 }
 
 template <bool kAT, bool kBT, int kEnd>
-cudaError_t launch_tiles(const ProductArgs &a, const Tiling &t, int sm_count, cudaStream_t st)
+cudaError_t launch_tiles(const ProductArgs &a, int sm_count, cudaStream_t st)
 {
     if constexpr (kEnd == kStore)
-        if (t.halves == 2) return launch_product<2, 2, kAT, kBT, kEnd>(a, t, sm_count, st);
-    return t.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd>(a, t, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd>(a, t, sm_count, st);
+        if (a.tiling.halves == 2) return launch_product<2, 2, kAT, kBT, kEnd>(a, sm_count, st);
+    return a.tiling.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd>(a, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd>(a, sm_count, st);
 }
 
 int64_t row_shared_bytes(int64_t k) { return (k + 511) / 512 * 512 * 2; }
-
-int64_t stages_of(int64_t k) { return (k + kBlockK - 1) / kBlockK; }
 
 }  // namespace
 
 cudaError_t launch_product_rows(ProductEnd end, const ProductArgs &a, int sm_count, cudaStream_t st)
 {
-    const Tiling t = tiling(end, false, a.m, a.n, stages_of(a.k), 1, false, sm_count);
-    if (end == kGated) return launch_tiles<false, false, kGated>(a, t, sm_count, st);
-    if (end == kLse) return launch_tiles<false, false, kLse>(a, t, sm_count, st);
-    if (end == kDlogits) return launch_tiles<false, false, kDlogits>(a, t, sm_count, st);
+    if (end == kGated) return launch_tiles<false, false, kGated>(a, sm_count, st);
+    if (end == kLse) return launch_tiles<false, false, kLse>(a, sm_count, st);
+    if (end == kDlogits) return launch_tiles<false, false, kDlogits>(a, sm_count, st);
     return cudaErrorInvalidValue;
 }
-cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st)
-{
-    return launch_tiles<false, true, kStore>(a, tiling(kStore, true, a.m, a.n, stages_of(a.k) * a.segments, 1, true, sm_count), sm_count, st);
-}
-cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st)
-{
-    return launch_tiles<true, true, kStore>(a, tiling(kStore, true, a.m, a.n, stages_of(a.k), a.batches, true, sm_count), sm_count, st);
-}
-
-int product_partials(int64_t m, int64_t n, int64_t k, int sm_count)
-{
-    return (int)(2 * tiling(kLse, false, m, n, stages_of(k), 1, false, sm_count).tiles_n);
-}
-int product_splits(int64_t m, int64_t n, int64_t k, int segments, int batches, int sm_count)
-{
-    return tiling(kStore, true, m, n, stages_of(k) * segments, batches, true, sm_count).splits;
-}
+cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st) { return launch_tiles<false, true, kStore>(a, sm_count, st); }
+cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st) { return launch_tiles<true, true, kStore>(a, sm_count, st); }
 
 bool tma_reads(const Bf16Matrix &m)
 {

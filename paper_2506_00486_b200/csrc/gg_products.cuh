@@ -22,13 +22,20 @@ enum ProductEnd : int {
 // there, bf16 of the sum with the fp32 that is there.
 enum StoreMode : int { kStoreBf16, kAddBf16, kStoreF32, kAddF32, kStoreBf16OfSum };
 
+// How C is cut into tiles (product_tiling): CTAs of a tile, its halves, rows of B and columns of C in it, splits of the long axis.
+struct Tiling {
+    int ctas, halves, tile_n, cols, splits;
+    int64_t tiles_m, tiles_n;
+};
+
 struct ProductArgs {
     // C[m, n] = sum over the segments of A B^T.  K-major operands are [m or n, k] matrices, the others [k, m or n].
     Bf16Matrix a[2], b[2];      // of a segment, or of a batch (one of the two); kGated: b[0] gate, b[1] up
     int64_t m, n, k;            // kGated: n counts the columns of h
-    int segments, batches, splits;
+    int segments, batches;
+    Tiling tiling;
     int act;                    // kGated
-    // kLse: [product_partials][m] partials; target[m], the logits of the targets.  kDlogits: target, lse, dloss, out.
+    // kLse: [2 * tiles_n][m] partials; target[m], the logits of the targets.  kDlogits: target, lse, dloss, out.
     float2 *part;
     float *target_logit;
     const int64_t *target;
@@ -52,10 +59,8 @@ cudaError_t launch_product_rows(ProductEnd end, const ProductArgs &a, int sm_cou
 // ... with A K-major and B [k, n] (the gradient of the rows), and with A [k, m] and B [k, n] (that of a weight); kStore
 cudaError_t launch_product_drows(const ProductArgs &a, int sm_count, cudaStream_t st);
 cudaError_t launch_product_dweight(const ProductArgs &a, int sm_count, cudaStream_t st);
-// the partials of a row that kLse leaves
-int product_partials(int64_t m, int64_t n, int64_t k, int sm_count);
-// how many pieces the long axis of launch_product_drows and launch_product_dweight is best cut into, so that all SMs have work
-int product_splits(int64_t m, int64_t n, int64_t k, int segments, int batches, int sm_count);
+// The cut that leaves least to wait for; bt: B is [k, n].  With may_split the long axis may be cut too (kStoreF32 then).
+Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, int segments, int batches, bool may_split, int sm_count);
 // kGated for a single row, without the tensor cores
 bool gated_row(int64_t m, int64_t k);
 cudaError_t launch_gated_row(const ProductArgs &a, int sm_count, cudaStream_t st);
