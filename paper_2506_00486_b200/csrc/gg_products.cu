@@ -236,10 +236,18 @@ struct Way {
         if (!o.whole) {
             // element by element: a lane takes columns lane and lane + 32 of every row (pairs from the first even element on measured
             // twice as long)
-            for (int r = 0; r < rows; ++r)
-#pragma unroll
-                for (int e = lane; e < kPieces * 8; e += 32)
-                    if (c + e < t.width) o.p[(t.row0 + r) * o.ld + t.col + c + e] = element(r, e);
+            const bool one = c + lane < t.width, two = kPieces == 8 && c + 32 + lane < t.width;
+            const uint32_t from = at + ((uint32_t)lane >> 3 << 4) + (lane & 7) * 2;
+            uint16_t *e = o.p + t.row0 * o.ld + t.col + c + lane;
+#pragma unroll 8
+            for (int r = 0; r < 32; ++r) {
+                uint16_t v = 0, w = 0;
+                asm volatile("ld.shared.u16 %0, [%1];" : "=h"(v) : "r"((from ^ (r & 7) << 4) + r * 128) : "memory");
+                if constexpr (kPieces == 8) asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"((from ^ ((r & 7) << 4 ^ 64)) + r * 128) : "memory");
+                if (one && r < rows) e[0] = v;
+                if (two && r < rows) e[32] = w;
+                e += o.ld;
+            }
         } else if (left >= 8) {
             for (int r = first; r < rows; r += kRows) {
                 uint32_t w[4];
