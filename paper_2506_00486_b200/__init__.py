@@ -1,5 +1,6 @@
 """B200-native generalized-Gaussian (GG) pass: moments, fit, penalty gradient, symbol histogram
-and entropy, and GG sampling, as hand-written sm_100a CUDA behind a small C interface.
+and entropy, GG sampling, and the operators of a training step around it (layer norm, vocabulary loss, gated
+block, dropout, AdamW), as hand-written sm_100a CUDA behind a small C interface.
 
 `binding` marshals torch tensors into that interface; `build` compiles the library in-tree.
 Nothing here computes on the CPU.

@@ -3,9 +3,15 @@
 // One kernel, C = A B^T in bf16 with fp32 sums, and four ends for its tiles (ProductEnd): the operators differ in what becomes
 // of a tile while it is still in tensor memory, so neither the logits nor the two projections need a pass of their own.
 // A persistent CTA (or pair of CTAs, each with half of A's and half of B's rows of a shared 256 x 256 tile) takes tiles in turn.
-// One thread copies the operands into a ring of stages of 64 summed elements by TMA, which also fills what lies beyond a matrix
-// with zeros, so no size is special; one thread feeds the tensor cores; eight warps end the tile before the last, which
-// lies in the other half of tensor memory.
+// One warp copies the operands into a ring of stages of 64 summed elements by TMA, which also fills what lies beyond a matrix
+// with zeros, so no size is special; one feeds the tensor cores; eight end the tile before, which lies in the other half of
+// tensor memory.
+//
+// What bounds it.  Large products: the tensor cores, then the power limit.  The logits of 8192 positions, width 4096, vocabulary 16384, with their
+// loss, keep the tensor pipe busy 94 % of the time (657 us, 1673 TFLOP/s); in a loop of seconds the clock falls to 1.25 - 1.45 GHz and
+// 16384 x 4096 x 32000 takes 2.97 ms = 1445 TFLOP/s, where a library product that only writes the logits takes 2.95 - 3.07.  A few rows: one pass over
+// B (5.1 - 5.7 TB/s).  What made most of it: pairs of CTAs on 256 x 256 tiles (3.74 -> 3.36 ms for that loss), loops that a whole warp
+// walks, so that addresses stay in uniform registers (-> 2.94 ms), barriers that do not wait for stores (below).
 #include <cuda.h>
 #include <math.h>
 
@@ -1107,12 +1113,13 @@ Divider divider(int d)
     return r;
 }
 
+}  // namespace
+
 // How C is cut into tiles.  All units (CTAs, or pairs of them) take tiles in turn, so the time is that of the unit with the
 // most, and a width is chosen that leaves the last round full: 517 rows against 32003 are 6 rounds of 3 x 126 tiles of 256 x 256, and 6 of
 // 3 x 143 of 224 columns, which are shorter (53.3 and 52.2 us; 128 columns 68.8).  Clocks of a stage of 64 summed elements for 128 rows, from a product of
 // 16384 x 4096 x 32000: 512 for 256 columns, 457 for 224, 421 for 192, 405 for 128, 302 for 64, 272 for 32; a single CTA, which brings in more bytes
 // for its products, takes 25 % longer (517 rows: 77 and 52 us), two halves of 256 rows, which bring in fewer, 7 % less.
-}  // namespace
 Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, int segments, int batches, bool may_split, int sm_count)
 {
     const int64_t stages = (k + kBlockK - 1) / kBlockK * segments;
