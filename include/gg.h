@@ -30,7 +30,7 @@
  *    layout in a full context frees the oldest plan, after waiting for the work last enqueued
  *    with it (an event).  A plan that a captured call used stays as it is until gg_destroy, and
  *    counts toward neither limit: the graph holds its tables.  And a call that needs more
- *    histogram, channel, layer norm or product scratch than any before it allocates it, outside stream
+ *    histogram, channel or layer norm scratch than any before it allocates it, outside stream
  *    capture too; what it had before stays until gg_destroy, for graphs captured earlier.  A
  *    context serves one stream at a time.
  *  - A segment is a contiguous run of `len` elements.  Pointers need only element alignment;

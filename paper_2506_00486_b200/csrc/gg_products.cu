@@ -278,15 +278,22 @@ struct Way {
 // The weights of the positions are mostly one number, 1 / their count, and d = weight * (p - 1) is then mostly that number too: rounded
 // to bf16 it may be off by 2^-8 in all of them alike (the gradient of 33 positions: 0.4 % off as a whole).  So d is kept relative to the
 // mantissa, 1 .. 2, of the first weight that is not 0, and the sums are multiplied by it: p - 1 itself is rounded (0.2 %, and
-// no longer alike).  A whole warp asks; only so many rows are looked at, beyond them it is 1.
+// no longer alike).  A whole warp asks; only so many rows are looked at, 256 at once (a padded batch may begin without any), beyond them it is 1.
 __device__ __forceinline__ float weight_mantissa(const float *dloss, const int64_t *target, int64_t rows)
 {
     const int lane = threadIdx.x & 31;
-    for (int64_t r = 0; r < rows && r < 4096; r += 32) {
-        float g = 0.0f;
-        if (r + lane < rows && target[r + lane] >= 0) g = fabsf(dloss[r + lane]);
-        const uint32_t some = __ballot_sync(~0u, g > 1e-30f && g < 1e30f);
-        if (some != 0) return __uint_as_float((__float_as_uint(__shfl_sync(~0u, g, __ffs(some) - 1)) & 0x7FFFFFu) | 0x3F800000u);
+    for (int64_t r = 0; r < rows && r < 4096; r += 256) {
+        float g[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int64_t at = r + 32 * j + lane;
+            g[j] = at < rows && target[at] >= 0 ? fabsf(dloss[at]) : 0.0f;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const uint32_t some = __ballot_sync(~0u, g[j] > 1e-30f && g[j] < 1e30f);
+            if (some != 0) return __uint_as_float((__float_as_uint(__shfl_sync(~0u, g[j], __ffs(some) - 1)) & 0x7FFFFFu) | 0x3F800000u);
+        }
     }
     return 1.0f;
 }

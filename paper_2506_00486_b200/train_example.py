@@ -9,6 +9,9 @@ vocabulary (gg_gated_linear, gg_dropout, gg_cross_entropy and their gradients). 
 forward and backward passes use gg_layer_norm and gg_layer_norm_grad (matrix products are torch's), the GG penalty of the
 weights is fitted and its gradient added to the loss's (gg_fused), and the step clips by the global norm and updates bf16
 weights with 32- or 8-bit states (gg_grad_norm, gg_adamw_step).
+
+A backward pass through the autograd forms below may be captured into a graph like any other of torch: with leaves whose eager graphs
+are gone, since torch ties their gradients to the stream that first made them.  Context's make_* calls have no such tie.
 """
 import argparse
 

@@ -181,6 +181,17 @@ def test_weights_of_the_loss(ctx):
     check_grad(dloss, h, w, target, lse, ctx.gg_cross_entropy_grad(dloss, h, w, target, lse))
 
 
+@pytest.mark.parametrize("first", [1, 40, 255, 300, 4097, 5000])
+def test_a_batch_that_begins_without_targets(ctx, first):
+    # whichever weight the gradient is kept relative to, or none
+    h, w, target, dloss = problem(18, 5300, 24, 100, ignored=0.0)
+    target[:first] = -100
+    dloss[first:first + 20] = 0.0
+    dloss[first + 20:first + 25] = torch.tensor([1e-35, float(torch.finfo(torch.float32).tiny), 1e-20, 3e4, -7.0], device="cuda")
+    lse = ctx.gg_cross_entropy(h, w, target)["lse"]
+    check_grad(dloss, h, w, target, lse, ctx.gg_cross_entropy_grad(dloss, h, w, target, lse))
+
+
 def test_one_gradient_at_a_time_accumulation_and_repeatability(ctx):
     h, w, target, dloss = problem(12, 333, 120, 1111)
     lse = ctx.gg_cross_entropy(h, w, target)["lse"]

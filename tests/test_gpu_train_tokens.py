@@ -112,6 +112,9 @@ def test_only_the_gradients_that_are_asked_for(ctx):
         assert [u.grad is not None for u in t] == [i == which for i in range(2)]
     y = Dropout.apply(x, None, 0.5, ctx, 0, 1, 0)
     assert not y.requires_grad
+    with torch.no_grad():
+        q = w.clone().requires_grad_(True)
+        assert not GatedLinear.apply(x, q, v, ctx).requires_grad and not CrossEntropy.apply(x, q, target, ctx).requires_grad
 
 
 def test_a_second_derivative_is_refused(ctx):
