@@ -1896,7 +1896,7 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
     const int64_t most = std::min(a->rows, kLossRows), last = (a->rows - 1) % kLossRows + 1;
     auto cut = [&](int64_t rows) { return product_tiling(kLse, false, rows, a->vocab, a->width, 1, 1, false, ctx->sm_count); };
     const Tiling most_cut = cut(most), last_cut = last == most ? most_cut : cut(last);
-    const int64_t part_bytes = 2 * (int64_t)sizeof(float2) * std::max(most * most_cut.tiles_n, last * last_cut.tiles_n);
+    const int64_t part_bytes = (int64_t)sizeof(float2) * std::max(most * most_cut.parts(), last * last_cut.parts());
     Operand h(matrix_of(a->h, a->rows, a->width, a->h_ld), s), w(matrix_of(a->w, a->vocab, a->width, a->w_ld), s);
     const int64_t part_at = s.place(part_bytes), logit_at = s.place(most * 4);
     if ((st = s.grow()) != GG_OK || (st = lay(s, {&h, &w})) != GG_OK) return st;
@@ -1912,7 +1912,7 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *st
         p.vocab = a->vocab;
         p.tiling = rows == most ? most_cut : last_cut;
         GG_CUDA(ctx, launch_product_rows(kLse, p, ctx->sm_count, s.st));
-        GG_CUDA(ctx, launch_lse_finish(p.part, (int)(2 * p.tiling.tiles_n), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
+        GG_CUDA(ctx, launch_lse_finish(p.part, (int)p.tiling.parts(), rows, p.target_logit, p.target, a->vocab, a->lse ? a->lse + r : nullptr,
                                        a->loss ? a->loss + r : nullptr, s.st));
         ctx->launches += 2;
     }

@@ -28,11 +28,11 @@ namespace gg {
 namespace {
 
 constexpr int kBlockK = 64;             // summed elements of a stage: 128 bytes, a row of the swizzle
-constexpr int kEndWarps = 8, kThreads = 32 * (4 + kEndWarps);
-constexpr int kRing = 192 * 1024;       // bytes of the ring of stages
+// Warps that end tiles: eight, with 192 KB for the ring of stages; or sixteen, which need 32 KB of that for what they send out.
+__host__ __device__ constexpr int ring_bytes(int end_warps) { return (end_warps == 16 ? 160 : 192) * 1024; }
 constexpr int kMostStages = 16;
 constexpr int kOutBytes = 4096;         // 32 rows of 64 bf16 on their way out, for each warp of the end
-constexpr int kShared = 1024 + kRing + kEndWarps * kOutBytes;
+constexpr int kShared = 1024 + ring_bytes(8) + 8 * kOutBytes;      // (either way)
 constexpr int kAccColumns = 256;        // of tensor memory for one accumulator; there are two
 constexpr int kLseRun = 16;             // stages after which the sums of a logit are taken out of the tensor cores
 constexpr float kLog2e = 1.4426950408889634f;
@@ -308,11 +308,11 @@ __device__ __forceinline__ void read_pairs(uint32_t at, f32x2 (&v)[16])
     for (int i = 0; i < 16; ++i) v[i] = pair(x[2 * i], x[2 * i + 1]);
 }
 
-// A tile's columns go to the two warps of a lane quarter in turn, 32 or 64 at a time.
-__device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int half, const Way &way)
+// A tile's columns go to the warps of a lane quarter in turn, 32 or 64 at a time.
+__device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int share, const Way &way)
 {
 #pragma unroll 1
-    for (int c = half * 32; c < t.width; c += 64) {
+    for (int c = share * 32; c < t.width; c += 64) {
         f32x2 g[16], u[16];
         {
             float x[32], y[32];
@@ -347,26 +347,28 @@ __device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int ha
     }
 }
 
-// The logits of a warp's half of the tile, four runs of 32 columns.  The tensor cores do not round their sums to nearest: a long one
+// The logits of a warp's share of the tile, 32 columns of every 32 * kShare.  The tensor cores do not round their sums to nearest: a long one
 // comes out too small (the loss of 16384 positions of width 4096 was 2.5e-6 off; it is 6e-7 now, at the same speed).  So after every kLseRun stages
 // what they have is added here, rounded, and they begin anew, in the other accumulator.
+template <int kShare>
 struct Logits {
-    f32x2 v[8][8];
+    static constexpr int kRuns = 16 / kShare;            // of 16 columns
+    f32x2 v[kRuns][8];
     __device__ __forceinline__ void clear()
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < kRuns; ++i)
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] = both(0.0f);
     }
-    static __device__ __forceinline__ int column(int half, int i) { return half * 32 + (i >> 1) * 64 + (i & 1) * 16; }
-    __device__ __forceinline__ void take(const Tile &t, int half)
+    static __device__ __forceinline__ int column(int share, int i) { return share * 32 + (i >> 1) * 32 * kShare + (i & 1) * 16; }
+    __device__ __forceinline__ void take(const Tile &t, int share)
     {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-            if (column(half, i) < t.width) {
+        for (int i = 0; i < kRuns; ++i)
+            if (column(share, i) < t.width) {
                 float x[16];
-                tmem_read(t.acc + column(half, i), x);
+                tmem_read(t.acc + column(share, i), x);
                 tmem_read_wait();
 #pragma unroll
                 for (int j = 0; j < 8; ++j) v[i][j] = add2(v[i][j], pair(x[2 * j], x[2 * j + 1]));
@@ -375,13 +377,14 @@ struct Logits {
 };
 
 // The sum is taken relative to the largest.  A NaN, which no maximum shows, reaches the sum by its own term.
-__device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half, Logits &l)
+template <int kShare>
+__device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int share, Logits<kShare> &l)
 {
     const int target = t.target(p.first);
     float most = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int c = Logits::column(half, i), left = t.width - c;
+    for (int i = 0; i < Logits<kShare>::kRuns; ++i) {
+        const int c = Logits<kShare>::column(share, i), left = t.width - c;
         if (left < 16) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
@@ -407,23 +410,24 @@ __device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int half
     const f32x2 base = both(most == -INFINITY ? 0.0f : -most);
     f32x2 sum[2] = {both(0.0f), both(0.0f)};
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-        if (Logits::column(half, i) < t.width) {
+    for (int i = 0; i < Logits<kShare>::kRuns; ++i)
+        if (Logits<kShare>::column(share, i) < t.width) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum[j & 1] = add2(sum[j & 1], power2(mul2(add2(l.v[i][j], base), both(kLog2e))));
         }
     const float2 s = halves(add2(sum[0], sum[1]));
-    if (t.row < p.m) p.part[(int64_t)(2 * t.n_tile + half) * p.m + t.row] = make_float2(most, s.x + s.y);
+    if (t.row < p.m) p.part[(int64_t)(kShare * t.n_tile + share) * p.m + t.row] = make_float2(most, s.x + s.y);
 }
 
-__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int half, const Way &way, float scale)
+template <int kShare>
+__device__ __forceinline__ void end_dlogits(const Params &p, const Tile &t, int share, const Way &way, float scale)
 {
     const int64_t of = t.of;
     const int target = t.target(p.first);
     const float g = of < 0 ? 0.0f : of >= p.vocab ? NAN : t.weight / scale;
     const f32x2 lse = both(-t.lse);
 #pragma unroll 1
-    for (int c = half * 64; c < t.width; c += 128) {
+    for (int c = share * 64; c < t.width; c += 64 * kShare) {
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             f32x2 v[16];
@@ -489,12 +493,13 @@ __device__ __forceinline__ void fp32_sums(const Params &p, const Tile &t, int c,
     }
 }
 
-__device__ __forceinline__ void end_store(const Params &p, const Tile &t, int half, const Way &way, float scale)
+template <int kShare>
+__device__ __forceinline__ void end_store(const Params &p, const Tile &t, int share, const Way &way, float scale)
 {
     const bool there = t.row < p.m;
     const f32x2 scales = both(scale);
 #pragma unroll 1
-    for (int c = half * 64; c < t.width; c += 128) {
+    for (int c = share * 64; c < t.width; c += 64 * kShare) {
 #pragma unroll
         for (int part = 0; part < 2; ++part) {
             f32x2 v[16];
@@ -536,16 +541,17 @@ __device__ __forceinline__ Work work_of(const Params &p, int w)
 __device__ __forceinline__ int split_start(const Params &p, int split) { return split * p.each_k + (split < p.more_k ? split : p.more_k); }
 
 // kHalves 2: a pair's tile has 512 rows, as two halves of 256 with an accumulator each.  Otherwise the two accumulators take turns.
-template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd>
-__global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_constant__ Params p)
+template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd, int kEndWarps>
+__global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const __grid_constant__ Params p)
 {
-    extern __shared__ uint8_t ring_bytes[];
+    constexpr int kShare = kEndWarps / 4;
+    extern __shared__ uint8_t shared_bytes[];
     __shared__ uint64_t bars[2 * kMostStages + 5];
     __shared__ uint32_t tmem_at;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = kCtas == 2 ? cluster_rank() : 0;
-    const uint32_t ring = (shared_address(ring_bytes) + 1023) & ~1023u, half_a = p.bytes_a, bytes_a = kHalves * half_a, bytes = bytes_a + p.bytes_b, stages = p.stages;
+    const uint32_t ring = (shared_address(shared_bytes) + 1023) & ~1023u, half_a = p.bytes_a, bytes_a = kHalves * half_a, bytes = bytes_a + p.bytes_b, stages = p.stages;
     const uint32_t full = shared_address(bars), empty = full + 8 * kMostStages, done = empty + 8 * kMostStages, free_at = done + 16, drained = done + 32;
 
     if (warp == 0 && lane == 0) {
@@ -695,9 +701,9 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
             barrier_wait(drained, 0, p.polls);
         }
     } else if (warp >= 4) {
-        // ---- ends
-        const int half = (warp - 4) >> 2, quarter = warp & 3;
-        const Way way(ring + kRing + (uint32_t)(warp - 4) * kOutBytes, lane);
+        // ---- ends (a lane quarter's warps share a tile's columns)
+        const int share = (warp - 4) >> 2, quarter = warp & 3;
+        const Way way(ring + ring_bytes(kEndWarps) + (uint32_t)(warp - 4) * kOutBytes, lane);      // (kLse sends nothing)
         const float scale = (kEnd == kDlogits || kEnd == kStore) && p.dloss != nullptr ? weight_mantissa(p.dloss, p.target, p.positions) : 1.0f;
         uint32_t units = 0;
         for (int w = first; w < p.total && !failed; w += step) {
@@ -717,7 +723,7 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 }
             }
             const int runs = kEnd == kLse ? (p.kblocks + kLseRun - 1) / kLseRun : kHalves;
-            Logits logits;
+            Logits<kShare> logits;
             if constexpr (kEnd == kLse) logits.clear();
 #pragma unroll 1
             for (int h = 0; h < runs; ++h, ++units) {
@@ -728,16 +734,16 @@ __global__ void __launch_bounds__(kThreads, 1) product_kernel(const __grid_const
                 tile.row0 = (int64_t)t.m_tile * 128 * kCtas * kHalves + (kHalves == 2 ? 256 * h : 0) + rank * 128 + quarter * 32;
                 tile.row = tile.row0 + lane;
                 tile.acc = tmem + acc * kAccColumns + ((uint32_t)quarter << 21);      // (lane 32 * quarter, in the upper half of the word)
-                if constexpr (kEnd == kGated) end_gated(p, tile, half, way);
-                if constexpr (kEnd == kLse) logits.take(tile, half);
-                if constexpr (kEnd == kDlogits) end_dlogits(p, tile, half, way, scale);
-                if constexpr (kEnd == kStore) end_store(p, tile, half, way, scale);
+                if constexpr (kEnd == kGated) end_gated(p, tile, share, way);
+                if constexpr (kEnd == kLse) logits.take(tile, share);
+                if constexpr (kEnd == kDlogits) end_dlogits<kShare>(p, tile, share, way, scale);
+                if constexpr (kEnd == kStore) end_store<kShare>(p, tile, share, way, scale);
                 __syncwarp();
                 tmem_before_sync();
                 if (lane == 0) barrier_arrive(peer_address(free_at + 8 * acc, 0));
             }
             if constexpr (kEnd == kLse)
-                if (!failed) end_lse(p, tile, half, logits);
+                if (!failed) end_lse<kShare>(p, tile, share, logits);
         }
     }
     if (failed && p.gave_up != nullptr) *reinterpret_cast<volatile uint32_t *>(p.gave_up) = 1;
@@ -1148,12 +1154,16 @@ Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, 
                 each = (stages + splits - 1) / splits;
             }
             const int64_t rounds = (tiles * splits + units - 1) / units;
-            const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage, store = (cols % 64 == 0 ? 15.0 : 20.0) * width;
+            // Sixteen warps for the end where the sums are short (loss of 526 x 128 x 34071: 31 us, with eight 52; 1000 x 256 x 50000: 38 and 42; the gradient of
+            // weights from 17 positions of width 1152: 25 and 30; but 300 x 512 x 30000 18.7 and 17.8, and longer sums more)
+            const int end_warps = end != kGated && halves == 1 && each <= 4 && m > 128 ? 16 : 8;
+            const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage;
+            const double store = (cols % 64 == 0 ? 15.0 : 20.0) * width * (end_warps == 16 ? 0.8 : 1.0);
             double cost = rounds * ((main > store ? main : store) + 200.0) * halves + store;
             if (splits > 1) cost += 4000.0 + (double)splits * batches * m * n * 8.0 / 3600.0;       // the sums of the splits, written and read
             if (least == 0.0 || cost < least) {
                 least = cost;
-                best = Tiling{ctas, halves, width, cols, (int)splits, tiles_m, tiles_n};
+                best = Tiling{ctas, halves, width, cols, (int)splits, end_warps, tiles_m, tiles_n};
             }
         }
     }
@@ -1161,7 +1171,7 @@ Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, 
 }
 namespace {
 
-template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd>
+template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd, int kEndWarps>
 cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
 {
     Params p{};
@@ -1192,7 +1202,7 @@ cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
     // (a product reads 128 rows of A from the ring, also where A has fewer and other bytes follow: rows of C that nobody stores)
     p.bytes_a = rows_a * 128;
     p.bytes_b = (kBT ? (t.tile_n / kCtas + 63) / 64 * 64 : t.tile_n / kCtas) * 128;
-    p.stages = (kRing - (16384 - p.bytes_a)) / (kHalves * p.bytes_a + p.bytes_b);
+    p.stages = (ring_bytes(kEndWarps) - (16384 - p.bytes_a)) / (kHalves * p.bytes_a + p.bytes_b);
     if (p.stages > kMostStages) p.stages = kMostStages;
     p.act = a.act;
     p.part = a.part; p.target_logit = a.target_logit; p.target = a.target; p.vocab = a.vocab; p.first = a.first;
@@ -1202,7 +1212,7 @@ cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
     const int64_t polls = (int64_t)(1 << 22) + 8 * (int64_t)p.all_k;
     p.polls = a.polls != 0 ? a.polls : polls < 0xFFFFFFFF ? (uint32_t)polls : 0xFFFFFFFF;
     p.extra_bytes = a.extra_bytes;
-    auto kernel = product_kernel<kCtas, kHalves, kAT, kBT, kEnd>;
+    auto kernel = product_kernel<kCtas, kHalves, kAT, kBT, kEnd, kEndWarps>;
     static std::atomic<uint64_t> known{0};      // devices on which the kernel has its shared memory
     int device = 0;
     e = cudaGetDevice(&device);
@@ -1214,7 +1224,7 @@ cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
     const int most = sm_count / kCtas, groups = p.total < most ? p.total : most;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3((unsigned)(groups * kCtas));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(32 * (4 + kEndWarps));
     cfg.dynamicSmemBytes = kShared;
     cfg.stream = st;
     cudaLaunchAttribute attr[2];
@@ -1231,8 +1241,11 @@ template <bool kAT, bool kBT, int kEnd>
 cudaError_t launch_tiles(const ProductArgs &a, int sm_count, cudaStream_t st)
 {
     if constexpr (kEnd == kStore)
-        if (a.tiling.halves == 2) return launch_product<2, 2, kAT, kBT, kEnd>(a, sm_count, st);
-    return a.tiling.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd>(a, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd>(a, sm_count, st);
+        if (a.tiling.halves == 2) return launch_product<2, 2, kAT, kBT, kEnd, 8>(a, sm_count, st);
+    if constexpr (kEnd != kGated)
+        if (a.tiling.end_warps == 16)
+            return a.tiling.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd, 16>(a, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd, 16>(a, sm_count, st);
+    return a.tiling.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd, 8>(a, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd, 8>(a, sm_count, st);
 }
 
 int64_t row_shared_bytes(int64_t k) { return (k + 511) / 512 * 512 * 2; }

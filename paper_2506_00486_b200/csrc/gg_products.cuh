@@ -22,9 +22,11 @@ enum ProductEnd : int {
 // there, bf16 of the sum with the fp32 that is there.
 enum StoreMode : int { kStoreBf16, kAddBf16, kStoreF32, kAddF32, kStoreBf16OfSum };
 
-// How C is cut into tiles (product_tiling): CTAs of a tile, its halves, rows of B and columns of C in it, splits of the long axis.
+// How C is cut into tiles (product_tiling): CTAs of a tile, its halves, rows of B and columns of C in it, splits of the long axis,
+// warps that end it.
 struct Tiling {
-    int ctas, halves, tile_n, cols, splits;
+    int ctas, halves, tile_n, cols, splits, end_warps;
+    int64_t parts() const { return end_warps / 4 * tiles_n; }      // of a row, that kLse leaves
     int64_t tiles_m, tiles_n;
 };
 
@@ -35,7 +37,7 @@ struct ProductArgs {
     int segments, batches;
     Tiling tiling;
     int act;                    // kGated
-    // kLse: [2 * tiles_n][m] partials; target[m], the logits of the targets.  kDlogits: target, lse, dloss, out.
+    // kLse: [end_warps / 4 * tiles_n][m] partials; target[m], the logits of the targets.  kDlogits: target, lse, dloss, out.
     float2 *part;
     float *target_logit;
     const int64_t *target;
