@@ -34,7 +34,7 @@ constexpr int kMostStages = 16;
 constexpr int kOutBytes = 4096;         // 32 rows of 64 bf16 on their way out, for each warp of the end
 constexpr int kShared = 1024 + ring_bytes(8) + 8 * kOutBytes;      // (either way)
 constexpr int kAccColumns = 256;        // of tensor memory for one accumulator; there are two
-constexpr int kLseRun = 16;             // stages after which the sums of a logit are taken out of the tensor cores
+constexpr int kLseRun = 8;              // stages after which the sums of a logit are taken out of the tensor cores
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Output {
@@ -348,8 +348,9 @@ __device__ __forceinline__ void end_gated(const Params &p, const Tile &t, int sh
 }
 
 // The logits of a warp's share of the tile, 32 columns of every 32 * kShare.  The tensor cores do not round their sums to nearest: a long one
-// comes out too small (the loss of 16384 positions of width 4096 was 2.5e-6 off; it is 6e-7 now, at the same speed).  So after every kLseRun stages
-// what they have is added here, rounded, and they begin anew, in the other accumulator.
+// comes out too small.  So after every kLseRun stages what they have is added here, rounded, and they begin anew, in the other
+// accumulator.  The loss of 16384 positions of width 4096: 2.5e-6 off without that, 6e-7 with runs of 16 stages, 2.8e-7 with 8, all at one speed; 1.4e-7
+// with 4, which takes 15 % longer.
 template <int kShare>
 struct Logits {
     static constexpr int kRuns = 16 / kShare;            // of 16 columns
