@@ -346,7 +346,8 @@ gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *args, v
  *     lse[r]  = log sum over v of exp(l[r][v]),     loss[r] = lse[r] - l[r][target[r]]
  * A negative target marks a position without one: its loss is 0 and its gradient too.  A target of `vocab` or more makes
  * the row's loss and gradient nan.  The logits stay fp32 and never reach memory.  A row
- * whose logits hold an inf or nan gets a lse and a loss that are not finite; other rows do not see it. */
+ * whose logits hold an inf or nan gets a lse and a loss that are not finite; other rows do not see it.  Scratch: 8 bytes for each
+ * tile of the vocabulary (tens to hundreds of columns) of up to 32768 positions, which are taken at a time. */
 typedef struct {
     const void    *h;            /* device, bf16 [rows][width]: the features                  */
     int64_t        rows, width, h_ld;
@@ -363,7 +364,9 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *args, void 
  * The logits are computed again, a piece of the vocabulary at a time; d of the piece lies in scratch, rounded to bf16 as the
  * products take it (relative to the mantissa of the first weight, so that the rounding is that of exp(l - lse) - 1 and not one
  * error that all positions share).  Sums are fp32, in a fixed order.  Where a target is negative, d is 0 whatever the logits are, but h has to be finite
- * there (dw adds 0 * h).  Scratch: up to 512 MB for d, and 4 bytes for each element of dh. */
+ * there (dw adds 0 * h).  Scratch: up to 512 MB for d (but 512 bytes a position at least); 4 bytes for each element of dh where the
+ * vocabulary takes more than one piece; and where few tiles are summed over a long axis, that axis is split, with 4 bytes for each
+ * element of dh or dw and each split (fewer splits times tiles than SMs: about 40 MB). */
 typedef struct {
     const float   *dloss;        /* device [rows]                                             */
     const void    *h;            /* device, bf16 [rows][width]                                */
@@ -398,7 +401,7 @@ typedef struct {
     int64_t     hidden, w_gate_ld, w_up_ld;
     int32_t     dtype;           /* gg_dtype of every matrix: GG_BF16                         */
     int32_t     act;             /* GG_ACT_*                                                  */
-    void       *h;               /* device [rows][hidden]                                     */
+    void       *h;               /* device [rows][hidden]; h, gate, up and x differ           */
     int64_t     h_ld;
     void       *gate, *up;       /* device [rows][hidden], each may be NULL (not wanted)      */
     int64_t     gate_ld, up_ld;

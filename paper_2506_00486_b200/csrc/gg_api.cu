@@ -2021,7 +2021,8 @@ gg_status gg_gated_linear(gg_ctx *ctx, const gg_gated_linear_args *a, void *stre
     if (st == GG_OK) st = check_bf16(a->h, a->rows, a->hidden, a->h_ld);
     if (st == GG_OK && a->gate) st = check_bf16(a->gate, a->rows, a->hidden, a->gate_ld);
     if (st == GG_OK && a->up) st = check_bf16(a->up, a->rows, a->hidden, a->up_ld);
-    if (st == GG_OK && a->rows > 0 && a->hidden > 0 && a->h == a->x) st = GG_ERR_INVALID_ARG;
+    if (st == GG_OK && a->rows > 0 && a->hidden > 0 && (a->h == a->x || (a->gate && (a->gate == a->x || a->gate == a->h || a->gate == a->up)) ||
+                                                        (a->up && (a->up == a->x || a->up == a->h)))) st = GG_ERR_INVALID_ARG;
     if (st != GG_OK) return st;
     if (a->rows == 0 || a->hidden == 0) return GG_OK;
     DeviceGuard guard(ctx->device);

@@ -275,3 +275,20 @@ def test_a_wait_that_runs_out_is_reported_and_leaves_the_context_usable(rows):
     grad = mine.gg_gated_linear_grad(dh, x, wg, wu, want["gate"], want["up"])
     assert all(torch.equal(again[k], want[k]) for k in want) and all(torch.equal(grad[k], wantg[k]) for k in wantg)
     mine.close()
+
+
+def test_outputs_that_are_one_another_are_refused(ctx):
+    # (the calls return before anything is launched)
+    from paper_2506_00486_b200 import GGError
+    x, wg, wu, _ = problem(11, 8, 16, 16)
+    run = ctx.make_gated_linear(x, wg, wu, keep=True)
+    before = ctx.launch_count
+    h, gate, up = (run.outputs[k].data_ptr() for k in ("h", "gate", "up"))
+    for change in (dict(gate=h), dict(up=h), dict(gate=up), dict(gate=x.data_ptr()), dict(up=x.data_ptr()), dict(h=x.data_ptr())):
+        now = dict(h=h, gate=gate, up=up) | change
+        for field, value in now.items():
+            setattr(run.args, field, value)
+        with pytest.raises(GGError) as e:
+            run()
+        assert e.value.status == 1
+    assert ctx.launch_count == before
