@@ -1133,7 +1133,11 @@ Divider divider(int d)
 // most, and a width is chosen that leaves the last round full: 517 rows against 32003 are 6 rounds of 3 x 126 tiles of 256 x 256, and 6 of
 // 3 x 143 of 224 columns, which are shorter (53.3 and 52.2 us; 128 columns 68.8).  Clocks of a stage of 64 summed elements for 128 rows, from a product of
 // 16384 x 4096 x 32000: 512 for 256 columns, 457 for 224, 421 for 192, 405 for 128, 302 for 64, 272 for 32; a single CTA, which brings in more bytes
-// for its products, takes 25 % longer (517 rows: 77 and 52 us), two halves of 256 rows, which bring in fewer, 7 % less.
+// for its products, takes 25 % longer (517 rows: 77 and 52 us), two halves of 256 rows, which bring in fewer, 7 % less.  The other figures (the end of
+// a tile, its turn, what a pair, sixteen warps and a split add) are those under which the choices lose the least against the fastest tiling of 248 products of
+// up to 2.5e11 multiplications: 1.4 % on average.  Where they are large: 247 x 80 x 25292 13.5 us with 176 columns of a single CTA, 24 with 64 of a pair;
+// dx of 700 x 640 x 1600 15.7 with 128 columns and four splits, 20.3 with 32 columns and none; a loss of 526 x 128 x 34071 22.7 with eight warps, 30.5 with narrower
+// tiles and sixteen.
 Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, int segments, int batches, bool may_split, int sm_count)
 {
     const int64_t stages = (k + kBlockK - 1) / kBlockK * segments;
@@ -1155,16 +1159,16 @@ Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, 
                 each = (stages + splits - 1) / splits;
             }
             const int64_t rounds = (tiles * splits + units - 1) / units;
-            // Sixteen warps for the end where the sums are short (loss of 526 x 128 x 34071: 31 us, with eight 52; 1000 x 256 x 50000: 38 and 42; the gradient of
-            // weights from 17 positions of width 1152: 25 and 30; but 300 x 512 x 30000 18.7 and 17.8, and longer sums more)
-            const int end_warps = end != kGated && halves == 1 && each <= 4 && m > 128 ? 16 : 8;
-            const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage;
-            const double store = (cols % 64 == 0 ? 15.0 : 20.0) * width * (end_warps == 16 ? 0.8 : 1.0);
-            double cost = rounds * ((main > store ? main : store) + 200.0) * halves + store;
-            if (splits > 1) cost += 4000.0 + (double)splits * batches * m * n * 8.0 / 3600.0;       // the sums of the splits, written and read
-            if (least == 0.0 || cost < least) {
-                least = cost;
-                best = Tiling{ctas, halves, width, cols, (int)splits, end_warps, tiles_m, tiles_n};
+            for (int end_warps = 8; end_warps <= 16; end_warps += 8) {
+                if (end_warps == 16 && (end == kGated || halves == 2 || each > 8 || m <= 128)) continue;
+                const double stage = (2.0 * width > 240.0 + width ? 2.0 * width : 240.0 + width) * factor, main = each * stage;
+                const double store = 6.5 * (cols % 64 == 0 ? 1.0 : 1.5) * (end_warps == 16 ? 0.75 : 1.0) * width + 450.0;
+                double cost = rounds * ((main > store ? main : store) + 200.0) * halves + store + (ctas == 2 ? 1500.0 : 0.0) + (end_warps == 16 ? 350.0 : 0.0);
+                if (splits > 1) cost += 600.0 + (double)splits * batches * m * n * 8.0 / 2500.0;       // the sums of the splits, written and read
+                if (least == 0.0 || cost < least) {
+                    least = cost;
+                    best = Tiling{ctas, halves, width, cols, (int)splits, end_warps, tiles_m, tiles_n};
+                }
             }
         }
     }
