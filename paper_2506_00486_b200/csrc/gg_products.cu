@@ -35,6 +35,7 @@ constexpr int kOutBytes = 4096;         // 32 rows of 64 bf16 on their way out, 
 constexpr int kShared = 1024 + ring_bytes(8) + 8 * kOutBytes;      // (either way)
 constexpr int kAccColumns = 256;        // of tensor memory for one accumulator; there are two
 constexpr int kLseRun = 8;              // stages after which the sums of a logit are taken out of the tensor cores
+constexpr int kLseOfOne = kStore + 1;       // kLse where the sum is one such run
 constexpr float kLog2e = 1.4426950408889634f;
 
 struct Output {
@@ -183,7 +184,7 @@ struct Tile {
     int width;           // its columns that C has
     int batch, sums, n_tile;      // sums: which of the fp32 matrices (kStore)
     uint32_t acc;        // its sums: tensor memory of the warp's lanes
-    // of this thread's row (kLse, kDlogits)
+    // of this thread's row (both ends of the loss, kDlogits)
     int64_t of;          // its target
     float lse, weight;
     __device__ __forceinline__ int target(int64_t first) const      // where in the tile that is, or -1
@@ -418,6 +419,55 @@ __device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int shar
         }
     const float2 s = halves(add2(sum[0], sum[1]));
     if (t.row < p.m) p.part[(int64_t)(kShare * t.n_tile + share) * p.m + t.row] = make_float2(most, s.x + s.y);
+}
+
+// The same for sums of one run: 32 columns at a time from tensor memory, a sum rescaled where the largest grows.  A tile of so few stages is
+// all end, and the end above, unrolled around its registers and run once a tile, is bound by the fetching of its instructions: 6909 x 64 x 50688 takes
+// 4560 clocks for a tile of 64 columns and 5600 for one of 256, this 2070 and 4250; with sixteen warps 4770 and 3750 for 256 (the
+// exponentials alone 2050).  The loss of 6909 x 64 x 50688 176 and 143 us, of 526 x 128 x 34071 22.7 and 19.3.
+template <int kShare>
+__device__ __forceinline__ void end_lse_of_one(const Params &p, const Tile &t, int share)
+{
+    const int target = t.target(p.first);
+    float most = -INFINITY, sum = 0.0f;
+#pragma unroll 1
+    for (int c = share * 32; c < t.width; c += 32 * kShare) {
+        f32x2 v[16];
+        read_pairs(t.acc + c, v);
+        const int left = t.width - c, at = target - c;
+        if (left < 32) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float2 x = halves(v[j]);
+                v[j] = pair(2 * j < left ? x.x : -INFINITY, 2 * j + 1 < left ? x.y : -INFINITY);
+            }
+        }
+        if ((unsigned)at < 32u) {
+            float x = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float2 y = halves(v[j]);
+                x = at == 2 * j ? y.x : at == 2 * j + 1 ? y.y : x;
+            }
+            p.target_logit[t.row] = x;
+        }
+        __syncwarp();
+        float top[4] = {most, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float2 x = halves(v[j]);
+            top[j & 3] = fmaxf(top[j & 3], fmaxf(x.x, x.y));
+        }
+        const float grown = fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])), from = grown == -INFINITY ? 0.0f : grown;
+        const f32x2 base = both(-from);
+        f32x2 part[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+        for (int j = 0; j < 16; ++j) part[j & 1] = add2(part[j & 1], power2(mul2(add2(v[j], base), both(kLog2e))));
+        const float2 s = halves(add2(part[0], part[1]));
+        sum = sum * power2((most - from) * kLog2e) + (s.x + s.y);
+        most = grown;
+    }
+    if (t.row < p.m) p.part[(int64_t)(kShare * t.n_tile + share) * p.m + t.row] = make_float2(most, sum);
 }
 
 template <int kShare>
@@ -704,7 +754,7 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
     } else if (warp >= 4) {
         // ---- ends (a lane quarter's warps share a tile's columns)
         const int share = (warp - 4) >> 2, quarter = warp & 3;
-        const Way way(ring + ring_bytes(kEndWarps) + (uint32_t)(warp - 4) * kOutBytes, lane);      // (kLse sends nothing)
+        const Way way(ring + ring_bytes(kEndWarps) + (uint32_t)(warp - 4) * kOutBytes, lane);      // (kLse and kLseOfOne send nothing)
         const float scale = (kEnd == kDlogits || kEnd == kStore) && p.dloss != nullptr ? weight_mantissa(p.dloss, p.target, p.positions) : 1.0f;
         uint32_t units = 0;
         for (int w = first; w < p.total && !failed; w += step) {
@@ -715,7 +765,7 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
             tile.batch = t.outer >= p.splits;
             tile.sums = t.outer;
             tile.n_tile = t.n_tile;
-            if constexpr (kEnd == kLse || kEnd == kDlogits) {      // (read while the tile is being summed)
+            if constexpr (kEnd == kLse || kEnd == kLseOfOne || kEnd == kDlogits) {      // (read while the tile is being summed)
                 const int64_t row = (int64_t)t.m_tile * 128 * kCtas + rank * 128 + quarter * 32 + lane;
                 tile.of = row < p.m ? p.target[row] : -1;
                 if constexpr (kEnd == kDlogits) {
@@ -737,6 +787,7 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
                 tile.acc = tmem + acc * kAccColumns + ((uint32_t)quarter << 21);      // (lane 32 * quarter, in the upper half of the word)
                 if constexpr (kEnd == kGated) end_gated(p, tile, share, way);
                 if constexpr (kEnd == kLse) logits.take(tile, share);
+                if constexpr (kEnd == kLseOfOne) end_lse_of_one<kShare>(p, tile, share);
                 if constexpr (kEnd == kDlogits) end_dlogits<kShare>(p, tile, share, way, scale);
                 if constexpr (kEnd == kStore) end_store<kShare>(p, tile, share, way, scale);
                 __syncwarp();
@@ -1136,8 +1187,7 @@ Divider divider(int d)
 // for its products, takes 25 % longer (517 rows: 77 and 52 us), two halves of 256 rows, which bring in fewer, 7 % less.  The other figures (the end of
 // a tile, its turn, what a pair, sixteen warps and a split add) are those under which the choices lose the least against the fastest tiling of 248 products of
 // up to 2.5e11 multiplications: 1.4 % on average.  Where they are large: 247 x 80 x 25292 13.5 us with 176 columns of a single CTA, 24 with 64 of a pair;
-// dx of 700 x 640 x 1600 15.7 with 128 columns and four splits, 20.3 with 32 columns and none; a loss of 526 x 128 x 34071 22.7 with eight warps, 30.5 with narrower
-// tiles and sixteen.
+// dx of 700 x 640 x 1600 15.7 with 128 columns and four splits, 20.3 with 32 columns and none; a loss of 526 x 128 x 34071 19 with 256 columns, with 128 a third more.
 Tiling product_tiling(ProductEnd end, bool bt, int64_t m, int64_t n, int64_t k, int segments, int batches, bool may_split, int sm_count)
 {
     const int64_t stages = (k + kBlockK - 1) / kBlockK * segments;
@@ -1260,7 +1310,8 @@ int64_t row_shared_bytes(int64_t k) { return (k + 511) / 512 * 512 * 2; }
 cudaError_t launch_product_rows(ProductEnd end, const ProductArgs &a, int sm_count, cudaStream_t st)
 {
     if (end == kGated) return launch_tiles<false, false, kGated>(a, sm_count, st);
-    if (end == kLse) return launch_tiles<false, false, kLse>(a, sm_count, st);
+    if (end == kLse)
+        return a.k <= kLseRun * kBlockK ? launch_tiles<false, false, kLseOfOne>(a, sm_count, st) : launch_tiles<false, false, kLse>(a, sm_count, st);
     if (end == kDlogits) return launch_tiles<false, false, kDlogits>(a, sm_count, st);
     return cudaErrorInvalidValue;
 }

@@ -301,3 +301,32 @@ def test_refusals(ctx):
         assert e.value.status == status, field
         setattr(run.args, field, keep)
     assert ctx.launch_count == before
+
+
+@pytest.mark.parametrize("width", [1, 64, 512, 513, 520, 1025])
+@pytest.mark.parametrize("shape", ["up", "down", "peak", "holes"])
+def test_logits_that_grow_along_the_vocabulary(ctx, width, shape):
+    # The largest logit moves through a tile's columns, and whole runs of columns are -infinity.  A sum is rescaled up to eight times on its
+    # way through a tile: each is an exponential, relative 4 U (step + 2), and the steps together are no more than the span.
+    vocab, rows = 700, 150
+    gen = torch.Generator(device="cuda").manual_seed(width)
+    l = torch.arange(vocab, device="cuda") / 16
+    l = {"up": l, "down": l.flip(0), "peak": (l - l[300]).abs().neg(), "holes": l.clone()}[shape].bfloat16()
+    if shape == "holes":
+        l[:96] = l[160:230] = l[512:] = -float("inf")
+    h, w = torch.zeros(rows, width, device="cuda").bfloat16(), torch.randn(vocab, width, generator=gen, device="cuda").bfloat16()
+    h[:, width // 2], w[:, width // 2] = 1.0, l
+    target = torch.randint(96, 160, (rows,), generator=gen, device="cuda")
+    target[::7] = -1
+    out = ctx.gg_cross_entropy(h, w, target)
+    x = host(l)
+    top = x.max()
+    lse = top + np.log(np.exp(x - top).sum())
+    p = np.exp(x - lse)
+    span = np.where(np.isinf(x), 0.0, np.abs(np.where(np.isinf(x), lse, x) - lse))
+    rel = (p * (8 * U * (span + 2) + 64 * U)).sum() + (64 + vocab / 256 + 1) * U
+    tol = rel + 4 * U * (abs(lse) + 1) + 4 * U * np.log(vocab + 1)
+    near(out["lse"], np.full(rows, lse), tol, "lse")
+    t = target.tolist()
+    want = np.array([0.0 if i < 0 else lse - x[i] for i in t])
+    near(out["loss"], want, tol + U * (abs(lse) + 2 * np.abs(x[np.maximum(t, 0)])), "loss")
