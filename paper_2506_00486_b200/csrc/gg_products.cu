@@ -591,6 +591,41 @@ __device__ __forceinline__ Work work_of(const Params &p, int w)
 }
 __device__ __forceinline__ int split_start(const Params &p, int split) { return split * p.each_k + (split < p.more_k ? split : p.more_k); }
 
+// What was started on its way to a CTA's shared memory, as the warps that started it leave it there for both CTAs of a pair.
+struct Started {
+    uint32_t failed;        // a wait ran out, in either CTA
+    uint32_t copied[2];     // stages that each CTA's copies were issued for (read in the first)
+    uint32_t used;          // stages that the products hand back
+    uint32_t ended[2];      // times that an accumulator was handed over
+};
+// A CTA may end only when nothing is under way to its shared memory any more.  Where every wait was met that is so: the copies
+// have been multiplied, the ends have waited for the accumulators and the copying warp for its stages.  Where one ran out, this waits for the copies, the
+// products and the arrivals that had been started, by the first two warps of each CTA; the second may have copied for more stages than the first.
+constexpr uint32_t kLeastPolls = 1 << 14;       // (8 ms or so, whatever the cap on waits is: a copy takes microseconds)
+template <int kCtas>
+__device__ __forceinline__ void settle(volatile const Started &was, int warp, uint32_t rank, uint32_t stages, uint32_t full, uint32_t empty, uint32_t done, uint32_t drained,
+                                       uint32_t polls)
+{
+    uint32_t left = polls / 16 > kLeastPolls ? polls / 16 : kLeastPolls;      // (for all of them together: they all started long ago)
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+        while (left > 0 && !barrier_test(bar, parity)) --left;
+    };
+    auto last_of = [&](uint32_t bars, uint32_t n) {
+        for (uint32_t i = n > stages ? n - stages : 0; i < n; ++i) wait(bars + 8 * (i % stages), (i / stages) & 1);
+    };
+    if (warp == 0) {
+        if (rank == 0) last_of(full, was.copied[0] > was.copied[1] ? was.copied[0] : was.copied[1]);
+        last_of(empty, was.used);
+    } else if (warp == 1) {
+        if (rank == 0 && elect_lane()) product_commit<kCtas>(drained);      // (the lane that issued the products)
+        __syncwarp();
+        wait(drained, 0);
+        for (uint32_t i = 0; i < 2; ++i)
+            if (was.ended[i] > 0) wait(done + 8 * i, (was.ended[i] - 1) & 1);
+    }
+    __syncwarp();
+}
+
 // kHalves 2: a pair's tile has 512 rows, as two halves of 256 with an accumulator each.  Otherwise the two accumulators take turns.
 template <int kCtas, int kHalves, bool kAT, bool kBT, int kEnd, int kEndWarps>
 __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const __grid_constant__ Params p)
@@ -599,6 +634,7 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
     extern __shared__ uint8_t shared_bytes[];
     __shared__ uint64_t bars[2 * kMostStages + 5];
     __shared__ uint32_t tmem_at;
+    __shared__ Started started;
 
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t rank = kCtas == 2 ? cluster_rank() : 0;
@@ -615,6 +651,7 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
             barrier_init(free_at + 8 * i, kEndWarps * kCtas);
         }
         barrier_init(drained, 1);
+        started = Started{};
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         prefetch_map(&p.a[0]);
         prefetch_map(&p.b[0]);
@@ -629,6 +666,7 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
 
     const int first = blockIdx.x / kCtas, step = gridDim.x / kCtas;
     bool failed = false;
+    auto leave = [&](const uint32_t &field, uint32_t value, uint32_t cta) { cluster_store(peer_address(shared_address(&field), cta), value); };
     // (a warp walks its loop as one, and one lane issues: so addresses and coordinates stay in uniform registers)
     if (warp == 0) {
         // ---- copies
@@ -672,18 +710,17 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
                 if (++stage == stages) { stage = 0; phase ^= 1; }
             }
         }
-        // what is still under way when a wait gave up has to land before the CTA may end
-        if (failed && rank == 0)
-            for (uint32_t i = 0; i < stages && i < issued; ++i) {
-                stage = stage == 0 ? stages - 1 : stage - 1;
-                if (stage == stages - 1) phase ^= 1;
-                barrier_wait(full + 8 * stage, phase, p.polls / 16 + 1);
-            }
+        if (leader) leave(started.copied[rank], issued, 0);
+        // the products hand every stage back, to both CTAs of a pair
+        for (uint32_t i = 0; i < stages && !failed; ++i) {
+            failed = !barrier_wait(empty + 8 * stage, phase ^ 1, p.polls);
+            if (++stage == stages) { stage = 0; phase ^= 1; }
+        }
     } else if (warp == 1 && rank == 0) {
         // ---- products
         const bool leader = elect_lane();
         const uint32_t shape = product_shape<128 * kCtas, kAT, kBT>(p.tile_n);
-        uint32_t stage = 0, phase = 0, units = 0;
+        uint32_t stage = 0, phase = 0, units = 0, used = 0, ended_first = 0, ended_second = 0;
         auto issue = [&](uint32_t at, uint32_t acc, bool fresh) {
             const uint64_t a = tile_descriptor<kAT>(ring + at * bytes + (kHalves == 2 ? acc * half_a : 0)), b = tile_descriptor<kBT>(ring + at * bytes + bytes_a);
             if (leader) {
@@ -710,9 +747,13 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
                         tmem_after_sync();
                         issue(stage, acc, kb == from);
                         commit(empty + 8 * stage);
+                        ++used;
                         if (++stage == stages) { stage = 0; phase ^= 1; }
                     }
-                    if (!failed) commit(done + 8 * acc);
+                    if (failed) break;
+                    commit(done + 8 * acc);
+                    ended_first += acc ^ 1;
+                    ended_second += acc;
                 }
             } else {
                 // Both accumulators belong to this tile.  At its start and its end a ring's worth of stages is taken for the first
@@ -733,23 +774,34 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
                         if (++at == stages) { at = 0; at_phase ^= 1; }
                     }
                     if (failed) break;
-                    if (last) commit(done);
+                    if (last) {
+                        commit(done);
+                        ++ended_first;
+                    }
                     if (head && !barrier_wait(free_at + 8, acc_phase ^ 1, p.polls)) { failed = true; break; }
                     tmem_after_sync();
                     for (int i = 0; i < run; ++i) {
                         issue(stage, 1, head && i == 0);
                         commit(empty + 8 * stage);
+                        ++used;
                         if (++stage == stages) { stage = 0; phase ^= 1; }
                     }
-                    if (last) commit(done + 8);
+                    if (last) {
+                        commit(done + 8);
+                        ++ended_second;
+                    }
                     kb += run;
                 }
                 ++units;
             }
         }
-        if (failed) {
-            commit(drained);
-            barrier_wait(drained, 0, p.polls);
+        if (leader) {
+#pragma unroll
+            for (int cta = 0; cta < kCtas; ++cta) {
+                leave(started.used, used, cta);
+                leave(started.ended[0], ended_first, cta);
+                leave(started.ended[1], ended_second, cta);
+            }
         }
     } else if (warp >= 4) {
         // ---- ends (a lane quarter's warps share a tile's columns)
@@ -798,12 +850,22 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
                 if (!failed) end_lse<kShare>(p, tile, share, logits);
         }
     }
-    if (failed && p.gave_up != nullptr) *reinterpret_cast<volatile uint32_t *>(p.gave_up) = 1;
-    __syncwarp();
-    tmem_before_sync();
-    if constexpr (kCtas == 2) cluster_sync();
-    else __syncthreads();
-    tmem_after_sync();
+    if (failed) {
+        for (int cta = 0; cta < kCtas; ++cta) leave(started.failed, 1, cta);
+        if (p.gave_up != nullptr) *reinterpret_cast<volatile uint32_t *>(p.gave_up) = 1;
+    }
+    auto meet = [&]() {
+        __syncwarp();
+        tmem_before_sync();
+        if constexpr (kCtas == 2) cluster_sync();
+        else __syncthreads();
+        tmem_after_sync();
+    };
+    meet();
+    if (*reinterpret_cast<volatile uint32_t *>(&started.failed) != 0) {
+        settle<kCtas>(started, warp, rank, stages, full, empty, done, drained, p.polls);
+        meet();
+    }
     if (warp == 2) tmem_free<kCtas>(tmem, 2 * kAccColumns);
 }
 

@@ -38,6 +38,7 @@ __device__ __forceinline__ uint32_t peer_address(uint32_t at, uint32_t rank)
     asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(at), "r"(rank));
     return d;
 }
+__device__ __forceinline__ void cluster_store(uint32_t at, uint32_t value) { asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(at), "r"(value) : "memory"); }
 __device__ __forceinline__ uint32_t cluster_rank()
 {
     uint32_t r;
