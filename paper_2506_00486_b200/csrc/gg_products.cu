@@ -831,7 +831,8 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
 #pragma unroll 1
             for (int h = 0; h < runs; ++h, ++units) {
                 const uint32_t acc = units & 1;
-                if (!barrier_wait(done + 8 * acc, units >> 1 & 1, p.polls)) { failed = true; break; }
+                // (tensor memory is read by whole warps: if one lane gave up, all do)
+                if (!__all_sync(~0u, barrier_wait(done + 8 * acc, units >> 1 & 1, p.polls))) { failed = true; break; }
                 __syncwarp();
                 tmem_after_sync();
                 tile.row0 = (int64_t)t.m_tile * 128 * kCtas * kHalves + (kHalves == 2 ? 256 * h : 0) + rank * 128 + quarter * 32;
