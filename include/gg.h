@@ -434,7 +434,10 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *arg
  * random bits are q * 65536 or more and q is p rounded to a multiple of 2^-16.  The bits are Philox4x32-10 at counter
  * (j mod 2^32, j div 2^32, t mod 2^32, tensor_id) and key `seed`, 128 bits for elements 8i .. 8i+7 of a row, j = row * ceil(cols / 8) + i
  * (the low half of a word first): whatever the strides and types, the same call makes the same mask.  So the gradient
- * is the same call on dy, without the residual.  A dropped element counts as 0 whatever it was, inf and nan included.  Arithmetic is fp32.
+ * is the same call on dy, without the residual.  gg_adamw_step counts by (j, t, segment index) and gg_sample by (i, attempt, tensor), so with one
+ * `seed` for all of them the bits that drop element e of tensor_id s in step t are those that round element e of segment s in step t, and in the first
+ * steps those that drew its initial value: give each of the three a seed of its own, or dropout tensor_ids from 2^31 on, which no segment index reaches.
+ * A dropped element counts as 0 whatever it was, inf and nan included.  Arithmetic is fp32.
  * y may be x or residual (the same address and ld).
  *   t_dev   device int64[1] or NULL: added to t (a captured graph advances it from replay to replay) */
 typedef struct {
@@ -482,7 +485,7 @@ gg_status gg_grad_norm(gg_ctx *ctx, const gg_seg *g, int32_t n_seg, gg_dtype dty
  * the state before the first step.  With 8-bit states 2^-126 is added to v before its root, which shows below
  * sqrt(v) = 2^-51 (4e-16; 2^-63 stands for 0): eps should be well above that.
  * The noise of the rounding is Philox4x32-10 at counter (j mod 2^32, j div 2^32, t mod 2^32, segment index) and key
- * `seed`, 128 bits for elements 8j .. 8j+7 of a segment: the same call gives the same bits. */
+ * `seed`, 128 bits for elements 8j .. 8j+7 of a segment: the same call gives the same bits (and so does gg_dropout with that seed: see there). */
 #define GG_ADAMW_BLOCK 256
 typedef struct {
     int32_t       n_seg;

@@ -24,6 +24,7 @@ HOOK_RESIDENT_MODE, HOOK_EXTRA_ARRIVALS, HOOK_WAIT_CAP, HOOK_CLUSTER_MODE = 0, 1
 BETA_LO, BETA_HI = 0.05, 20.0
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3}
 ADAMW_BLOCK = 256          # elements that share one scale of an 8-bit AdamW state
+DROPOUT_SEED = 1 << 32     # make_dropout's default: not make_adamw_step's, which would round by the bits that drop
 
 _SEG_DTYPE = np.dtype([("ptr", np.uint64), ("len", np.int64)])
 _P = ctypes.c_void_p
@@ -1003,12 +1004,13 @@ class Context:
         return ACTIVATIONS[act]
 
     # ----------------------------------------------------------------- dropout
-    def make_dropout(self, x, p, residual=None, out=None, seed=0, tensor_id=0, t_dev=None):
+    def make_dropout(self, x, p, residual=None, out=None, seed=DROPOUT_SEED, tensor_id=0, t_dev=None):
         """Dropout of the 2-D tensor x (rows may be strided) with a mask that is drawn, not stored.
 
         Returns drop(t), which enqueues y = [residual +] x * mask / (1 - p) and returns dict(y); y is allocated once unless
         `out` is given (it may be x or residual).  The mask depends on seed, tensor_id, t and the shape alone: the gradient is drop(t) of
-        another make_dropout on dy.  t_dev: an int64 device tensor of one value that is added to t, for captured graphs."""
+        another make_dropout on dy.  seed: another one than AdamW's and the sampler's, which draw from the same generator.  t_dev: an int64
+        device tensor of one value that is added to t, for captured graphs."""
         rows, cols = self._rows(x, "x")
         if residual is not None:
             self._rows(residual, "residual", x)

@@ -138,15 +138,21 @@ class Mlp:
         return x
 
 
+def draws(seed):
+    """The seeds of a decoder's initial weights, dropout masks and rounding: one generator serves all three, counted by tensor and
+    step, and with one seed it would round an update by the bits that dropped an element of the same number."""
+    return dict(weights=seed + (1 << 32), dropout=seed, rounding=seed + (2 << 32))
+
+
 class Decoder:
     """Token embedding, `layers` blocks x + dropout(W_down (silu(W_gate norm(x)) * W_up norm(x))), norm, output matrix; all bf16."""
 
     def __init__(self, ctx, layers, width, hidden, vocab, beta, p, seed):
         dev = ctx.device
-        self.ctx, self.layers, self.p, self.seed = ctx, layers, p, seed
+        self.ctx, self.layers, self.p, self.seed = ctx, layers, p, draws(seed)["dropout"]
         shapes = [s for _ in range(layers) for s in ((hidden, width), (hidden, width), (width, hidden))] + [(vocab, width)] * 2
         self.matrices = [torch.empty(s, dtype=torch.bfloat16, device=dev) for s in shapes]
-        ctx.gg_sample([m.view(-1) for m in self.matrices], [beta] * len(shapes), [gg_init_alpha(s[1], 2.0, beta) for s in shapes], seed)
+        ctx.gg_sample([m.view(-1) for m in self.matrices], [beta] * len(shapes), [gg_init_alpha(s[1], 2.0, beta) for s in shapes], draws(seed)["weights"])
         self.vectors = [f(width, dtype=torch.bfloat16, device=dev) for _ in range(layers + 1) for f in (torch.ones, torch.zeros)]
 
     @property
@@ -182,7 +188,7 @@ def stepper(ctx, model, bits, lam, seed):
 def train_tokens(ctx, bits=8, steps=200, lam=1e-6, lr=2e-3, layers=2, width=256, hidden=512, vocab=1000, batch=512, p=0.1, seed=1):
     """As train, for the decoder: every token has four successors, and a tenth of the positions has no target."""
     model = Decoder(ctx, layers, width, hidden, vocab, 1.0, p, seed)
-    params, penalty, step = stepper(ctx, model, bits, lam, seed)
+    params, penalty, step = stepper(ctx, model, bits, lam, draws(seed)["rounding"])
     gen = torch.Generator(device=ctx.device).manual_seed(seed)
     successors = torch.randint(0, vocab, (vocab, 4), generator=gen, device=ctx.device)
     losses, scales = [], []
