@@ -340,7 +340,12 @@ gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *args, v
  * scratch first.  Scratch is the context's: a call that needs more than any before it allocates, during a stream
  * capture too, and what it had stays until gg_destroy for graphs captured earlier.  Outputs may not overlap the operands.
  * The kernels wait for copies and for one another's warps inside a pair of CTAs; every such wait is bounded, and one that
- * ran out is reported by the next of these calls as GG_ERR_CUDA. */
+ * ran out is reported by the next of these calls, which then does nothing else, or by gg_product_status, as GG_ERR_CUDA. */
+
+/* GG_ERR_CUDA if a wait ran out in one of these kernels and nothing has reported it yet: what they wrote since the last report is not to be
+ * used.  A kernel leaves word as it ends, also in the replay of a graph, so this tells of those that have ended: after the last call of a step, synchronise
+ * and ask.  It enqueues nothing and does not wait. */
+gg_status gg_product_status(gg_ctx *ctx);
 
 /* Softmax cross entropy of a linear output layer, without its logits: with l = h w^T,
  *     lse[r]  = log sum over v of exp(l[r][v]),     loss[r] = lse[r] - l[r][target[r]]

@@ -197,12 +197,14 @@ def lib():
         L.gg_layer_norm_grad.argtypes = [_P, ctypes.POINTER(LayerNormGradArgs), _P]
         L.gg_grad_norm.argtypes = [_P, _P, i32, ctypes.c_int, d, _P, _P, _P]
         L.gg_adamw_step.argtypes = [_P, ctypes.POINTER(AdamwArgs), _P]
+        L.gg_product_status.argtypes = [_P]
         L.gg_cross_entropy.argtypes = [_P, ctypes.POINTER(CrossEntropyArgs), _P]
         L.gg_cross_entropy_grad.argtypes = [_P, ctypes.POINTER(CrossEntropyGradArgs), _P]
         L.gg_gated_linear.argtypes = [_P, ctypes.POINTER(GatedLinearArgs), _P]
         L.gg_gated_linear_grad.argtypes = [_P, ctypes.POINTER(GatedLinearGradArgs), _P]
         L.gg_dropout.argtypes = [_P, ctypes.POINTER(DropoutArgs), _P]
-        for name in ("gg_layer_norm", "gg_layer_norm_grad", "gg_grad_norm", "gg_adamw_step", "gg_cross_entropy", "gg_cross_entropy_grad",
+        for name in ("gg_layer_norm", "gg_layer_norm_grad", "gg_grad_norm", "gg_adamw_step", "gg_product_status", "gg_cross_entropy",
+                     "gg_cross_entropy_grad",
                      "gg_gated_linear", "gg_gated_linear_grad", "gg_dropout"):
             getattr(L, name).restype = ctypes.c_int
         L.gg_compression_ratio.argtypes = [d, d]
@@ -871,6 +873,11 @@ class Context:
         return self.make_adamw_step(w, g, m, v, **kw)(t, lr)
 
     # --------------------------------------------------------- vocabulary loss
+    def gg_product_status(self):
+        """Raises GGError if a wait ran out in a kernel of the vocabulary loss, the gated block or their gradients and nothing has
+        reported it: what they wrote is not to be used.  It tells of the kernels that have ended, so synchronise first."""
+        self._check(lib().gg_product_status(self._h))
+
     def make_cross_entropy(self, h, w, target):
         """Softmax cross entropy of the logits h @ w.t(), which are never stored.
 

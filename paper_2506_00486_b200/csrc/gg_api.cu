@@ -1843,7 +1843,7 @@ ProductArgs product_args(gg_ctx *ctx)
     return p;
 }
 
-// A wait that ran out in an earlier call is this call's error: its results were not finished.
+// A wait that ran out in an earlier call, whose results were not finished.
 gg_status product_alive(gg_ctx *ctx)
 {
     volatile uint32_t *word = ctx->gave_up;
@@ -1876,6 +1876,8 @@ gg_status zero_matrix(gg_ctx *ctx, void *p, int64_t rows, int64_t cols, int64_t 
 }  // namespace
 
 extern "C" {
+
+gg_status gg_product_status(gg_ctx *ctx) { return ctx ? product_alive(ctx) : GG_ERR_INVALID_ARG; }
 
 gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *a, void *stream)
 {

@@ -203,6 +203,8 @@ def train_tokens(ctx, bits=8, steps=200, lam=1e-6, lr=2e-3, layers=2, width=256,
         penalty()
         scales.append(step(t, lr)["scale"].clone())
         losses.append(loss.detach())
+    torch.cuda.synchronize(ctx.device)
+    ctx.gg_product_status()
     return torch.stack(losses), torch.cat(scales), penalty.outputs["beta"].clone()
 
 

@@ -82,3 +82,47 @@ def test_gated_block_and_gradient(rows, width, hidden, forms):
     args = (dh, x, wg, wu, gate, up)
     runs = [("gg_gated_linear_grad", args, {}), ("gg_gated_linear_grad", args, dict(want_dx=False)), ("gg_gated_linear_grad", args, dict(want_dweight=False))]
     check(([("gg_gated_linear", (x, wg, wu), dict(keep=True))] if rows > 1 else []) + runs)
+
+
+def small_problem():
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    return matrix(gen, 200, 136), *(matrix(gen, 300, 136, scale=0.1) for _ in range(2))
+
+
+def test_it_can_be_asked_for():
+    from paper_2506_00486_b200 import Context, GGError
+    mine, args = Context(0), small_problem()
+    want = mine.gg_gated_linear(*args, keep=True)
+    torch.cuda.synchronize()
+    mine.gg_product_status()
+    stuck(mine, True)
+    mine.gg_gated_linear(*args, keep=True)
+    torch.cuda.synchronize()
+    stuck(mine, False)
+    with pytest.raises(GGError, match="ran out") as e:
+        mine.gg_product_status()
+    assert e.value.status == 6
+    mine.gg_product_status()                # (told once)
+    assert same(mine.gg_gated_linear(*args, keep=True), want)
+    mine.close()
+
+
+def test_replays_of_a_graph_can_be_asked_about():
+    from paper_2506_00486_b200 import Context, GGError
+    mine, args = Context(0), small_problem()
+    run = mine.make_gated_linear(*args)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    stuck(mine, True)
+    with torch.cuda.graph(graph):
+        run()
+    stuck(mine, False)
+    mine.gg_product_status()                # (captured, not run)
+    for _ in range(2):
+        graph.replay()
+        torch.cuda.synchronize()
+        with pytest.raises(GGError, match="ran out"):
+            mine.gg_product_status()
+    mine.gg_product_status()
+    del graph
+    mine.close()
