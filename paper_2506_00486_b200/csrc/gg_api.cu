@@ -1861,7 +1861,7 @@ gg_status store_weights(gg_ctx *ctx, ProductArgs &q, bool add, cudaStream_t st)
     GG_CUDA(ctx, launch_product_dweight(q, ctx->sm_count, st));
     ctx->launches += 1;
     for (int i = 0; splits > 1 && i < q.batches; ++i) {
-        GG_CUDA(ctx, launch_sum_splits(q.f32 + (int64_t)i * splits * q.m * q.f32_ld, splits, q.m, q.n, q.f32_ld, q.out[i], q.out_ld[i], q.dloss, q.target, q.positions, add, st));
+        GG_CUDA(ctx, launch_sum_splits(q.f32 + (int64_t)i * splits * q.m * q.f32_ld, splits, q.m, q.n, q.f32_ld, q.out[i], q.out_ld[i], q.scale, add, st));
         ctx->launches += 1;
     }
     return GG_OK;
@@ -1961,6 +1961,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
     const int64_t f32_at = s.place(a->dh && (splits > 1 || n_pieces > 1) ? 4 * (int64_t)splits * a->rows * f32_ld : 0);
     const int64_t sums[2] = {cuts[1][0].splits > 1 ? cuts[1][0].splits * piece : 0, cuts[1][1].splits > 1 ? cuts[1][1].splits * last : 0};
     const int64_t f32w_at = s.place(4 * std::max(sums[0], sums[1]) * f32_ld);
+    const int64_t scale_at = s.place(4);
     if ((st = s.grow()) != GG_OK || (st = lay(s, {&h, &w})) != GG_OK) return st;
     for (int64_t i = 0; i < n_pieces; ++i) {
         const int64_t first = i * piece, n = std::min(piece, a->vocab - first);
@@ -1970,7 +1971,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
         p.b[0] = rows_of_w;
         p.m = a->rows; p.n = n; p.k = a->width;
         p.target = a->target; p.vocab = a->vocab; p.first = first;
-        p.lse = a->lse; p.dloss = a->dloss; p.positions = a->rows;
+        p.lse = a->lse; p.dloss = a->dloss; p.positions = a->rows; p.scale = s.at<float>(scale_at);
         p.out[0] = s.at<uint16_t>(d_at);
         p.out_ld[0] = piece;
         p.tiling = cuts[0][n != piece];
@@ -2005,8 +2006,8 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
         }
     }
     if (a->dh && splits > 1) {
-        GG_CUDA(ctx, launch_sum_splits(s.at<float>(f32_at), splits, a->rows, a->width, f32_ld, static_cast<uint16_t *>(a->dh), a->dh_ld, a->dloss, a->target,
-                                       a->rows, false, s.st));
+        GG_CUDA(ctx, launch_sum_splits(s.at<float>(f32_at), splits, a->rows, a->width, f32_ld, static_cast<uint16_t *>(a->dh), a->dh_ld, s.at<float>(scale_at),
+                                       false, s.st));
         ctx->launches += 1;
     }
     return GG_OK;
@@ -2114,7 +2115,7 @@ gg_status gg_gated_linear_grad(gg_ctx *ctx, const gg_gated_linear_grad_args *a, 
         GG_CUDA(ctx, launch_product_drows(q, ctx->sm_count, s.st));
         ctx->launches += 1;
         if (splits > 1) {
-            GG_CUDA(ctx, launch_sum_splits(q.f32, splits, a->rows, a->width, f32_ld, q.out[0], a->dx_ld, nullptr, nullptr, 0, false, s.st));
+            GG_CUDA(ctx, launch_sum_splits(q.f32, splits, a->rows, a->width, f32_ld, q.out[0], a->dx_ld, nullptr, false, s.st));
             ctx->launches += 1;
         }
     }

@@ -68,6 +68,7 @@ struct Params {
     int64_t vocab, first;
     const float *lse, *dloss;
     int64_t positions;
+    float *scale;
     float *f32;
     int64_t f32_ld;
     int mode;
@@ -279,11 +280,11 @@ struct Way {
 // The weights of the positions are mostly one number, 1 / their count, and d = weight * (p - 1) is then mostly that number too: rounded
 // to bf16 it may be off by 2^-8 in all of them alike (the gradient of 33 positions: 0.4 % off as a whole).  So d is kept relative to the
 // mantissa, 1 .. 2, of the first weight that is not 0, and the sums are multiplied by it: p - 1 itself is rounded (0.2 %, and
-// no longer alike).  A whole warp asks; only so many rows are looked at, 256 at once (a padded batch may begin without any), beyond them it is 1.
+// no longer alike).  A whole warp asks, 256 rows at once (a padded batch may begin without any); the products that sum d are told.
 __device__ __forceinline__ float weight_mantissa(const float *dloss, const int64_t *target, int64_t rows)
 {
     const int lane = threadIdx.x & 31;
-    for (int64_t r = 0; r < rows && r < 4096; r += 256) {
+    for (int64_t r = 0; r < rows; r += 256) {
         float g[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -807,7 +808,13 @@ __global__ void __launch_bounds__(32 * (4 + kEndWarps), 1) product_kernel(const 
         // ---- ends (a lane quarter's warps share a tile's columns)
         const int share = (warp - 4) >> 2, quarter = warp & 3;
         const Way way(ring + ring_bytes(kEndWarps) + (uint32_t)(warp - 4) * kOutBytes, lane);      // (kLse and kLseOfOne send nothing)
-        const float scale = (kEnd == kDlogits || kEnd == kStore) && p.dloss != nullptr ? weight_mantissa(p.dloss, p.target, p.positions) : 1.0f;
+        float scale = 1.0f;
+        if constexpr (kEnd == kDlogits) {
+            scale = weight_mantissa(p.dloss, p.target, p.positions);
+            if (blockIdx.x == 0 && warp == 4 && lane == 0) *p.scale = scale;
+        }
+        if constexpr (kEnd == kStore)
+            if (p.scale != nullptr) scale = *p.scale;
         uint32_t units = 0;
         for (int w = first; w < p.total && !failed; w += step) {
             const Work t = work_of(p, w);
@@ -1024,14 +1031,14 @@ __global__ void __launch_bounds__(1024) lse_finish_kernel(const float2 *part, in
 // A thread for four columns; or, where there are many splits, kParts of them, which take every kParts-th split and are added in order.
 template <int kParts>
 __global__ void __launch_bounds__(256) sum_splits_kernel(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld,
-                                                         const float *dloss, const int64_t *target, int64_t positions, int add)
+                                                         const float *scale_of, int add)
 {
     constexpr int kRuns = 256 / kParts;
     __shared__ float4 of[kParts][kRuns];
     const int64_t groups = (cols + 3) / 4;
     const int lane = threadIdx.x % kRuns, part = threadIdx.x / kRuns;
     wait_for_the_one_before();
-    const float scale = dloss != nullptr ? weight_mantissa(dloss, target, positions) : 1.0f;
+    const float scale = scale_of != nullptr ? *scale_of : 1.0f;
     for (int64_t first = blockIdx.x * (int64_t)kRuns; first < groups * rows; first += gridDim.x * (int64_t)kRuns) {
         const int64_t i = first + lane, row = i / groups, col = (i - row * groups) * 4;
         float4 s = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -1324,7 +1331,7 @@ cudaError_t launch_product(const ProductArgs &a, int sm_count, cudaStream_t st)
     if (p.stages > kMostStages) p.stages = kMostStages;
     p.act = a.act;
     p.part = a.part; p.target_logit = a.target_logit; p.target = a.target; p.vocab = a.vocab; p.first = a.first;
-    p.lse = a.lse; p.dloss = a.dloss; p.positions = a.positions;
+    p.lse = a.lse; p.dloss = a.dloss; p.positions = a.positions; p.scale = a.scale;
     p.f32 = a.f32; p.f32_ld = a.f32_ld; p.mode = a.mode; p.gave_up = a.gave_up;
     // (the longest wait, for the sums of a tile, grows with the stages: about 0.3 us each)
     const int64_t polls = (int64_t)(1 << 22) + 8 * (int64_t)p.all_k;
@@ -1404,12 +1411,12 @@ cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, cons
     return launch_after(st, dim3((unsigned)((rows + each - 1) / each)), 1024, 0, lse_finish_kernel, part, n_part, rows, each, target_logit, target, vocab, lse, loss);
 }
 
-cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *dloss,
-                              const int64_t *target, int64_t positions, bool add, cudaStream_t st)
+cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *scale,
+                              bool add, cudaStream_t st)
 {
     const int64_t threads = (cols + 3) / 4 * rows;
-    if (splits < 8) return launch_after(st, dim3(grid_of(threads)), 256, 0, sum_splits_kernel<1>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target, positions, (int)add);
-    return launch_after(st, dim3(grid_of(threads * 8)), 256, 0, sum_splits_kernel<8>, f32, splits, rows, cols, f32_ld, out, out_ld, dloss, target, positions, (int)add);
+    if (splits < 8) return launch_after(st, dim3(grid_of(threads)), 256, 0, sum_splits_kernel<1>, f32, splits, rows, cols, f32_ld, out, out_ld, scale, (int)add);
+    return launch_after(st, dim3(grid_of(threads * 8)), 256, 0, sum_splits_kernel<8>, f32, splits, rows, cols, f32_ld, out, out_ld, scale, (int)add);
 }
 
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,

@@ -43,8 +43,9 @@ struct ProductArgs {
     const int64_t *target;
     int64_t vocab;              // targets count from 0 to vocab - 1 ...
     int64_t first;              // ... and this call's columns begin there
-    const float *lse, *dloss;   // (kStore: sums of kDlogits' numbers; null: of others)
+    const float *lse, *dloss;
     int64_t positions;          // entries of target and dloss
+    float *scale;               // what kDlogits' numbers are relative to: it leaves it here, kStore multiplies its sums by it (null: 1)
     // kGated: h, gate, up (each of the last two may be null); kDlogits: out[0]; kStore: of a batch
     uint16_t *out[3];
     int64_t out_ld[3];
@@ -81,9 +82,9 @@ cudaError_t launch_realign(Copies c, cudaStream_t st);
 // lse and loss of a row from its partials; a negative target has loss 0, one beyond the vocabulary NaN
 cudaError_t launch_lse_finish(const float2 *part, int n_part, int64_t rows, const float *target_logit, const int64_t *target, int64_t vocab, float *lse,
                               float *loss, cudaStream_t st);
-// out = bf16 of the sum of `splits` fp32 matrices (dloss, target, positions as in ProductArgs), and of what is there with `add`
-cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *dloss,
-                              const int64_t *target, int64_t positions, bool add, cudaStream_t st);
+// out = bf16 of the sum of `splits` fp32 matrices (scale as in ProductArgs), and of what is there with `add`
+cudaError_t launch_sum_splits(const float *f32, int splits, int64_t rows, int64_t cols, int64_t f32_ld, uint16_t *out, int64_t out_ld, const float *scale,
+                              bool add, cudaStream_t st);
 // dgate = dh * up * act'(gate), dup = dh * act(gate)
 cudaError_t launch_gated_slopes(const Bf16Matrix &dh, const Bf16Matrix &gate, const Bf16Matrix &up, int act, uint16_t *dgate, uint16_t *dup, int64_t ld,
                                 cudaStream_t st);
