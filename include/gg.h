@@ -337,8 +337,10 @@ gg_status gg_layer_norm_grad(gg_ctx *ctx, const gg_layer_norm_grad_args *args, v
 
 /* The operators around matrix products that follow take their operands in bf16 (what the tensor cores multiply; gg_adamw_step keeps
  * such a copy of fp32 weights) and sum in fp32.  A matrix whose rows do not all start on a 16-byte boundary is copied into
- * scratch first.  Scratch is the context's: a call that needs more than any before it allocates, during a stream
- * capture too, and what it had stays until gg_destroy for graphs captured earlier.  Outputs may not overlap the operands.
+ * scratch first (2 bytes an element: 1.2 GB for weights of 151936 x 4096).  Scratch is the context's: a call that needs more than any before it
+ * allocates, during a stream capture too, and what it had stays until gg_destroy for graphs captured earlier.  It allocates twice
+ * what there was, from 64 MB on a quarter more, or what it needs if that is more or the rest does not fit: a context that needed 500 MB and then
+ * 510 holds 500 + 625.  Outputs may not overlap the operands.
  * The kernels wait for copies and for one another's warps inside a pair of CTAs; every such wait is bounded, and one that
  * ran out is reported by the next of these calls, which then does nothing else, or by gg_product_status, as GG_ERR_CUDA. */
 
@@ -351,8 +353,8 @@ gg_status gg_product_status(gg_ctx *ctx);
  *     lse[r]  = log sum over v of exp(l[r][v]),     loss[r] = lse[r] - l[r][target[r]]
  * A negative target marks a position without one: its loss is 0 and its gradient too.  A target of `vocab` or more makes
  * the row's loss and gradient nan.  The logits stay fp32 and never reach memory.  A row
- * whose logits hold an inf or nan gets a lse and a loss that are not finite; other rows do not see it.  Scratch: 8 bytes for each
- * tile of the vocabulary (tens to hundreds of columns) of up to 32768 positions, which are taken at a time. */
+ * whose logits hold an inf or nan gets a lse and a loss that are not finite; other rows do not see it.  Scratch, for each of up to 32768
+ * positions, which are taken at a time: 16 or 32 bytes for each tile of the vocabulary (tens to hundreds of columns), and 4. */
 typedef struct {
     const void    *h;            /* device, bf16 [rows][width]: the features                  */
     int64_t        rows, width, h_ld;

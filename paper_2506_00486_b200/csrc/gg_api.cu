@@ -96,9 +96,9 @@ struct gg_ctx {
     void *product_buf = nullptr;  // scratch of the vocabulary loss, the gated block and their gradients
     int64_t product_bytes = 0;
     uint32_t *gave_up = nullptr;  // pinned host word that a product kernel sets when one of its waits runs out
-    // scratch that was outgrown: kept until the end, because a captured graph may hold its address.  Each buffer is at most half of the
-    // one that replaced it, so that all of them together are less than what is in use, and there are never so many of them.
-    void *outgrown[192] = {};
+    // scratch that was outgrown: kept until the end, because a captured graph may hold its address.  Buffers below 64 MB are at most half of
+    // the one that replaced them, larger ones four fifths (grow_kept), so that there are never so many of them.
+    void *outgrown[512] = {};
     int n_outgrown = 0;
     uint32_t *norm_ticket = nullptr;    // counter of gg_grad_norm's one-launch form (zero between calls)
     double *seed = nullptr;       // device table that seeds the moment-ratio inversion of the short-segment kernel
@@ -459,12 +459,20 @@ void keep(gg_ctx *ctx, void *outgrown)
 gg_status grow_kept(gg_ctx *ctx, void **buf, int64_t *have, int64_t need)
 {
     if (need <= *have) return GG_OK;
-    const int64_t bytes = std::max(need, 2 * *have);
+    // more than is needed, so that a need that creeps up does not allocate each time: twice what there was, a quarter more of what is large
+    const int64_t bytes = std::max(need, *have < (64ll << 20) ? 2 * *have : *have + *have / 4);
     void *p = nullptr;
-    GG_CUDA(ctx, cudaMalloc(&p, (size_t)bytes));
+    cudaError_t e = cudaMalloc(&p, (size_t)bytes);
+    if (e == cudaErrorMemoryAllocation && bytes > need) {
+        cudaGetLastError();
+        e = cudaMalloc(&p, (size_t)need);
+        if (e == cudaSuccess) *have = need;
+    } else if (e == cudaSuccess) {
+        *have = bytes;
+    }
+    GG_CUDA(ctx, e);
     keep(ctx, *buf);
     *buf = p;
-    *have = bytes;
     return GG_OK;
 }
 
