@@ -1367,7 +1367,8 @@ cudaError_t launch_tiles(const ProductArgs &a, int sm_count, cudaStream_t st)
 {
     if constexpr (kEnd == kStore)
         if (a.tiling.halves == 2) return launch_product<2, 2, kAT, kBT, kEnd, 8>(a, sm_count, st);
-    if constexpr (kEnd != kGated)
+    // (kLse has more than eight stages a tile)
+    if constexpr (kEnd != kGated && kEnd != kLse)
         if (a.tiling.end_warps == 16)
             return a.tiling.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd, 16>(a, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd, 16>(a, sm_count, st);
     return a.tiling.ctas == 2 ? launch_product<2, 1, kAT, kBT, kEnd, 8>(a, sm_count, st) : launch_product<1, 1, kAT, kBT, kEnd, 8>(a, sm_count, st);
