@@ -45,8 +45,10 @@ def test_pieces_of_the_vocabulary_cover_it_and_fit():
 
 def test_shapes_of_the_forms_that_are_tested_on_the_device():
     # (the tests there assert the same: this one tells without a device that the rule has moved a shape to another form)
+    import test_gpu_product_forms as values
     import test_gpu_product_waits as waits
-    for rows, width, vocab, forms in waits.LOSS:
+    for rows, width, vocab, forms in waits.LOSS + values.LOSS:
         assert forms.items() <= loss_forms(rows, width, vocab).items(), (rows, width, vocab)
-    for rows, width, hidden, forms in waits.GATED:
+    for rows, width, hidden, forms in waits.GATED + values.GATED:
         assert forms.items() <= gated_forms(rows, width, hidden).items(), (rows, width, hidden)
+    values.test_no_form_is_left_out()
