@@ -11,7 +11,8 @@ weights is fitted and its gradient added to the loss's (gg_fused), and the step 
 weights with 32- or 8-bit states (gg_grad_norm, gg_adamw_step).
 
 A backward pass through the autograd forms below may be captured into a graph like any other of torch: with leaves whose eager graphs
-are gone, since torch ties their gradients to the stream that first made them.  Context's make_* calls have no such tie.
+are gone, since torch ties their gradients to the stream that first made them.  Context's make_* calls have no such tie.  Dropout in such
+a step takes its counter from the device.
 """
 import argparse
 
@@ -102,17 +103,26 @@ class CrossEntropy(torch.autograd.Function):
 class Dropout(torch.autograd.Function):
     """residual + dropout of x (residual may be None) over the last dimension for autograd; the mask is drawn again for the gradient.
 
-    Dropout.apply(x, residual, p, ctx, seed, t, tensor_id): seed, step t and tensor_id as in Context.make_dropout.  Its gradient cannot be
-    differentiated again."""
+    Dropout.apply(x, residual, p, ctx, seed, t, tensor_id): seed, step t and tensor_id as in Context.make_dropout.  A graph keeps a t that is a
+    number, and every replay draws one mask: a step that is captured takes an int64 device tensor of one value for t and advances it
+    after its backward pass.  Its gradient cannot be differentiated again."""
 
     @staticmethod
     def forward(fctx, x, residual, p, ctx, seed, t, tensor_id):
-        fctx.draw = lambda v, r=None: ctx.gg_dropout(_matrix(v), p, t, residual=None if r is None else _matrix(r), seed=seed, tensor_id=tensor_id)["y"].view(v.shape)
-        return fctx.draw(x, residual)
+        t_dev = t if isinstance(t, torch.Tensor) else None
+
+        def draw(v, r=None):
+            return ctx.gg_dropout(_matrix(v), p, t if t_dev is None else 0, residual=None if r is None else _matrix(r), seed=seed, tensor_id=tensor_id,
+                                  t_dev=t_dev)["y"].view(v.shape)
+
+        fctx.draw = draw
+        fctx.save_for_backward(t_dev)
+        return draw(x, residual)
 
     @staticmethod
     @once_differentiable
     def backward(fctx, dy):
+        fctx.saved_tensors       # (raises if the step has been advanced since: this would be another mask)
         return fctx.draw(dy) if fctx.needs_input_grad[0] else None, dy if fctx.needs_input_grad[1] else None, None, None, None, None, None
 
 
