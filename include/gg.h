@@ -352,8 +352,9 @@ gg_status gg_product_status(gg_ctx *ctx);
 /* Softmax cross entropy of a linear output layer, without its logits: with l = h w^T,
  *     lse[r]  = log sum over v of exp(l[r][v]),     loss[r] = lse[r] - l[r][target[r]]
  * A negative target marks a position without one: its loss is 0 and its gradient too.  A target of `vocab` or more makes
- * the row's loss and gradient nan.  The logits stay fp32 and never reach memory.  A row
- * whose logits hold an inf or nan gets a lse and a loss that are not finite; other rows do not see it.  Scratch, for each of up to 32768
+ * the row's loss and dh nan, and all of dw, which sums over the rows.  The logits stay fp32 and never reach memory.  A row
+ * with a logit of +inf or nan, or with nothing but -inf, gets a lse and a loss that are not finite; a logit of -inf beside finite ones
+ * counts as 0.  Other rows see none of it (dw does).  Scratch, for each of up to 32768
  * positions, which are taken at a time: 16 or 32 bytes for each tile of the vocabulary (tens to hundreds of columns), and 4. */
 typedef struct {
     const void    *h;            /* device, bf16 [rows][width]: the features                  */
@@ -369,9 +370,11 @@ gg_status gg_cross_entropy(gg_ctx *ctx, const gg_cross_entropy_args *args, void 
 /* Its gradient for dloss = dL/dloss and the lse that gg_cross_entropy wrote.  With
  *     d[r][v] = dloss[r] (exp(l[r][v] - lse[r]) - [v = target[r]]):     dh = d w,     dw = d^T h
  * The logits are computed again, a piece of the vocabulary at a time; d of the piece lies in scratch, rounded to bf16 as the
- * products take it (relative to the mantissa of the first weight, so that the rounding is that of exp(l - lse) - 1 and not one
- * error that all positions share).  Sums are fp32, in a fixed order.  Where a target is negative, d is 0 whatever the logits are, but h has to be finite
- * there (dw adds 0 * h).  Scratch: up to 512 MB for d (but 512 bytes a position at least); 4 bytes for each element of dh where the
+ * products take it (relative to the mantissa of the first weight that is not 0, so that the rounding is that of exp(l - lse) - 1 and not one
+ * error that all positions share).  Sums are fp32, in a fixed order; here, as in the gated block, the tensor cores hold them from the first product to
+ * the last (they do not round to nearest), while gg_cross_entropy takes its logits out every 512 products: so exp(l - lse) is of logits that differ by
+ * some 1e-6 of themselves from those behind lse, well below the rounding of d.  Where a target is negative, d is 0 whatever the logits are, but h has to be finite
+ * there (dw adds 0 * h).  Scratch, besides copies of operands off the boundary: up to 512 MB for d (but 512 bytes a position at least); 4 bytes for each element of dh where the
  * vocabulary takes more than one piece; and where few tiles are summed over a long axis, that axis is split, with 4 bytes for each
  * element of dh or dw and each split (fewer splits times tiles than SMs: about 40 MB). */
 typedef struct {

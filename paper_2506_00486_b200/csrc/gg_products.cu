@@ -44,7 +44,8 @@ struct Output {
     int whole;           // every row starts on a 16-byte boundary
 };
 
-// n / d for 0 <= n < 2^31 without a division (five of them stand in the path of each tile otherwise): mul is
+// n / d for 0 <= n < 2^31 without a division (five of them stand in the path of each tile otherwise), as Granlund and Montgomery
+// divide by invariant integers (1994): mul is
 // 2^(32 + shift) / d rounded up, and the error of that stays below 1 / d as 2^(31 + ceil(log2 d)) / d has 32 bits.
 struct Divider {
     uint32_t d, mul, shift;
@@ -423,9 +424,9 @@ __device__ __forceinline__ void end_lse(const Params &p, const Tile &t, int shar
 }
 
 // The same for sums of one run: 32 columns at a time from tensor memory, a sum rescaled where the largest grows.  A tile of so few stages is
-// all end, and the end above, unrolled around its registers and run once a tile, is bound by the fetching of its instructions: 6909 x 64 x 50688 takes
-// 4560 clocks for a tile of 64 columns and 5600 for one of 256, this 2070 and 4250; with sixteen warps 4770 and 3750 for 256 (the
-// exponentials alone 2050).  The loss of 6909 x 64 x 50688 176 and 143 us, of 526 x 128 x 34071 22.7 and 19.3.
+// all end, and the end above, unrolled around its registers and run once a tile, is bound by the fetching of its instructions: in a build that read
+// the clock around it, 6909 x 64 x 50688 took 4560 clocks for a tile of 64 columns and 5600 for one of 256, this 2070 and 4250; with sixteen warps
+// 4770 and 3750 for 256 (the exponentials alone 2050).  The loss of 6909 x 64 x 50688 176 and 143 us, of 526 x 128 x 34071 22.7 and 19.3.
 template <int kShare>
 __device__ __forceinline__ void end_lse_of_one(const Params &p, const Tile &t, int share)
 {
@@ -914,6 +915,8 @@ __global__ void __launch_bounds__(256) realign_kernel(const Copies c)
     }
 }
 
+// dgate and dup are rounded to bf16, because the products that follow multiply bf16: the gradients are 0.23 % off in the 2-norm where fp32 operands would
+// leave the rounding of the result, 0.17 %, at two or three times the products.
 // Eight columns a thread, two of them under way, where every row starts on a 16-byte boundary ...
 template <int kAct>
 __global__ void __launch_bounds__(256) gated_slopes_kernel(const Bf16Matrix dh, const Bf16Matrix gate, const Bf16Matrix up, uint16_t *dgate, uint16_t *dup,
