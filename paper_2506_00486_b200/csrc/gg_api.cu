@@ -1979,7 +1979,7 @@ gg_status gg_cross_entropy_grad(gg_ctx *ctx, const gg_cross_entropy_grad_args *a
         p.b[0] = rows_of_w;
         p.m = a->rows; p.n = n; p.k = a->width;
         p.target = a->target; p.vocab = a->vocab; p.first = first;
-        p.lse = a->lse; p.dloss = a->dloss; p.positions = a->rows; p.scale = s.at<float>(scale_at);
+        p.lse = a->lse; p.dloss = a->dloss; p.positions = i == 0 ? a->rows : 0; p.scale = s.at<float>(scale_at);
         p.out[0] = s.at<uint16_t>(d_at);
         p.out_ld[0] = piece;
         p.tiling = cuts[0][n != piece];

@@ -44,7 +44,7 @@ struct ProductArgs {
     int64_t vocab;              // targets count from 0 to vocab - 1 ...
     int64_t first;              // ... and this call's columns begin there
     const float *lse, *dloss;
-    int64_t positions;          // entries of target and dloss
+    int64_t positions;          // entries of target and dloss to look for `scale` in (0: it is there)
     float *scale;               // what kDlogits' numbers are relative to: it leaves it here, kStore multiplies its sums by it (null: 1)
     // kGated: h, gate, up (each of the last two may be null); kDlogits: out[0]; kStore: of a batch
     uint16_t *out[3];

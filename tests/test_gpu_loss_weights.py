@@ -20,7 +20,7 @@ def ctx():
     c.close()
 
 
-@pytest.mark.parametrize("first", [0, 4095, 4096, 9000])
+@pytest.mark.parametrize("first", [0, 255, 256, 257, 4095, 4096, 8447, 8448, 9000, 70000])
 def test_no_shared_error(ctx, first):
     rows, width, vocab = first + 800, 64, 2000
     gen = torch.Generator(device="cuda").manual_seed(first)
